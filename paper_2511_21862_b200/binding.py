@@ -25,6 +25,10 @@ EXPORTS = (
     "ooco_decode_workspace_bytes_mq", "ooco_decode_attention_mq", "ooco_kv_append_mq", "ooco_attention_bytes_model",
     "ooco_decode_step_mq", "ooco_decode_step_mq_fp8", "ooco_get_tuning", "ooco_checked_build", "ooco_check_predicate",
     "ooco_last_host_step_ns",
+    # speculative decoding (bound in `spec`)
+    "ooco_plan_slots_workspace_bytes", "ooco_plan_slots", "ooco_rope_frequencies", "ooco_rope_kv_append",
+    "ooco_rope_kv_append_fp8", "ooco_tree_workspace_bytes", "ooco_tree_attention", "ooco_tree_attention_fp8",
+    "ooco_verify_drafts", "ooco_kv_keep_path", "ooco_kv_keep_path_fp8",
 )
 
 

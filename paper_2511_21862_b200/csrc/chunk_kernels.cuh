@@ -37,11 +37,13 @@ struct ChunkSmem {
 //   e0 / e1   tokens [0, e) of the stage the lane's rows g / g + 8 may see
 //   NTOK      tokens the call covers, starting at row 0 of `kst` / `vst`: a whole 64-token stage, or the
 //             16-token slice of a warp that shares its rows with the other warps (row16_main_kernel)
-template <int D, int NTOK, bool kTail>
+//   w0 / w1   kTree only: which of the call's tokens the lane's rows see (tree_window), shifted down by 2 t
+template <int D, int NTOK, bool kTail, bool kTree = false>
 __device__ __forceinline__ void chunk_consume(uint32_t kst, uint32_t vst, const uint32_t (&k_off)[2],
                                               const uint32_t (&v_off)[4], const uint32_t (&qf)[D / 16][4],
                                               float (&m_run)[2], float (&l_run)[2], float (&o_acc)[D / 8][4],
-                                              float scale_log2e, int ntok, int e0, int e1, int t) {
+                                              float scale_log2e, int ntok, int e0, int e1, int t,
+                                              uint64_t w0 = 0ull, uint64_t w1 = 0ull) {
   constexpr int KS = D / 16, NS = NTOK / 8, NO = D / 8;
   float s[NS][4];
 #pragma unroll
@@ -74,6 +76,12 @@ __device__ __forceinline__ void chunk_consume(uint32_t kst, uint32_t vst, const 
       if (c + 1 >= e0) s[j][1] = -INFINITY;
       if (c >= e1) s[j][2] = -INFINITY;
       if (c + 1 >= e1) s[j][3] = -INFINITY;
+      if (kTree) {
+        if (!((w0 >> (8 * j)) & 1ull)) s[j][0] = -INFINITY;
+        if (!((w0 >> (8 * j + 1)) & 1ull)) s[j][1] = -INFINITY;
+        if (!((w1 >> (8 * j)) & 1ull)) s[j][2] = -INFINITY;
+        if (!((w1 >> (8 * j + 1)) & 1ull)) s[j][3] = -INFINITY;
+      }
     }
     mx0 = fmaxf(mx0, fmaxf(s[j][0], s[j][1]));
     mx1 = fmaxf(mx1, fmaxf(s[j][2], s[j][3]));
@@ -141,12 +149,19 @@ __device__ __forceinline__ void chunk_consume(uint32_t kst, uint32_t vst, const 
   }
 }
 
+// tree_window of score row `qi` (rows beyond the last query token see nothing behind the tree's start), shifted for
+// lane column t of the accumulator layout.
+__device__ __forceinline__ uint64_t tree_row_window(const DecodeParams& p, int b, int qi, int o, int t) {
+  const bool there = qi < p.Sq;
+  return tree_window(p.tree_mask + ((size_t)b * p.Sq + (there ? qi : 0)) * p.tree_words, there ? p.tree_words : 0, o) >> (2 * t);
+}
+
 // The producer warp of both kernels below: walks its units of work (item, row tile of RT score columns),
 // streams the K / V stages of each through TMA and describes every stage in two int4 of `g_meta`:
 //   {partial slot, sequence, kv head, tokens | first << 16 | last << 17}  {first token, T - S_q + 1, chunk end, row tile}
 // KV8: the caches hold 8-bit codes; a stage is [64 tok][D bytes] of K, then of V (one 128-byte row per token at
 // head_dim 128, one copy per box), for a consumer that widens it before use.
-template <int D, bool KV8 = false>
+template <int D, bool KV8 = false, bool kTree = false>
 __device__ __forceinline__ void chunk_produce(const CUtensorMap& tm_k, const CUtensorMap& tm_v, const DecodeParams& p,
                                               const int RT, const int nst, const uint32_t s_stage,
                                               const uint32_t s_full, const uint32_t s_empty, int4* g_meta,
@@ -196,7 +211,7 @@ __device__ __forceinline__ void chunk_produce(const CUtensorMap& tm_k, const CUt
     const int b = d.x, h = d.y % p.Hkv, t0 = d.z, t1 = d.w;
     long long T = p.context_lens[b];
     T = T < 0 ? 0 : (T > cap_tokens ? cap_tokens : T);
-    const int lim_base = (int)T - p.Sq + 1;                       // tokens the first query token sees
+    const int lim_base = (int)T - query_tokens<kTree>(p, b) + 1;  // tokens the first query token sees
     const int col_hi = min(p.GQ, (rt + 1) * RT) - 1;
     const int t1e = min(t1, lim_base + col_hi / p.G);              // nothing beyond is visible to this tile
     const int nstage = t1e > t0 ? (t1e - t0 + kChunkStageTok - 1) / kChunkStageTok : 0;
@@ -299,7 +314,7 @@ __device__ __forceinline__ void chunk_produce(const CUtensorMap& tm_k, const CUt
 
 // NCW consumer warps (16 score rows each) + one producer warp.  p.grid_main is the number of CTAs the
 // plan sized its chunks for (not this grid); the work counter starts at this grid's size.
-template <int D, int NCW>
+template <int D, int NCW, bool kTree = false>
 __global__ void __launch_bounds__((NCW + 1) * 32, NCW == 8 ? 1 : 2)
 chunk_main_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
                   const DecodeParams p) {
@@ -332,7 +347,7 @@ chunk_main_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
   grid_dep_launch();  // the merge kernel may queue up behind this grid
 
   if (warp == NCW) {
-    chunk_produce<D>(tm_k, tm_v, p, RT, nst, s_stage, s_full, s_empty, g_meta, s_abort, lane);
+    chunk_produce<D, false, kTree>(tm_k, tm_v, p, RT, nst, s_stage, s_full, s_empty, g_meta, s_abort, lane);
     return;
   }
 
@@ -403,13 +418,18 @@ chunk_main_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
       const int tok0 = meta2.x, t1 = meta2.z;
       const int e0 = min(t1, lim_row0) - tok0, e1 = min(t1, lim_row1) - tok0;
       // warp-uniform bounds: the first row sees the fewest tokens, the last (real) row the most
-      const int e_first = min(t1, lim_base + colw / p.G) - tok0;
+      // (a tree: from its first node on, a token may be hidden from any row)
+      const int e_first = min(t1, kTree ? lim_base - 1 : lim_base + colw / p.G) - tok0;
       const int e_last = min(t1, lim_base + min(colw + 15, p.GQ - 1) / p.G) - tok0;
       if (e_last > 0) {
         const uint32_t kst = s_stage + (uint32_t)slot * L::kStageBytes;
         const uint32_t vst = kst + L::kTileBytes;
         if (e_first >= kChunkStageTok)
           chunk_consume<D, kChunkStageTok, false>(kst, vst, k_off, v_off, qf, m_run, l_run, o_acc, p.scale_log2e, ntok, e0, e1, t);
+        else if (kTree)
+          chunk_consume<D, kChunkStageTok, true, true>(kst, vst, k_off, v_off, qf, m_run, l_run, o_acc, p.scale_log2e, ntok, e0, e1, t,
+                                                       tree_row_window(p, b, (colw + g) / p.G, tok0 - lim_base + 1, t),
+                                                       tree_row_window(p, b, (colw + g + 8) / p.G, tok0 - lim_base + 1, t));
         else
           chunk_consume<D, kChunkStageTok, true>(kst, vst, k_off, v_off, qf, m_run, l_run, o_acc, p.scale_log2e, ntok, e0, e1, t);
       }
@@ -432,7 +452,7 @@ chunk_main_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
 #pragma unroll
       for (int r = 0; r < 2; ++r) {
         const int col = colw + g + 8 * r;
-        if (col >= p.GQ || (kChecked && !dst_ok)) continue;
+        if (col >= (kTree ? p.G * tree_nodes(p, b) : p.GQ) || (kChecked && !dst_ok)) continue;
         const float l = r ? l1 : l0, m = r ? m_run[1] : m_run[0];
         const float inv = l > 0.f ? 1.f / l : 0.f;  // l = 0: the row saw no token of this chunk
         if (n_chunks == 1 && !p.out_f32) {
@@ -472,7 +492,7 @@ struct Row16Smem {
   }
 };
 
-template <int D, int NCW>
+template <int D, int NCW, bool kTree = false>
 __global__ void __launch_bounds__((NCW + 1) * 32, 2)
 row16_main_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
                   const DecodeParams p) {
@@ -512,7 +532,7 @@ row16_main_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
   grid_dep_launch();  // the merge kernel may queue up behind this grid
 
   if (warp == NCW) {
-    chunk_produce<D>(tm_k, tm_v, p, 16, nst, s_stage, s_full, s_empty, g_meta, s_abort, lane);
+    chunk_produce<D, false, kTree>(tm_k, tm_v, p, 16, nst, s_stage, s_full, s_empty, g_meta, s_abort, lane);
     return;
   }
 
@@ -578,13 +598,17 @@ row16_main_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
     if (nslice > 0) {
       const int tokw = meta2.x + 16 * warp, t1 = meta2.z;
       const int e0 = min(t1, lim_row0) - tokw, e1 = min(t1, lim_row1) - tokw;
-      const int e_first = min(t1, lim_base) - tokw;                       // row 0 sees the fewest tokens
+      const int e_first = min(t1, kTree ? lim_base - 1 : lim_base) - tokw;  // row 0 sees the fewest tokens
       const int e_last = min(t1, lim_base + (p.GQ - 1) / p.G) - tokw;     // the last real row the most
       if (e_last > 0) {
         const uint32_t kst = s_stage + (uint32_t)slot * L::kStageBytes + slice;
         const uint32_t vst = kst + L::kTileBytes;
         if (e_first >= 16)
           chunk_consume<D, 16, false>(kst, vst, k_off, v_off, qf, m_run, l_run, o_acc, p.scale_log2e, nslice, e0, e1, t);
+        else if (kTree)
+          chunk_consume<D, 16, true, true>(kst, vst, k_off, v_off, qf, m_run, l_run, o_acc, p.scale_log2e, nslice, e0, e1, t,
+                                           tree_row_window(p, b, g / p.G, tokw - lim_base + 1, t),
+                                           tree_row_window(p, b, (g + 8) / p.G, tokw - lim_base + 1, t));
         else
           chunk_consume<D, 16, true>(kst, vst, k_off, v_off, qf, m_run, l_run, o_acc, p.scale_log2e, nslice, e0, e1, t);
       }
@@ -637,7 +661,8 @@ row16_main_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
         return;
       }
       mphase ^= 1u;
-      for (int idx = threadIdx.x; idx < p.GQ * (D / 4); idx += NCW * 32) {
+      const int cols = kTree ? p.G * tree_nodes(p, b) : p.GQ;  // rows of nodes that do not exist are left alone
+      for (int idx = threadIdx.x; idx < cols * (D / 4); idx += NCW * 32) {
         const int col = idx / (D / 4), c = idx % (D / 4);  // four dims 4c .. 4c + 3 of score column `col`
         float mx = -INFINITY;
 #pragma unroll

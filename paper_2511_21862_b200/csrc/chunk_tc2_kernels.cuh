@@ -55,7 +55,7 @@ struct ChunkTc2Smem {
 // is the third V slot otherwise -- and the eight warps that would be tile 1's softmax warps widen every stage into the
 // 16-bit slot layout, exactly, to f16 holding value / 256 (e4m3x2_to_f16x2; the factor is part of the softmax scale
 // and of the output scale), so both contractions run as kind::f16 MMAs with f16 operands (Q and P rounded to f16).
-template <bool KV8>
+template <bool KV8, bool kTree = false>
 __global__ void __launch_bounds__(kTc2Threads, 1)
 chunk_tc2_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
                  const DecodeParams p) {
@@ -180,7 +180,7 @@ chunk_tc2_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
       const int b = d.x, h = d.y % p.Hkv, t0 = d.z, t1 = d.w;
       long long T = p.context_lens[b];
       T = T < 0 ? 0 : (T > cap_tokens ? cap_tokens : T);
-      const int lim_base = (int)T - p.Sq + 1;                      // tokens the first query token sees
+      const int lim_base = (int)T - query_tokens<kTree>(p, b) + 1;  // tokens the first query token sees
       const int col_hi = min(p.GQ, (rt + 1) * kTc2Rows) - 1;
       const int t1e = min(t1, lim_base + col_hi / p.G);             // nothing beyond is visible to this tile pair
       const int nstage = t1e > t0 ? (t1e - t0 + kTc2StageTok - 1) / kTc2StageTok : 0;
@@ -672,7 +672,16 @@ chunk_tc2_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
         // keeps the threads clear of spills.  sh[4 i + 2 rr + c] = score of row (row0 + 8 rr), token 64 h2 + 8 i + 2 tq + c.
         // tokens [0, e) of the stage are visible to the row
         const int e0 = min(min(meta2.z, lim_row[0]) - meta2.x, ntok), e1 = min(min(meta2.z, lim_row[1]) - meta2.x, ntok);
-        const bool masked = __any_sync(0xffffffffu, min(e0, e1) < kTc2StageTok);
+        const bool nodes = kTree && meta2.x + kTc2StageTok >= lim_base;  // the stage holds nodes of the tree
+        const bool masked = nodes || __any_sync(0xffffffffu, min(e0, e1) < kTc2StageTok);
+        uint64_t see[2][2] = {{0ull, 0ull}, {0ull, 0ull}};  // kTree: the tokens of either half the rows see, from token 2 tq on
+        if (nodes) {
+#pragma unroll
+          for (int h2 = 0; h2 < 2; ++h2)
+#pragma unroll
+            for (int rr = 0; rr < 2; ++rr)
+              see[h2][rr] = tree_row_window(p, b, (col0 + 32 * rr) / p.G, meta2.x + 64 * h2 - lim_base + 1, tq);
+        }
         const uint32_t srow = trow + (solo ? 256u * (n & 1) : 0u);  // the stage's S (and P) columns
         auto load_half = [&](int h2, uint32_t (&sh)[32]) {
           tmem_ld_16x256b_x8(srow + 64 * h2, sh);
@@ -685,6 +694,10 @@ chunk_tc2_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
                 const int j = 64 * h2 + 8 * i + 2 * tq + c;
                 if (j >= e0) sh[4 * i + c] = 0xff800000u;  // -inf
                 if (j >= e1) sh[4 * i + 2 + c] = 0xff800000u;
+                if (kTree && nodes) {
+                  if (!((see[h2][0] >> (8 * i + c)) & 1ull)) sh[4 * i + c] = 0xff800000u;
+                  if (!((see[h2][1] >> (8 * i + c)) & 1ull)) sh[4 * i + 2 + c] = 0xff800000u;
+                }
               }
           }
         };
@@ -834,7 +847,7 @@ chunk_tc2_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
           lse[rr] = l > 0.f ? m_ref[rr] + lg2(l) : -INFINITY;
           const int col = col0 + 32 * rr;
           const int qi = col / p.G, head = col - qi * p.G;
-          write_row[rr] = col < p.GQ && (!kChecked || dst_ok);
+          write_row[rr] = col < (kTree ? p.G * tree_nodes(p, b) : p.GQ) && (!kChecked || dst_ok);
           orow[rr] = p.out + (((size_t)b * p.Sq + qi) * p.Hq + (size_t)h * p.G + head) * D;
           prow[rr] = p.part_o + ((size_t)slot_id * p.GQ + col) * D;
           if (write_row[rr] && tq == 0 && (n_chunks > 1 || p.out_f32)) p.part_lse[(size_t)slot_id * p.GQ + col] = lse[rr];

@@ -44,7 +44,7 @@ struct ChunkTcSmem {
 // Barrier bookkeeping.  Barriers that come in pairs ([2]) are used alternately by consecutive stages, and use
 // number n of a pair takes barrier n & 1 with phase parity (n >> 1) & 1: a waiter can then never be overtaken
 // by two completions of the barrier it waits on (the completion after next needs the waiter's own progress).
-template <bool KV8>
+template <bool KV8, bool kTree = false>
 __global__ void __launch_bounds__(KV8 ? 256 : 192, 2)
 chunk_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
                 const DecodeParams p) {
@@ -107,9 +107,9 @@ chunk_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
 
   if (warp == 4) {
     if (KV8)
-      chunk_produce<D, true>(tm_k, tm_v, p, kTcRows, nraw, s_rstage, s_rfull, s_rempty, g_rmeta, s_abort, lane);
+      chunk_produce<D, true, kTree>(tm_k, tm_v, p, kTcRows, nraw, s_rstage, s_rfull, s_rempty, g_rmeta, s_abort, lane);
     else
-      chunk_produce<D>(tm_k, tm_v, p, kTcRows, nst, s_stage, s_full, s_empty, g_meta, s_abort, lane);
+      chunk_produce<D, false, kTree>(tm_k, tm_v, p, kTcRows, nst, s_stage, s_full, s_empty, g_meta, s_abort, lane);
   } else if (KV8 && warp >= 6) {
     // ================================================================= widening warps (8-bit cache only)
     // Stage number `it` of the 8-bit ring becomes stage number `it` of the 16-bit ring (bookkeeping stages and
@@ -326,6 +326,12 @@ chunk_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
           for (int j = 0; j < 64; ++j)
             if (j >= e) sr[j >> 5][j & 31] = 0xff800000u;  // -inf
         }
+        if (kTree && meta2.x + kChunkStageTok >= lim_base) {  // nodes of the tree in this stage
+          const uint64_t see = tree_row_window(p, b, qi, meta2.x - lim_base + 1, 0);
+#pragma unroll
+          for (int j = 0; j < 64; ++j)
+            if (!((see >> j) & 1ull)) sr[j >> 5][j & 31] = 0xff800000u;
+        }
         float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};  // four chains: the row is one thread's work
 #pragma unroll
         for (int j = 0; j < 64; j += 2)  // three-input maximum: two scores per instruction
@@ -399,7 +405,7 @@ chunk_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
         const bool dst_ok = checked(chk_index(slot_id, p.max_items) && chk_index(b, p.B) && chk_index(h, p.Hkv),
                                     &p.hdr->status, kStatusBadIndex);
         const int n_chunks = dst_ok ? p.seq_first[b + 1] - p.seq_first[b] : 1;
-        const bool write_row = real_row && (!kChecked || dst_ok);
+        const bool write_row = (kTree ? qi < tree_nodes(p, b) : real_row) && (!kChecked || dst_ok);
         if (ntok > 0) {
           if (!wait_pv(n_pv - 1)) {
             ok = false;

@@ -94,7 +94,56 @@ struct DecodeParams {
   int32_t chunk_min, chunk_max, items_per_cta;
   float scale_log2e;        // softmax scale * log2(e) (* the K tensor scale of an 8-bit cache)
   float v_scale;            // V tensor scale of an 8-bit cache (1 for bf16)
+  // Tree attention: the query tokens of a sequence are the nodes of a tree (NULL parents: causal attention).
+  const int32_t* tree_parents;  // [B, Sq]
+  const int32_t* tree_sizes;    // [B] nodes that exist, or NULL: Sq of them
+  uint64_t* tree_mask;          // [B, Sq, tree_words] bit j of row i: node j is node i or one of its ancestors
+  int32_t tree_words;
 };
+
+// Nodes of sequence b's tree.
+__device__ __forceinline__ int tree_nodes(const DecodeParams& p, int b) {
+  return p.tree_sizes ? min(max(0, p.tree_sizes[b]), p.Sq) : p.Sq;
+}
+// Query tokens of sequence b that exist.
+template <bool kTree>
+__device__ __forceinline__ int query_tokens(const DecodeParams& p, int b) {
+  return kTree ? tree_nodes(p, b) : p.Sq;
+}
+// Which of 64 consecutive tokens a node sees, the first of them `o` tokens behind the first node's: tokens before
+// the tree are seen by all, tokens behind it by none.  `row` = the node's row of tree_mask.
+__device__ __forceinline__ uint64_t tree_window(const uint64_t* row, int words, int o) {
+  if (o <= -64) return ~0ull;
+  const int w = o >> 6, s = o & 63;
+  const uint64_t lo = w < 0 ? ~0ull : (w < words ? row[w] : 0ull);
+  if (s == 0) return lo;
+  const uint64_t hi = w + 1 < words ? row[w + 1] : 0ull;  // (w + 1 >= 0)
+  return (lo >> s) | (hi << (64 - s));
+}
+// Whether node `k` (negative: a token before the tree) is seen by a node with at most 32 nodes in its tree.
+__device__ __forceinline__ bool tree_sees(uint32_t mask, int k) { return k < 0 || (k < 32 && ((mask >> k) & 1u)); }
+
+// The mask rows of all sequences, one thread per node, walking up to the root (parents lie below their children, so
+// the walk ends).  Rows of nodes that do not exist are empty.
+__device__ __forceinline__ void tree_mask_body(const DecodeParams& p, int block, int nblocks) {
+  const long long n = (long long)p.B * p.Sq;
+  for (long long i = block * (long long)blockDim.x + threadIdx.x; i < n; i += (long long)nblocks * blockDim.x) {
+    const int b = (int)(i / p.Sq), node = (int)(i - (long long)b * p.Sq);
+    const int32_t* up = p.tree_parents + (size_t)b * p.Sq;
+    uint64_t m[4] = {0ull, 0ull, 0ull, 0ull};  // (at most 256 nodes)
+    if (node < tree_nodes(p, b))
+      for (int j = node; j >= 0;) {
+#pragma unroll
+        for (int w = 0; w < 4; ++w)
+          if ((j >> 6) == w) m[w] |= 1ull << (j & 63);
+        const int above = up[j];
+        j = above < j ? above : -1;
+      }
+#pragma unroll
+    for (int w = 0; w < 4; ++w)
+      if (w < p.tree_words) p.tree_mask[i * p.tree_words + w] = m[w];
+  }
+}
 
 // ------------------------------------------------------------------------------------ append
 struct AppendParams {
@@ -187,7 +236,8 @@ __device__ __forceinline__ void host_stage_body(const HostStageParams& p, int bl
 
 // ------------------------------------------------------------------------------------ plan
 // CTA 0 plans; CTAs 1 .. n_append (present only in the fused step) do the KV append; any further CTAs
-// (host-buffer step only) stage the inputs the attention kernel reads.  The plan chooses the chunk
+// (host-buffer step only) stage the inputs the attention kernel reads.  (Tree attention: the further CTAs build the
+// nodes' masks.)  The plan chooses the chunk
 // length from the total work, splits every sequence into near-equal chunks that are multiples of
 // `stage_tok`, and writes the item list.
 template <int kThreads>
@@ -201,7 +251,9 @@ __global__ void __launch_bounds__(kThreads) plan_kernel(DecodeParams p, int stag
   grid_dep_wait();
   grid_dep_launch();
   if (blockIdx.x > 0) {
-    if ((int)blockIdx.x <= n_append)
+    if (p.tree_parents)
+      tree_mask_body(p, blockIdx.x - 1, gridDim.x - 1);
+    else if ((int)blockIdx.x <= n_append)
       kv_append_body(ap, blockIdx.x - 1, n_append);
     else
       host_stage_body(hs, blockIdx.x - 1 - n_append, gridDim.x - 1 - n_append);
@@ -215,15 +267,15 @@ __global__ void __launch_bounds__(kThreads) plan_kernel(DecodeParams p, int stag
   const long long cap = (long long)p.MB * p.bs;
 
   int* s_len = s_first + p.B + 1;
-  auto len_of = [&](int b) -> long long {  // context length clamped to [0, table capacity]
-    if (first_in_smem) return s_len[b];
+  auto read_len = [&](int b) -> long long {  // context length clamped to [0, table capacity]
     const long long t = p.context_lens[b];
+    if (p.tree_parents && tree_nodes(p, b) == 0) return 0;  // no query token: nothing to read
     return t < 0 ? 0 : (t > cap ? cap : t);
   };
+  auto len_of = [&](int b) -> long long { return first_in_smem ? s_len[b] : read_len(b); };
   long long acc = 0;
   for (int b = tid; b < p.B; b += kThreads) {
-    long long t = p.context_lens[b];
-    t = t < 0 ? 0 : (t > cap ? cap : t);
+    const long long t = read_len(b);
     if (first_in_smem) s_len[b] = (int)t;
     acc += t;
   }
@@ -358,10 +410,11 @@ __global__ void __launch_bounds__(kThreads) plan_kernel(DecodeParams p, int stag
   const int row = p.Sq * p.Hq * p.D;
   for (int b = wid; b < p.B; b += kThreads / 32) {
     if (len_of(b) > 0) continue;
+    const int used = p.tree_parents ? tree_nodes(p, b) * p.Hq * p.D : row;
     if (p.out_f32) {
-      for (int i = lane; i < row; i += 32) reinterpret_cast<float*>(p.out)[(size_t)b * row + i] = 0.f;
+      for (int i = lane; i < used; i += 32) reinterpret_cast<float*>(p.out)[(size_t)b * row + i] = 0.f;
     } else {
-      for (int i = lane; i < row; i += 32) p.out[(size_t)b * row + i] = __float2bfloat16(0.f);
+      for (int i = lane; i < used; i += 32) p.out[(size_t)b * row + i] = __float2bfloat16(0.f);
     }
   }
 }
@@ -413,16 +466,18 @@ struct SmemLayout {
 // One consumer warp's work on its TPW tiles of a stage.  kTail: some of the warp's rows lie
 // beyond the chunk (`valid` < 16 * TPW of them count); masked rows get weight 0 and their V
 // words are cleared in registers, so NaN / stale bytes there never reach an accumulator.
-template <int D, int NT, int TPW, bool kTail>
+template <int D, int NT, int TPW, bool kTail, bool kTree = false>
 __device__ __forceinline__ void consume_tiles(uint32_t kst, uint32_t vst, const uint32_t (&tile_k)[TPW],
                                               const uint32_t (&tile_v)[TPW], const uint32_t (&kpat)[D / 16],
                                               const uint32_t (&vpat)[D / 16],
                                               const uint32_t (&qf)[NT][D / 16][2], float (&m_run)[NT][2],
                                               float (&l_run)[NT][2], float (&o_acc)[NT][D / 16][4],
                                               float scale_log2e, int valid, int g, int t, int lim_w = 0,
-                                              const int (*qi_col)[2] = nullptr) {
+                                              const int (*qi_col)[2] = nullptr,
+                                              const uint32_t (*tmask)[2] = nullptr) {
   // kTail only: lim_w = rows of this warp the first query token may see (causal limit, several query
   // tokens per sequence), qi_col[nt][c] = query token of the lane's score column c of tile nt.
+  // kTree only: tmask[nt][c] = which nodes that query sees (token row lim_w - 1 + k of the warp is node k).
   constexpr int KS = D / 16;
   constexpr int NACC = TPW == 1 ? 2 : 1;  // a lone tile splits its k-steps over two accumulators
   // ---- scores: S = K_tile x Q^T
@@ -466,6 +521,13 @@ __device__ __forceinline__ void consume_tiles(uint32_t kst, uint32_t vst, const 
         if (16 * u + g >= l1) s[u][1] = -INFINITY;
         if (16 * u + g + 8 >= l0) s[u][2] = -INFINITY;
         if (16 * u + g + 8 >= l1) s[u][3] = -INFINITY;
+        if (kTree) {
+          const int k = 16 * u + g - lim_w + 1;
+          if (!tree_sees(tmask[nt][0], k)) s[u][0] = -INFINITY;
+          if (!tree_sees(tmask[nt][1], k)) s[u][1] = -INFINITY;
+          if (!tree_sees(tmask[nt][0], k + 8)) s[u][2] = -INFINITY;
+          if (!tree_sees(tmask[nt][1], k + 8)) s[u][3] = -INFINITY;
+        }
       }
       mx0 = fmaxf(mx0, fmaxf(s[u][0], s[u][2]));
       mx1 = fmaxf(mx1, fmaxf(s[u][1], s[u][3]));
@@ -565,11 +627,11 @@ __device__ __forceinline__ float f16_hi(uint32_t x) { return __half2float(__usho
 
 // Softmax and value part of a 16-token tile over the 8-bit cache; `sv[nt]` holds the tile's scaled scores (log2
 // domain) in the MMA accumulator layout: (token g, head 2t) (token g, head 2t+1) (token g+8, 2t) (token g+8, 2t+1).
-template <int D, int NT, bool kTail>
+template <int D, int NT, bool kTail, bool kTree = false>
 __device__ __forceinline__ void kv8_softmax_values(uint32_t vst, uint32_t tile_off, const uint32_t (&pat)[D / 16],
                                                    float (&sv)[NT][4], float (&m_run)[NT][2], float (&l_run)[NT][2],
                                                    float (&o_acc)[NT][D / 16][4], int valid, int g, int t, int lim_w,
-                                                   const int (*qi_col)[2]);
+                                                   const int (*qi_col)[2], const uint32_t (*tmask)[2] = nullptr);
 
 template <int D, int NT, bool kTail>
 __device__ __forceinline__ void consume_tile_kv8(uint32_t kst, uint32_t vst, uint32_t tile_off,
@@ -608,11 +670,11 @@ __device__ __forceinline__ void consume_tile_kv8(uint32_t kst, uint32_t vst, uin
   kv8_softmax_values<D, NT, kTail>(vst, tile_off, pat, sv, m_run, l_run, o_acc, valid, g, t, lim_w, qi_col);
 }
 
-template <int D, int NT, bool kTail>
+template <int D, int NT, bool kTail, bool kTree>
 __device__ __forceinline__ void kv8_softmax_values(uint32_t vst, uint32_t tile_off, const uint32_t (&pat)[D / 16],
                                                    float (&sv)[NT][4], float (&m_run)[NT][2], float (&l_run)[NT][2],
                                                    float (&o_acc)[NT][D / 16][4], int valid, int g, int t, int lim_w,
-                                                   const int (*qi_col)[2]) {
+                                                   const int (*qi_col)[2], const uint32_t (*tmask)[2]) {
   constexpr int KS = D / 16;
   uint32_t pb[NT][2];
 #pragma unroll
@@ -624,6 +686,13 @@ __device__ __forceinline__ void kv8_softmax_values(uint32_t vst, uint32_t tile_o
       if (g >= l1) s[1] = -INFINITY;
       if (g + 8 >= l0) s[2] = -INFINITY;
       if (g + 8 >= l1) s[3] = -INFINITY;
+      if (kTree) {  // as in consume_tiles
+        const int k = g - lim_w + 1;
+        if (!tree_sees(tmask[nt][0], k)) s[0] = -INFINITY;
+        if (!tree_sees(tmask[nt][1], k)) s[1] = -INFINITY;
+        if (!tree_sees(tmask[nt][0], k + 8)) s[2] = -INFINITY;
+        if (!tree_sees(tmask[nt][1], k + 8)) s[3] = -INFINITY;
+      }
     }
     float mx0 = fmaxf(s[0], s[2]), mx1 = fmaxf(s[1], s[3]);
 #pragma unroll
@@ -737,7 +806,7 @@ static_assert(sizeof(VStageDesc) == 96, "descriptor slot is 96 bytes");
 // shared memory, K as the TMA wrote it) into the stage's own tensor-memory columns.  The consumer warps load their
 // 16-token tile of S in the mma.sync accumulator layout and go on with the softmax and the value MMAs as in KVM 1;
 // the codes of K are never widened.
-template <int D, int NCW, int NT, int TPW, int KVM>
+template <int D, int NCW, int NT, int TPW, int KVM, bool kTree>
 __device__ __forceinline__ uint32_t decode_main_body(const CUtensorMap& tm_k, const CUtensorMap& tm_v,
                                                      const DecodeParams& p, uint8_t* smem_raw) {
   constexpr bool KV8 = KVM != 0, KVTC = KVM == 2;
@@ -746,6 +815,7 @@ __device__ __forceinline__ uint32_t decode_main_body(const CUtensorMap& tm_k, co
   using L = SmemLayout<D, NCW, NT, TPW, KVM>;
   static_assert(!KV8 || (D == 128 && TPW == 1), "the 8-bit path is built for head_dim 128, one tile per warp");
   static_assert(!KVTC || NCW == 8, "a stage must hold the 128 tokens of one tcgen05 MMA");
+  static_assert(!kTree || KVM != 1, "tree attention over the 8-bit cache runs its tcgen05 shape");
   constexpr int kStageTok = L::kStageTok;
   constexpr int KS = D / 16;  // k-steps of the score MMA = m-tiles of the value MMA
 
@@ -1035,7 +1105,7 @@ __device__ __forceinline__ uint32_t decode_main_body(const CUtensorMap& tm_k, co
           // (one query token: everything)
           int cm = 1023;
           if (p.Sq > 1) {
-            const long long lim0 = (long long)T_cur - p.Sq + 1 - tok0 + 16;
+            const long long lim0 = (long long)T_cur - query_tokens<kTree>(p, b) + 1 - tok0 + 16;
             cm = lim0 < 0 ? 0 : (lim0 > 1023 ? 1023 : (int)lim0);
           }
           const int4 meta = make_int4(slot_id, b, h, ntok | (flags << 16) | (cm << 18));
@@ -1213,6 +1283,9 @@ __device__ __forceinline__ uint32_t decode_main_body(const CUtensorMap& tm_k, co
     qi_col[nt][0] = p.Sq > 1 ? (8 * nt + 2 * t) / p.G : 0;
     qi_col[nt][1] = p.Sq > 1 ? (8 * nt + 2 * t + 1) / p.G : 0;
   }
+  uint32_t tmask[NT][2];  // kTree: the nodes those query tokens see (at most 16 score columns, so at most 16 nodes)
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) tmask[nt][0] = tmask[nt][1] = 0u;
   uint32_t mphase = 0;  // parity of the next merge-barrier phase to wait for
   bool merge_pending_read = false;
 
@@ -1231,6 +1304,13 @@ __device__ __forceinline__ uint32_t decode_main_body(const CUtensorMap& tm_k, co
     const bool first = (meta.w >> 16) & 1, last = (meta.w >> 17) & 1;
     if (first) {
       const uint8_t* qs = g_q + (size_t)slot * qslot;
+      if (kTree) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int c = 0; c < 2; ++c)  // (columns beyond the last query token see no node)
+            tmask[nt][c] = qi_col[nt][c] < p.Sq ? (uint32_t)p.tree_mask[((size_t)meta.y * p.Sq + qi_col[nt][c]) * p.tree_words] : 0u;
+      }
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         const int head = 8 * nt + g;
@@ -1262,6 +1342,8 @@ __device__ __forceinline__ uint32_t decode_main_body(const CUtensorMap& tm_k, co
       const uint32_t vst = KVTC ? s_vring + (uint32_t)slot * L::kTileBytes : kst + L::kTileBytes;
       // rows of this warp the first query token may see; with one query token that is all of them
       const int lim_w = ((meta.w >> 18) & 1023) - 16 - r0;
+      // tokens that every query sees: all but the last one the first query token may see, when that is a tree's node
+      const int lim_all = kTree ? lim_w - 1 : lim_w;
       if (KVTC) {
         // this warp's 16 x (2 * heads) tile of the stage's scores, in the accumulator layout of mma.sync
         const uint32_t sbuf = (uint32_t)it % kNS;
@@ -1283,10 +1365,10 @@ __device__ __forceinline__ uint32_t decode_main_body(const CUtensorMap& tm_k, co
           for (int e = 0; e < 4; ++e)  // high term + low term / 16
             sv[nt][e] = fmaf(__uint_as_float(f[4 * (NT + nt) + e]), 0.0625f, __uint_as_float(f[4 * nt + e])) * ((e & 1) ? m1 : m0);
         }
-        if (valid >= 16 && lim_w >= 16)
+        if (valid >= 16 && lim_all >= 16)
           kv8_softmax_values<D, NT, false>(vst, tile_k[0], kpat, sv, m_run, l_run, o_acc, valid, g, t, 0, nullptr);
         else
-          kv8_softmax_values<D, NT, true>(vst, tile_k[0], kpat, sv, m_run, l_run, o_acc, valid, g, t, lim_w, qi_col);
+          kv8_softmax_values<D, NT, true, kTree>(vst, tile_k[0], kpat, sv, m_run, l_run, o_acc, valid, g, t, lim_w, qi_col, tmask);
       } else if (KV8) {
         if (valid >= 16 && lim_w >= 16)
           consume_tile_kv8<D, NT, false>(kst, vst, tile_k[0], kpat, qf, m_run, l_run, o_acc, p.scale_log2e, valid, g, t);
@@ -1294,12 +1376,12 @@ __device__ __forceinline__ uint32_t decode_main_body(const CUtensorMap& tm_k, co
           consume_tile_kv8<D, NT, true>(kst, vst, tile_k[0], kpat, qf, m_run, l_run, o_acc, p.scale_log2e, valid, g, t,
                                         lim_w, qi_col);
       } else {
-        if (valid >= 16 * TPW && lim_w >= 16 * TPW)
+        if (valid >= 16 * TPW && lim_all >= 16 * TPW)
           consume_tiles<D, NT, TPW, false>(kst, vst, tile_k, tile_v, kpat, vpat, qf, m_run, l_run, o_acc,
                                            p.scale_log2e, valid, g, t);
         else
-          consume_tiles<D, NT, TPW, true>(kst, vst, tile_k, tile_v, kpat, vpat, qf, m_run, l_run, o_acc,
-                                          p.scale_log2e, valid, g, t, lim_w, qi_col);
+          consume_tiles<D, NT, TPW, true, kTree>(kst, vst, tile_k, tile_v, kpat, vpat, qf, m_run, l_run, o_acc,
+                                                 p.scale_log2e, valid, g, t, lim_w, qi_col, tmask);
       }
     }
     __syncwarp();
@@ -1362,7 +1444,8 @@ __device__ __forceinline__ uint32_t decode_main_body(const CUtensorMap& tm_k, co
           return tmem;
         }
         mphase ^= 1u;
-        for (int idx = threadIdx.x; idx < p.GQ * 64; idx += NCW * 32) {
+        const int cols = kTree ? p.G * tree_nodes(p, b) : p.GQ;  // rows of nodes that do not exist are left alone
+        for (int idx = threadIdx.x; idx < cols * 64; idx += NCW * 32) {
           const int col = idx >> 6, dl = idx & 63, dim = 64 * pass + dl;  // column = query * G + head
           float M = -INFINITY;
 #pragma unroll
@@ -1394,12 +1477,12 @@ __device__ __forceinline__ uint32_t decode_main_body(const CUtensorMap& tm_k, co
   return tmem;
 }
 
-template <int D, int NCW, int NT, int TPW, int KVM = 0>
+template <int D, int NCW, int NT, int TPW, int KVM = 0, bool kTree = false>
 __global__ void __launch_bounds__(SmemLayout<D, NCW, NT, TPW, KVM>::kWarps * 32, (KVM && NCW == 8 && NT == 1) ? 2 : 1)
 decode_main_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
                    const DecodeParams p) {
   extern __shared__ uint8_t smem_raw[];
-  const uint32_t tmem = decode_main_body<D, NCW, NT, TPW, KVM>(tm_k, tm_v, p, smem_raw);
+  const uint32_t tmem = decode_main_body<D, NCW, NT, TPW, KVM, kTree>(tm_k, tm_v, p, smem_raw);
   if (KVM == 2) {  // common exit: release the tensor memory once every warp is done with it
     tc_fence_before_sync();
     __syncthreads();
@@ -1455,6 +1538,7 @@ __global__ void __launch_bounds__(256) lse_merge_kernel(const DecodeParams p, co
     // unsplit (or empty) sequence: the attention kernel wrote the row itself -- except with fp32 output, where
     // every row is a partial (an unsplit row passes through unchanged: one chunk of weight 1)
     bool work = live && (n > 1 || (p.out_f32 && n == 1));
+    if (p.tree_parents && work && qi >= tree_nodes(p, b)) work = false;  // a node that does not exist
     if (work && !checked(chk_index((long long)(first + n) * p.Hkv - 1, p.max_items) && first >= 0, &p.hdr->status,
                          kStatusBadIndex))
       work = false;

@@ -12,6 +12,8 @@
 #include <vector>
 
 #include "../../include/ooco.h"
+#include "../../include/ooco_spec.h"
+#include "api_internal.h"
 #include "block_copy_kernels.cuh"
 #include "chunk_kernels.cuh"
 #include "chunk_tc_kernels.cuh"
@@ -34,7 +36,7 @@ static thread_local char tl_detail[160] = "";
 static thread_local int64_t tl_host_ns[2] = {0, 0};  // last host-buffer step: host work before the wait, the wait
 
 // Remembers where a CUDA-side failure happened (read back through ooco_last_error_detail).
-static int fail_cuda(const char* where, long code) {
+int fail_cuda(const char* where, long code) {
   snprintf(tl_detail, sizeof tl_detail, "%s failed with code %ld", where, code);
   return OOCO_E_CUDA;
 }
@@ -48,11 +50,7 @@ struct Profiler {
 static Profiler g_prof;
 static std::atomic<int> g_prof_on{0};
 
-struct DeviceInfo {
-  int sm_count = 0;
-  int smem_optin = 0;
-};
-static DeviceInfo device_info(int dev) {
+DeviceInfo device_info(int dev) {
   static DeviceInfo cache[64];
   static std::atomic<int> ready[64];
   if (dev >= 0 && dev < 64 && ready[dev].load(std::memory_order_acquire)) return cache[dev];
@@ -86,7 +84,7 @@ static EncodeTiledFn encode_fn() {
 
 static bool supported_block(int bs) { return bs == 16 || bs == 32 || bs == 64 || bs == 128 || bs == 256; }
 
-static int validate_shape(const ooco_shape_t* s) {
+int validate_shape(const ooco_shape_t* s) {
   if (!s) return OOCO_E_NULLPTR;
   if (s->batch <= 0 || s->num_q_heads <= 0 || s->num_kv_heads <= 0 || s->head_dim <= 0 ||
       s->block_size <= 0 || s->num_blocks <= 0 || s->max_blocks_per_seq <= 0 || s->reserved != 0)
@@ -190,29 +188,11 @@ static int encode_kv8_map(CUtensorMap* tm, const ooco_shape_t* s, const void* ba
   return r == CUDA_SUCCESS ? OOCO_OK : fail_cuda("cuTensorMapEncodeTiled(8-bit)", (long)r);
 }
 
-// Launch with the programmatic-stream-serialization attribute (the kernel itself waits for its
-// predecessor with griddepcontrol.wait) when `pdl`, else an ordinary launch.
-template <typename... KArgs, typename... Args>
-static cudaError_t launch_ex(void (*kern)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t st,
-                             bool pdl, Args&&... args) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = grid;
-  cfg.blockDim = block;
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = st;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = pdl ? 1 : 0;
-  return cudaLaunchKernelEx(&cfg, kern, std::forward<Args>(args)...);
-}
-
-template <int D, int NCW, int NT, int TPW, int KVM = 0>
+template <int D, int NCW, int NT, int TPW, int KVM = 0, bool kTree = false>
 static int launch_main(const CUtensorMap& tk, const CUtensorMap& tv, DecodeParams& p, const DeviceInfo& di,
                        int ctas_per_sm, int want_stages, cudaStream_t st, int dev, bool dry) {
   using L = SmemLayout<D, NCW, NT, TPW, KVM>;
-  auto kern = decode_main_kernel<D, NCW, NT, TPW, KVM>;
+  auto kern = decode_main_kernel<D, NCW, NT, TPW, KVM, kTree>;
   // the opt-in limit covers static + dynamic shared memory of the kernel
   static std::atomic<int> static_smem{-1};
   if (static_smem.load() < 0) {
@@ -288,11 +268,11 @@ static int launch_main_ncw(int ncw, int tpw, const CUtensorMap& tk, const CUtens
 }
 
 // Prefill-chunk kernel: as many 64-token stages as the CTA's share of shared memory holds (at most 8).
-template <int D, int NCW>
+template <int D, int NCW, bool kTree = false>
 static int launch_chunk(const CUtensorMap& tk, const CUtensorMap& tv, DecodeParams& p, const DeviceInfo& di,
                         int ctas_per_sm, cudaStream_t st, int dev, bool dry) {
   using L = ChunkSmem<D>;
-  auto kern = chunk_main_kernel<D, NCW>;
+  auto kern = chunk_main_kernel<D, NCW, kTree>;
   static std::atomic<int> static_smem{-1};
   if (static_smem.load() < 0) {
     cudaFuncAttributes fa;
@@ -323,10 +303,10 @@ static int launch_chunk(const CUtensorMap& tk, const CUtensorMap& tv, DecodePara
 
 // Prefill chunk on tcgen05 with one 128-row tile per CTA and two CTAs per SM (head_dim 128): what the 8-bit cache
 // runs, and the bf16 cache when the kernel below is switched off.
-template <bool KV8>
+template <bool KV8, bool kTree = false>
 static int launch_chunk_tc(const CUtensorMap& tk, const CUtensorMap& tv, DecodeParams& p, const DeviceInfo& di,
                            int ctas_per_sm, cudaStream_t st, int dev, bool dry) {
-  auto kern = chunk_tc_kernel<KV8>;
+  auto kern = chunk_tc_kernel<KV8, kTree>;
   static std::atomic<int> static_smem{-1};
   if (static_smem.load() < 0) {
     cudaFuncAttributes fa;
@@ -363,10 +343,10 @@ static int launch_chunk_tc(const CUtensorMap& tk, const CUtensorMap& tv, DecodeP
 // second tile's resources (score columns, issuing warp, Q region) pipeline the one tile -- it beats the one-tile
 // kernel and the mma.sync kernel on every workload measured, from 17 columns on.  KV8: the one-tile mode over the 8-bit
 // cache (the idle softmax warps widen the codes), 1.25 to 1.5 times as fast as the two-CTA kernel on these shapes.
-template <bool KV8>
+template <bool KV8, bool kTree = false>
 static int launch_chunk_tc2(const CUtensorMap& tk, const CUtensorMap& tv, DecodeParams& p, const DeviceInfo& di,
                             cudaStream_t st, int dev, bool dry) {
-  auto kern = chunk_tc2_kernel<KV8>;
+  auto kern = chunk_tc2_kernel<KV8, kTree>;
   static std::atomic<int> static_smem{-1};
   if (static_smem.load() < 0) {
     cudaFuncAttributes fa;
@@ -391,12 +371,12 @@ static int launch_chunk_tc2(const CUtensorMap& tk, const CUtensorMap& tv, Decode
 }
 
 // 9 .. 16 score columns: the warps of a CTA share one 16-row tile and split the tokens of a stage.
-template <int D>
+template <int D, bool kTree = false>
 static int launch_row16(const CUtensorMap& tk, const CUtensorMap& tv, DecodeParams& p, const DeviceInfo& di,
                         int ctas_per_sm, cudaStream_t st, int dev, bool dry) {
   constexpr int NCW = 4;
   using M = Row16Smem<NCW>;
-  auto kern = row16_main_kernel<D, NCW>;
+  auto kern = row16_main_kernel<D, NCW, kTree>;
   static std::atomic<int> static_smem{-1};
   if (static_smem.load() < 0) {
     cudaFuncAttributes fa;
@@ -425,14 +405,36 @@ static int launch_row16(const CUtensorMap& tk, const CUtensorMap& tv, DecodePara
   return e == cudaSuccess ? OOCO_OK : fail_cuda("launch of the 16-row attention kernel", (long)e);
 }
 
-template <int D>
+template <int D, bool kTree = false>
 static int launch_chunk_ncw(int ncw, const CUtensorMap& tk, const CUtensorMap& tv, DecodeParams& p,
                             const DeviceInfo& di, int cps, cudaStream_t st, int dev, bool dry) {
   switch (ncw) {
-    case 2: return launch_chunk<D, 2>(tk, tv, p, di, cps, st, dev, dry);
-    case 4: return launch_chunk<D, 4>(tk, tv, p, di, cps, st, dev, dry);
-    default: return launch_chunk<D, 8>(tk, tv, p, di, cps, st, dev, dry);
+    case 2: return launch_chunk<D, 2, kTree>(tk, tv, p, di, cps, st, dev, dry);
+    case 4: return launch_chunk<D, 4, kTree>(tk, tv, p, di, cps, st, dev, dry);
+    default: return launch_chunk<D, 8, kTree>(tk, tv, p, di, cps, st, dev, dry);
   }
+}
+
+// Tree attention: the decode shapes that the rules of decode_core pick without a knob, compiled with the tree's mask.
+// `tc` / `tc2`: the tcgen05 chunk kernels (head_dim 128).
+static int launch_tree(int head_dim, bool kv8, bool chunk, bool tc2, bool row16, int ncw, const CUtensorMap& tk,
+                       const CUtensorMap& tv, DecodeParams& p, const DeviceInfo& di, int cps, cudaStream_t st, int dev,
+                       bool dry) {
+  if (chunk && head_dim == 128) {
+    if (tc2)
+      return kv8 ? launch_chunk_tc2<true, true>(tk, tv, p, di, st, dev, dry)
+                 : launch_chunk_tc2<false, true>(tk, tv, p, di, st, dev, dry);
+    return launch_chunk_tc<true, true>(tk, tv, p, di, cps, st, dev, dry);
+  }
+  if (chunk) return launch_chunk_ncw<64, true>(ncw, tk, tv, p, di, cps, st, dev, dry);
+  if (row16)
+    return head_dim == 128 ? launch_row16<128, true>(tk, tv, p, di, cps, st, dev, dry)
+                           : launch_row16<64, true>(tk, tv, p, di, cps, st, dev, dry);
+  if (kv8)
+    return p.GQ > 8 ? launch_main<128, 8, 2, 1, 2, true>(tk, tv, p, di, cps, 0, st, dev, dry)
+                    : launch_main<128, 8, 1, 1, 2, true>(tk, tv, p, di, cps, 0, st, dev, dry);
+  return head_dim == 128 ? launch_main<128, 4, 1, 1, 0, true>(tk, tv, p, di, cps, 0, st, dev, dry)
+                         : launch_main<64, 4, 1, 1, 0, true>(tk, tv, p, di, cps, 0, st, dev, dry);
 }
 
 static AppendParams make_append_params(const ooco_shape_t* s, const void* k_new, const void* v_new,
@@ -491,7 +493,9 @@ static int static_scratch_ptr(void** ptr_out) {
   return OOCO_OK;
 }
 
-static int current_device(int* dev) { return cudaGetDevice(dev) == cudaSuccess ? OOCO_OK : OOCO_E_CUDA; }
+bool pdl_enabled() { return g_knobs[kKnobPdl].load() != 0; }
+
+int current_device(int* dev) { return cudaGetDevice(dev) == cudaSuccess ? OOCO_OK : OOCO_E_CUDA; }
 
 // Device-visible address of a page-locked (pinned / registered) host buffer on the current device,
 // or nullptr when `host` is ordinary pageable memory (which a kernel must never be given).
@@ -708,11 +712,18 @@ static int validate_kv8(const ooco_shape_t* s, const Kv8Scales* kv8) {
   return OOCO_OK;
 }
 
+struct TreeArgs {  // present: the q_len query tokens are the nodes of a tree
+  const int32_t *parents, *sizes;
+};
+static size_t tree_mask_bytes(const ooco_shape_t* s, int nodes) {
+  return ((size_t)s->batch * nodes * ((nodes + 63) / 64) * 8 + 255) & ~(size_t)255;
+}
+
 static int decode_core(const ooco_shape_t* s, const void* q, const void* k_cache, const void* v_cache,
                        const int32_t* block_table, const int32_t* context_lens, float scale, void* out,
                        void* workspace, size_t workspace_bytes, void* cuda_stream, const AppendParams* append,
                        const Kv8Scales* kv8 = nullptr, int q_len = 1, const HostStageParams* host_stage = nullptr,
-                       const int32_t* plan_context_lens = nullptr) {
+                       const int32_t* plan_context_lens = nullptr, const TreeArgs* tree = nullptr) {
   // host_stage / plan_context_lens (host-buffer step): extra CTAs of the first launch stage q and the
   // block table for the attention kernel while its planning CTA reads the lengths, and its append CTAs
   // the new rows, straight from the mapped host buffers.
@@ -724,7 +735,7 @@ static int decode_core(const ooco_shape_t* s, const void* q, const void* k_cache
   if (!q || !k_cache || !v_cache || !block_table || !context_lens || !out || !workspace) return OOCO_E_NULLPTR;
   if (((uintptr_t)k_cache | (uintptr_t)v_cache | (uintptr_t)q | (uintptr_t)out) & 15) return OOCO_E_UNSUPPORTED;
   const WsLayout w = ws_layout(s, q_len);
-  if (workspace_bytes < w.total || ((uintptr_t)workspace & 255)) return OOCO_E_WORKSPACE;
+  if (workspace_bytes < w.total + (tree ? tree_mask_bytes(s, q_len) : 0) || ((uintptr_t)workspace & 255)) return OOCO_E_WORKSPACE;
   int dev = 0;
   if ((rc = current_device(&dev))) return rc;
   const DeviceInfo di = device_info(dev);
@@ -745,24 +756,29 @@ static int decode_core(const ooco_shape_t* s, const void* q, const void* k_cache
     cps = 4;
   int tpw = g_knobs[kKnobTilesPerWarp].load();
   if (ncw == 8 || kv8) tpw = 1;
+  if (tree) {  // the shapes above without any knob
+    ncw = kv8 || G_ > 8 ? 8 : 4;
+    cps = G_ > 8 ? 1 : (s->head_dim == 64 ? 4 : 2);
+    tpw = 1;
+  }
   // prefill chunk: 64-token stages; 8 warps (128 columns) x 1 CTA per SM, fewer columns: smaller CTAs x 2
   const bool chunk = G_ > kDecodeMaxColumns;
   // 9 .. 16 columns: the row layout with the tokens of a stage split over 4 warps x 2 CTAs per SM (the
   // column layout of the decode kernel needs a second MMA tile and a transposition per tile there)
-  const bool row16 = !chunk && !kv8 && G_ > 8 && g_knobs[kKnobRowLayout16].load() != 0;
+  const bool row16 = !chunk && !kv8 && G_ > 8 && (tree || g_knobs[kKnobRowLayout16].load() != 0);
   // (the 8-bit cache has no mma.sync chunk kernel: every chunk over it runs the tcgen05 kernel)
   // (knob 12: 0 = never; 1 = every prefill chunk, i.e. from 17 score columns; n >= 17 = from n columns)
-  const int tc_knob = g_knobs[kKnobChunkTcgen05].load();
+  const int tc_knob = tree ? 1 : g_knobs[kKnobChunkTcgen05].load();
   const int tc_from = tc_knob == 1 ? 17 : tc_knob;
   const bool chunk_tc = chunk && s->head_dim == 128 && (kv8 || (tc_knob != 0 && G_ >= tc_from));
   // (more than one 128-row tile per item, bf16: the kernel that keeps two tiles per CTA on the tensor pipe in turns)
-  const int two_tiles = g_knobs[kKnobChunkTwoTiles].load();  // 1: beyond 128 columns only; 2: its one-tile mode below, too
+  const int two_tiles = tree ? 2 : g_knobs[kKnobChunkTwoTiles].load();  // 1: beyond 128 columns only; 2: its one-tile mode below, too
   // (8-bit cache: only the one-tile mode has a variant that widens the codes, so up to 128 columns)
   const bool chunk_tc2 = chunk_tc && two_tiles != 0 && (kv8 ? (G_ <= kTcRows && two_tiles == 2) : (G_ > kTcRows || two_tiles == 2));
   if (chunk) {
     ncw = chunk_warps(G_);
     cps = (ncw == 8 && !chunk_tc) ? 1 : 2;
-    if (chunk_tc && g_overridden[kKnobCtasPerSm].load()) cps = g_knobs[kKnobCtasPerSm].load() > 1 ? 2 : 1;
+    if (chunk_tc && !tree && g_overridden[kKnobCtasPerSm].load()) cps = g_knobs[kKnobCtasPerSm].load() > 1 ? 2 : 1;
     if (chunk_tc2) cps = 1;
   } else if (row16) {
     ncw = 4;
@@ -807,9 +823,15 @@ static int decode_core(const ooco_shape_t* s, const void* q, const void* k_cache
   p.items_per_cta = plan_items_per_cta(G_);
   // the 8-bit path widens codes to value / 256 (kE4m3WidenFactor): both scales carry the factor back (K's only
   // where K is widened: the tcgen05 score path multiplies the codes' own values)
-  const bool kv8_tc = kv8 && !chunk && ncw == 8 && g_knobs[kKnobKv8Tcgen05].load() != 0;
+  const bool kv8_tc = kv8 && !chunk && ncw == 8 && (tree || g_knobs[kKnobKv8Tcgen05].load() != 0);
   p.scale_log2e = scale * 1.4426950408889634f * (kv8 ? kv8->k_scale * (kv8_tc ? 1.f : kE4m3WidenFactor) : 1.f);
   p.v_scale = kv8 ? kv8->v_scale * kE4m3WidenFactor : 1.f;
+  if (tree) {
+    p.tree_parents = tree->parents;
+    p.tree_sizes = tree->sizes;
+    p.tree_mask = (uint64_t*)(ws + w.total);
+    p.tree_words = (q_len + 63) / 64;
+  }
 
   CUtensorMap tk, tv;
   bool five_d = !kv8 && !chunk && !row16 && s->head_dim == 128 && !g_knobs[kKnobSplitHalves].load();
@@ -829,6 +851,8 @@ static int decode_core(const ooco_shape_t* s, const void* q, const void* k_cache
   // once without launching, before the first kernel of the call is enqueued.
   const int stages = g_knobs[kKnobStages].load();
   auto launch_attention = [&](bool dry) -> int {
+    if (tree)
+      return launch_tree(s->head_dim, kv8 != nullptr, chunk, chunk_tc2, row16, ncw, tk, tv, p, di, cps, st, dev, dry);
     if (chunk_tc2)
       return kv8 ? launch_chunk_tc2<true>(tk, tv, p, di, st, dev, dry) : launch_chunk_tc2<false>(tk, tv, p, di, st, dev, dry);
     if (chunk_tc)
@@ -872,6 +896,10 @@ static int decode_core(const ooco_shape_t* s, const void* q, const void* k_cache
   const bool pdl_on = g_knobs[kKnobPdl].load() != 0 && !pe;
   DecodeParams pp = p;  // the planning CTA may read the lengths from another (host-mapped) copy
   if (plan_context_lens) pp.context_lens = plan_context_lens;
+  if (tree) {  // one thread per node
+    const long long want = ((long long)p.B * q_len + 1023) / 1024;
+    n_stage = (int)(want < di.sm_count ? want : di.sm_count);
+  }
   cudaError_t e = launch_ex(plan_kernel<1024>, dim3(1 + n_append + n_stage), dim3(1024),
                             first_in_smem ? first_bytes : 0, st, pdl_on, pp, stage_tok, first_in_smem, ap, n_append,
                             hs);
@@ -1052,6 +1080,42 @@ int ooco_decode_attention_static(const ooco_shape_t* s, const void* q, const voi
   if ((rc = static_scratch_ptr(&scratch))) return rc;
   return ooco_decode_attention(s, q, k_cache, v_cache, block_table, context_lens, scale, out, scratch,
                                (size_t)OOCO_STATIC_SCRATCH_BYTES, cuda_stream);
+}
+
+size_t ooco_tree_workspace_bytes(const ooco_shape_t* s, int32_t max_nodes) {
+  if (validate_shape(s) || max_nodes < 1 || max_nodes > OOCO_TREE_MAX_NODES) return 0;
+  return ws_layout(s, max_nodes).total + tree_mask_bytes(s, max_nodes);
+}
+
+static int tree_core(const ooco_shape_t* s, int32_t max_nodes, const void* q, const void* k_cache, const void* v_cache,
+                     const int32_t* block_table, const int32_t* context_lens, const int32_t* parents,
+                     const int32_t* tree_sizes, float scale, const Kv8Scales* kv8, void* out, void* workspace,
+                     size_t workspace_bytes, void* cuda_stream) {
+  int rc = validate_shape(s);
+  if (rc) return rc;
+  if (max_nodes < 1) return OOCO_E_SHAPE;
+  if (max_nodes > OOCO_TREE_MAX_NODES) return OOCO_E_UNSUPPORTED;
+  if (!parents) return OOCO_E_NULLPTR;
+  const TreeArgs tree = {parents, tree_sizes};
+  return decode_core(s, q, k_cache, v_cache, block_table, context_lens, scale, out, workspace, workspace_bytes, cuda_stream,
+                     nullptr, kv8, max_nodes, nullptr, nullptr, &tree);
+}
+
+int ooco_tree_attention(const ooco_shape_t* s, int32_t max_nodes, const void* q, const void* k_cache,
+                        const void* v_cache, const int32_t* block_table, const int32_t* context_lens,
+                        const int32_t* parents, const int32_t* tree_sizes, float scale, void* out, void* workspace,
+                        size_t workspace_bytes, void* cuda_stream) {
+  return tree_core(s, max_nodes, q, k_cache, v_cache, block_table, context_lens, parents, tree_sizes, scale, nullptr, out,
+                   workspace, workspace_bytes, cuda_stream);
+}
+
+int ooco_tree_attention_fp8(const ooco_shape_t* s, int32_t max_nodes, const void* q, const void* k_cache,
+                            const void* v_cache, const int32_t* block_table, const int32_t* context_lens,
+                            const int32_t* parents, const int32_t* tree_sizes, float scale, float k_scale, float v_scale,
+                            void* out, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+  const Kv8Scales sc = {k_scale, v_scale};
+  return tree_core(s, max_nodes, q, k_cache, v_cache, block_table, context_lens, parents, tree_sizes, scale, &sc, out,
+                   workspace, workspace_bytes, cuda_stream);
 }
 
 static int check_block_args(const ooco_shape_t* s, int32_t n, const void* a, const void* b, const void* c,
