@@ -1,9 +1,11 @@
-"""Compile the CUDA sources into `libooco.so` next to this file (sm_100a only, in-tree)."""
+"""Compile the CUDA sources into `libooco.so` and the call marshalling of `spec` into `_spec_calls.so`, next to this file
+(sm_100a only, in-tree)."""
 from __future__ import annotations
 
 import os
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
@@ -18,12 +20,36 @@ NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "-shared", "--expt-relaxed-constexpr", "-t", "0"]
 
 
+CALLS = os.path.join(HERE, "_spec_calls.so")             # CPython module, host code only
+CALLS_SOURCES = ["py_spec.cpp"]
+CALLS_HEADERS = [os.path.join("..", "..", "include", "ooco.h"), os.path.join("..", "..", "include", "ooco_spec.h")]
+
+
 def is_stale(lib: str = LIB) -> bool:
     if not os.path.exists(lib):
         return True
     t = os.path.getmtime(lib)
-    deps = [os.path.join(CSRC, f) for f in SOURCES + HEADERS] + [os.path.abspath(__file__)]
+    files = CALLS_SOURCES + CALLS_HEADERS if lib == CALLS else SOURCES + HEADERS
+    deps = [os.path.join(CSRC, f) for f in files] + [os.path.abspath(__file__)]
     return any(os.path.getmtime(d) > t for d in deps if os.path.exists(d))
+
+
+def build_calls(force: bool = False) -> str:
+    """Run the C++ compiler on the marshalling module if it is missing or older than its sources."""
+    if force or is_stale(CALLS):
+        import torch
+        from torch.utils.cpp_extension import include_paths, library_paths
+        # (the system's compiler: it shares the C++ runtime that torch and the interpreter use)
+        cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-DNDEBUG",
+               f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}",
+               *[f"-I{p}" for p in include_paths("cuda") + [sysconfig.get_path("include")]], "-o", CALLS,
+               *[os.path.join(CSRC, f) for f in CALLS_SOURCES], *[f"-L{p}" for p in library_paths()],
+               "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_python"]
+        res = subprocess.run(cmd, capture_output=True, text=True)
+        if res.returncode != 0:
+            sys.stderr.write(res.stdout + res.stderr)
+            raise RuntimeError(f"the C++ compiler failed building {os.path.basename(CALLS)}")
+    return CALLS
 
 
 def build(force: bool = False, verbose: bool = False, checked: bool = False) -> str:
@@ -39,6 +65,8 @@ def build(force: bool = False, verbose: bool = False, checked: bool = False) -> 
             sys.stderr.write(res.stdout + res.stderr)
         if res.returncode != 0:
             raise RuntimeError(f"nvcc failed building {os.path.basename(lib)}")
+    if not checked:
+        build_calls(force)
     return lib
 
 

@@ -298,12 +298,27 @@ int ooco_verify_drafts(const ooco_verify_t* s, const float* target_probs, const 
   p.B = s->batch;
   p.N = s->max_nodes;
   p.V = s->vocab;
-  // CTAs per sequence: as many as fill the SMs about twice, at most one per tile of the vocabulary, and at least
-  // so many that a share's bit map fits shared memory (2^17 values)
-  int cluster = kVerifyMaxCluster;
-  while (cluster > 1 && (int64_t)s->batch * cluster > 4ll * sms && (int64_t)(cluster / 2) << 17 >= s->vocab) cluster /= 2;
+  // CTAs per sequence and their threads.  Few sequences (16 CTAs each do not fill the SMs twice): the largest cluster of
+  // large CTAs shortens the pass over the vocabulary (4 sequences of 152064 values: 13.3 us, 17.8 with 8 x 256).  Else 8
+  // CTAs of 256 threads, so that four CTAs per SM hide each other's serial phases (128 sequences of 128256 values: 68 us,
+  // 73 with 4 x 512, 95 with 4 x 256), and fewer as the sequences alone give the GPU enough CTAs.  At least so many that
+  // a share's bit map fits shared memory (2^17 values), at most one per tile of the vocabulary.
+  int cluster = kVerifyMaxCluster, threads = kVerifyThreads;
+  if ((int64_t)s->batch * cluster > 2ll * sms) {
+    threads = 256;
+    cluster = 8;
+    while (cluster > 1 && (int64_t)s->batch * cluster > 8ll * sms) cluster /= 2;
+    while ((int64_t)cluster << 17 < s->vocab) cluster *= 2;
+  }
   while (cluster > 1 && (int64_t)(cluster / 2) * kVerifyTile >= s->vocab) cluster /= 2;
-  return finish(launch_clustered(verify_kernel, dim3((unsigned)(s->batch * cluster)), dim3(kVerifyThreads), 0,
+  static std::atomic<int> configured[64];
+  int dev = 0;
+  if (cluster > 8 && (current_device(&dev) || dev >= 64 || !configured[dev].load())) {
+    const cudaError_t e = cudaFuncSetAttribute(verify_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (e != cudaSuccess) return fail_cuda("cudaFuncSetAttribute(cluster size)", (long)e);
+    if (dev < 64) configured[dev].store(1);
+  }
+  return finish(launch_clustered(verify_kernel, dim3((unsigned)(s->batch * cluster)), dim3(threads), 0,
                                  (cudaStream_t)cuda_stream, pdl_enabled(), (unsigned)cluster, p, cluster),
                 "launch of the verification kernel");
 }

@@ -101,6 +101,19 @@ __device__ __forceinline__ void slots_fill_body(const SlotsParams& p, int block,
   const bool vec = (((uintptr_t)p.slot_map | (uintptr_t)p.positions) & 15) == 0;
   const int used = p.row_len ? p.num_rows : p.first_token[p.B];
   bool bad = false;
+  auto store_rows = [&](int r0, int n, const int (&slot)[4], const int (&pos)[4]) {
+    if (vec && n == 4) {
+      *reinterpret_cast<int4*>(p.slot_map + r0) = make_int4(slot[0], slot[1], slot[2], slot[3]);
+      *reinterpret_cast<int4*>(p.positions + r0) = make_int4(pos[0], pos[1], pos[2], pos[3]);
+      return;
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (k < n) {
+        p.slot_map[r0 + k] = slot[k];
+        p.positions[r0 + k] = pos[k];
+      }
+  };
   for (long long gi = block * (long long)blockDim.x + threadIdx.x; gi < groups; gi += (long long)nblocks * blockDim.x) {
     const int r0 = (int)(4 * gi);
     int slot[4] = {-1, -1, -1, -1}, pos[4] = {-1, -1, -1, -1};
@@ -116,6 +129,34 @@ __device__ __forceinline__ void slots_fill_body(const SlotsParams& p, int block,
           if (p.first_token[mid] <= r0) lo = mid; else hi = mid;
         }
         b = lo;
+      }
+      const int seq_lo = p.row_len ? b * p.row_len : p.first_token[b];
+      const int seq_hi = p.row_len ? seq_lo + p.row_len : p.first_token[b + 1];
+      const int i0 = r0 - seq_lo;
+      if (!p.parents && r0 + 4 <= seq_hi && i0 + 4 <= p.granted[b]) {
+        // four granted tokens of one sequence: at most two blocks
+        const int t0 = p.context_lens[b] > 0 ? p.context_lens[b] + i0 : i0, held = p.ws_held[b], from = p.ws_from[b];
+        const int ia = t0 >> p.bs_log2, ib = (t0 + 3) >> p.bs_log2, mask = (1 << p.bs_log2) - 1;
+        int32_t* row = p.block_table + (size_t)b * p.MB;
+        const int blk_a = ia < held ? row[ia] : p.free_ids[from + ia - held];
+        int blk_b = blk_a;
+        if (ib != ia) {
+          blk_b = ib < held ? row[ib] : p.free_ids[from + ib - held];
+          if (ib >= held) row[ib] = blk_b;
+        } else if (ia >= held && (t0 & mask) == 0) {
+          row[ia] = blk_a;
+        }
+        const bool ok_a = blk_a >= 0 && blk_a < p.NB, ok_b = blk_b >= 0 && blk_b < p.NB;
+        bad |= !ok_a || !ok_b;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int t = t0 + k;
+          const bool first_blk = (t >> p.bs_log2) == ia;
+          pos[k] = t;
+          slot[k] = (first_blk ? ok_a : ok_b) ? ((first_blk ? blk_a : blk_b) << p.bs_log2) + (t & mask) : -1;
+        }
+        store_rows(r0, n, slot, pos);
+        continue;
       }
       int cur = -1, row_lo = 0, row_hi = 0, ctx = 0, held = 0, from = 0, granted = 0, add = 0, blk_at = -1, blk = 0;
 #pragma unroll
@@ -157,17 +198,7 @@ __device__ __forceinline__ void slots_fill_body(const SlotsParams& p, int block,
         else bad = true;
       }
     }
-    if (vec && n == 4) {
-      *reinterpret_cast<int4*>(p.slot_map + r0) = make_int4(slot[0], slot[1], slot[2], slot[3]);
-      *reinterpret_cast<int4*>(p.positions + r0) = make_int4(pos[0], pos[1], pos[2], pos[3]);
-    } else {
-#pragma unroll
-      for (int k = 0; k < 4; ++k)
-        if (k < n) {
-          p.slot_map[r0 + k] = slot[k];
-          p.positions[r0 + k] = pos[k];
-        }
-    }
+    store_rows(r0, n, slot, pos);
   }
   if (bad && p.status) atomicOr(p.status, kSlotsStatusBadBlock);
 }
@@ -342,7 +373,7 @@ struct VerifyParams {
   int32_t B, N, V;
 };
 
-constexpr int kVerifyThreads = 512, kVerifyMaxCluster = 8;
+constexpr int kVerifyThreads = 512, kVerifyMaxCluster = 16;  // most threads of a CTA, most CTAs of a cluster
 constexpr int kVerifyTile = 512;  // values whose weights are summed by one warp at a time: 16 per lane
 constexpr int kVerifyMaxTiles = (1 << 20) / kVerifyTile;
 
@@ -359,21 +390,54 @@ __device__ __forceinline__ uint32_t map_cluster(uint32_t addr, uint32_t rank) {
   asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
   return r;
 }
-__device__ __forceinline__ void st_cluster(uint32_t addr, double v) {
-  asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(addr), "d"(v) : "memory");
+__device__ __forceinline__ void st_cluster(uint32_t addr, float v) {
+  asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory");
 }
 __device__ __forceinline__ void st_cluster(uint32_t addr, int v) {
   asm volatile("st.shared::cluster.s32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
 }
 
-__device__ __forceinline__ double warp_sum(double v) {
-  for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-  return v;
+// ---- double-float arithmetic: an unevaluated sum hi + lo of two fp32 values, 2^-46 relative or better for the sums of
+// non-negative terms formed here.  fp64 instructions issue at about 1 / 60 of the fp32 rate on this part (measured: a
+// pass in fp64 took 0.45 weights per cycle and SM, 1/6 of what HBM delivers).
+struct Df {
+  float hi, lo;
+};
+__device__ __forceinline__ Df two_sum(float a, float b) {  // exact (error-free transformation, Knuth)
+  const float s = __fadd_rn(a, b), bb = __fsub_rn(s, a);
+  return {s, __fadd_rn(__fsub_rn(a, __fsub_rn(s, bb)), __fsub_rn(b, bb))};
 }
-__device__ __forceinline__ double warp_scan(double v, int lane) {
+__device__ __forceinline__ Df df_add(Df a, Df b) {
+  const Df s = two_sum(a.hi, b.hi);
+  const float e = __fadd_rn(s.lo, __fadd_rn(a.lo, b.lo)), h = __fadd_rn(s.hi, e);
+  return {h, __fsub_rn(e, __fsub_rn(h, s.hi))};
+}
+__device__ __forceinline__ bool df_greater(Df a, Df b) { return a.hi > b.hi || (a.hi == b.hi && a.lo > b.lo); }
+__device__ __forceinline__ Df df_times(Df a, float b) {
+  const float m = __fmul_rn(a.hi, b), e = __fmaf_rn(a.lo, b, __fmaf_rn(a.hi, b, -m)), h = __fadd_rn(m, e);
+  return {h, __fsub_rn(e, __fsub_rn(h, m))};
+}
+__device__ __forceinline__ Df df_shfl(Df v, int src) {
+  return {__shfl_sync(0xffffffffu, v.hi, src), __shfl_sync(0xffffffffu, v.lo, src)};
+}
+__device__ __forceinline__ Df df_shfl_up1(Df v) {
+  return {__shfl_up_sync(0xffffffffu, v.hi, 1), __shfl_up_sync(0xffffffffu, v.lo, 1)};
+}
+// max(p - s q, 0); NaN counts as 0
+__device__ __forceinline__ Df df_weight(float p, float q, Df s) {
+  const float m = __fmul_rn(s.hi, q);                                  // s q = m + e
+  const float e = __fmaf_rn(s.lo, q, __fmaf_rn(s.hi, q, -m));
+  const Df d = two_sum(p, -m);
+  const float l = __fsub_rn(d.lo, e), h = __fadd_rn(d.hi, l);
+  return h > 0.f ? Df{h, __fsub_rn(l, __fsub_rn(h, d.hi))} : Df{0.f, 0.f};
+}
+__device__ __forceinline__ Df df_shfl_xor(Df v, int o) {
+  return {__shfl_xor_sync(0xffffffffu, v.hi, o), __shfl_xor_sync(0xffffffffu, v.lo, o)};
+}
+__device__ __forceinline__ Df df_warp_scan(Df v, int lane) {  // inclusive
   for (int o = 1; o < 32; o <<= 1) {
-    const double u = __shfl_up_sync(0xffffffffu, v, o);
-    if (lane >= o) v += u;
+    const Df u = {__shfl_up_sync(0xffffffffu, v.hi, o), __shfl_up_sync(0xffffffffu, v.lo, o)};
+    if (lane >= o) v = df_add(v, u);
   }
   return v;
 }
@@ -384,7 +448,9 @@ struct VerifyCommand {
   int node;
   int drops;    // without draft probabilities: refused siblings whose tokens have left the weights
   int count;    // drafts accepted so far
-  double spent; // S: weights are max(p - S q, 0)
+  Df spent;     // S: weights are max(p - S q, 0)
+  float u;      // uniform number of the last token
+  int pad;
 };
 
 // One cluster of CTAs per sequence.  CTA 0 walks down the tree (a warp, from the few values per node that it
@@ -394,19 +460,18 @@ struct VerifyCommand {
 // many nodes there are.  Bound by HBM for many sequences (two rows of V fp32 values each), by latency for few
 // (gather, walk, pass and draw follow one another), which is why a sequence is spread over several CTAs then.
 //
-// Sums are fp64 (p, q fp32: every weight has one rounding of 2^-53 relative): the drawn index depends on a
-// cumulative sum of up to 2^20 weights, and an fp32 sum would move its borders by more than the smallest weights.
-__global__ void __launch_bounds__(kVerifyThreads) verify_kernel(const VerifyParams p, const int cluster) {
+// Weights and their sums are double-floats: the drawn index depends on a cumulative sum of up to 2^20 weights, and an
+// fp32 sum would move its borders by more than the smallest weights.
+__global__ void __launch_bounds__(kVerifyThreads, 2) verify_kernel(const VerifyParams p, const int cluster) {
   __shared__ int s_token[kTreeMaxNodes], s_parent[kTreeMaxNodes];
   __shared__ float s_p[kTreeMaxNodes], s_q[kTreeMaxNodes], s_u[kTreeMaxNodes];
   __shared__ uint8_t s_drop[kTreeMaxNodes];
   __shared__ int s_drop_tok[kTreeMaxNodes];          // tokens that have left the weights (same in every CTA)
   __shared__ VerifyCommand s_cmd;
-  __shared__ double s_part[kVerifyMaxCluster];       // sum of each CTA's share
-  __shared__ double s_tile[kVerifyMaxTiles];
-  __shared__ double s_warp[kVerifyThreads / 32];
+  __shared__ Df s_part[kVerifyMaxCluster];           // sum of each CTA's share
+  __shared__ Df s_tile[kVerifyMaxTiles];
   __shared__ uint32_t s_bits[(1 << 20) / 32 / 8 + 1];
-  const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
+  const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5, threads = blockDim.x, warps = threads >> 5;
   const int rank = cluster > 1 ? (int)cluster_rank() : 0;
   const int b = blockIdx.x / cluster;
   grid_dep_wait();
@@ -422,7 +487,7 @@ __global__ void __launch_bounds__(kVerifyThreads) verify_kernel(const VerifyPara
   const int v_lo = tile0 * kVerifyTile, v_hi = min(V, v_lo + ntile * kVerifyTile);
 
   if (rank == 0) {
-    for (int i = tid; i < N; i += kVerifyThreads) {
+    for (int i = tid; i < N; i += threads) {
       int par = -1, x = -1;
       float pp = 0.f, qq = 0.f;
       if (i > 0 && i < n) {
@@ -449,7 +514,8 @@ __global__ void __launch_bounds__(kVerifyThreads) verify_kernel(const VerifyPara
 
   // the walk's state, in warp 0 of CTA 0 (the same in every lane)
   int cur = 0, last = 0, count = 0;
-  double spent = 0.0, mass = 1.0;
+  Df spent = {0.f, 0.f}, mass = {1.f, 0.f};
+  const float u_last = rank == 0 && n > 0 ? s_u[0] : 0.f;
 
   for (;;) {
     if (rank == 0 && wid == 0) {
@@ -464,24 +530,21 @@ __global__ void __launch_bounds__(kVerifyThreads) verify_kernel(const VerifyPara
         if (next == N) break;
         last = next;
         const int x = s_token[next];
-        double w = s_p[next];
-        bool take;
+        Df w = {s_p[next], 0.f}, bar = df_times(mass, s_u[next]);
         if (draft) {
-          const double q = s_q[next];
-          w -= spent * q;
-          w = w > 0.0 ? w : 0.0;
-          take = (double)s_u[next] * mass * q < w;
+          const float q = s_q[next];
+          w = df_weight(w.hi, q, spent);
+          bar = df_times(bar, q);
         } else {
           bool gone = false;  // the token was refused already
           for (int c0 = 0; c0 < next; c0 += 32)
             gone |= __any_sync(0xffffffffu, c0 + lane < next && s_drop[c0 + lane] && s_token[c0 + lane] == x);
-          w = gone || !(w > 0.0) ? 0.0 : w;
-          take = (double)s_u[next] * mass < w;
+          if (gone || !(w.hi > 0.f)) w.hi = 0.f;
         }
-        if (take) {
+        if (df_greater(w, bar)) {
           cur = next;
-          spent = 0.0;
-          mass = 1.0;
+          spent = Df{0.f, 0.f};
+          mass = Df{1.f, 0.f};
           ++count;
           for (int i = lane; i < n; i += 32) s_drop[i] = 0;
           __syncwarp();
@@ -490,7 +553,7 @@ __global__ void __launch_bounds__(kVerifyThreads) verify_kernel(const VerifyPara
             p.out_tokens[(size_t)b * N + count - 1] = x;
           }
         } else if (draft) {
-          spent += mass;
+          spent = df_add(spent, mass);
           // another sibling to ask needs the new mass; without one the pass is the last
           bool more = false;
           for (int c0 = (last + 1) & ~31; c0 < n; c0 += 32)
@@ -498,7 +561,7 @@ __global__ void __launch_bounds__(kVerifyThreads) verify_kernel(const VerifyPara
           if (more) op = 1;
           break;
         } else {
-          mass -= w;
+          mass = df_add(mass, Df{-w.hi, -w.lo});
           if (lane == 0) s_drop[next] = 1;
           __syncwarp();
         }
@@ -523,13 +586,16 @@ __global__ void __launch_bounds__(kVerifyThreads) verify_kernel(const VerifyPara
           st_cluster(at + 4, cur);
           st_cluster(at + 8, drops);
           st_cluster(at + 12, count);
-          st_cluster(at + 16, spent);
+          st_cluster(at + 16, spent.hi);
+          st_cluster(at + 20, spent.lo);
+          st_cluster(at + 24, u_last);
         } else {
           s_cmd.op = op;
           s_cmd.node = cur;
           s_cmd.drops = drops;
           s_cmd.count = count;
           s_cmd.spent = spent;
+          s_cmd.u = u_last;
         }
       }
       if (lane == 0) p.num_accepted[b] = count;
@@ -545,51 +611,65 @@ __global__ void __launch_bounds__(kVerifyThreads) verify_kernel(const VerifyPara
     if (op == 0) return;
     const float* pr = target + (int64_t)s_cmd.node * p.t_node;
     const float* qr = draft ? draft + (int64_t)s_cmd.node * p.d_node : nullptr;
-    double S = s_cmd.spent;
-    if (S == 0.0) qr = nullptr;
+    Df S = s_cmd.spent;
+    if (S.hi == 0.f) qr = nullptr;
     int drops = s_cmd.drops;
 
     for (int attempt = 0;; ++attempt) {
       if (drops > 0) {
-        for (int i = tid; i < (v_hi - v_lo + 31) / 32; i += kVerifyThreads) s_bits[i] = 0u;
+        for (int i = tid; i < (v_hi - v_lo + 31) / 32; i += threads) s_bits[i] = 0u;
         __syncthreads();
-        for (int i = tid; i < drops; i += kVerifyThreads) {
+        for (int i = tid; i < drops; i += threads) {
           const int x = s_drop_tok[i] - v_lo;
           if (x >= 0 && x < v_hi - v_lo) atomicOr(&s_bits[x >> 5], 1u << (x & 31));
         }
         __syncthreads();
       }
       auto weight = [&](int v, float pv, float qv) {
-        double w = (double)pv - S * (double)qv;
-        if (drops > 0 && (s_bits[(v - v_lo) >> 5] >> ((v - v_lo) & 31) & 1u)) w = 0.0;
-        return w > 0.0 ? w : 0.0;
+        Df w = qr ? df_weight(pv, qv, S) : Df{pv > 0.f ? pv : 0.f, 0.f};
+        if (drops > 0 && (s_bits[(v - v_lo) >> 5] >> ((v - v_lo) & 31) & 1u)) w = Df{0.f, 0.f};
+        return w;
       };
-      double mine = 0.0;
-      for (int k = wid; k < ntile; k += kVerifyThreads / 32) {
+      auto add_to = [](Df& s, Df w) {  // (the low parts may grow a little: they are folded in by the next df_add)
+        const Df a = two_sum(s.hi, w.hi);
+        s = Df{a.hi, __fadd_rn(s.lo, __fadd_rn(a.lo, w.lo))};
+      };
+      for (int k = wid; k < ntile; k += warps) {
         const int v0 = v_lo + k * kVerifyTile + lane;
-        float pv[16], qv[16];
+        Df s0 = {0.f, 0.f}, s1 = {0.f, 0.f};
+        if (v0 - lane + kVerifyTile <= v_hi) {
+          float pv[16], qv[16];
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const int v = v0 + 32 * e;
-          pv[e] = v < v_hi ? pr[v] : 0.f;
-          qv[e] = qr && v < v_hi ? qr[v] : 0.f;
+          for (int e = 0; e < 16; ++e) pv[e] = pr[v0 + 32 * e];
+          if (qr) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) qv[e] = qr[v0 + 32 * e];
+          }
+#pragma unroll
+          for (int e = 0; e < 16; e += 2) {
+            add_to(s0, weight(v0 + 32 * e, pv[e], qv[e]));
+            add_to(s1, weight(v0 + 32 * e + 32, pv[e + 1], qv[e + 1]));
+          }
+        } else {
+          for (int v = v0; v < v_hi; v += 32) add_to(s0, weight(v, pr[v], qr ? qr[v] : 0.f));
         }
-        double s = 0.0;
-#pragma unroll
-        for (int e = 0; e < 16; ++e)
-          if (v0 + 32 * e < v_hi) s += weight(v0 + 32 * e, pv[e], qv[e]);
-        s = warp_sum(s);
+        Df s = df_add(s0, s1);
+        for (int o = 16; o; o >>= 1) s = df_add(s, df_shfl_xor(s, o));
         if (lane == 0) s_tile[k] = s;
-        mine += s;
       }
-      if (lane == 0) s_warp[wid] = mine;
       __syncthreads();
-      if (wid == 0) {
-        double s = lane < kVerifyThreads / 32 ? s_warp[lane] : 0.0;
-        s = warp_sum(s);
+      if (wid == 0) {  // the share's sum, to every CTA of the cluster
+        Df s = {0.f, 0.f};
+        for (int k = lane; k < ntile; k += 32) s = df_add(s, s_tile[k]);
+        for (int o = 16; o; o >>= 1) s = df_add(s, df_shfl_xor(s, o));
         if (lane < cluster) {
-          if (cluster > 1) st_cluster(map_cluster(smem_u32(&s_part[rank]), lane), s);
-          else s_part[0] = s;
+          if (cluster > 1) {
+            const uint32_t at = map_cluster(smem_u32(&s_part[rank]), lane);
+            st_cluster(at, s.hi);
+            st_cluster(at + 4, s.lo);
+          } else {
+            s_part[0] = s;
+          }
         }
       }
       __syncwarp();
@@ -599,102 +679,95 @@ __global__ void __launch_bounds__(kVerifyThreads) verify_kernel(const VerifyPara
       } else {
         __syncthreads();
       }
-      double sum = 0.0;
-      for (int r = 0; r < cluster; ++r) sum += s_part[r];
+      // shares' sums in order, one per lane (the same in every warp of every CTA)
+      const Df part = lane < cluster ? s_part[lane] : Df{0.f, 0.f};
+      const Df part_upto = df_warp_scan(part, lane), sum = df_shfl(part_upto, 31);
       if (op == 1) {  // the walk goes on with the new mass
         mass = sum;
         break;
       }
-      const bool usable = sum > 0.0 && sum <= 1e300;
-      if (!usable && attempt == 0) {  // nothing is left: the target's own row
-        S = 0.0;
-        qr = nullptr;
-        drops = 0;
-        if (cluster > 1) {  // the sums of this attempt have been read before they are written again
-          cluster_arrive();
-          cluster_wait();
-        } else {
-          __syncthreads();
+      if (!(sum.hi > 0.f && sum.hi <= 1e30f)) {
+        if (attempt == 0) {  // nothing is left: the target's own row
+          S = Df{0.f, 0.f};
+          qr = nullptr;
+          drops = 0;
+          if (cluster > 1) {  // the sums of this attempt have been read before they are written again
+            cluster_arrive();
+            cluster_wait();
+          } else {
+            __syncthreads();
+          }
+          continue;
         }
-        continue;
-      }
-      if (!usable) {
         if (rank == 0 && tid == 0) p.out_tokens[(size_t)b * N + s_cmd.count] = 0;
         return;
       }
-      // ---- draw: the CTA whose share holds the target value, then its tile, then the index
       if (wid != 0) return;
-      const double t = (double)p.uniforms[(size_t)b * N] * sum;
-      int owner = 0;
-      double before = 0.0, acc = 0.0;  // sum before the owner's share
-      bool found = false;
-      for (int r = 0; r < cluster; ++r) {
-        if (!found && s_part[r] > 0.0) {  // (the last share with weight if rounding leaves t beyond them all)
-          owner = r;
-          before = acc;
-          found = acc + s_part[r] > t;
+      // ---- draw: the first lane whose cumulative sum exceeds the target value, of the CTAs' shares, of runs of tiles,
+      // of the tiles of a run, of runs of 16 values, of those values.  Where rounding leaves the target beyond all
+      // sums, the last one with weight is taken.
+      Df t = df_times(sum, s_cmd.u);
+      auto first_over = [&](Df upto, bool some) {
+        uint32_t m = __ballot_sync(0xffffffffu, some && df_greater(upto, t));
+        if (m) return __ffs(m) - 1;
+        m = __ballot_sync(0xffffffffu, some);
+        return m ? 31 - __clz(m) : 0;
+      };
+      // moves the origin to the start of the range that lane `src` holds; `upto` are the lanes' inclusive sums
+      auto enter = [&](Df upto, int src) {
+        Df before = df_shfl_up1(upto);
+        if (lane == 0) before = Df{0.f, 0.f};
+        before = df_shfl(before, src);
+        t = df_add(t, Df{-before.hi, -before.lo});
+      };
+      int src = first_over(part_upto, part.hi > 0.f);
+      if (src != rank) return;
+      enter(part_upto, src);
+      const int run = (ntile + 31) / 32;
+      Df s = {0.f, 0.f};
+      for (int k = lane * run; k < min(ntile, lane * run + run); ++k) s = df_add(s, s_tile[k]);
+      Df upto = df_warp_scan(s, lane);
+      src = first_over(upto, s.hi > 0.f);
+      enter(upto, src);
+      int tile = src * run;
+      for (int k0 = tile;; k0 += 32) {  // (one round unless a share has over 1024 tiles)
+        const int k_hi = min(ntile, src * run + run);
+        s = k0 + lane < k_hi ? s_tile[k0 + lane] : Df{0.f, 0.f};
+        upto = df_warp_scan(s, lane);
+        const int f = first_over(upto, s.hi > 0.f);
+        const bool over = df_greater(df_shfl(upto, 31), t);
+        tile = k0 + f;
+        if (over || k0 + 32 >= k_hi) {
+          enter(upto, f);
+          break;
         }
-        acc += s_part[r];
+        const Df all = df_shfl(upto, 31);
+        t = df_add(t, Df{-all.hi, -all.lo});
       }
-      if (owner != rank) return;
-      // tiles, 32 lanes x a run of consecutive ones each
-      const int run = (ntile + 31) / 32, k_lo = min(ntile, lane * run), k_hi = min(ntile, k_lo + run);
-      double s = 0.0;
-      for (int k = k_lo; k < k_hi; ++k) s += s_tile[k];
-      const double s_in = warp_scan(s, lane);
-      uint32_t m = __ballot_sync(0xffffffffu, before + s_in > t && s > 0.0);
-      if (!m) {
-        m = __ballot_sync(0xffffffffu, s > 0.0);
-        m = m ? 1u << (31 - __clz(m)) : 1u;
-      }
-      const int src = __ffs(m) - 1;
-      int tile = 0;
-      double tb = 0.0;
-      if (lane == src) {
-        double a = before + s_in - s;
-        tile = k_lo;
-        tb = a;
-        for (int k = k_lo; k < k_hi; ++k) {
-          if (s_tile[k] > 0.0) {
-            tile = k;
-            tb = a;
-            if (a + s_tile[k] > t) break;
-          }
-          a += s_tile[k];
-        }
-      }
-      tile = __shfl_sync(0xffffffffu, tile, src);
-      tb = __shfl_sync(0xffffffffu, tb, src);
-      // the tile's 512 values, 16 consecutive ones per lane
-      const int v0 = v_lo + tile * kVerifyTile + 16 * lane;
-      double w[16];
-      s = 0.0;
+      const int v0 = v_lo + tile * kVerifyTile;
+      float pv[16], qv[16];
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        const int v = v0 + e;
-        w[e] = v < v_hi ? weight(v, pr[v], qr ? qr[v] : 0.f) : 0.0;
-        s += w[e];
+        const int v = v0 + 16 * lane + e;
+        pv[e] = v < v_hi ? pr[v] : 0.f;
+        qv[e] = qr && v < v_hi ? qr[v] : 0.f;
       }
-      const double e_in = warp_scan(s, lane);
-      m = __ballot_sync(0xffffffffu, tb + e_in > t && s > 0.0);
-      if (!m) {
-        m = __ballot_sync(0xffffffffu, s > 0.0);
-        m = m ? 1u << (31 - __clz(m)) : 1u;
-      }
-      if (lane == __ffs(m) - 1) {
-        double a = tb + e_in - s;
-        int pick = v0;
-        bool done = false;
+      s = Df{0.f, 0.f};
+      Df s1 = {0.f, 0.f};
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          if (!done && w[e] > 0.0) {
-            pick = v0 + e;
-            done = a + w[e] > t;
-          }
-          a += w[e];
-        }
-        p.out_tokens[(size_t)b * N + s_cmd.count] = min(pick, V - 1);
+      for (int e = 0; e < 16; e += 2) {
+        const int v = v0 + 16 * lane + e;
+        if (v < v_hi) add_to(s, weight(v, pv[e], qv[e]));
+        if (v + 1 < v_hi) add_to(s1, weight(v + 1, pv[e + 1], qv[e + 1]));
       }
+      s = df_add(s, s1);
+      upto = df_warp_scan(s, lane);
+      src = first_over(upto, s.hi > 0.f);
+      enter(upto, src);
+      const int run_lo = v0 + 16 * src, v = run_lo + lane;
+      s = lane < 16 && v < v_hi ? weight(v, pr[v], qr ? qr[v] : 0.f) : Df{0.f, 0.f};
+      src = first_over(df_warp_scan(s, lane), s.hi > 0.f);
+      if (lane == 0) p.out_tokens[(size_t)b * N + s_cmd.count] = min(run_lo + src, V - 1);
       return;
     }
     // (op 1) the next command is written by CTA 0 after it has read the sums; the other CTAs read theirs before
