@@ -19,6 +19,7 @@
 #include "chunk_tc_kernels.cuh"
 #include "chunk_tc2_kernels.cuh"
 #include "decode_kernels.cuh"
+#include "tree_kernels.cuh"
 
 namespace ooco {
 
@@ -415,12 +416,58 @@ static int launch_chunk_ncw(int ncw, const CUtensorMap& tk, const CUtensorMap& t
   }
 }
 
+// Query rows of tree attention: (64 dims, query head, query token of any sequence), one box = [Sq][G][64] at head_dim 128.
+static int encode_q_map(CUtensorMap* tm, const DecodeParams& p) {
+  EncodeTiledFn enc = encode_fn();
+  if (!enc) return fail_cuda("cudaGetDriverEntryPoint(cuTensorMapEncodeTiled)", -1);
+  cuuint64_t dims[3] = {128, (cuuint64_t)p.Hq, (cuuint64_t)p.B * p.Sq};
+  cuuint64_t strides[2] = {128 * 2, (cuuint64_t)p.Hq * 128 * 2};
+  cuuint32_t box[3] = {64, (cuuint32_t)p.G, (cuuint32_t)p.Sq};
+  cuuint32_t estr[3] = {1, 1, 1};
+  CUresult r = enc(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<__nv_bfloat16*>(p.q), dims, strides, box, estr,
+                   CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? OOCO_OK : fail_cuda("cuTensorMapEncodeTiled(queries)", (long)r);
+}
+
+// Tree attention of 17 to 96 score columns at head_dim 128: one persistent CTA per SM with the tokens on the M axis.
+template <int NC, bool KV8>
+static int launch_tree_tok(const CUtensorMap& tk, const CUtensorMap& tv, DecodeParams& p, const DeviceInfo& di,
+                           cudaStream_t st, int dev, bool dry) {
+  auto kern = tree_tok_kernel<NC, KV8>;
+  constexpr size_t smem = TokSmem<NC, KV8>::total();
+  if (smem > (size_t)di.smem_optin) return OOCO_E_UNSUPPORTED;
+  static std::atomic<int> configured[64];
+  if (dev < 0 || dev >= 64 || !configured[dev].load()) {
+    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e != cudaSuccess) return fail_cuda("cudaFuncSetAttribute(max dynamic smem)", (long)e);
+    if (dev >= 0 && dev < 64) configured[dev].store(1);
+  }
+  CUtensorMap tq;
+  if (int rc = encode_q_map(&tq, p)) return rc;
+  if (dry) return OOCO_OK;  // sizing and attributes only: the caller launches nothing before these have passed
+  cudaError_t e = launch_ex(kern, dim3(p.next_item_init), dim3(TokSmem<NC, KV8>::kWarps * 32), smem, st,
+                            g_knobs[kKnobPdl].load() != 0 && !tl_events_between_kernels, tk, tv, tq, p);
+  if (e == cudaSuccess) e = cudaGetLastError();
+  return e == cudaSuccess ? OOCO_OK : fail_cuda("launch of the tree attention kernel", (long)e);
+}
+template <bool KV8>
+static int launch_tree_tok_nc(const CUtensorMap& tk, const CUtensorMap& tv, DecodeParams& p, const DeviceInfo& di,
+                              cudaStream_t st, int dev, bool dry) {
+  if (p.GQ <= 32) return launch_tree_tok<32, KV8>(tk, tv, p, di, st, dev, dry);
+  if (p.GQ <= 48) return launch_tree_tok<48, KV8>(tk, tv, p, di, st, dev, dry);
+  if (p.GQ <= 64) return launch_tree_tok<64, KV8>(tk, tv, p, di, st, dev, dry);
+  return launch_tree_tok<96, KV8>(tk, tv, p, di, st, dev, dry);
+}
+
 // Tree attention: the decode shapes that the rules of decode_core pick without a knob, compiled with the tree's mask.
 // `tc` / `tc2`: the tcgen05 chunk kernels (head_dim 128).
 static int launch_tree(int head_dim, bool kv8, bool chunk, bool tc2, bool row16, int ncw, const CUtensorMap& tk,
                        const CUtensorMap& tv, DecodeParams& p, const DeviceInfo& di, int cps, cudaStream_t st, int dev,
                        bool dry) {
   if (chunk && head_dim == 128) {
+    if (p.GQ <= kTokMaxColumns)
+      return kv8 ? launch_tree_tok_nc<true>(tk, tv, p, di, st, dev, dry) : launch_tree_tok_nc<false>(tk, tv, p, di, st, dev, dry);
     if (tc2)
       return kv8 ? launch_chunk_tc2<true, true>(tk, tv, p, di, st, dev, dry)
                  : launch_chunk_tc2<false, true>(tk, tv, p, di, st, dev, dry);
@@ -823,7 +870,8 @@ static int decode_core(const ooco_shape_t* s, const void* q, const void* k_cache
   p.items_per_cta = plan_items_per_cta(G_);
   // the 8-bit path widens codes to value / 256 (kE4m3WidenFactor): both scales carry the factor back (K's only
   // where K is widened: the tcgen05 score path multiplies the codes' own values)
-  const bool kv8_tc = kv8 && !chunk && ncw == 8 && (tree || g_knobs[kKnobKv8Tcgen05].load() != 0);
+  const bool kv8_tc = (kv8 && tree && chunk && G_ <= kTokMaxColumns) ||
+                      (kv8 && !chunk && ncw == 8 && (tree || g_knobs[kKnobKv8Tcgen05].load() != 0));
   p.scale_log2e = scale * 1.4426950408889634f * (kv8 ? kv8->k_scale * (kv8_tc ? 1.f : kE4m3WidenFactor) : 1.f);
   p.v_scale = kv8 ? kv8->v_scale * kE4m3WidenFactor : 1.f;
   if (tree) {
