@@ -69,9 +69,9 @@ struct TokSmem {
   __host__ __device__ static constexpr size_t total() {
     return 1024 + (size_t)(QB + (KV8 ? 1 : 0)) * kQBytes + 2 * PB * (size_t)kPBytes + (size_t)(NK + NV) * kLandBytes +
            (KV8 ? (size_t)NW * kTc2SlotBytes : 0) + kTokMeta * 32 + kTokDesc * sizeof(VStageDesc) + kTokUnits * 16 +
-           kColumnBytes + kScratchBytes + 592;
+           kColumnBytes + kScratchBytes + 608;
   }
-  static_assert(kPBytes >= NC * 10 * 4, "scratch in a weight buffer");
+  static_assert(kPBytes >= NC * 10 * 4 && (kOwnScratch || PB == 1), "scratch in a weight buffer");
   static constexpr size_t kMost = 227 * 1024;  // shared memory of a CTA
 };
 
@@ -163,10 +163,12 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
   const uint32_t s_bar = (s_scr + (uint32_t)L::kScratchBytes + 7u) & ~7u;
   const uint32_t s_kfull = s_bar;                    // [NK] K has landed                              (TMA)
   const uint32_t s_kempty = s_kfull + NK * 8;        // [NK] the score MMAs that read it are complete  (commit)
-  const uint32_t s_vland = s_kempty + NK * 8;        // [NV] V has landed                              (TMA)
-  const uint32_t s_vtaken = s_vland + NV * 8;        // [NV] it may be overwritten                     (commit / widening threads)
-  const uint32_t s_wfull = s_vtaken + NV * 8;        // KV8 [NW] the widened slot is written           (widening threads)
-  const uint32_t s_wempty = s_wfull + NW * 8;        // KV8 [NW] the P.V MMAs that read it are complete (commit)
+  // (V has landed, V is widened: twice as many barriers as slots, of which stage n takes number n % (2 slots).  So a barrier
+  // is one pipeline's, which sees each of its phases; one per slot could be two phases behind, and let a wait through.)
+  const uint32_t s_vland = s_kempty + NK * 8;        // [2 NV] V has landed                            (TMA)
+  const uint32_t s_vtaken = s_vland + 2 * NV * 8;    // [NV] it may be overwritten                     (commit / widening threads)
+  const uint32_t s_wfull = s_vtaken + NV * 8;        // KV8 [2 NW] the widened slot is written         (widening threads)
+  const uint32_t s_wempty = s_wfull + 2 * NW * 8;    // KV8 [NW] the P.V MMAs that read it are complete (commit)
   const uint32_t s_vdfull = s_wempty + NW * 8;       // [kTokDesc] the stage's V descriptor is posted
   const uint32_t s_mfull = s_vdfull + kTokDesc * 8;  // [kTokMeta] the stage's meta words are posted
   const uint32_t s_qready = s_mfull + kTokMeta * 8;  // [2] the unit's query tile is written           (TMA / widening threads)
@@ -197,14 +199,10 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
       mbar_init(s_kfull + 8 * i, 1);
       mbar_init(s_kempty + 8 * i, 1);
     }
-    for (int i = 0; i < NV; ++i) {
-      mbar_init(s_vland + 8 * i, 1);
-      mbar_init(s_vtaken + 8 * i, KV8 ? L::kWiden : 1);
-    }
-    for (int i = 0; i < NW; ++i) {
-      mbar_init(s_wfull + 8 * i, L::kWiden);
-      mbar_init(s_wempty + 8 * i, 1);
-    }
+    for (int i = 0; i < 2 * NV; ++i) mbar_init(s_vland + 8 * i, 1);
+    for (int i = 0; i < NV; ++i) mbar_init(s_vtaken + 8 * i, KV8 ? L::kWiden : 1);
+    for (int i = 0; i < 2 * NW; ++i) mbar_init(s_wfull + 8 * i, L::kWiden);
+    for (int i = 0; i < NW; ++i) mbar_init(s_wempty + 8 * i, 1);
     for (int i = 0; i < kTokDesc; ++i) mbar_init(s_vdfull + 8 * i, 1);
     for (int i = 0; i < kTokMeta; ++i) mbar_init(s_mfull + 8 * i, 1);
     for (int i = 0; i < 2; ++i) {
@@ -433,7 +431,7 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
         ok = false;
         break;
       }
-      const uint32_t vland = s_vland + 8 * vs;
+      const uint32_t vland = s_vland + 8 * (it % (2 * NV));
       if (nbox == 0) {  // a stage without tokens
         if (lane == 0) mbar_arrive(vland);
         continue;
@@ -451,7 +449,7 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
       int dummy_abort = 0;
       for (int k = 0; k < (it < NV ? it : NV); ++k) {
         const int j = it - 1 - k;
-        mbar_wait_bounded(s_vland + 8 * (j % NV), (uint32_t)(j / NV) & 1u, &dummy_abort, kWaitLimitNs / 8);
+        mbar_wait_bounded(s_vland + 8 * (j % (2 * NV)), (uint32_t)(j / (2 * NV)) & 1u, &dummy_abort, kWaitLimitNs / 8);
       }
     }
   } else if (warp == kWarpM || warp == kWarpM + 1) {
@@ -480,7 +478,7 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
             const int4 meta = g_meta[2 * ms];
             const int unit = g_meta[2 * ms + 1].w;
             if (meta.x < 0 || ((i < SB || now(sfree, spar)) &&
-                               ((meta.w & 0xffff) == 0 || !((meta.w >> 16) & 1) || now(s_qready + 8 * (unit % QB), (uint32_t)(unit / QB) & 1u))))
+                               (!((meta.w >> 16) & 1) || now(s_qready + 8 * (unit % QB), (uint32_t)(unit / QB) & 1u))))
               break;
           }
           if (now(s_pready + 8 * (2 * t + j % PB), (j / PB) & 1u)) {
@@ -506,8 +504,9 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
         const int ntok = meta.w & 0xffff;
         const bool first = (meta.w >> 16) & 1, last = (meta.w >> 17) & 1;
         const int qb = meta2.w % QB;
+        // (a stage without tokens waits for its unit's query rows, too: the arrivals at s_qfree below count for that unit)
         if ((i >= SB && !tok_wait(sfree, spar, s_abort)) ||
-            (ntok > 0 && first && !tok_wait(s_qready + 8 * qb, (uint32_t)(meta2.w / QB) & 1u, s_abort))) {
+            (first && !tok_wait(s_qready + 8 * qb, (uint32_t)(meta2.w / QB) & 1u, s_abort))) {
           ok = false;
           break;
         }
@@ -540,7 +539,7 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
         } else if (lane == 0) {  // the turn of the barriers is taken all the same
           mbar_arrive(sready);
           mbar_arrive(s_kempty + 8 * ks);
-          if (last) mbar_arrive(s_qfree + 8 * qb);
+          if (last) umma_commit(s_qfree + 8 * qb);  // the pipeline's scores of the stage before may still be on their way
         }
         __syncwarp();
         ++i;
@@ -551,7 +550,7 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
         const int unit = g_meta[2 * (m % kTokMeta) + 1].w;
         const bool some = (meta.w & 0xffff) > 0, first = (meta.w >> 16) & 1;
         // (a unit's first P.V overwrites the accumulator that the softmax warps read at the end of the unit before)
-        if (!tok_wait((KV8 ? s_wfull : s_vland) + 8 * vs, (m / ring) & 1u, s_abort) ||
+        if (!tok_wait((KV8 ? s_wfull : s_vland) + 8 * (m % (2 * ring)), (m / (2 * ring)) & 1u, s_abort) ||
             !tok_wait(s_pready + 8 * (2 * t + j % PB), (j / PB) & 1u, s_abort) ||
             (some && first && unit > 0 && !tok_wait(s_ofree, (uint32_t)(unit - 1) & 1u, s_abort))) {
           ok = false;
@@ -635,7 +634,7 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
         ++u;
       }
       // ---- V codes to f16, as in chunk_tc2_kernel: exact, to value / 256; 1024 units of 16 codes, eight per thread
-      if (!tok_wait(s_vland + 8 * vs, (n / NV) & 1u, s_abort) ||
+      if (!tok_wait(s_vland + 8 * (n % (2 * NV)), (n / (2 * NV)) & 1u, s_abort) ||
           !tok_wait(s_wempty + 8 * ws, ((n / NW) & 1u) ^ 1u, s_abort)) {
         ok = false;
         break;
@@ -666,7 +665,7 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
         }
         fence_proxy_async_smem();  // the widened slot is read by the MMAs through the async proxy
       }
-      mbar_arrive(s_wfull + 8 * ws);
+      mbar_arrive(s_wfull + 8 * (n % (2 * NW)));
       mbar_arrive(s_vtaken + 8 * vs);
     }
     if (!ok && lane == 0) atomicOr(&p.hdr->status, kStatusWaitTimeout);
@@ -914,10 +913,15 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
         ok = false;
         break;
       }
+      // (without an exchange of its own the finish of a unit uses the weight buffer: it comes first)
+      if (!L::kOwnScratch && unit_open && !finish_unit(open_sums)) {
+        ok = false;
+        break;
+      }
       uint8_t* prow = gen + (s_p - base) + (size_t)(t * PB + i % PB) * L::kPBytes + (size_t)r * 128;  // this token's weights
       const float* sum_in = sum_s + (sum_set * 8 + warp) * NC;
       float* sum_out = sum_s + ((sum_set ^ 1) * 8 + warp) * NC;
-      for (bool formed = ntok == 0;;) {
+      for (bool formed = ntok == 0, raised = false;;) {
         if (!formed && !refs_due) {
           // ---- weights: 2^(score * factor - reference), into the second MMA's operand, and the warp's sums of them
           float top = -INFINITY;  // largest exponent
@@ -960,7 +964,7 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
             const int c = 16 * cc + (lane >> 1);
             if (!(lane & 1)) sum_out[c] = w[0] + (first ? 0.f : sum_in[c]);
           }
-          refs_due = wg_any(top > kTokRaise<KV8>);
+          refs_due = wg_any(top > kTokRaise<KV8> && !raised);  // (once: the rounding of the two comparisons may differ)
           if (!vote_ok) {
             ok = false;
             break;
@@ -972,7 +976,7 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
           }
         }
         if (!values_seen) {  // a unit that ended is written now
-          if (!wait_values(1) || (unit_open && !finish_unit(open_sums))) {
+          if (!wait_values(1) || (L::kOwnScratch && unit_open && !finish_unit(open_sums))) {
             ok = false;
             break;
           }
@@ -1049,6 +1053,7 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
           }
         }
         refs_due = false;
+        raised = true;
       }
       if (!ok || end) break;
       if (ntok > 0) {
@@ -1057,7 +1062,7 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
         if (ntok < TOK) {
           // V rows beyond the stage's tokens may hold anything (NaN included): clear them once the slot is written
           const int ring = KV8 ? NW : NV, vs = n % ring;
-          if (!tok_wait((KV8 ? s_wfull : s_vland) + 8 * vs, (n / ring) & 1u, s_abort)) {
+          if (!tok_wait((KV8 ? s_wfull : s_vland) + 8 * (n % (2 * ring)), (n / (2 * ring)) & 1u, s_abort)) {
             ok = false;
             break;
           }

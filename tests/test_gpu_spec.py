@@ -384,6 +384,36 @@ def test_tree_attention_chain_is_causal_attention():
         assert bool((got.view(torch.int16) == out.view(torch.int16)).all()), N
 
 
+@pytest.mark.parametrize("fp8", [None, (0.02, 0.03)], ids=["bf16", "fp8"])
+@pytest.mark.parametrize("hq,N", [(16, 9), (40, 8), (32, 16), (48, 16)])
+def test_tree_attention_many_short_units(hq, N, fp8):
+    """Several units of one to three stages of 128 tokens per CTA: odd counts leave one of its two pipelines without tokens
+    at a unit's end, single stages for the whole unit, again and again."""
+    rng = np.random.default_rng(hq * N)
+    lens = [int(x) for x in rng.integers(N, 385, 56)] + [128, 129, 256, 257, 384, 1, 0, 16]
+    c = tree_case(lens, hq, 8, 128, 16, N, seed=N, fp8=fp8, sigma=0.7, sizes=[N if i % 3 else 1 + i % N for i in range(64)])
+    first = both(c, seqs=[0, 7, 20, 41, 56, 57, 58, 59, 60, 61, 62, 63])
+    ws = torch.full((spec.tree_workspace_bytes(c["shape"], c["N"]),), 255, dtype=torch.uint8, device=DEV)
+    for _ in range(20):
+        assert torch.equal(run_tree(c, ws=ws).view(torch.int16), first.view(torch.int16))
+
+
+@pytest.mark.parametrize("fp8", [None, (0.02, 0.03)], ids=["bf16", "fp8"])
+@pytest.mark.parametrize("hq,N", [(16, 2), (32, 4), (16, 9), (48, 8), (48, 16), (64, 16)])
+def test_tree_attention_scores_far_apart(hq, N, fp8):
+    """Scores of hundreds, whose running maximum rises again and again by more than the weights' types can hold."""
+    c = tree_case([N, 200, 700, 1500], hq, 8, 128, 16, N, seed=N + hq, fp8=fp8, sigma=1.0)
+    for x in (c["q"],):
+        x.mul_(torch.logspace(-1, 1.3, x.shape[2], device=DEV)[None, None, :, None])
+    ramp = torch.linspace(0.05, 1.0, c["k"].shape[0], device=DEV)[:, None, None, None]
+    if fp8:
+        k = c["k"].view(E4M3).float()
+        c["k"] = (k * ramp).to(E4M3).view(torch.uint8)
+    else:
+        c["k"] = c["k"] * ramp.to(torch.bfloat16)
+    both(c)
+
+
 def test_tree_attention_random_shapes():
     rng = np.random.default_rng(99)
     for i in range(24):
