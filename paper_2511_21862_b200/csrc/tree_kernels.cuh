@@ -32,46 +32,38 @@
 // Every wait is bounded; a wait that gives up sets the status bit and the CTA's abort flag, every warp falls through to
 // the common exit, and the tensor memory is released after the MMAs in flight.
 #pragma once
+#include <type_traits>
+
 #include "chunk_tc2_kernels.cuh"
 
 namespace ooco {
 
-constexpr int kTokMeta = 8, kTokDesc = 8, kTokUnits = 4;  // ring sizes: meta words, V descriptors, units
-constexpr int kTokMaxColumns = 96;                          // score columns the kernel is built for
-// A reference is raised when a score passes it by this much (log2 units).  Weights stay below 2^16 for f16 (the 8-bit cache),
-// where small ones lose bits below 2^-14; bf16 has the range of fp32, and a column's sum stays below 2^60 times its tokens.
-template <bool KV8>
-constexpr float kTokRaise = KV8 ? 14.f : 60.f;
+constexpr int kTokMeta = 8, kTokDesc = 8;  // ring sizes: meta words, V descriptors
+constexpr int kTokMaxColumns = 64;         // score columns the kernel is built for
+// A reference is raised when a score passes it by this much (log2 units): weights stay below 2^16 for f16, where small ones
+// lose bits below 2^-14.
+constexpr float kTokRaise = 14.f;
 
-template <int NC, bool KV8>
+template <int NC>
 struct TokSmem {
-  static constexpr int QB = !KV8 && NC <= 48 ? 2 : 1;                       // query tiles
-  static constexpr int SB = NC <= 64 ? 2 : 1;                               // score buffers of a pipeline
-  static constexpr int PB = KV8 && NC <= 48 ? 2 : 1;                        // weight buffers of a pipeline
+  static constexpr int SB = NC <= 48 ? 2 : 1;                               // score buffers of a pipeline
+  static constexpr int PB = NC <= 48 ? 2 : 1;                               // weight buffers of a pipeline
   static constexpr int kQBytes = NC * 256;                                  // [2][NC rows][128 bytes]
-  static constexpr int kPBytes = (NC + 63) / 64 * 128 * 128;                // [NC / 64][128 tok][64 columns] 16-bit
-  static constexpr int kLandBytes = KV8 ? kTc2RawSlotBytes : kTc2SlotBytes; // K (or V) of one stage as TMA writes it
-  // K slots, V slots, widened V slots.  A V slot is taken for longer (until the softmax and P.V are done), so V gets more
-  // (3 K and 2 V slots: a stage took 2200 cycles of waiting for V).
-  static constexpr int NK = 2, NV = NC <= 64 && PB == 1 ? 3 : 2, NW = NC <= 64 ? 2 : 1;
-  static constexpr int kWiden = 128;                                        // widening threads
-  static constexpr int kWarps = KV8 ? 16 : 12;
+  static constexpr int kPBytes = 128 * 128;                                 // [128 tok][64 columns] f16
+  static constexpr int kLandBytes = kTc2RawSlotBytes;                       // K (or V) of one stage as TMA writes it
+  static constexpr int NK = 2, NV = PB == 1 ? 3 : 2, NW = 2;                // K slots, V slots, widened V slots
+  static constexpr int kWarps = 16;
+  // tensor memory: scores [2 pipelines][SB], values [2], sums [2], the operand of ones
   static constexpr int kTmemCols = 512;
-  static constexpr int kColStride = NC <= 32 ? 32 : (NC <= 64 ? 64 : 128);  // tensor-memory columns of a buffer
-  static constexpr int kScoreCols = 2 * SB * kColStride;                    // O_t at column kScoreCols + t * kColStride
-  static_assert(kScoreCols + 2 * kColStride <= kTmemCols, "tensor memory");
-  // per column: factors and references of both pipelines, factors of the unit, the warps' sums (two sets)
-  static constexpr int kColumnBytes = NC * (2 * 8 + QB * 4 + 2 * 8 * 4);
-  // what the pipelines exchange when a unit ends: sums of the 8 warps and references, 10 floats per column; two sets take
-  // turns, or, where shared memory is short, one in pipeline 0's weight buffer
-  static constexpr bool kOwnScratch = NC <= 64;
-  static constexpr int kScratchBytes = kOwnScratch ? 2 * 10 * NC * 4 : 0;
+  static constexpr int kColO = 2 * SB * NC, kColL = kColO + 2 * NC, kColOne = kColL + 2 * NC;
+  static_assert(kColOne + 8 <= kTmemCols, "tensor memory");
+  // per column: factors and references of both pipelines, factors of the unit, the warps' maxima, factors of a rescaling,
+  // the references at a unit's end (two sets take turns)
+  static constexpr int kColumnBytes = NC * (2 * 8 + 4 + 2 * 4 * 4 + 2 * 4 + 4 * 4);
   __host__ __device__ static constexpr size_t total() {
-    return 1024 + (size_t)(QB + (KV8 ? 1 : 0)) * kQBytes + 2 * PB * (size_t)kPBytes + (size_t)(NK + NV) * kLandBytes +
-           (KV8 ? (size_t)NW * kTc2SlotBytes : 0) + kTokMeta * 32 + kTokDesc * sizeof(VStageDesc) + kTokUnits * 16 +
-           kColumnBytes + kScratchBytes + 608;
+    return 1024 + 2 * (size_t)kQBytes + 2 * PB * (size_t)kPBytes + (size_t)(NK + NV) * kLandBytes +
+           (size_t)NW * kTc2SlotBytes + kTokMeta * 32 + kTokDesc * sizeof(VStageDesc) + kColumnBytes + 608;
   }
-  static_assert(kPBytes >= NC * 10 * 4 && (kOwnScratch || PB == 1), "scratch in a weight buffer");
   static constexpr size_t kMost = 227 * 1024;  // shared memory of a CTA
 };
 
@@ -84,22 +76,6 @@ __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
       : "r"(taddr));
 }
 
-// Sum (or maximum) over the warp's lanes of 32 values each: lane L gets that of v[L] (a butterfly that halves the values
-// it carries at every step: 31 shuffles in place of 160).
-template <bool kMax>
-__device__ __forceinline__ float warp_transpose(float (&v)[32], int lane) {
-#pragma unroll
-  for (int o = 16; o; o >>= 1) {
-    const bool up = lane & o;
-#pragma unroll
-    for (int i = 0; i < o; ++i) {
-      const float keep = up ? v[i + o] : v[i], send = up ? v[i] : v[i + o];
-      const float got = __shfl_xor_sync(0xffffffffu, send, o);
-      v[i] = kMax ? fmaxf(keep, got) : keep + got;
-    }
-  }
-  return v[0];
-}
 // Whether the barrier's phase of parity `parity` is complete, without waiting for it.
 __device__ __forceinline__ bool mbar_test_wait(uint32_t bar, uint32_t parity) {
   uint32_t ok;
@@ -114,10 +90,31 @@ __device__ __forceinline__ bool mbar_test_wait(uint32_t bar, uint32_t parity) {
 }
 // warp_wait out of line: the kernel has dozens of waits, and its code has to fit the instruction cache.
 __device__ __noinline__ bool tok_wait_slow(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
-  return mbar_wait_bounded(bar, parity, abort_flag, kWaitLimitNs);
+  uint64_t t0 = 0;  // (reading the clock takes some hundred cycles: not before it is a long wait)
+  for (;;) {
+#pragma unroll 1
+    for (int i = 0; i < 64; ++i)
+      if (mbar_try_wait(bar, parity)) return true;
+    if (*abort_flag) return false;
+    const uint64_t now = globaltimer_ns();
+    if (t0 == 0) t0 = now;
+    if (now - t0 > kWaitLimitNs) {
+      *abort_flag = 1;
+      return false;
+    }
+  }
 }
 __device__ __forceinline__ bool tok_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
   return __all_sync(0xffffffffu, mbar_try_wait(bar, parity) || tok_wait_slow(bar, parity, abort_flag));
+}
+__device__ __forceinline__ void tmem_st8(uint32_t taddr, uint32_t v) {  // the same word into 8 columns
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%1,%1,%1,%1,%1,%1,%1};" ::"r"(taddr), "r"(v));
+}
+// True in one lane of the converged warp, always the same.
+__device__ __forceinline__ bool elect_one() {
+  uint32_t yes;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(yes));
+  return yes != 0;
 }
 __device__ __forceinline__ float warp_max(float v) {
   float r;
@@ -133,61 +130,60 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const void* tmap, uint
       : "memory");
 }
 
-template <int NC, bool KV8>
-__global__ void __launch_bounds__(TokSmem<NC, KV8>::kWarps * 32, 1)
+template <int NC>
+__global__ void __launch_bounds__(TokSmem<NC>::kWarps * 32, 1)
 tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
                 const __grid_constant__ CUtensorMap tm_q, const DecodeParams p) {
-  using L = TokSmem<NC, KV8>;
-  constexpr int D = 128, TOK = kTc2StageTok, NCH = (NC + 31) / 32;
-  constexpr int QB = L::QB, SB = L::SB, PB = L::PB, NK = L::NK, NV = L::NV, NW = L::NW;
+  using L = TokSmem<NC>;
+  constexpr int D = 128, TOK = kTc2StageTok;
+  constexpr int SB = L::SB, PB = L::PB, NK = L::NK, NV = L::NV, NW = L::NW;
   constexpr int kWarpK = 8, kWarpV = 9, kWarpM = 10, kWarpX = 12;
   static_assert(L::total() <= L::kMost, "shared memory");
-  static_assert(NC % 16 == 0 && NC <= 96, "columns of an MMA with M = 128, and what shared memory holds");
+  static_assert(NC % 16 == 0 && NC <= 64, "columns of an MMA with M = 128, and what shared memory holds");
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw);
   const uint32_t base = (raw + 1023u) & ~1023u;
   uint8_t* gen = smem_raw + (base - raw);
-  const uint32_t s_q = base;                                             // [QB] query tiles
-  const uint32_t s_qraw = s_q + (uint32_t)QB * L::kQBytes;               // KV8: the unit's query rows in bf16
-  const uint32_t s_p = s_qraw + (KV8 ? (uint32_t)L::kQBytes : 0u);       // [2 pipelines][PB] weights
+  const uint32_t s_q = base;                                             // the unit's query rows as two terms
+  const uint32_t s_qraw = s_q + (uint32_t)L::kQBytes;                    // ... in bf16
+  const uint32_t s_p = s_qraw + (uint32_t)L::kQBytes;                    // [2 pipelines][PB] weights
   const uint32_t s_k = s_p + 2u * PB * L::kPBytes;                       // [NK] K slots
   const uint32_t s_v = s_k + (uint32_t)NK * L::kLandBytes;               // [NV] V slots
-  const uint32_t s_w = s_v + (uint32_t)NV * L::kLandBytes;               // KV8: [NW] widened V slots
-  const uint32_t s_meta = s_w + (KV8 ? (uint32_t)NW * kTc2SlotBytes : 0u);  // [kTokMeta] two int4
+  const uint32_t s_w = s_v + (uint32_t)NV * L::kLandBytes;               // [NW] widened V slots
+  const uint32_t s_meta = s_w + (uint32_t)NW * kTc2SlotBytes;            // [kTokMeta] two int4
   const uint32_t s_vdesc = s_meta + kTokMeta * 32;                       // [kTokDesc] VStageDesc
-  const uint32_t s_unit = s_vdesc + kTokDesc * (uint32_t)sizeof(VStageDesc);  // [kTokUnits] int4 {sequence, kv head, -, -}
-  const uint32_t s_cr = s_unit + kTokUnits * 16;                         // [2][NC / 2] {score factors, -references} of column pairs
-  const uint32_t s_mul = s_cr + 2u * NC * 8;                             // [QB][NC] score factor of the unit's columns
-  const uint32_t s_sum = s_mul + (uint32_t)QB * NC * 4;                  // [2][8 warps][NC] sums of the warps' weights
-  const uint32_t s_scr = s_sum + 2u * 8 * NC * 4;                        // [2][10][NC] exchange at a unit's end
-  const uint32_t s_bar = (s_scr + (uint32_t)L::kScratchBytes + 7u) & ~7u;
+  const uint32_t s_cr = s_vdesc + kTokDesc * (uint32_t)sizeof(VStageDesc);  // [2][NC / 2] {score factors, -references} of column pairs
+  const uint32_t s_mul = s_cr + 2u * NC * 8;                             // [NC] score factor of the unit's columns
+  const uint32_t s_max = s_mul + NC * 4;                                 // [2][4 warps][NC] maxima
+  const uint32_t s_alpha = s_max + 2u * 4 * NC * 4;                      // [2][NC] factors of a rescaling
+  const uint32_t s_ref = s_alpha + 2u * NC * 4;                          // [2 sets][2][NC] references at a unit's end
+  const uint32_t s_bar = (s_ref + 4u * NC * 4 + 7u) & ~7u;
   const uint32_t s_kfull = s_bar;                    // [NK] K has landed                              (TMA)
   const uint32_t s_kempty = s_kfull + NK * 8;        // [NK] the score MMAs that read it are complete  (commit)
   // (V has landed, V is widened: twice as many barriers as slots, of which stage n takes number n % (2 slots).  So a barrier
   // is one pipeline's, which sees each of its phases; one per slot could be two phases behind, and let a wait through.)
   const uint32_t s_vland = s_kempty + NK * 8;        // [2 NV] V has landed                            (TMA)
-  const uint32_t s_vtaken = s_vland + 2 * NV * 8;    // [NV] it may be overwritten                     (commit / widening threads)
-  const uint32_t s_wfull = s_vtaken + NV * 8;        // KV8 [2 NW] the widened slot is written         (widening threads)
-  const uint32_t s_wempty = s_wfull + 2 * NW * 8;    // KV8 [NW] the P.V MMAs that read it are complete (commit)
+  const uint32_t s_vtaken = s_vland + 2 * NV * 8;    // [NV] it may be overwritten                     (widening threads)
+  const uint32_t s_wfull = s_vtaken + NV * 8;        // [2 NW] the widened slot is written         (widening threads)
+  const uint32_t s_wempty = s_wfull + 2 * NW * 8;    // [NW] the P.V MMAs that read it are complete (commit)
   const uint32_t s_vdfull = s_wempty + NW * 8;       // [kTokDesc] the stage's V descriptor is posted
   const uint32_t s_mfull = s_vdfull + kTokDesc * 8;  // [kTokMeta] the stage's meta words are posted
-  const uint32_t s_qready = s_mfull + kTokMeta * 8;  // [2] the unit's query tile is written           (TMA / widening threads)
-  const uint32_t s_qfree = s_qready + 16;            // [2] ... may be overwritten: both pipelines' last score MMAs are
+  const uint32_t s_qready = s_mfull + kTokMeta * 8;  // the unit's query tile is written              (widening threads)
+  const uint32_t s_qfree = s_qready + 8;             // ... may be overwritten: both pipelines' last score MMAs are
                                                      //     complete, both have read the columns' factors (4)
-  const uint32_t s_sready = s_qfree + 16;            // [2 pipelines][2] the scores are in tensor memory (commit)
-  const uint32_t s_sfree = s_sready + 32;            // [2][2] ... have been read                      (128 threads)
-  const uint32_t s_pready = s_sfree + 32;            // [2][2] weights written, O rescaled, V rows clean (128 threads)
+  const uint32_t s_sready = s_qfree + 8;             // [2 pipelines][2] the scores are in tensor memory (commit)
+  const uint32_t s_sfree = s_sready + 32;            // [2][2] ... have been read                      (4 warps)
+  const uint32_t s_pready = s_sfree + 32;            // [2][2] weights written, O rescaled, V rows clean (4 warps)
   const uint32_t s_pvdone = s_pready + 32;           // [2][2] the stage's P.V is complete             (commit)
   const uint32_t s_wg = s_pvdone + 32;               // [2] the four warps of a pipeline meet          (4)
   const uint32_t s_both = s_wg + 16;                 // [1] the softmax warps of both pipelines meet   (8)
-  const uint32_t s_qland = s_both + 8;               // KV8: the unit's bf16 query rows have landed     (TMA)
-  const uint32_t s_qtaken = s_qland + 8;             // KV8: ... have been split                       (widening threads)
+  const uint32_t s_qland = s_both + 8;               // the unit's bf16 query rows have landed         (TMA)
+  const uint32_t s_qtaken = s_qland + 8;             // ... have been split                            (widening threads)
   const uint32_t s_ofree = s_qtaken + 8;             // the unit's accumulators have been read               (8 warps)
   const uint32_t s_drain = s_ofree + 8;              // [2]
   const uint32_t s_slot = s_drain + 16;              // tensor-memory base, abort flag, votes [2 pipelines][2][4 warps]
   int4* g_meta = reinterpret_cast<int4*>(gen + (s_meta - base));
   VStageDesc* g_vdesc = reinterpret_cast<VStageDesc*>(gen + (s_vdesc - base));
-  int4* g_unit = reinterpret_cast<int4*>(gen + (s_unit - base));
   volatile uint32_t* g_slot = reinterpret_cast<volatile uint32_t*>(gen + (s_slot - base));
   volatile int* s_abort = reinterpret_cast<volatile int*>(gen + (s_slot + 4 - base));
   volatile int* g_vote = reinterpret_cast<volatile int*>(gen + (s_slot + 8 - base));
@@ -200,27 +196,27 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
       mbar_init(s_kempty + 8 * i, 1);
     }
     for (int i = 0; i < 2 * NV; ++i) mbar_init(s_vland + 8 * i, 1);
-    for (int i = 0; i < NV; ++i) mbar_init(s_vtaken + 8 * i, KV8 ? L::kWiden : 1);
-    for (int i = 0; i < 2 * NW; ++i) mbar_init(s_wfull + 8 * i, L::kWiden);
+    for (int i = 0; i < NV; ++i) mbar_init(s_vtaken + 8 * i, 4);
+    for (int i = 0; i < 2 * NW; ++i) mbar_init(s_wfull + 8 * i, 4);
     for (int i = 0; i < NW; ++i) mbar_init(s_wempty + 8 * i, 1);
     for (int i = 0; i < kTokDesc; ++i) mbar_init(s_vdfull + 8 * i, 1);
     for (int i = 0; i < kTokMeta; ++i) mbar_init(s_mfull + 8 * i, 1);
     for (int i = 0; i < 2; ++i) {
-      mbar_init(s_qready + 8 * i, KV8 ? L::kWiden : 1);
-      mbar_init(s_qfree + 8 * i, 4);
       mbar_init(s_wg + 8 * i, 4);
       mbar_init(s_drain + 8 * i, 1);
     }
     for (int i = 0; i < 4; ++i) {
       mbar_init(s_sready + 8 * i, 1);
-      mbar_init(s_sfree + 8 * i, 128);
-      mbar_init(s_pready + 8 * i, 128);
+      mbar_init(s_sfree + 8 * i, 4);
+      mbar_init(s_pready + 8 * i, 4);
       mbar_init(s_pvdone + 8 * i, 1);
     }
+    mbar_init(s_qready, 4);
+    mbar_init(s_qfree, 4);
     mbar_init(s_both, 8);
     mbar_init(s_ofree, 8);
     mbar_init(s_qland, 1);
-    mbar_init(s_qtaken, L::kWiden);
+    mbar_init(s_qtaken, 4);
     fence_mbar_init();
   }
   // query rows of columns that do not exist are never copied: zero, so that their scores are
@@ -232,6 +228,13 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
   __syncthreads();
   tc_fence_after_sync();
   const uint32_t tmem = *g_slot;
+  if (warp < 4) {  // the operand that sums the weights: ones, f16
+    tmem_st8(tmem + ((uint32_t)(32 * warp) << 16) + L::kColOne, 0x3c003c00u);
+    tmem_st_wait();
+  }
+  tc_fence_before_sync();
+  __syncthreads();
+  tc_fence_after_sync();
   grid_dep_wait();    // the plan must have completed
   grid_dep_launch();  // the merge kernel may queue up behind this grid
 
@@ -253,43 +256,10 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
       const int v = *e;
       return checked(chk_table_entry(v, p.NB), &p.hdr->status, kStatusBadTableEntry) ? v : p.NB;
     };
-    int uq = 0;  // units whose query rows have been copied (16-bit cache)
-    // Copies the query rows of the next unit as soon as its tile is free.  Score column (query token qi, head g) is row
-    // qi * G + g of the operand tile: per 64-dim half a box of [Sq][G][64 dims], swizzled like K.
-    auto copy_queries = [&]() {
-      while (!KV8 && uq < u) {
-        const int qb = uq % QB;
-        if (!__all_sync(0xffffffffu, mbar_test_wait(s_qfree + 8 * qb, ((uint32_t)(uq / QB) & 1u) ^ 1u))) return;
-        if (lane == 0) {
-          const int4 unit = g_unit[uq % kTokUnits];
-          const uint32_t dst = s_q + (uint32_t)qb * L::kQBytes, bar = s_qready + 8 * qb;
-          mbar_arrive_expect_tx(bar, 2u * (uint32_t)p.GQ * 128u);
-          tma_load_3d(dst, &tm_q, bar, 0, unit.y * p.G, unit.x * p.Sq);
-          tma_load_3d(dst + NC * 128, &tm_q, bar, 64, unit.y * p.G, unit.x * p.Sq);
-        }
-        __syncwarp();
-        ++uq;
-      }
-    };
-    // Waits (bounded) for stage `it`'s K slot.  The scores that free it may be waiting for query rows, whose tile is freed
-    // meanwhile: both are looked at.  A free K slot also means that the meta words, the V descriptor and the unit that this
-    // stage overwrites have been used: the scores of stage it - NK are complete, a pipeline issues the P.V of a stage
-    // before the scores of the stage after the next, hence everything about stages up to it - NK - 4 is done with.
-    auto acquire = [&]() {
-      const uint32_t bar = s_kempty + 8 * (it % NK), par = (((uint32_t)(it / NK)) & 1u) ^ 1u;
-      copy_queries();
-      if (KV8 || uq == u) return tok_wait(bar, par, s_abort);
-      const uint64_t t_start = globaltimer_ns();
-      while (!__all_sync(0xffffffffu, mbar_test_wait(bar, par))) {
-        copy_queries();
-        if (uq == u) return tok_wait(bar, par, s_abort);
-        if (__any_sync(0xffffffffu, *s_abort != 0 || globaltimer_ns() - t_start > kWaitLimitNs)) {
-          *s_abort = 1;
-          return false;
-        }
-      }
-      return true;
-    };
+    // Waits for stage `it`'s K slot.  A free K slot also means that the meta words and the V descriptor that this stage
+    // overwrites have been used: the scores of stage it - NK are complete, a pipeline issues the P.V of a stage before the
+    // scores of the stage after the next, hence everything about stages up to it - NK - 4 is done with.
+    auto acquire = [&]() { return tok_wait(s_kempty + 8 * (it % NK), (((uint32_t)(it / NK)) & 1u) ^ 1u, s_abort); };
     while (item < n_units && ok) {
       int nxt = 0;
       if (lane == 0) nxt = atomicAdd(&p.hdr->next_item, 1);
@@ -306,27 +276,24 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
       T = T < 0 ? 0 : (T > cap_tokens ? cap_tokens : T);
       const int nodes = tree_nodes(p, b), first_node = (int)T - nodes;  // token index of node 0
       const int nstage = t1 > t0 ? (t1 - t0 + TOK - 1) / TOK : 0, npad = nstage < 2 ? 2 : (nstage + 1) & ~1;
-      if (KV8) {  // the bf16 query rows, one copy per 64-dim half, for the widening warps to split
-        if (!tok_wait(s_qtaken, ((uint32_t)u & 1u) ^ 1u, s_abort)) {
-          ok = false;
-          break;
-        }
-        if (lane == 0) {
-          mbar_arrive_expect_tx(s_qland, 2u * (uint32_t)p.GQ * 128u);
-          tma_load_3d(s_qraw, &tm_q, s_qland, 0, h * p.G, b * p.Sq);
-          tma_load_3d(s_qraw + NC * 128, &tm_q, s_qland, 64, h * p.G, b * p.Sq);
-        }
-        __syncwarp();
-        ++uq;
+      // the query rows for the widening warps to split: score column (query token qi, head g) is row qi * G + g, per 64-dim
+      // half a box of [Sq][G][64 dims], swizzled
+      if (!tok_wait(s_qtaken, ((uint32_t)u & 1u) ^ 1u, s_abort)) {
+        ok = false;
+        break;
       }
+      if (lane == 0) {
+        mbar_arrive_expect_tx(s_qland, 2u * (uint32_t)p.GQ * 128u);
+        tma_load_3d(s_qraw, &tm_q, s_qland, 0, h * p.G, b * p.Sq);
+        tma_load_3d(s_qraw + NC * 128, &tm_q, s_qland, 64, h * p.G, b * p.Sq);
+      }
+      __syncwarp();
       const int32_t* row = p.block_table + (size_t)b * p.MB;
       int blk_cur = 0;
       {
         const int tb = t0 + lane * p.tile_rows;
         if (lane < boxes_per_stage && tb < t1) blk_cur = table_entry(row + tb / p.bs);
       }
-      if (lane == 0) g_unit[u % kTokUnits] = make_int4(b, h, 0, 0);  // (read by this warp only)
-      __syncwarp();
       ++u;
       for (int s = 0; s < npad; ++s, ++it) {
         const int tok0 = t0 + s * TOK;
@@ -350,7 +317,7 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
           g_vdesc[ds].nbox = nbox;
           g_vdesc[ds].h = h;
           if (nbox > 0)
-            mbar_arrive_expect_tx(kfull, (KV8 ? 1u : 2u) * (uint32_t)nbox * box_bytes);
+            mbar_arrive_expect_tx(kfull, (uint32_t)nbox * box_bytes);
           else
             mbar_arrive(kfull);
         }
@@ -364,8 +331,7 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
           span_ok = checked(chk_span(dk, box_bytes, k0, (long long)k0 + kTc2HalfBytes) && chk_span(lane, 1, 0, 8),
                             &p.hdr->status, kStatusBadSmem);
           if (span_ok) {
-            tma_load_4d(dk, &tm_k, kfull, 0, c_tok, h, blk_cur);  // (KV8: the row's 128 codes; else its first 64 dims)
-            if (!KV8) tma_load_4d(dk + kTc2HalfBytes, &tm_k, kfull, 64, c_tok, h, blk_cur);
+            tma_load_4d(dk, &tm_k, kfull, 0, c_tok, h, blk_cur);  // 128 codes per token
             g_vdesc[ds].blk[lane & 7] = blk_cur;
             g_vdesc[ds].c_tok[lane & 7] = c_tok;
           }
@@ -406,11 +372,7 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
         const int j = it - 1 - k;
         mbar_wait_bounded(s_kfull + 8 * (j % NK), (uint32_t)(j / NK) & 1u, &dummy_abort, kWaitLimitNs / 8);
       }
-      if (KV8 && uq > 0) mbar_wait_bounded(s_qland, (uint32_t)(uq - 1) & 1u, &dummy_abort, kWaitLimitNs / 8);
-      for (int k = 0; !KV8 && k < (uq < QB ? uq : QB); ++k) {
-        const int j = uq - 1 - k;
-        mbar_wait_bounded(s_qready + 8 * (j % QB), (uint32_t)(j / QB) & 1u, &dummy_abort, kWaitLimitNs / 8);
-      }
+      if (u > 0) mbar_wait_bounded(s_qland, (uint32_t)(u - 1) & 1u, &dummy_abort, kWaitLimitNs / 8);
     }
   } else if (warp == kWarpV) {
     // ================================================================= V producer
@@ -436,12 +398,11 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
         if (lane == 0) mbar_arrive(vland);
         continue;
       }
-      if (lane == 0) mbar_arrive_expect_tx(vland, (KV8 ? 1u : 2u) * (uint32_t)nbox * box_bytes);
+      if (lane == 0) mbar_arrive_expect_tx(vland, (uint32_t)nbox * box_bytes);
       __syncwarp();
       if (lane < nbox && lane < 8) {
         const uint32_t dv = s_v + (uint32_t)vs * L::kLandBytes + (uint32_t)lane * box_bytes;
         tma_load_4d(dv, &tm_v, vland, 0, vd.c_tok[lane], vd.h, vd.blk[lane]);
-        if (!KV8) tma_load_4d(dv + kTc2HalfBytes, &tm_v, vland, 64, vd.c_tok[lane], vd.h, vd.blk[lane]);
       }
     }
     if (!ok) {
@@ -456,11 +417,12 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
     // ================================================================= MMA warps: warp kWarpM + t issues pipeline t's MMAs
     // Stage i of the pipeline is stage 2 i + t of the CTA.  The scores of stage i + 1 are issued before the P.V of stage i, so
     // that they run beside the softmax of stage i, unless the weights are there before the scores' operands.
-    const int t = warp - kWarpM;
-    const uint32_t idesc_s = KV8 ? (1u << 4) | ((uint32_t)(NC >> 3) << 17) | ((uint32_t)(TOK >> 4) << 24)
-                                 : umma_idesc_16bit(TOK, NC, 0, true);
-    const uint32_t idesc_o = umma_idesc_16bit(D, NC, 1, !KV8) | (1u << 15);  // A (V) is M-major, too
-    const uint32_t to = tmem + L::kScoreCols + (uint32_t)t * L::kColStride;
+    // (the pipeline is a compile-time constant, so that the operands' addresses are known to be the same in all lanes)
+    auto issue = [&](auto pipeline) {
+    constexpr int t = decltype(pipeline)::value;
+    const uint32_t idesc_s = (1u << 4) | ((uint32_t)(NC >> 3) << 17) | ((uint32_t)(TOK >> 4) << 24);  // E4M3 by E4M3
+    const uint32_t idesc_l = umma_idesc_16bit(D, NC, 1, false), idesc_o = idesc_l | (1u << 15);  // A (V) is M-major, too
+    const uint32_t to = tmem + L::kColO + (uint32_t)t * NC, tl = tmem + L::kColL + (uint32_t)t * NC;
     bool issued = false, ok = true, ended = false;
     uint32_t i = 0, j = 0;  // next stage whose scores / P.V are issued; i - j <= 2
     auto now = [](uint32_t bar, uint32_t par) { return __all_sync(0xffffffffu, mbar_test_wait(bar, par)); };
@@ -470,29 +432,35 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
       const uint32_t kfull = s_kfull + 8 * ks, kpar = (n / NK) & 1u;
       const uint32_t sfree = s_sfree + 8 * (2 * t + i % SB), spar = ((i - SB) / SB) & 1u;
       const bool may_s = !ended && i - j < 2, may_v = j < i;
-      bool scores = may_s;
+      bool scores = may_s, there = false;  // (the scores' operands)
       if (may_s && may_v) {  // whichever can go ahead first
-        const uint64_t t_start = globaltimer_ns();
+        uint64_t t_start = 0;
         for (uint32_t spin = 1;; ++spin) {
           if (now(kfull, kpar)) {
             const int4 meta = g_meta[2 * ms];
             const int unit = g_meta[2 * ms + 1].w;
             if (meta.x < 0 || ((i < SB || now(sfree, spar)) &&
-                               (!((meta.w >> 16) & 1) || now(s_qready + 8 * (unit % QB), (uint32_t)(unit / QB) & 1u))))
+                               (!((meta.w >> 16) & 1) || now(s_qready, (uint32_t)unit & 1u)))) {
+              there = true;
               break;
+            }
           }
           if (now(s_pready + 8 * (2 * t + j % PB), (j / PB) & 1u)) {
             scores = false;
             break;
           }
-          if (spin % 64 == 0 && __any_sync(0xffffffffu, *s_abort != 0 || globaltimer_ns() - t_start > kWaitLimitNs)) {
-            *s_abort = 1;
-            break;  // (the waits below give up at once)
+          if (spin % 1024 == 0) {
+            const uint64_t t_now = globaltimer_ns();
+            if (t_start == 0) t_start = t_now;
+            if (__any_sync(0xffffffffu, *s_abort != 0 || t_now - t_start > kWaitLimitNs)) {
+              *s_abort = 1;
+              break;  // (the waits below give up soon)
+            }
           }
         }
       }
       if (scores) {
-        if (!tok_wait(kfull, kpar, s_abort)) {
+        if (!there && !tok_wait(kfull, kpar, s_abort)) {
           ok = false;
           break;
         }
@@ -503,73 +471,65 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
         }
         const int ntok = meta.w & 0xffff;
         const bool first = (meta.w >> 16) & 1, last = (meta.w >> 17) & 1;
-        const int qb = meta2.w % QB;
         // (a stage without tokens waits for its unit's query rows, too: the arrivals at s_qfree below count for that unit)
-        if ((i >= SB && !tok_wait(sfree, spar, s_abort)) ||
-            (first && !tok_wait(s_qready + 8 * qb, (uint32_t)(meta2.w / QB) & 1u, s_abort))) {
+        if ((i >= SB && !there && !tok_wait(sfree, spar, s_abort)) ||
+            (first && !there && !tok_wait(s_qready, (uint32_t)meta2.w & 1u, s_abort))) {
           ok = false;
           break;
         }
         const uint32_t sready = s_sready + 8 * (2 * t + i % SB);
         if (ntok > 0) {
           tc_fence_after_sync();
-          if (lane == 0) {
-            const uint32_t kst = s_k + (uint32_t)ks * L::kLandBytes, qst = s_q + (uint32_t)qb * L::kQBytes;
-            const uint32_t ts = tmem + (uint32_t)(t * SB + i % SB) * L::kColStride;
-            if (KV8) {
+          if (elect_one()) {
+            const uint32_t ts = tmem + (uint32_t)(t * SB + i % SB) * NC;
+            const uint64_t dk = umma_smem_desc(s_k + (uint32_t)ks * L::kLandBytes, 0, 1024), dq = umma_smem_desc(s_q, 0, 1024);
 #pragma unroll
-              for (int term = 0; term < 2; ++term)
+            for (int term = 0; term < 2; ++term)
 #pragma unroll
-                for (int k = 0; k < 4; ++k)  // 32 codes per MMA
-                  umma_f8_ss(ts, umma_smem_desc(kst + k * 32, 0, 1024), umma_smem_desc(qst + term * NC * 128 + k * 32, 0, 1024),
-                             idesc_s, (term | k) ? 1u : 0u);
-            } else {
-#pragma unroll
-              for (int hh = 0; hh < 2; ++hh)
-#pragma unroll
-                for (int k = 0; k < 4; ++k)  // 16 dims per MMA
-                  umma_ss(ts, umma_smem_desc(kst + hh * kTc2HalfBytes + k * 32, 0, 1024),
-                          umma_smem_desc(qst + hh * NC * 128 + k * 32, 0, 1024), idesc_s, (hh | k) ? 1u : 0u);
-            }
+              for (int k = 0; k < 4; ++k)  // 32 codes per MMA
+                umma_f8_ss(ts, dk + 2 * k, dq + (uint64_t)(term * NC * 8 + 2 * k), idesc_s, (term | k) ? 1u : 0u);
             umma_commit(sready);
             umma_commit(s_kempty + 8 * ks);
-            if (last) umma_commit(s_qfree + 8 * qb);
+            if (last) umma_commit(s_qfree);
           }
           issued = true;
-        } else if (lane == 0) {  // the turn of the barriers is taken all the same
+        } else if (elect_one()) {  // the turn of the barriers is taken all the same
           mbar_arrive(sready);
           mbar_arrive(s_kempty + 8 * ks);
-          if (last) umma_commit(s_qfree + 8 * qb);  // the pipeline's scores of the stage before may still be on their way
+          if (last) umma_commit(s_qfree);  // the pipeline's scores of the stage before may still be on their way
         }
         __syncwarp();
         ++i;
       } else {
         const uint32_t m = 2 * j + t;
-        const int ring = KV8 ? NW : NV, vs = m % ring;
+        const int vs = m % NW;
         const int4 meta = g_meta[2 * (m % kTokMeta)];
         const int unit = g_meta[2 * (m % kTokMeta) + 1].w;
         const bool some = (meta.w & 0xffff) > 0, first = (meta.w >> 16) & 1;
         // (a unit's first P.V overwrites the accumulator that the softmax warps read at the end of the unit before)
-        if (!tok_wait((KV8 ? s_wfull : s_vland) + 8 * (m % (2 * ring)), (m / (2 * ring)) & 1u, s_abort) ||
+        if (!tok_wait(s_wfull + 8 * (m % (2 * NW)), (m / (2 * NW)) & 1u, s_abort) ||
             !tok_wait(s_pready + 8 * (2 * t + j % PB), (j / PB) & 1u, s_abort) ||
             (some && first && unit > 0 && !tok_wait(s_ofree, (uint32_t)(unit - 1) & 1u, s_abort))) {
           ok = false;
           break;
         }
-        const uint32_t freed = (KV8 ? s_wempty : s_vtaken) + 8 * vs;
+        const uint32_t freed = s_wempty + 8 * vs;
         if (some) {
           tc_fence_after_sync();
-          if (lane == 0) {
-            const uint64_t dp = umma_smem_desc(s_p + (uint32_t)(t * PB + j % PB) * L::kPBytes, 128 * 128, 1024);
-            const uint64_t dv = umma_smem_desc((KV8 ? s_w : s_v) + (uint32_t)vs * kTc2SlotBytes, kTc2HalfBytes, 1024);
+          if (elect_one()) {
+            const uint64_t dp = umma_smem_desc(s_p + (uint32_t)(t * PB + j % PB) * L::kPBytes, 0, 1024);
+            const uint64_t dv = umma_smem_desc(s_w + (uint32_t)vs * kTc2SlotBytes, kTc2HalfBytes, 1024);
 #pragma unroll
             for (int k = 0; k < TOK / 16; ++k)  // 16 tokens: 16 rows of 128 bytes of V and of P
               umma_ss(to, dv + (uint64_t)(k * (2048 >> 4)), dp + (uint64_t)(k * (2048 >> 4)), idesc_o, (first && k == 0) ? 0u : 1u);
+#pragma unroll
+            for (int k = 0; k < TOK / 16; ++k)  // the columns' sums of weights, in every lane
+              umma_ts(tl, tmem + L::kColOne, dp + (uint64_t)(k * (2048 >> 4)), idesc_l, (first && k == 0) ? 0u : 1u);
             umma_commit(s_pvdone + 8 * (2 * t + j % PB));
             umma_commit(freed);
           }
           issued = true;
-        } else if (lane == 0) {
+        } else if (elect_one()) {
           mbar_arrive(s_pvdone + 8 * (2 * t + j % PB));
           mbar_arrive(freed);
         }
@@ -579,14 +539,19 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
     }
     if (!ok && lane == 0) atomicOr(&p.hdr->status, kStatusWaitTimeout);
     if (!ok && issued) {  // the tensor memory must not be released under MMAs in flight
-      if (lane == 0) umma_commit(s_drain + 8 * t);
+      if (elect_one()) umma_commit(s_drain + 8 * t);
       __syncwarp();
       int dummy = 0;
       mbar_wait_bounded(s_drain + 8 * t, 0u, &dummy, kWaitLimitNs / 8);
     }
+    };
+    if (warp == kWarpM)
+      issue(std::integral_constant<int, 0>{});
+    else
+      issue(std::integral_constant<int, 1>{});
   } else if (warp >= kWarpX) {
     // ================================================================= widening warps (8-bit cache)
-    const int tid_w = threadIdx.x - kWarpX * 32;
+    const int tid_w = threadIdx.x & 127;
     bool ok = true;
     uint32_t u = 0;
     for (uint32_t n = 0;; ++n) {
@@ -598,7 +563,7 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
       const int4 meta = g_meta[2 * ms];
       if (meta.x < 0) break;
       const int ntok = meta.w & 0xffff;
-      if ((n & 1) == 0 && ((meta.w >> 16) & 1)) {
+      if (!(n & 1) && ((meta.w >> 16) & 1)) {
         // ---- a unit starts: its query rows as hi + lo, scaled by a power of two that brings the row's largest magnitude
         // into [128, 256) (E4M3 goes up to 448).  A warp takes every fourth row, lane l dims 4 l .. 4 l + 3.
         if (!tok_wait(s_qland, u & 1u, s_abort) || !tok_wait(s_qfree, (u & 1u) ^ 1u, s_abort)) {
@@ -629,8 +594,11 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
           if (lane == 0) mul[c] = p.scale_log2e * inv_a;
         }
         fence_proxy_async_smem();  // the terms are read by the MMAs, the rows overwritten by TMA, through the async proxy
-        mbar_arrive(s_qready);
-        mbar_arrive(s_qtaken);
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive(s_qready);
+          mbar_arrive(s_qtaken);
+        }
         ++u;
       }
       // ---- V codes to f16, as in chunk_tc2_kernel: exact, to value / 256; 1024 units of 16 codes, eight per thread
@@ -642,31 +610,38 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
       if (ntok > 0) {
         const uint8_t* src = gen + (s_v - base) + (size_t)vs * kTc2RawSlotBytes;
         uint8_t* dst = gen + (s_w - base) + (size_t)ws * kTc2SlotBytes;
-        constexpr int kUnits = TOK * 8 / L::kWiden;
         const int c = tid_w & 7, r0 = tid_w >> 3;  // unit i of the thread: rows r0 + 16 i, chunk c
         const uint8_t* s0 = src + (size_t)r0 * 128 + ((c ^ (r0 & 7)) << 4);
         uint8_t* d0 = dst + (size_t)(c >> 2) * kTc2HalfBytes + (size_t)r0 * 128;
-        const int x0 = ((2 * (c & 3)) ^ (r0 & 7)) << 4, x1 = ((2 * (c & 3) + 1) ^ (r0 & 7)) << 4;
+        // a unit becomes two 16-byte chunks; chunks c and c + 4 lie in different halves, at the same banks, so the second
+        // four threads of a row write theirs in the other order
+        const bool swap = c >> 2;
+        const int x0 = ((2 * (c & 3) + (swap ? 1 : 0)) ^ (r0 & 7)) << 4, x1 = x0 ^ 16;
 #pragma unroll 1
-        for (int k = 0; k < kUnits / 4; ++k, s0 += 4 * 2048, d0 += 4 * 2048) {
-        uint4 w[4];
+        for (int k = 0; k < 2; ++k, s0 += 4 * 2048, d0 += 4 * 2048) {
+          uint4 w[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i)  // (rows beyond the stage's tokens: stale, cleared by the softmax threads)
-          w[i] = *reinterpret_cast<const uint4*>(s0 + i * 2048);
+          for (int i = 0; i < 4; ++i)  // (rows beyond the stage's tokens: stale, cleared by the softmax threads)
+            w[i] = *reinterpret_cast<const uint4*>(s0 + i * 2048);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          *reinterpret_cast<uint4*>(d0 + i * 2048 + x0) =
-              make_uint4(e4m3x2_to_f16x2<kSelB0B1>(w[i].x), e4m3x2_to_f16x2<kSelB2B3>(w[i].x),
-                         e4m3x2_to_f16x2<kSelB0B1>(w[i].y), e4m3x2_to_f16x2<kSelB2B3>(w[i].y));
-          *reinterpret_cast<uint4*>(d0 + i * 2048 + x1) =
-              make_uint4(e4m3x2_to_f16x2<kSelB0B1>(w[i].z), e4m3x2_to_f16x2<kSelB2B3>(w[i].z),
-                         e4m3x2_to_f16x2<kSelB0B1>(w[i].w), e4m3x2_to_f16x2<kSelB2B3>(w[i].w));
-        }
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t a0 = swap ? w[i].z : w[i].x, a1 = swap ? w[i].w : w[i].y;
+            const uint32_t b0 = swap ? w[i].x : w[i].z, b1 = swap ? w[i].y : w[i].w;
+            *reinterpret_cast<uint4*>(d0 + i * 2048 + x0) =
+                make_uint4(e4m3x2_to_f16x2<kSelB0B1>(a0), e4m3x2_to_f16x2<kSelB2B3>(a0), e4m3x2_to_f16x2<kSelB0B1>(a1),
+                           e4m3x2_to_f16x2<kSelB2B3>(a1));
+            *reinterpret_cast<uint4*>(d0 + i * 2048 + x1) =
+                make_uint4(e4m3x2_to_f16x2<kSelB0B1>(b0), e4m3x2_to_f16x2<kSelB2B3>(b0), e4m3x2_to_f16x2<kSelB0B1>(b1),
+                           e4m3x2_to_f16x2<kSelB2B3>(b1));
+          }
         }
         fence_proxy_async_smem();  // the widened slot is read by the MMAs through the async proxy
       }
-      mbar_arrive(s_wfull + 8 * (n % (2 * NW)));
-      mbar_arrive(s_vtaken + 8 * vs);
+      __syncwarp();
+      if (lane == 0) {
+        mbar_arrive(s_wfull + 8 * (n % (2 * NW)));
+        mbar_arrive(s_vtaken + 8 * vs);
+      }
     }
     if (!ok && lane == 0) atomicOr(&p.hdr->status, kStatusWaitTimeout);
   } else {
@@ -674,15 +649,12 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
     const int t = warp >> 2, w4 = warp & 3;           // pipeline; lane quarter of tensor memory
     const int r = 32 * w4 + lane;                     // this thread's token of the stage (and dim of the accumulator)
     const uint32_t tlane = tmem + ((uint32_t)(32 * w4) << 16);
-    const uint32_t to = tlane + L::kScoreCols + (uint32_t)t * L::kColStride;
     float4* cr = reinterpret_cast<float4*>(gen + (s_cr - base)) + t * (NC / 2);    // column pairs: two factors, two -references
     float* crf = reinterpret_cast<float*>(cr);
     auto cr_mul = [&](int c) -> float& { return crf[4 * (c >> 1) + (c & 1)]; };
     auto cr_ref = [&](int c) -> float& { return crf[4 * (c >> 1) + 2 + (c & 1)]; };
-    // sums of the warp's weights per column, two sets: a stage reads one and writes the other, and only a stage whose
-    // weights stand turns them over.  [2][8 warps][NC]
-    float* sum_s = reinterpret_cast<float*>(gen + (s_sum - base));
-    uint32_t sum_set = 0;
+    float* wmax = reinterpret_cast<float*>(gen + (s_max - base)) + t * 4 * NC;     // [4 warps][NC]
+    float* alpha_s = reinterpret_cast<float*>(gen + (s_alpha - base)) + t * NC;
     float ref_own = -INFINITY;                        // warp w4, lane l: reference of column 32 w4 + l
     constexpr int NCC = NC / 16;                      // columns are worked on 16 at a time
     uint32_t ph_wg = 0, ph_both = 0, par_vote = 0;
@@ -718,56 +690,44 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
     bool unit_open = false;               // a unit's results are still in the accumulators
     float e_ref = -INFINITY;              // reference of column 32 w4 + lane
     int e_slot = 0, e_b = 0, e_h = 0, e_nodes = 0, e_chunks = 1, e_unit = 0;
-    auto finish_unit = [&](const float* e_sums) {  // (after the wait for the unit's last P.V); the warp's sums of the unit
+    auto finish_unit = [&]() {  // (after the wait for the unit's last P.V)
       unit_open = false;
       tc_fence_after_sync();
-      if (!L::kOwnScratch && !both_sync()) return false;  // pipeline 0's last P.V may still be reading its weights
-      float* sums = reinterpret_cast<float*>(gen + ((L::kOwnScratch ? s_scr + (uint32_t)(e_unit & 1) * 10 * NC * 4 : s_p) - base));
-      float* refs = sums + 8 * NC;
-#pragma unroll
-      for (int ch = 0; ch < NCH; ++ch)
-        if (32 * ch + lane < NC) sums[warp * NC + 32 * ch + lane] = e_sums[32 * ch + lane];
+      float* refs = reinterpret_cast<float*>(gen + (s_ref - base)) + (e_unit & 1) * 2 * NC;
       if (32 * w4 + lane < NC) refs[t * NC + 32 * w4 + lane] = e_ref;
       if (!both_sync()) return false;
       const bool dst_ok = checked(chk_index(e_slot, p.max_items) && chk_index(e_b, p.B) && chk_index(e_h, p.Hkv),
                                   &p.hdr->status, kStatusBadIndex);
       const bool partial = e_chunks > 1 || p.out_f32;
       const int cols = p.G * e_nodes;  // (rows of nodes that do not exist are left alone)
-      float f0[NCH], f1[NCH];          // lane l: what the pipelines' accumulators of column 32 ch + l are multiplied by
-#pragma unroll
-      for (int ch = 0; ch < NCH; ++ch) {
-        const int c = 32 * ch + lane;
-        f0[ch] = f1[ch] = 0.f;
-        if (c >= NC) continue;
-        const float l0 = (sums[c] + sums[NC + c]) + (sums[2 * NC + c] + sums[3 * NC + c]);
-        const float l1 = (sums[4 * NC + c] + sums[5 * NC + c]) + (sums[6 * NC + c] + sums[7 * NC + c]);
-        const float m0 = l0 > 0.f ? refs[c] : -INFINITY, m1 = l1 > 0.f ? refs[NC + c] : -INFINITY;
-        const float M = fmaxf(m0, m1), Ms = M == -INFINITY ? 0.f : M;
-        const float x0 = ex2(m0 - Ms), x1 = ex2(m1 - Ms);  // (0 for a pipeline in which the column saw nothing)
-        const float den = (l0 > 0.f ? x0 * l0 : 0.f) + (l1 > 0.f ? x1 * l1 : 0.f);
-        const float inv = (den > 0.f ? 1.f / den : 0.f) * (KV8 ? p.v_scale : 1.f);
-        f0[ch] = x0 * inv;
-        f1[ch] = x1 * inv;
-        if (warp == 0 && partial && c < cols && (!kChecked || dst_ok))
-          p.part_lse[(size_t)e_slot * p.GQ + c] = den > 0.f ? M + lg2(den) : -INFINITY;
-      }
 #pragma unroll 1
       for (int g16 = t; 16 * g16 < min(NC, cols); g16 += 2) {  // 16 columns at a time, the pipelines' warps in turns; thread = dim
         uint32_t o0[16], o1[16];
-        tmem_ld16(tlane + L::kScoreCols + 16 * g16, o0);
-        tmem_ld16(tlane + L::kScoreCols + L::kColStride + 16 * g16, o1);
-        float a0 = f0[0], a1 = f1[0];
+        tmem_ld16(tlane + L::kColL + 16 * g16, o0);
+        tmem_ld16(tlane + L::kColL + NC + 16 * g16, o1);
+        // lane j: the common reference of column j, the pipelines' distances from it (0 where a pipeline's column saw
+        // nothing: its accumulators may hold anything then, and are not used), and what their values are multiplied by
+        const int cj = 16 * g16 + (lane & 15);
+        const float m0 = refs[cj], m1 = refs[NC + cj], M = fmaxf(m0, m1), Ms = M == -INFINITY ? 0.f : M;
+        float f0 = ex2(m0 - Ms), f1 = ex2(m1 - Ms), l0 = 0.f, l1 = 0.f;
+        tmem_ld_wait();
 #pragma unroll
-        for (int ch = 1; ch < NCH; ++ch) {
-          a0 = (g16 >> 1) == ch ? f0[ch] : a0;
-          a1 = (g16 >> 1) == ch ? f1[ch] : a1;
+        for (int j = 0; j < 16; ++j) {
+          l0 = (lane & 15) == j ? __uint_as_float(o0[j]) : l0;
+          l1 = (lane & 15) == j ? __uint_as_float(o1[j]) : l1;
         }
+        tmem_ld16(tlane + L::kColO + 16 * g16, o0);
+        tmem_ld16(tlane + L::kColO + NC + 16 * g16, o1);
+        const float den = (f0 != 0.f ? l0 * f0 : 0.f) + (f1 != 0.f ? l1 * f1 : 0.f), inv = den > 0.f ? p.v_scale / den : 0.f;
+        if (partial && w4 == 0 && lane < 16 && cj < cols && (!kChecked || dst_ok))
+          p.part_lse[(size_t)e_slot * p.GQ + cj] = den > 0.f ? M + lg2(den) : -INFINITY;
+        f0 *= inv;
+        f1 *= inv;
         tmem_ld_wait();
         float v[16];
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
-          const float b0 = __shfl_sync(0xffffffffu, a0, 16 * (g16 & 1) + j), b1 = __shfl_sync(0xffffffffu, a1, 16 * (g16 & 1) + j);
-          // (an accumulator that nothing was added to holds anything: it is not multiplied)
+          const float b0 = __shfl_sync(0xffffffffu, f0, j), b1 = __shfl_sync(0xffffffffu, f1, j);
           v[j] = (b0 != 0.f ? __uint_as_float(o0[j]) * b0 : 0.f) + (b1 != 0.f ? __uint_as_float(o1[j]) * b1 : 0.f);
         }
         if (partial && (!kChecked || dst_ok)) {
@@ -804,7 +764,7 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
       tc_fence_before_sync();
       __syncwarp();
       if (lane == 0) mbar_arrive(s_ofree);
-      return L::kOwnScratch || both_sync();
+      return true;
     };
     for (uint32_t i = 0; ok; ++i) {
       const uint32_t n = 2 * i + t;
@@ -818,47 +778,38 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
       const int ntok = end ? 0 : meta.w & 0xffff, b = meta.y, h = meta.z, tok0 = meta2.x, first_node = meta2.y, nodes = meta2.z;
       const bool first = !end && ((meta.w >> 16) & 1), last = !end && ((meta.w >> 17) & 1);
       if (first) ref_own = -INFINITY;
+      // which columns see this thread's token: of a node's, those whose query token has the node's bit in its mask (at most 64
+      // tokens, one word each; a lane fetches a word, while the scores are on their way)
+      const bool tree = tok0 + ntok > first_node;  // the stage holds nodes
+      uint32_t seen[2];
+      seen[0] = seen[1] = r < ntok ? 0xffffffffu : 0u;
+      if (tree) {
+        const uint64_t* rows = p.tree_mask + (size_t)b * p.Sq;
+        const uint64_t r0 = lane < p.Sq ? rows[lane] : 0ull, r1 = lane + 32 < p.Sq ? rows[lane + 32] : 0ull;
+        const int node = tok0 + r - first_node;
+        const uint64_t mine = (1ull << p.G) - 1ull;
+        uint64_t m = 0ull;
+#pragma unroll 1
+        for (int qi = 0; qi < p.Sq; ++qi) {
+          const uint64_t row = __shfl_sync(0xffffffffu, qi < 32 ? r0 : r1, qi & 31);
+          if ((row >> (node & 63)) & 1ull) m |= mine << (qi * p.G);
+        }
+        if (r < ntok && node >= 0) {
+          seen[0] = (uint32_t)m;
+          seen[1] = (uint32_t)(m >> 32);
+        }
+      }
       const uint32_t sb = i % SB, sfree = s_sfree + 8 * (2 * t + sb);
       if (!end && !tok_wait(s_sready + 8 * (2 * t + sb), (i / SB) & 1u, s_abort)) {
         ok = false;
         break;
       }
-      const uint32_t srow = tlane + (uint32_t)(t * SB + sb) * L::kColStride;
-      const bool tree = tok0 + ntok > first_node;  // the stage holds nodes
-      const bool quick = !tree && ntok >= 32 * NCH;
+      const uint32_t srow = tlane + (uint32_t)(t * SB + sb) * NC;
+      const bool quick = !tree && ntok > 32 * (NCC - 1);
       bool refs_due = tree || (first && !quick);
-      const float* open_sums = sum_s + (sum_set * 8 + warp) * NC;  // (of the unit that ended, should one be open)
-      // which columns see this thread's token
-      uint32_t seen[NCH];
-#pragma unroll
-      for (int ch = 0; ch < NCH; ++ch) seen[ch] = r < ntok ? 0xffffffffu : 0u;
-      const int node = tok0 + r - first_node;
-      if (tree && r < ntok && node >= 0) {
-        const uint64_t* rows = p.tree_mask + (size_t)b * p.Sq * p.tree_words + (node >> 6);
-        int left = 0, qi = -1;  // columns that the current query token still has
-        bool sees = false;
-#pragma unroll
-        for (int ch = 0; ch < NCH; ++ch) {
-          uint32_t m = 0u;
-#pragma unroll 1
-          for (int c = 0; c < 32; ++c) {
-            if (left == 0) {
-              left = p.G;
-              ++qi;
-              sees = qi < p.Sq && ((rows[(size_t)qi * p.tree_words] >> (node & 63)) & 1ull);
-            }
-            m |= (uint32_t)sees << c;
-            --left;
-          }
-          seen[ch] = m;
-        }
-      }
       const bool masked = tree || ntok < TOK;
       auto hide = [&](int cc, uint32_t (&s)[16]) {  // scores of 16 columns: -inf where the token is hidden
-        uint32_t m = seen[0];
-#pragma unroll
-        for (int ch = 1; ch < NCH; ++ch) m = (cc >> 1) == ch ? seen[ch] : m;
-        m >>= 16 * (cc & 1);
+        const uint32_t m = (cc >> 1 ? seen[1] : seen[0]) >> (16 * (cc & 1));
 #pragma unroll
         for (int j = 0; j < 16; ++j)
           if (!((m >> j) & 1u)) s[j] = 0xff800000u;
@@ -866,41 +817,33 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
       if (ntok > 0) {
         tc_fence_after_sync();
         if (first) {
-          // The columns' factors and first references.  Any value near the scores will do as a reference: the largest of
-          // 32 tokens, warp w for columns 32 w ..  (Stages with nodes or few tokens form the maxima below, which replace
-          // a reference of -inf.)
-          if (KV8 && !tok_wait(s_qready + 8 * (meta2.w % QB), (uint32_t)(meta2.w / QB) & 1u, s_abort)) {
+          // The columns' factors and first references.  Any value near the scores will do as a reference: those of one token,
+          // warp w's first for columns 16 w ..  (Stages with nodes or few tokens form the maxima below, which replace a
+          // reference of -inf.)
+          if (!tok_wait(s_qready, (uint32_t)meta2.w & 1u, s_abort)) {
             ok = false;
             break;
           }
-          if (w4 < NCH) {
-            float m = -INFINITY;
-            if (quick) {
-              uint32_t lo[16], hi[16];
-              float s[32];
-              tmem_ld16(srow + 32 * w4, lo);
-              if (32 * w4 + 16 < NC) tmem_ld16(srow + 32 * w4 + 16, hi);
-              tmem_ld_wait();
+          const float* mul = reinterpret_cast<const float*>(gen + (s_mul - base));
+          if (w4 < NCC) {
+            uint32_t s[16];
+            tmem_ld16(srow + 16 * w4, s);
+            tmem_ld_wait();
+            if (lane == 0) {
 #pragma unroll
-              for (int j = 0; j < 16; ++j) {
-                s[j] = __uint_as_float(lo[j]);
-                s[16 + j] = 32 * w4 + 16 < NC ? __uint_as_float(hi[j]) : 0.f;
+              for (int j = 0; j < 16; j += 2) {
+                const float2 f = *reinterpret_cast<const float2*>(mul + 16 * w4 + j);
+                cr[8 * w4 + j / 2] = make_float4(f.x, f.y, quick ? -__uint_as_float(s[j]) * f.x : 0.f,
+                                                 quick ? -__uint_as_float(s[j + 1]) * f.y : 0.f);
               }
-              m = warp_transpose<true>(s, lane);
-            }
-            const int c = 32 * w4 + lane;
-            if (c < NC) {
-              const float f = KV8 ? reinterpret_cast<const float*>(gen + (s_mul - base))[(meta2.w % QB) * NC + c] : p.scale_log2e;
-              ref_own = m * f;
-              cr_mul(c) = f;
-              cr_ref(c) = ref_own == -INFINITY ? 0.f : -ref_own;
             }
           }
           if (!wg_sync()) {
             ok = false;
             break;
           }
-          if (w4 == 0 && lane == 0) mbar_arrive(s_qfree + 8 * (meta2.w % QB));
+          if (quick && 32 * w4 + lane < NC) ref_own = -cr_ref(32 * w4 + lane);
+          if (w4 == 0 && lane == 0) mbar_arrive(s_qfree);
         }
       }
       // The weight buffer has to be free, and the accumulators complete where they are touched: by the P.V that used the
@@ -913,21 +856,14 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
         ok = false;
         break;
       }
-      // (without an exchange of its own the finish of a unit uses the weight buffer: it comes first)
-      if (!L::kOwnScratch && unit_open && !finish_unit(open_sums)) {
-        ok = false;
-        break;
-      }
       uint8_t* prow = gen + (s_p - base) + (size_t)(t * PB + i % PB) * L::kPBytes + (size_t)r * 128;  // this token's weights
-      const float* sum_in = sum_s + (sum_set * 8 + warp) * NC;
-      float* sum_out = sum_s + ((sum_set ^ 1) * 8 + warp) * NC;
       for (bool formed = ntok == 0, raised = false;;) {
         if (!formed && !refs_due) {
-          // ---- weights: 2^(score * factor - reference), into the second MMA's operand, and the warp's sums of them
+          // ---- weights: 2^(score * factor - reference), into the second MMAs' operand
           float top = -INFINITY;  // largest exponent
           uint32_t nxt[16];
           tmem_ld16(srow, nxt);
-#pragma unroll 1
+#pragma unroll
           for (int cc = 0; cc < NCC; ++cc) {
             uint32_t s[16];
             tmem_ld_wait();
@@ -935,7 +871,6 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
             for (int j = 0; j < 16; ++j) s[j] = nxt[j];
             if (cc + 1 < NCC) tmem_ld16(srow + 16 * (cc + 1), nxt);
             if (masked) hide(cc, s);
-            float w[16];
             uint32_t pw[8];
 #pragma unroll
             for (int j = 0; j < 16; j += 2) {
@@ -943,28 +878,12 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
               const float2 x = ffma2(make_float2(__uint_as_float(s[j]), __uint_as_float(s[j + 1])), make_float2(f.x, f.y),
                                      make_float2(f.z, f.w));
               top = fmax3(top, x.x, x.y);
-              w[j] = ex2(x.x);
-              w[j + 1] = ex2(x.y);
-              pw[j / 2] = KV8 ? pack_f16x2(w[j], w[j + 1]) : pack_bf16x2(w[j], w[j + 1]);
+              pw[j / 2] = pack_f16x2(ex2(x.x), ex2(x.y));
             }
-            uint8_t* dst = prow + (size_t)(cc >> 2) * 128 * 128;
-            *reinterpret_cast<uint4*>(dst + (((2 * (cc & 3)) ^ (r & 7)) << 4)) = make_uint4(pw[0], pw[1], pw[2], pw[3]);
-            *reinterpret_cast<uint4*>(dst + (((2 * (cc & 3) + 1) ^ (r & 7)) << 4)) = make_uint4(pw[4], pw[5], pw[6], pw[7]);
-            // lanes 2 k, 2 k + 1 get the sum of column k over the warp's tokens (a butterfly that halves the values it carries)
-#pragma unroll
-            for (int o = 16, n8 = 8; o > 1; o >>= 1, n8 >>= 1) {
-              const bool up = lane & o;
-#pragma unroll
-              for (int j = 0; j < n8; ++j) {
-                const float keep = up ? w[j + n8] : w[j], send = up ? w[j] : w[j + n8];
-                w[j] = keep + __shfl_xor_sync(0xffffffffu, send, o);
-              }
-            }
-            w[0] += __shfl_xor_sync(0xffffffffu, w[0], 1);
-            const int c = 16 * cc + (lane >> 1);
-            if (!(lane & 1)) sum_out[c] = w[0] + (first ? 0.f : sum_in[c]);
+            *reinterpret_cast<uint4*>(prow + (((2 * cc) ^ (r & 7)) << 4)) = make_uint4(pw[0], pw[1], pw[2], pw[3]);
+            *reinterpret_cast<uint4*>(prow + (((2 * cc + 1) ^ (r & 7)) << 4)) = make_uint4(pw[4], pw[5], pw[6], pw[7]);
           }
-          refs_due = wg_any(top > kTokRaise<KV8> && !raised);  // (once: the rounding of the two comparisons may differ)
+          refs_due = wg_any(top > kTokRaise && !raised);  // (once: the rounding of the two comparisons may differ)
           if (!vote_ok) {
             ok = false;
             break;
@@ -972,19 +891,19 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
           formed = !refs_due;
           if (formed) {  // the score buffer is free
             tc_fence_before_sync();
-            mbar_arrive(sfree);
+            __syncwarp();
+            if (lane == 0) mbar_arrive(sfree);
           }
         }
         if (!values_seen) {  // a unit that ended is written now
-          if (!wait_values(1) || (L::kOwnScratch && unit_open && !finish_unit(open_sums))) {
+          if (!wait_values(1) || (unit_open && !finish_unit())) {
             ok = false;
             break;
           }
           values_seen = true;
         }
         if (formed) break;
-        // ---- references: the columns' maxima over the stage, of the warp's tokens (in the sums that are not in use), then
-        // of the warps
+        // ---- references: the columns' maxima over the stage, of the warp's tokens, then of the warps
         tc_fence_after_sync();
 #pragma unroll 1
         for (int cc = 0; cc < NCC; ++cc) {
@@ -1005,22 +924,21 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
             }
           }
           m[0] = fmaxf(m[0], __shfl_xor_sync(0xffffffffu, m[0], 1));
-          if (!(lane & 1)) sum_out[16 * cc + (lane >> 1)] = m[0];
+          if (!(lane & 1)) wmax[w4 * NC + 16 * cc + (lane >> 1)] = m[0];
         }
         if (!wg_sync()) {
           ok = false;
           break;
         }
         bool changed = false;
-        float* alpha_s = sum_s + ((sum_set ^ 1) * 8 + 4 * t) * NC;  // (takes the place of the first warp's maxima)
         if (32 * w4 + lane < NC) {
           const int c = 32 * w4 + lane;
-          const float* mx = alpha_s + c;
+          const float* mx = wmax + c;
           const float m = fmaxf(fmaxf(mx[0], mx[NC]), fmaxf(mx[2 * NC], mx[3 * NC])) * cr_mul(c);
           float a = 1.f;
           if (ref_own == -INFINITY) {
             ref_own = m;  // nothing accumulated for this column so far
-          } else if (m > ref_own + kTokRaise<KV8>) {
+          } else if (m > ref_own + kTokRaise) {
             a = first ? 1.f : ex2(ref_own - m);
             ref_own = m;
             changed = !first;  // (on the unit's first stage nothing has been accumulated)
@@ -1035,16 +953,15 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
         }
         if (rescale) {
 #pragma unroll 1
-          for (int c = lane; c < NC; c += 32) sum_s[(sum_set * 8 + warp) * NC + c] *= alpha_s[c];
-          __syncwarp();
-#pragma unroll 1
-          for (int g16 = 0; g16 < NCC; ++g16) {
+          for (int g16 = 0; g16 < 2 * NCC; ++g16) {  // values, then sums
+            const int c0 = 16 * (g16 < NCC ? g16 : g16 - NCC);
+            const uint32_t at = tlane + (g16 < NCC ? L::kColO : L::kColL) + (uint32_t)(t * NC + c0);
             uint32_t o[16];
-            tmem_ld16(to + 16 * g16, o);
+            tmem_ld16(at, o);
             tmem_ld_wait();
 #pragma unroll
-            for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * alpha_s[16 * g16 + j]);
-            tmem_st16(to + 16 * g16, o);
+            for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * alpha_s[c0 + j]);
+            tmem_st16(at, o);
           }
           tmem_st_wait();
           if (!wg_sync()) {  // everybody has read alpha
@@ -1057,17 +974,15 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
       }
       if (!ok || end) break;
       if (ntok > 0) {
-        __syncwarp();
-        sum_set ^= 1u;
         if (ntok < TOK) {
           // V rows beyond the stage's tokens may hold anything (NaN included): clear them once the slot is written
-          const int ring = KV8 ? NW : NV, vs = n % ring;
-          if (!tok_wait((KV8 ? s_wfull : s_vland) + 8 * (n % (2 * ring)), (n / (2 * ring)) & 1u, s_abort)) {
+          const int vs = n % NW;
+          if (!tok_wait(s_wfull + 8 * (n % (2 * NW)), (n / (2 * NW)) & 1u, s_abort)) {
             ok = false;
             break;
           }
           if (r >= ntok) {
-            uint8_t* vrow = gen + ((KV8 ? s_w : s_v) - base) + (size_t)vs * kTc2SlotBytes + (size_t)r * 128;
+            uint8_t* vrow = gen + (s_w - base) + (size_t)vs * kTc2SlotBytes + (size_t)r * 128;
 #pragma unroll
             for (int c = 0; c < 16; ++c)
               *reinterpret_cast<uint4*>(vrow + (size_t)(c >> 3) * kTc2HalfBytes + ((c & 7) << 4)) = make_uint4(0u, 0u, 0u, 0u);
@@ -1076,16 +991,11 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
         fence_proxy_async_smem();  // the weights (and cleared rows) are read by the MMAs through the async proxy
         tc_fence_before_sync();
       } else {
-        if (first && w4 == 0 && lane == 0) mbar_arrive(s_qfree + 8 * (meta2.w % QB));
-        mbar_arrive(sfree);
-        if (first) {  // the pipeline has no part in this unit
-#pragma unroll 1
-          for (int c = lane; c < NC; c += 32) sum_out[c] = 0.f;
-          __syncwarp();
-          sum_set ^= 1u;
-        }
+        if (first && w4 == 0 && lane == 0) mbar_arrive(s_qfree);
+        if (lane == 0) mbar_arrive(sfree);
       }
-      mbar_arrive(s_pready + 8 * (2 * t + i % PB));
+      __syncwarp();
+      if (lane == 0) mbar_arrive(s_pready + 8 * (2 * t + i % PB));
 
       if (last) {  // the rest of the unit's work is put off (finish_unit)
         unit_open = true;
