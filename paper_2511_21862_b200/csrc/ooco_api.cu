@@ -430,12 +430,12 @@ static int encode_q_map(CUtensorMap* tm, const DecodeParams& p) {
   return r == CUDA_SUCCESS ? OOCO_OK : fail_cuda("cuTensorMapEncodeTiled(queries)", (long)r);
 }
 
-// Tree attention of 17 to 96 score columns at head_dim 128: one persistent CTA per SM with the tokens on the M axis.
-template <int NC>
+// Tree attention of few score columns at head_dim 128: one persistent CTA per SM with the tokens on the M axis.
+template <int NC, bool KV8>
 static int launch_tree_tok(const CUtensorMap& tk, const CUtensorMap& tv, DecodeParams& p, const DeviceInfo& di,
                            cudaStream_t st, int dev, bool dry) {
-  auto kern = tree_tok_kernel<NC>;
-  constexpr size_t smem = TokSmem<NC>::total();
+  auto kern = tree_tok_kernel<NC, KV8>;
+  constexpr size_t smem = TokSmem<NC, KV8>::total();
   if (smem > (size_t)di.smem_optin) return OOCO_E_UNSUPPORTED;
   static std::atomic<int> configured[64];
   if (dev < 0 || dev >= 64 || !configured[dev].load()) {
@@ -446,21 +446,28 @@ static int launch_tree_tok(const CUtensorMap& tk, const CUtensorMap& tv, DecodeP
   CUtensorMap tq;
   if (int rc = encode_q_map(&tq, p)) return rc;
   if (dry) return OOCO_OK;  // sizing and attributes only: the caller launches nothing before these have passed
-  cudaError_t e = launch_ex(kern, dim3(p.next_item_init), dim3(TokSmem<NC>::kWarps * 32), smem, st,
+  cudaError_t e = launch_ex(kern, dim3(p.next_item_init), dim3(TokSmem<NC, KV8>::kWarps * 32), smem, st,
                             g_knobs[kKnobPdl].load() != 0 && !tl_events_between_kernels, tk, tv, tq, p);
   if (e == cudaSuccess) e = cudaGetLastError();
   return e == cudaSuccess ? OOCO_OK : fail_cuda("launch of the tree attention kernel", (long)e);
 }
+template <bool KV8>
+static int launch_tree_tok_nc(const CUtensorMap& tk, const CUtensorMap& tv, DecodeParams& p, const DeviceInfo& di,
+                              cudaStream_t st, int dev, bool dry) {
+  if (p.GQ <= 32) return launch_tree_tok<32, KV8>(tk, tv, p, di, st, dev, dry);
+  if (p.GQ <= 48) return launch_tree_tok<48, KV8>(tk, tv, p, di, st, dev, dry);
+  if constexpr (KV8) return launch_tree_tok<64, true>(tk, tv, p, di, st, dev, dry);
+  return OOCO_E_UNSUPPORTED;  // (not reached: kTokMaxColumns)
+}
+
 // Tree attention: the decode shapes that the rules of decode_core pick without a knob, compiled with the tree's mask.
 // `tc` / `tc2`: the tcgen05 chunk kernels (head_dim 128).
 static int launch_tree(int head_dim, bool kv8, bool chunk, bool tc2, bool row16, int ncw, const CUtensorMap& tk,
                        const CUtensorMap& tv, DecodeParams& p, const DeviceInfo& di, int cps, cudaStream_t st, int dev,
                        bool dry) {
   if (chunk && head_dim == 128) {
-    if (kv8 && p.GQ <= kTokMaxColumns)
-      return p.GQ <= 32   ? launch_tree_tok<32>(tk, tv, p, di, st, dev, dry)
-             : p.GQ <= 48 ? launch_tree_tok<48>(tk, tv, p, di, st, dev, dry)
-                          : launch_tree_tok<64>(tk, tv, p, di, st, dev, dry);
+    if (kv8 && p.GQ <= kTokMaxColumns<true>) return launch_tree_tok_nc<true>(tk, tv, p, di, st, dev, dry);
+    if (!kv8 && p.GQ <= kTokMaxColumns<false>) return launch_tree_tok_nc<false>(tk, tv, p, di, st, dev, dry);
     if (tc2)
       return kv8 ? launch_chunk_tc2<true, true>(tk, tv, p, di, st, dev, dry)
                  : launch_chunk_tc2<false, true>(tk, tv, p, di, st, dev, dry);
@@ -863,7 +870,7 @@ static int decode_core(const ooco_shape_t* s, const void* q, const void* k_cache
   p.items_per_cta = plan_items_per_cta(G_);
   // the 8-bit path widens codes to value / 256 (kE4m3WidenFactor): both scales carry the factor back (K's only
   // where K is widened: the tcgen05 score path multiplies the codes' own values)
-  const bool kv8_tc = (kv8 && tree && chunk && G_ <= kTokMaxColumns) ||
+  const bool kv8_tc = (kv8 && tree && chunk && G_ <= kTokMaxColumns<true>) ||
                       (kv8 && !chunk && ncw == 8 && (tree || g_knobs[kKnobKv8Tcgen05].load() != 0));
   p.scale_log2e = scale * 1.4426950408889634f * (kv8 ? kv8->k_scale * (kv8_tc ? 1.f : kE4m3WidenFactor) : 1.f);
   p.v_scale = kv8 ? kv8->v_scale * kE4m3WidenFactor : 1.f;

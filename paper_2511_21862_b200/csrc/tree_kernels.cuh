@@ -1,22 +1,23 @@
-// Tree attention of 17 to 96 score columns per (sequence, kv head) at head_dim 128, with the TOKENS on the MMA's M axis.
+// Tree attention of 17 to 48 (8-bit cache: 64) score columns per (sequence, kv head) at head_dim 128, with the TOKENS on the
+// MMA's M axis.
 //
 //   S^T[128 tok x NC]   = K_slot[128 tok x 128] . Q^T          tcgen05.mma M128, N = NC columns
 //   O^T[128 dim x NC] (+)= V_slot^T[128 dim x 128 tok] . P     tcgen05.mma M128, N = NC columns
+//   L  [any     x NC] (+)= ones . P                            the columns' sums of weights, the same in every lane
 //
 // Why this way round.  The chunk kernel with score columns on M (chunk_tc2_kernels.cuh) spends the same time on a stage
-// of 128 tokens whether its 128 rows are full or not, and the row-wise softmax is a chain through shuffles; over the
+// of 128 tokens whether its 128 rows are full or not, and its row-wise softmax is a chain through shuffles; over the
 // 8-bit cache it widens K and V to 16 bits first.  Here the work of a stage is proportional to the columns there are: a
-// thread owns a token, reads its NC scores from tensor memory, and writes its NC weights as one row of the second MMA's
-// B operand; no transposition, no shuffle on the way.  The 8-bit scores come straight from the stored codes
-// (kind::f8f6f4): a bf16 query value has 8 significant bits, so it is the sum of two E4M3 terms of 4 each, exactly
-// (down to 2^-17 of its row's largest), and both terms accumulate into the same scores.  Only V is widened.  What is
-// left is bound by HBM: a stage is 64 KiB (32 KiB of codes) and takes 2800 (1400) cycles of an SM's share of it, the
-// special-function pipe needs NC * 128 / 16 of them.
+// thread owns a token, reads its NC scores from tensor memory, and writes its NC weights as one row of the second MMAs'
+// B operand; no transposition, no shuffle.  The sums over tokens, which would need them, come from the tensor core, which
+// is idle most of the time: summed with the same rounded weights as the numerator, in fp32.  The 8-bit scores come straight
+// from the stored codes (kind::f8f6f4): a bf16 query value has 8 significant bits, so it is the sum of two E4M3 terms of
+// 4 each, exactly (down to 2^-17 of its row's largest), and both terms accumulate into the same scores.  Only V is widened.
 //
 // A column's running maximum spans tokens, i.e. threads and warps.  It is only a reference: weights are 2^(x - ref),
-// and ref, a score among the unit's first, follows the true maximum when that is far above it (kTokRaise).  So a stage needs no maximum; its
-// threads vote once whether any score did, and only then (and on stages with nodes of the tree, where a column may see its
-// first token) the maxima are formed and the accumulators rescaled.
+// and ref, a score of the unit's first tokens, follows the true maximum when that is far above it (kTokRaise).  So a stage
+// needs no maximum; its threads vote once whether any score did, and only then (and on stages with nodes of the tree, where
+// a column may see its first token) the maxima are formed and the accumulators rescaled.
 //
 // Two pipelines t = 0, 1 work on alternating stages with softmax warps, score and weight buffers and an accumulator
 // each (a split of the tokens, merged by log-sum-exp when the unit of work ends): each is a serial chain scores ->
@@ -24,13 +25,22 @@
 // tokens, so that both take part in every unit.
 //
 //   warps 0 - 3, 4 - 7   softmax of pipeline 0, 1 (thread = token)
-//   warp 8               K producer: walks the units, TMA copies of K and of the query rows (16-bit cache: straight into
-//                        the operand tile), posts meta words and V boxes
+//   warp 8               K producer: walks the units, TMA copies of K, posts meta words and V boxes
 //   warp 9               V producer
 //   warps 10, 11         one lane issues the MMAs of pipeline 0, 1
-//   warps 12 - 15        8-bit cache only: split the query rows into the two terms, widen V
+//   warps 12 - 15        8-bit cache: split the query rows into the two terms, widen V
+//   warp 12              16-bit cache: TMA copies of the query rows, straight into the operand tile
 // Every wait is bounded; a wait that gives up sets the status bit and the CTA's abort flag, every warp falls through to
 // the common exit, and the tensor memory is released after the MMAs in flight.
+//
+// Measured, whole call (plan 10 us, this kernel, merge 12 us; 64 sequences of 256 to 8192 tokens, 8 kv heads; in brackets
+// the kernel with columns on M): 16-bit cache 18 columns 118 us (131), 32: 120 (134), 48: 129 (138), 64: 142 (141, hence the
+// limit); 8-bit cache 18: 120 (168), 32: 122 (171), 48: 135 (173), 64: 153 (176), 96: 267 with an earlier version (193).
+// 32 sequences of 4096 to 32768 tokens, 8-bit, 40 columns: 292 us (411), 3.1 TB/s of codes.  At 18 columns the 16-bit call runs at 0.80
+// of the measured copy rate, plan and merge included.  Over the 8-bit cache a stage of 128 tokens takes about 2000 cycles
+// where its 32 KiB would take 1400: a pipeline's chain (1300 cycles of weights, 1000 of barriers between the roles, 1300 of
+// widening and P.V) is what bounds it, two pipelines cannot hide all of it, and four sets of softmax warps do not fit the
+// register file.
 #pragma once
 #include <type_traits>
 
@@ -39,20 +49,23 @@
 namespace ooco {
 
 constexpr int kTokMeta = 8, kTokDesc = 8;  // ring sizes: meta words, V descriptors
-constexpr int kTokMaxColumns = 64;         // score columns the kernel is built for
-// A reference is raised when a score passes it by this much (log2 units): weights stay below 2^16 for f16, where small ones
-// lose bits below 2^-14.
-constexpr float kTokRaise = 14.f;
+// score columns that the kernel takes, from 17 (both sides measured above)
+template <bool KV8>
+constexpr int kTokMaxColumns = KV8 ? 64 : 48;
+// A reference is raised when a score passes it by this much (log2 units): weights stay below 2^16 for f16 (the 8-bit
+// cache), where small ones lose bits below 2^-14; bf16 has the range of fp32, and a column's sum stays below 2^60 times its tokens.
+template <bool KV8>
+constexpr float kTokRaise = KV8 ? 14.f : 60.f;
 
-template <int NC>
+template <int NC, bool KV8>
 struct TokSmem {
-  static constexpr int SB = NC <= 48 ? 2 : 1;                               // score buffers of a pipeline
-  static constexpr int PB = NC <= 48 ? 2 : 1;                               // weight buffers of a pipeline
+  static constexpr int SB = NC <= 48 ? 2 : 1;                               // score buffers of a pipeline (tensor memory is full)
+  static constexpr int PB = KV8 && NC <= 48 ? 2 : 1;                        // weight buffers of a pipeline
   static constexpr int kQBytes = NC * 256;                                  // [2][NC rows][128 bytes]
   static constexpr int kPBytes = 128 * 128;                                 // [128 tok][64 columns] f16
-  static constexpr int kLandBytes = kTc2RawSlotBytes;                       // K (or V) of one stage as TMA writes it
+  static constexpr int kLandBytes = KV8 ? kTc2RawSlotBytes : kTc2SlotBytes; // K (or V) of one stage as TMA writes it
   static constexpr int NK = 2, NV = PB == 1 ? 3 : 2, NW = 2;                // K slots, V slots, widened V slots
-  static constexpr int kWarps = 16;
+  static constexpr int kWarps = KV8 ? 16 : 13;
   // tensor memory: scores [2 pipelines][SB], values [2], sums [2], the operand of ones
   static constexpr int kTmemCols = 512;
   static constexpr int kColO = 2 * SB * NC, kColL = kColO + 2 * NC, kColOne = kColL + 2 * NC;
@@ -61,8 +74,8 @@ struct TokSmem {
   // the references at a unit's end (two sets take turns)
   static constexpr int kColumnBytes = NC * (2 * 8 + 4 + 2 * 4 * 4 + 2 * 4 + 4 * 4);
   __host__ __device__ static constexpr size_t total() {
-    return 1024 + 2 * (size_t)kQBytes + 2 * PB * (size_t)kPBytes + (size_t)(NK + NV) * kLandBytes +
-           (size_t)NW * kTc2SlotBytes + kTokMeta * 32 + kTokDesc * sizeof(VStageDesc) + kColumnBytes + 608;
+    return 1024 + (KV8 ? 2 : 1) * (size_t)kQBytes + 2 * PB * (size_t)kPBytes + (size_t)(NK + NV) * kLandBytes +
+           (KV8 ? (size_t)NW * kTc2SlotBytes : 0) + kTokMeta * 32 + 2 * 16 + kTokDesc * sizeof(VStageDesc) + kColumnBytes + 640;
   }
   static constexpr size_t kMost = 227 * 1024;  // shared memory of a CTA
 };
@@ -130,27 +143,28 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const void* tmap, uint
       : "memory");
 }
 
-template <int NC>
-__global__ void __launch_bounds__(TokSmem<NC>::kWarps * 32, 1)
+template <int NC, bool KV8>
+__global__ void __launch_bounds__(TokSmem<NC, KV8>::kWarps * 32, 1)
 tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
                 const __grid_constant__ CUtensorMap tm_q, const DecodeParams p) {
-  using L = TokSmem<NC>;
+  using L = TokSmem<NC, KV8>;
   constexpr int D = 128, TOK = kTc2StageTok;
   constexpr int SB = L::SB, PB = L::PB, NK = L::NK, NV = L::NV, NW = L::NW;
   constexpr int kWarpK = 8, kWarpV = 9, kWarpM = 10, kWarpX = 12;
   static_assert(L::total() <= L::kMost, "shared memory");
-  static_assert(NC % 16 == 0 && NC <= 64, "columns of an MMA with M = 128, and what shared memory holds");
+  static_assert(NC % 16 == 0 && NC <= 64 && NC <= kTokMaxColumns<KV8>, "columns of an MMA with M = 128, and what shared memory holds");
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw);
   const uint32_t base = (raw + 1023u) & ~1023u;
   uint8_t* gen = smem_raw + (base - raw);
   const uint32_t s_q = base;                                             // the unit's query rows as two terms
   const uint32_t s_qraw = s_q + (uint32_t)L::kQBytes;                    // ... in bf16
-  const uint32_t s_p = s_qraw + (uint32_t)L::kQBytes;                    // [2 pipelines][PB] weights
+  const uint32_t s_p = s_qraw + (KV8 ? (uint32_t)L::kQBytes : 0u);                   // [2 pipelines][PB] weights
   const uint32_t s_k = s_p + 2u * PB * L::kPBytes;                       // [NK] K slots
   const uint32_t s_v = s_k + (uint32_t)NK * L::kLandBytes;               // [NV] V slots
   const uint32_t s_w = s_v + (uint32_t)NV * L::kLandBytes;               // [NW] widened V slots
-  const uint32_t s_meta = s_w + (uint32_t)NW * kTc2SlotBytes;            // [kTokMeta] two int4
+  const uint32_t s_unit = s_w + (KV8 ? (uint32_t)NW * kTc2SlotBytes : 0u);  // [2] int4 {sequence, kv head}, 16-bit cache
+  const uint32_t s_meta = s_unit + 32;            // [kTokMeta] two int4
   const uint32_t s_vdesc = s_meta + kTokMeta * 32;                       // [kTokDesc] VStageDesc
   const uint32_t s_cr = s_vdesc + kTokDesc * (uint32_t)sizeof(VStageDesc);  // [2][NC / 2] {score factors, -references} of column pairs
   const uint32_t s_mul = s_cr + 2u * NC * 8;                             // [NC] score factor of the unit's columns
@@ -180,8 +194,10 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
   const uint32_t s_qland = s_both + 8;               // the unit's bf16 query rows have landed         (TMA)
   const uint32_t s_qtaken = s_qland + 8;             // ... have been split                            (widening threads)
   const uint32_t s_ofree = s_qtaken + 8;             // the unit's accumulators have been read               (8 warps)
-  const uint32_t s_drain = s_ofree + 8;              // [2]
+  const uint32_t s_ufull = s_ofree + 8;              // [2] the unit is posted                          (16-bit cache)
+  const uint32_t s_drain = s_ufull + 16;             // [2]
   const uint32_t s_slot = s_drain + 16;              // tensor-memory base, abort flag, votes [2 pipelines][2][4 warps]
+  int4* g_unit = reinterpret_cast<int4*>(gen + (s_unit - base));
   int4* g_meta = reinterpret_cast<int4*>(gen + (s_meta - base));
   VStageDesc* g_vdesc = reinterpret_cast<VStageDesc*>(gen + (s_vdesc - base));
   volatile uint32_t* g_slot = reinterpret_cast<volatile uint32_t*>(gen + (s_slot - base));
@@ -196,7 +212,7 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
       mbar_init(s_kempty + 8 * i, 1);
     }
     for (int i = 0; i < 2 * NV; ++i) mbar_init(s_vland + 8 * i, 1);
-    for (int i = 0; i < NV; ++i) mbar_init(s_vtaken + 8 * i, 4);
+    for (int i = 0; i < NV; ++i) mbar_init(s_vtaken + 8 * i, KV8 ? 4 : 1);
     for (int i = 0; i < 2 * NW; ++i) mbar_init(s_wfull + 8 * i, 4);
     for (int i = 0; i < NW; ++i) mbar_init(s_wempty + 8 * i, 1);
     for (int i = 0; i < kTokDesc; ++i) mbar_init(s_vdfull + 8 * i, 1);
@@ -204,6 +220,7 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
     for (int i = 0; i < 2; ++i) {
       mbar_init(s_wg + 8 * i, 4);
       mbar_init(s_drain + 8 * i, 1);
+      mbar_init(s_ufull + 8 * i, 1);
     }
     for (int i = 0; i < 4; ++i) {
       mbar_init(s_sready + 8 * i, 1);
@@ -211,7 +228,7 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
       mbar_init(s_pready + 8 * i, 4);
       mbar_init(s_pvdone + 8 * i, 1);
     }
-    mbar_init(s_qready, 4);
+    mbar_init(s_qready, KV8 ? 4 : 1);
     mbar_init(s_qfree, 4);
     mbar_init(s_both, 8);
     mbar_init(s_ofree, 8);
@@ -228,8 +245,8 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
   __syncthreads();
   tc_fence_after_sync();
   const uint32_t tmem = *g_slot;
-  if (warp < 4) {  // the operand that sums the weights: ones, f16
-    tmem_st8(tmem + ((uint32_t)(32 * warp) << 16) + L::kColOne, 0x3c003c00u);
+  if (warp < 4) {  // the operand that sums the weights: ones
+    tmem_st8(tmem + ((uint32_t)(32 * warp) << 16) + L::kColOne, KV8 ? 0x3c003c00u : 0x3f803f80u);
     tmem_st_wait();
   }
   tc_fence_before_sync();
@@ -240,6 +257,13 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
 
   const long long cap_tokens = (long long)p.MB * p.bs;
 
+  // The unit's query rows: score column (query token qi, head g) is row qi * G + g, per 64-dim half a box of [Sq][G][64 dims],
+  // swizzled.
+  auto copy_queries = [&](uint32_t dst, uint32_t bar, int b, int h) {
+    mbar_arrive_expect_tx(bar, 2u * (uint32_t)p.GQ * 128u);
+    tma_load_3d(dst, &tm_q, bar, 0, h * p.G, b * p.Sq);
+    tma_load_3d(dst + NC * 128, &tm_q, bar, 64, h * p.G, b * p.Sq);
+  };
   if (warp == kWarpK) {
     // ================================================================= K producer (and the walk over the units)
     if (lane == 0) {
@@ -276,16 +300,15 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
       T = T < 0 ? 0 : (T > cap_tokens ? cap_tokens : T);
       const int nodes = tree_nodes(p, b), first_node = (int)T - nodes;  // token index of node 0
       const int nstage = t1 > t0 ? (t1 - t0 + TOK - 1) / TOK : 0, npad = nstage < 2 ? 2 : (nstage + 1) & ~1;
-      // the query rows for the widening warps to split: score column (query token qi, head g) is row qi * G + g, per 64-dim
-      // half a box of [Sq][G][64 dims], swizzled
-      if (!tok_wait(s_qtaken, ((uint32_t)u & 1u) ^ 1u, s_abort)) {
-        ok = false;
-        break;
-      }
-      if (lane == 0) {
-        mbar_arrive_expect_tx(s_qland, 2u * (uint32_t)p.GQ * 128u);
-        tma_load_3d(s_qraw, &tm_q, s_qland, 0, h * p.G, b * p.Sq);
-        tma_load_3d(s_qraw + NC * 128, &tm_q, s_qland, 64, h * p.G, b * p.Sq);
+      if (KV8) {  // the query rows, for the widening warps to split
+        if (!tok_wait(s_qtaken, ((uint32_t)u & 1u) ^ 1u, s_abort)) {
+          ok = false;
+          break;
+        }
+        if (lane == 0) copy_queries(s_qraw, s_qland, b, h);
+      } else if (lane == 0) {  // (the unit before the last has been taken: its scores are complete)
+        g_unit[u & 1] = make_int4(b, h, 0, 0);
+        mbar_arrive(s_ufull + 8 * (u & 1));
       }
       __syncwarp();
       const int32_t* row = p.block_table + (size_t)b * p.MB;
@@ -317,7 +340,7 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
           g_vdesc[ds].nbox = nbox;
           g_vdesc[ds].h = h;
           if (nbox > 0)
-            mbar_arrive_expect_tx(kfull, (uint32_t)nbox * box_bytes);
+            mbar_arrive_expect_tx(kfull, (KV8 ? 1u : 2u) * (uint32_t)nbox * box_bytes);
           else
             mbar_arrive(kfull);
         }
@@ -331,7 +354,8 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
           span_ok = checked(chk_span(dk, box_bytes, k0, (long long)k0 + kTc2HalfBytes) && chk_span(lane, 1, 0, 8),
                             &p.hdr->status, kStatusBadSmem);
           if (span_ok) {
-            tma_load_4d(dk, &tm_k, kfull, 0, c_tok, h, blk_cur);  // 128 codes per token
+            tma_load_4d(dk, &tm_k, kfull, 0, c_tok, h, blk_cur);  // (KV8: the row's 128 codes; else its first 64 dims)
+            if (!KV8) tma_load_4d(dk + kTc2HalfBytes, &tm_k, kfull, 64, c_tok, h, blk_cur);
             g_vdesc[ds].blk[lane & 7] = blk_cur;
             g_vdesc[ds].c_tok[lane & 7] = c_tok;
           }
@@ -350,6 +374,10 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
         blk_cur = blk_n;
       }
       item = nxt;
+    }
+    if (!KV8 && ok && lane == 0) {
+      g_unit[u & 1] = make_int4(-1, 0, 0, 0);
+      mbar_arrive(s_ufull + 8 * (u & 1));
     }
     for (int k = 0; k < 2 && ok; ++k) {  // end markers, one for each pipeline
       if (!acquire()) {
@@ -372,7 +400,7 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
         const int j = it - 1 - k;
         mbar_wait_bounded(s_kfull + 8 * (j % NK), (uint32_t)(j / NK) & 1u, &dummy_abort, kWaitLimitNs / 8);
       }
-      if (u > 0) mbar_wait_bounded(s_qland, (uint32_t)(u - 1) & 1u, &dummy_abort, kWaitLimitNs / 8);
+      if (KV8 && u > 0) mbar_wait_bounded(s_qland, (uint32_t)(u - 1) & 1u, &dummy_abort, kWaitLimitNs / 8);
     }
   } else if (warp == kWarpV) {
     // ================================================================= V producer
@@ -398,11 +426,12 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
         if (lane == 0) mbar_arrive(vland);
         continue;
       }
-      if (lane == 0) mbar_arrive_expect_tx(vland, (uint32_t)nbox * box_bytes);
+      if (lane == 0) mbar_arrive_expect_tx(vland, (KV8 ? 1u : 2u) * (uint32_t)nbox * box_bytes);
       __syncwarp();
       if (lane < nbox && lane < 8) {
         const uint32_t dv = s_v + (uint32_t)vs * L::kLandBytes + (uint32_t)lane * box_bytes;
         tma_load_4d(dv, &tm_v, vland, 0, vd.c_tok[lane], vd.h, vd.blk[lane]);
+        if (!KV8) tma_load_4d(dv + kTc2HalfBytes, &tm_v, vland, 64, vd.c_tok[lane], vd.h, vd.blk[lane]);
       }
     }
     if (!ok) {
@@ -420,8 +449,9 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
     // (the pipeline is a compile-time constant, so that the operands' addresses are known to be the same in all lanes)
     auto issue = [&](auto pipeline) {
     constexpr int t = decltype(pipeline)::value;
-    const uint32_t idesc_s = (1u << 4) | ((uint32_t)(NC >> 3) << 17) | ((uint32_t)(TOK >> 4) << 24);  // E4M3 by E4M3
-    const uint32_t idesc_l = umma_idesc_16bit(D, NC, 1, false), idesc_o = idesc_l | (1u << 15);  // A (V) is M-major, too
+    const uint32_t idesc_s = KV8 ? (1u << 4) | ((uint32_t)(NC >> 3) << 17) | ((uint32_t)(TOK >> 4) << 24)  // E4M3 by E4M3
+                                 : umma_idesc_16bit(TOK, NC, 0, true);
+    const uint32_t idesc_l = umma_idesc_16bit(D, NC, 1, !KV8), idesc_o = idesc_l | (1u << 15);  // A (V) is M-major, too
     const uint32_t to = tmem + L::kColO + (uint32_t)t * NC, tl = tmem + L::kColL + (uint32_t)t * NC;
     bool issued = false, ok = true, ended = false;
     uint32_t i = 0, j = 0;  // next stage whose scores / P.V are issued; i - j <= 2
@@ -484,10 +514,14 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
             const uint32_t ts = tmem + (uint32_t)(t * SB + i % SB) * NC;
             const uint64_t dk = umma_smem_desc(s_k + (uint32_t)ks * L::kLandBytes, 0, 1024), dq = umma_smem_desc(s_q, 0, 1024);
 #pragma unroll
-            for (int term = 0; term < 2; ++term)
+            for (int hh = 0; hh < 2; ++hh)  // the two terms; the two halves of the dims
 #pragma unroll
-              for (int k = 0; k < 4; ++k)  // 32 codes per MMA
-                umma_f8_ss(ts, dk + 2 * k, dq + (uint64_t)(term * NC * 8 + 2 * k), idesc_s, (term | k) ? 1u : 0u);
+              for (int k = 0; k < 4; ++k)  // 32 bytes per MMA
+                if (KV8)
+                  umma_f8_ss(ts, dk + 2 * k, dq + (uint64_t)(hh * NC * 8 + 2 * k), idesc_s, (hh | k) ? 1u : 0u);
+                else
+                  umma_ss(ts, dk + (uint64_t)(hh * (kTc2HalfBytes >> 4) + 2 * k), dq + (uint64_t)(hh * NC * 8 + 2 * k), idesc_s,
+                          (hh | k) ? 1u : 0u);
             umma_commit(sready);
             umma_commit(s_kempty + 8 * ks);
             if (last) umma_commit(s_qfree);
@@ -502,23 +536,24 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
         ++i;
       } else {
         const uint32_t m = 2 * j + t;
-        const int vs = m % NW;
+        constexpr int ring = KV8 ? NW : NV;
+        const int vs = m % ring;
         const int4 meta = g_meta[2 * (m % kTokMeta)];
         const int unit = g_meta[2 * (m % kTokMeta) + 1].w;
         const bool some = (meta.w & 0xffff) > 0, first = (meta.w >> 16) & 1;
         // (a unit's first P.V overwrites the accumulator that the softmax warps read at the end of the unit before)
-        if (!tok_wait(s_wfull + 8 * (m % (2 * NW)), (m / (2 * NW)) & 1u, s_abort) ||
+        if (!tok_wait((KV8 ? s_wfull : s_vland) + 8 * (m % (2 * ring)), (m / (2 * ring)) & 1u, s_abort) ||
             !tok_wait(s_pready + 8 * (2 * t + j % PB), (j / PB) & 1u, s_abort) ||
             (some && first && unit > 0 && !tok_wait(s_ofree, (uint32_t)(unit - 1) & 1u, s_abort))) {
           ok = false;
           break;
         }
-        const uint32_t freed = s_wempty + 8 * vs;
+        const uint32_t freed = (KV8 ? s_wempty : s_vtaken) + 8 * vs;
         if (some) {
           tc_fence_after_sync();
           if (elect_one()) {
             const uint64_t dp = umma_smem_desc(s_p + (uint32_t)(t * PB + j % PB) * L::kPBytes, 0, 1024);
-            const uint64_t dv = umma_smem_desc(s_w + (uint32_t)vs * kTc2SlotBytes, kTc2HalfBytes, 1024);
+            const uint64_t dv = umma_smem_desc((KV8 ? s_w : s_v) + (uint32_t)vs * kTc2SlotBytes, kTc2HalfBytes, 1024);
 #pragma unroll
             for (int k = 0; k < TOK / 16; ++k)  // 16 tokens: 16 rows of 128 bytes of V and of P
               umma_ss(to, dv + (uint64_t)(k * (2048 >> 4)), dp + (uint64_t)(k * (2048 >> 4)), idesc_o, (first && k == 0) ? 0u : 1u);
@@ -549,7 +584,30 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
       issue(std::integral_constant<int, 0>{});
     else
       issue(std::integral_constant<int, 1>{});
-  } else if (warp >= kWarpX) {
+  } else if (!KV8 && warp == kWarpX) {
+    // ================================================================= query rows (16-bit cache)
+    bool ok = true;
+    uint32_t u = 0;
+    for (;; ++u) {
+      if (!tok_wait(s_ufull + 8 * (u & 1), (u >> 1) & 1u, s_abort)) {
+        ok = false;
+        break;
+      }
+      const int4 unit = g_unit[u & 1];
+      if (unit.x < 0) break;
+      if (!tok_wait(s_qfree, (u & 1u) ^ 1u, s_abort)) {
+        ok = false;
+        break;
+      }
+      if (lane == 0) copy_queries(s_q, s_qready, unit.x, unit.y);
+      __syncwarp();
+    }
+    if (!ok) {
+      if (lane == 0) atomicOr(&p.hdr->status, kStatusWaitTimeout);
+      int dummy_abort = 0;
+      if (u > 0) mbar_wait_bounded(s_qready, (u - 1) & 1u, &dummy_abort, kWaitLimitNs / 8);
+    }
+  } else if (KV8 && warp >= kWarpX) {
     // ================================================================= widening warps (8-bit cache)
     const int tid_w = threadIdx.x & 127;
     bool ok = true;
@@ -820,7 +878,7 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
           // The columns' factors and first references.  Any value near the scores will do as a reference: those of one token,
           // warp w's first for columns 16 w ..  (Stages with nodes or few tokens form the maxima below, which replace a
           // reference of -inf.)
-          if (!tok_wait(s_qready, (uint32_t)meta2.w & 1u, s_abort)) {
+          if (KV8 && !tok_wait(s_qready, (uint32_t)meta2.w & 1u, s_abort)) {
             ok = false;
             break;
           }
@@ -832,7 +890,7 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
             if (lane == 0) {
 #pragma unroll
               for (int j = 0; j < 16; j += 2) {
-                const float2 f = *reinterpret_cast<const float2*>(mul + 16 * w4 + j);
+                const float2 f = KV8 ? *reinterpret_cast<const float2*>(mul + 16 * w4 + j) : make_float2(p.scale_log2e, p.scale_log2e);
                 cr[8 * w4 + j / 2] = make_float4(f.x, f.y, quick ? -__uint_as_float(s[j]) * f.x : 0.f,
                                                  quick ? -__uint_as_float(s[j + 1]) * f.y : 0.f);
               }
@@ -878,12 +936,12 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
               const float2 x = ffma2(make_float2(__uint_as_float(s[j]), __uint_as_float(s[j + 1])), make_float2(f.x, f.y),
                                      make_float2(f.z, f.w));
               top = fmax3(top, x.x, x.y);
-              pw[j / 2] = pack_f16x2(ex2(x.x), ex2(x.y));
+              pw[j / 2] = KV8 ? pack_f16x2(ex2(x.x), ex2(x.y)) : pack_bf16x2(ex2(x.x), ex2(x.y));
             }
             *reinterpret_cast<uint4*>(prow + (((2 * cc) ^ (r & 7)) << 4)) = make_uint4(pw[0], pw[1], pw[2], pw[3]);
             *reinterpret_cast<uint4*>(prow + (((2 * cc + 1) ^ (r & 7)) << 4)) = make_uint4(pw[4], pw[5], pw[6], pw[7]);
           }
-          refs_due = wg_any(top > kTokRaise && !raised);  // (once: the rounding of the two comparisons may differ)
+          refs_due = wg_any(top > kTokRaise<KV8> && !raised);  // (once: the rounding of the two comparisons may differ)
           if (!vote_ok) {
             ok = false;
             break;
@@ -938,7 +996,7 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
           float a = 1.f;
           if (ref_own == -INFINITY) {
             ref_own = m;  // nothing accumulated for this column so far
-          } else if (m > ref_own + kTokRaise) {
+          } else if (m > ref_own + kTokRaise<KV8>) {
             a = first ? 1.f : ex2(ref_own - m);
             ref_own = m;
             changed = !first;  // (on the unit's first stage nothing has been accumulated)
@@ -976,13 +1034,14 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
       if (ntok > 0) {
         if (ntok < TOK) {
           // V rows beyond the stage's tokens may hold anything (NaN included): clear them once the slot is written
-          const int vs = n % NW;
-          if (!tok_wait(s_wfull + 8 * (n % (2 * NW)), (n / (2 * NW)) & 1u, s_abort)) {
+          constexpr int ring = KV8 ? NW : NV;
+          const int vs = n % ring;
+          if (!tok_wait((KV8 ? s_wfull : s_vland) + 8 * (n % (2 * ring)), (n / (2 * ring)) & 1u, s_abort)) {
             ok = false;
             break;
           }
           if (r >= ntok) {
-            uint8_t* vrow = gen + (s_w - base) + (size_t)vs * kTc2SlotBytes + (size_t)r * 128;
+            uint8_t* vrow = gen + ((KV8 ? s_w : s_v) - base) + (size_t)vs * kTc2SlotBytes + (size_t)r * 128;
 #pragma unroll
             for (int c = 0; c < 16; ++c)
               *reinterpret_cast<uint4*>(vrow + (size_t)(c >> 3) * kTc2HalfBytes + ((c & 7) << 4)) = make_uint4(0u, 0u, 0u, 0u);
