@@ -5,6 +5,7 @@
 #include <cuda_fp8.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
+#include <type_traits>
 
 #include "ptx.cuh"
 
@@ -642,29 +643,55 @@ __global__ void __launch_bounds__(kVerifyThreads, 2) verify_kernel(const VerifyP
         const Df a = two_sum(s.hi, w.hi);
         s = Df{a.hi, __fadd_rn(s.lo, __fadd_rn(a.lo, w.lo))};
       };
-      for (int k = wid; k < ntile; k += warps) {
-        const int v0 = v_lo + k * kVerifyTile + lane;
-        Df s0 = {0.f, 0.f}, s1 = {0.f, 0.f};
-        if (v0 - lane + kVerifyTile <= v_hi) {
-          float pv[16], qv[16];
+      // Sums of the tiles' weights.  kKind: 0 the target's values (3: without the tokens that left), 1 p - q (one refusal: s = 1, the difference needs no
+      // product), 2 p - s q.  The weights are added as they come, without bringing hi and lo apart first.
+      auto sum_tiles = [&](auto kind) {
+        constexpr int kKind = decltype(kind)::value;
+        for (int k = wid; k < ntile; k += warps) {
+          const int v0 = v_lo + k * kVerifyTile + lane;
+          Df s0 = {0.f, 0.f}, s1 = {0.f, 0.f};
+          if (v0 - lane + kVerifyTile <= v_hi) {
+            float pv[16], qv[16];
 #pragma unroll
-          for (int e = 0; e < 16; ++e) pv[e] = pr[v0 + 32 * e];
-          if (qr) {
+            for (int e = 0; e < 16; ++e) pv[e] = pr[v0 + 32 * e];
+            if (kKind == 1 || kKind == 2) {
 #pragma unroll
-            for (int e = 0; e < 16; ++e) qv[e] = qr[v0 + 32 * e];
+              for (int e = 0; e < 16; ++e) qv[e] = qr[v0 + 32 * e];
+            }
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              Df w;
+              bool some;
+              if (kKind == 0 || kKind == 3) {
+                w = Df{pv[e], 0.f};
+                some = pv[e] > 0.f && !(kKind == 3 && (s_bits[(kVerifyTile / 32) * k + e] >> lane & 1u));
+              } else if (kKind == 1) {
+                w = two_sum(pv[e], -qv[e]);
+                some = w.hi > 0.f;
+              } else {
+                const float m = __fmul_rn(S.hi, qv[e]);
+                w = two_sum(pv[e], -m);
+                w.lo = __fsub_rn(w.lo, __fmaf_rn(S.lo, qv[e], __fmaf_rn(S.hi, qv[e], -m)));
+                some = __fadd_rn(w.hi, w.lo) > 0.f;
+              }
+              add_to(e & 1 ? s1 : s0, some ? w : Df{0.f, 0.f});
+            }
+          } else {
+            for (int v = v0; v < min(v_hi, v0 - lane + kVerifyTile); v += 32) add_to(s0, weight(v, pr[v], qr ? qr[v] : 0.f));
           }
-#pragma unroll
-          for (int e = 0; e < 16; e += 2) {
-            add_to(s0, weight(v0 + 32 * e, pv[e], qv[e]));
-            add_to(s1, weight(v0 + 32 * e + 32, pv[e + 1], qv[e + 1]));
-          }
-        } else {
-          for (int v = v0; v < v_hi; v += 32) add_to(s0, weight(v, pr[v], qr ? qr[v] : 0.f));
+          Df s = df_add(s0, s1);
+          for (int o = 16; o; o >>= 1) s = df_add(s, df_shfl_xor(s, o));
+          if (lane == 0) s_tile[k] = s;
         }
-        Df s = df_add(s0, s1);
-        for (int o = 16; o; o >>= 1) s = df_add(s, df_shfl_xor(s, o));
-        if (lane == 0) s_tile[k] = s;
-      }
+      };
+      if (!qr && drops > 0)
+        sum_tiles(std::integral_constant<int, 3>{});
+      else if (!qr)
+        sum_tiles(std::integral_constant<int, 0>{});
+      else if (S.hi == 1.f && S.lo == 0.f)
+        sum_tiles(std::integral_constant<int, 1>{});
+      else
+        sum_tiles(std::integral_constant<int, 2>{});
       __syncthreads();
       if (wid == 0) {  // the share's sum, to every CTA of the cluster
         Df s = {0.f, 0.f};
