@@ -89,6 +89,14 @@ def test_plan_slots(B, bs, ctx_hi, new_hi, row_len, short, extra, in_place):
     assert (want["status"] != 0) == (short > 0)
 
 
+@pytest.mark.parametrize("B,new_hi,row_len", [(40000, 2, 0), (30000, 3, 3), (9, 60000, 0), (600, 400, 0)])
+def test_plan_slots_many_rows(B, new_hi, row_len):
+    """Rows over many CTAs: runs of sequences without new tokens, sequences that end inside a thread's rows."""
+    ctx, new, table, held, free, head, kw = slots_case(B, B, 16, 20, new_hi)
+    new[B // 3: B // 2] = 0
+    run_slots(ctx, new, table, held, free, head, row_len=row_len, **kw)
+
+
 def test_plan_slots_tree_positions():
     rng = np.random.default_rng(5)
     for B, L in ((3, 7), (40, 64), (9, 256), (700, 12)):
@@ -428,6 +436,48 @@ def test_tree_attention_random_shapes():
         fp8 = (0.02, 0.03) if D == 128 and rng.random() < 0.4 else None
         kind = str(rng.choice(["tree", "forest", "chain", "star"]))
         both(tree_case(lens, hq, hkv, D, bs, N, seed=1000 + i, sizes=sizes, fp8=fp8, kind=kind, sigma=0.7))
+
+
+@pytest.mark.parametrize("fp8,hq,N", [(None, 8, 2), (None, 16, 16), (None, 32, 16), ((0.02, 0.03), 8, 2), ((0.02, 0.03), 32, 8),
+                                      ((0.02, 0.03), 64, 16)])
+def test_pools_beyond_32_bits(fp8, hq, N):
+    """Blocks at the far end of pools of more than 2^31 elements give what they give in a small pool; so do the append
+    and the moves of accepted tokens there."""
+    c = tree_case([N, 60, 300, 700], hq, 8, 128, 16, N, seed=hq, fp8=fp8, sigma=0.7)
+    small_nb, NB = c["k"].shape[0], 140000
+    assert NB * 8 * 16 * 128 > 2 ** 31
+    far = dict(c, table=np.where(c["table"] >= 0, NB - small_nb + c["table"], -1), k=None, v=None)
+    for name in "kv":
+        far[name] = torch.empty((NB,) + tuple(c[name].shape[1:]), dtype=c[name].dtype, device=DEV)
+        far[name][NB - small_nb:] = c[name]
+    far["shape"] = pool_shape(4, hq, 8, 128, 16, NB, c["table"].shape[1], "head_major")
+    near_out, far_out = run_tree(c), run_tree(far)
+    assert torch.equal(near_out.view(torch.int16), far_out.view(torch.int16))
+    # append the trees' tokens again, then keep the nodes 0, 1, 3, 4 ..
+    rope = spec.Rope(128, False, torch.logspace(0, -3, 64, device=DEV))
+    rows = torch.arange(4, device=DEV).repeat_interleave(N)
+    at = (gpu(c["lens"]) - N)[rows] + torch.arange(N, device=DEV, dtype=I32).repeat(4)
+    path = torch.full((4, N), -1, dtype=I32, device=DEV)
+    kept = [0] + [i for i in range(1, N) if i != 2]
+    path[:, : len(kept)] = torch.tensor(kept, dtype=I32, device=DEV)
+    count = torch.full((4,), len(kept) - 1, dtype=I32, device=DEV)
+    g = torch.Generator(device=DEV).manual_seed(5)
+    qkv = torch.randn((4 * N, hq + 16, 128), generator=g, device=DEV).to(torch.bfloat16)
+    for x in (c, far):
+        table = gpu(x["table"])
+        slots = (table[rows, (at // 16).long()] * 16 + at % 16).to(I32)
+        args = (x["shape"], rope, qkv[:, :hq], qkv[:, hq: hq + 8], qkv[:, hq + 8:], at.to(I32), slots,
+                torch.empty((4 * N, hq, 128), dtype=torch.bfloat16, device=DEV), x["k"], x["v"])
+        base, lens_out = gpu(c["lens"] - N), torch.empty(4, dtype=I32, device=DEV)
+        if fp8:
+            spec.rope_kv_append_fp8(*args, *fp8)
+            spec.kv_keep_path_fp8(x["shape"], x["k"], x["v"], table, base, path, count, lens_out)
+        else:
+            spec.rope_kv_append(*args)
+            spec.kv_keep_path(x["shape"], x["k"], x["v"], table, base, path, count, lens_out)
+    torch.cuda.synchronize()
+    for name in "kv":
+        assert torch.equal(far[name][NB - small_nb:].view(torch.uint8), c[name].view(torch.uint8))
 
 
 # ------------------------------------------------------------------------------------------------ verification
