@@ -830,8 +830,8 @@ constexpr int kKeepThreads = 128, kKeepBatch = 8;
 // A thread owns one 16-byte column of a sequence (cache, head, piece of the row) through all moves: entries of the
 // path increase, so a move's source is never below its target, and a source that has not been read yet is never a
 // target of an earlier move; a batch of moves is read before it is written.  HBM-bound (each row read and written
-// once): 512 sequences, 8 heads, up to 31 moves of 256-byte rows, take 17.3 us, 4.5 TB/s; for few sequences the chain path ->
-// table -> rows is what it takes (8 sequences: 3.0 us).
+// once): 512 sequences, 8 heads, up to 31 moves of 256-byte rows, take 16.8 us, 4.7 TB/s; for few sequences the chain path ->
+// table -> rows is what it takes (8 sequences: 2.7 us).
 __global__ void __launch_bounds__(kKeepThreads) keep_path_kernel(const KeepParams p) {
   __shared__ int64_t s_src[kTreeMaxNodes], s_dst[kTreeMaxNodes];
   __shared__ int s_count, s_path[kTreeMaxNodes];
@@ -840,14 +840,13 @@ __global__ void __launch_bounds__(kKeepThreads) keep_path_kernel(const KeepParam
   const int b = blockIdx.x, tid = threadIdx.x;
   const long long cap = (long long)p.MB << p.bs_log2;
   const int acc = min(max(0, p.num_accepted[b]), p.N - 1);
-  for (int j = tid; j <= acc; j += kKeepThreads) s_path[j] = p.path[(size_t)b * p.N + j];
+  const int32_t* path = p.path + (size_t)b * p.N;
+  if (tid == 0) s_count = acc + 1;
   __syncthreads();
-  if (tid == 0) {  // how far the branch is well formed
-    int j = 0;
-    if (s_path[0] == 0)
-      for (j = 1; j <= acc && s_path[j] > s_path[j - 1] && s_path[j] < p.N; ++j) {
-      }
-    s_count = j;
+  for (int j = tid; j < p.N; j += kKeepThreads) {  // how far the branch is well formed (entries are read beside the count)
+    const int node = path[j], before = j ? path[j - 1] : -1;
+    s_path[j] = node;
+    if (j <= acc && (node <= before || node >= p.N || (j == 0 && node != 0))) atomicMin(&s_count, j);
   }
   __syncthreads();
   const int count = s_count;
