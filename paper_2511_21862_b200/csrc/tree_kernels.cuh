@@ -890,7 +890,10 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
             if (lane == 0) {
 #pragma unroll
               for (int j = 0; j < 16; j += 2) {
-                const float2 f = KV8 ? *reinterpret_cast<const float2*>(mul + 16 * w4 + j) : make_float2(p.scale_log2e, p.scale_log2e);
+                float2 f = KV8 ? *reinterpret_cast<const float2*>(mul + 16 * w4 + j) : make_float2(p.scale_log2e, p.scale_log2e);
+                // (a factor that underflows to zero, of tiny queries or a tiny scale, would make NaN of hidden scores, -inf)
+                f.x = fmaxf(f.x, 1.17549435e-38f);
+                f.y = fmaxf(f.y, 1.17549435e-38f);
                 cr[8 * w4 + j / 2] = make_float4(f.x, f.y, quick ? -__uint_as_float(s[j]) * f.x : 0.f,
                                                  quick ? -__uint_as_float(s[j + 1]) * f.y : 0.f);
               }

@@ -438,6 +438,18 @@ def test_tree_attention_random_shapes():
         both(tree_case(lens, hq, hkv, D, bs, N, seed=1000 + i, sizes=sizes, fp8=fp8, kind=kind, sigma=0.7))
 
 
+@pytest.mark.parametrize("fp8", [None, (0.02, 0.03)], ids=["bf16", "fp8"])
+@pytest.mark.parametrize("hq,N", [(16, 2), (32, 4), (16, 9), (40, 8), (32, 12), (48, 16)])
+def test_tree_attention_tiny_and_zero_queries(hq, N, fp8):
+    """Rows of the smallest queries (all weights alike), zeros, and ordinary ones beside them."""
+    c = tree_case([N, 130, 300, 520], hq, 8, 128, 16, N, seed=N * hq, fp8=fp8, sigma=0.7, sizes=[N, N, max(1, N - 3), N])
+    c["q"][:, :, ::3] *= 2.0 ** -60
+    c["q"][:, :, ::3] *= 2.0 ** -66                       # around the smallest normal number, and below it
+    c["q"][:, :, 1::5] = 0.0
+    c["q"][2, max(1, N - 3):] = float("nan")
+    both(c)
+
+
 @pytest.mark.parametrize("fp8,hq,N", [(None, 8, 2), (None, 16, 16), (None, 32, 16), ((0.02, 0.03), 8, 2), ((0.02, 0.03), 32, 8),
                                       ((0.02, 0.03), 64, 16)])
 def test_pools_beyond_32_bits(fp8, hq, N):
