@@ -659,7 +659,7 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
         }
         ++u;
       }
-      // ---- V codes to f16, as in chunk_tc2_kernel: exact, to value / 256; 1024 units of 16 codes, eight per thread
+      // ---- V codes to f16: exact, to value / 256; 1024 units of 16 codes, eight per thread
       if (!tok_wait(s_vland + 8 * (n % (2 * NV)), (n / (2 * NV)) & 1u, s_abort) ||
           !tok_wait(s_wempty + 8 * ws, ((n / NW) & 1u) ^ 1u, s_abort)) {
         ok = false;
@@ -668,29 +668,32 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
       if (ntok > 0) {
         const uint8_t* src = gen + (s_v - base) + (size_t)vs * kTc2RawSlotBytes;
         uint8_t* dst = gen + (s_w - base) + (size_t)ws * kTc2SlotBytes;
-        const int c = tid_w & 7, r0 = tid_w >> 3;  // unit i of the thread: rows r0 + 16 i, chunk c
-        const uint8_t* s0 = src + (size_t)r0 * 128 + ((c ^ (r0 & 7)) << 4);
-        uint8_t* d0 = dst + (size_t)(c >> 2) * kTc2HalfBytes + (size_t)r0 * 128;
-        // a unit becomes two 16-byte chunks; chunks c and c + 4 lie in different halves, at the same banks, so the second
-        // four threads of a row write theirs in the other order
-        const bool swap = c >> 2;
-        const int x0 = ((2 * (c & 3) + (swap ? 1 : 0)) ^ (r0 & 7)) << 4, x1 = x0 ^ 16;
+        // A unit of 16 codes (a 16-byte chunk of a row) becomes two chunks.  Eight lanes take four chunks of an even row and the
+        // other four of the odd row behind it, so that neither their loads nor their stores meet at a bank.
+        const int cl = tid_w & 3, odd = (tid_w >> 2) & 1, r0 = 2 * (tid_w >> 3) + odd;  // rows r0 + 32 k
+        const uint8_t* s0 = src + (size_t)r0 * 128;
+        const int sa = ((cl + 4 * odd) ^ (r0 & 7)) << 4, sb = sa ^ 64;
+        uint8_t* da = dst + (size_t)odd * kTc2HalfBytes + (size_t)r0 * 128;
+        uint8_t* db = dst + (size_t)(odd ^ 1) * kTc2HalfBytes + (size_t)r0 * 128;
+        const int x0 = ((2 * cl) ^ (r0 & 7)) << 4, x1 = x0 ^ 16;
+        auto widened = [&](uint8_t* d, const uint4 w) {
+          *reinterpret_cast<uint4*>(d + x0) = make_uint4(e4m3x2_to_f16x2<kSelB0B1>(w.x), e4m3x2_to_f16x2<kSelB2B3>(w.x),
+                                                         e4m3x2_to_f16x2<kSelB0B1>(w.y), e4m3x2_to_f16x2<kSelB2B3>(w.y));
+          *reinterpret_cast<uint4*>(d + x1) = make_uint4(e4m3x2_to_f16x2<kSelB0B1>(w.z), e4m3x2_to_f16x2<kSelB2B3>(w.z),
+                                                         e4m3x2_to_f16x2<kSelB0B1>(w.w), e4m3x2_to_f16x2<kSelB2B3>(w.w));
+        };
 #pragma unroll 1
-        for (int k = 0; k < 2; ++k, s0 += 4 * 2048, d0 += 4 * 2048) {
+        for (int k = 0; k < TOK; k += 64) {
           uint4 w[4];
 #pragma unroll
-          for (int i = 0; i < 4; ++i)  // (rows beyond the stage's tokens: stale, cleared by the softmax threads)
-            w[i] = *reinterpret_cast<const uint4*>(s0 + i * 2048);
+          for (int i = 0; i < 2; ++i) {  // (rows beyond the stage's tokens: stale, cleared by the softmax threads)
+            w[2 * i] = *reinterpret_cast<const uint4*>(s0 + (k + 32 * i) * 128 + sa);
+            w[2 * i + 1] = *reinterpret_cast<const uint4*>(s0 + (k + 32 * i) * 128 + sb);
+          }
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const uint32_t a0 = swap ? w[i].z : w[i].x, a1 = swap ? w[i].w : w[i].y;
-            const uint32_t b0 = swap ? w[i].x : w[i].z, b1 = swap ? w[i].y : w[i].w;
-            *reinterpret_cast<uint4*>(d0 + i * 2048 + x0) =
-                make_uint4(e4m3x2_to_f16x2<kSelB0B1>(a0), e4m3x2_to_f16x2<kSelB2B3>(a0), e4m3x2_to_f16x2<kSelB0B1>(a1),
-                           e4m3x2_to_f16x2<kSelB2B3>(a1));
-            *reinterpret_cast<uint4*>(d0 + i * 2048 + x1) =
-                make_uint4(e4m3x2_to_f16x2<kSelB0B1>(b0), e4m3x2_to_f16x2<kSelB2B3>(b0), e4m3x2_to_f16x2<kSelB0B1>(b1),
-                           e4m3x2_to_f16x2<kSelB2B3>(b1));
+          for (int i = 0; i < 2; ++i) {
+            widened(da + (k + 32 * i) * 128, w[2 * i]);
+            widened(db + (k + 32 * i) * 128, w[2 * i + 1]);
           }
         }
         fence_proxy_async_smem();  // the widened slot is read by the MMAs through the async proxy
