@@ -60,11 +60,11 @@ constexpr float kTokRaise = KV8 ? 14.f : 60.f;
 template <int NC, bool KV8>
 struct TokSmem {
   static constexpr int SB = NC <= 48 ? 2 : 1;                               // score buffers of a pipeline (tensor memory is full)
-  static constexpr int PB = KV8 && NC <= 48 ? 2 : 1;                        // weight buffers of a pipeline
+  static constexpr int PB = 1;                                              // weight buffers of a pipeline
   static constexpr int kQBytes = NC * 256;                                  // [2][NC rows][128 bytes]
   static constexpr int kPBytes = 128 * 128;                                 // [128 tok][64 columns] f16
   static constexpr int kLandBytes = KV8 ? kTc2RawSlotBytes : kTc2SlotBytes; // K (or V) of one stage as TMA writes it
-  static constexpr int NK = 2, NV = PB == 1 ? 3 : 2, NW = 2;                // K slots, V slots, widened V slots
+  static constexpr int NK = KV8 && NC <= 48 ? 3 : 2, NV = 3, NW = 2;        // K slots, V slots, widened V slots
   static constexpr int kWarps = KV8 ? 16 : 13;
   // tensor memory: scores [2 pipelines][SB], values [2], sums [2], the operand of ones
   static constexpr int kTmemCols = 512;
@@ -75,7 +75,7 @@ struct TokSmem {
   static constexpr int kColumnBytes = NC * (2 * 8 + 4 + 2 * 4 * 4 + 2 * 4 + 4 * 4);
   __host__ __device__ static constexpr size_t total() {
     return 1024 + (KV8 ? 2 : 1) * (size_t)kQBytes + 2 * PB * (size_t)kPBytes + (size_t)(NK + NV) * kLandBytes +
-           (KV8 ? (size_t)NW * kTc2SlotBytes : 0) + kTokMeta * 32 + 2 * 16 + kTokDesc * sizeof(VStageDesc) + kColumnBytes + 640;
+           (KV8 ? (size_t)NW * kTc2SlotBytes : 0) + kTokMeta * 32 + 2 * 16 + kTokDesc * sizeof(VStageDesc) + kColumnBytes + 672;
   }
   static constexpr size_t kMost = 227 * 1024;  // shared memory of a CTA
 };
@@ -172,9 +172,9 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
   const uint32_t s_alpha = s_max + 2u * 4 * NC * 4;                      // [2][NC] factors of a rescaling
   const uint32_t s_ref = s_alpha + 2u * NC * 4;                          // [2 sets][2][NC] references at a unit's end
   const uint32_t s_bar = (s_ref + 4u * NC * 4 + 7u) & ~7u;
-  const uint32_t s_kfull = s_bar;                    // [NK] K has landed                              (TMA)
-  const uint32_t s_kempty = s_kfull + NK * 8;        // [NK] the score MMAs that read it are complete  (commit)
-  // (V has landed, V is widened: twice as many barriers as slots, of which stage n takes number n % (2 slots).  So a barrier
+  const uint32_t s_kfull = s_bar;                    // [2 NK] K has landed                            (TMA)
+  const uint32_t s_kempty = s_kfull + 2 * NK * 8;    // [NK] the score MMAs that read it are complete  (commit)
+  // (K or V has landed, V is widened: twice as many barriers as slots, of which stage n takes number n % (2 slots).  So a barrier
   // is one pipeline's, which sees each of its phases; one per slot could be two phases behind, and let a wait through.)
   const uint32_t s_vland = s_kempty + NK * 8;        // [2 NV] V has landed                            (TMA)
   const uint32_t s_vtaken = s_vland + 2 * NV * 8;    // [NV] it may be overwritten                     (widening threads)
@@ -207,10 +207,8 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
 
   if (threadIdx.x == 0) {
     *s_abort = 0;
-    for (int i = 0; i < NK; ++i) {
-      mbar_init(s_kfull + 8 * i, 1);
-      mbar_init(s_kempty + 8 * i, 1);
-    }
+    for (int i = 0; i < 2 * NK; ++i) mbar_init(s_kfull + 8 * i, 1);
+    for (int i = 0; i < NK; ++i) mbar_init(s_kempty + 8 * i, 1);
     for (int i = 0; i < 2 * NV; ++i) mbar_init(s_vland + 8 * i, 1);
     for (int i = 0; i < NV; ++i) mbar_init(s_vtaken + 8 * i, KV8 ? 4 : 1);
     for (int i = 0; i < 2 * NW; ++i) mbar_init(s_wfull + 8 * i, 4);
@@ -332,7 +330,7 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
           break;
         }
         const int ks = it % NK, ms = it % kTokMeta, ds = it % kTokDesc;
-        const uint32_t kfull = s_kfull + 8 * ks;
+        const uint32_t kfull = s_kfull + 8 * (it % (2 * NK));
         if (lane == 0) {
           const int flags = (s < 2 ? 1 : 0) | (s >= npad - 2 ? 2 : 0);  // a pipeline's first / last stage of the unit
           g_meta[2 * ms] = make_int4(d.y, b, h, ntok | (flags << 16));
@@ -387,7 +385,7 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
       if (lane == 0) {
         g_meta[2 * (it % kTokMeta)] = make_int4(-1, 0, 0, 0);
         g_vdesc[it % kTokDesc].nbox = -1;
-        mbar_arrive(s_kfull + 8 * (it % NK));
+        mbar_arrive(s_kfull + 8 * (it % (2 * NK)));
         mbar_arrive(s_vdfull + 8 * (it % kTokDesc));
         mbar_arrive(s_mfull + 8 * (it % kTokMeta));
       }
@@ -398,7 +396,7 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
       int dummy_abort = 0;
       for (int k = 0; k < (it < NK ? it : NK); ++k) {
         const int j = it - 1 - k;
-        mbar_wait_bounded(s_kfull + 8 * (j % NK), (uint32_t)(j / NK) & 1u, &dummy_abort, kWaitLimitNs / 8);
+        mbar_wait_bounded(s_kfull + 8 * (j % (2 * NK)), (uint32_t)(j / (2 * NK)) & 1u, &dummy_abort, kWaitLimitNs / 8);
       }
       if (KV8 && u > 0) mbar_wait_bounded(s_qland, (uint32_t)(u - 1) & 1u, &dummy_abort, kWaitLimitNs / 8);
     }
@@ -459,7 +457,7 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
     while (!ended || j < i) {
       const uint32_t n = 2 * i + t;
       const int ks = n % NK, ms = n % kTokMeta;
-      const uint32_t kfull = s_kfull + 8 * ks, kpar = (n / NK) & 1u;
+      const uint32_t kfull = s_kfull + 8 * (n % (2 * NK)), kpar = (n / (2 * NK)) & 1u;
       const uint32_t sfree = s_sfree + 8 * (2 * t + i % SB), spar = ((i - SB) / SB) & 1u;
       const bool may_s = !ended && i - j < 2, may_v = j < i;
       bool scores = may_s, there = false;  // (the scores' operands)
