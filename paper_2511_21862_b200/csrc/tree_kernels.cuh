@@ -35,12 +35,13 @@
 //
 // Measured, whole call (plan 10 us, this kernel, merge 12 us; 64 sequences of 256 to 8192 tokens, 8 kv heads; in brackets
 // the kernel with columns on M): 16-bit cache 18 columns 118 us (131), 32: 120 (134), 48: 129 (138), 64: 142 (141, hence the
-// limit); 8-bit cache 18: 120 (168), 32: 122 (171), 48: 135 (173), 64: 153 (176), 96: 267 with an earlier version (193).
-// 32 sequences of 4096 to 32768 tokens, 8-bit, 40 columns: 292 us (411), 3.1 TB/s of codes.  At 18 columns the 16-bit call runs at 0.80
-// of the measured copy rate, plan and merge included.  Over the 8-bit cache a stage of 128 tokens takes about 2000 cycles
-// where its 32 KiB would take 1400: a pipeline's chain (1300 cycles of weights, 1000 of barriers between the roles, 1300 of
-// widening and P.V) is what bounds it, two pipelines cannot hide all of it, and four sets of softmax warps do not fit the
-// register file.
+// limit); 8-bit cache 18: 114 (168), 32: 116 (171), 48: 127 (173), 64: 154 (176), 96: 267 with an earlier version (193).
+// 32 sequences of 4096 to 32768 tokens, 8-bit, 40 columns: 278 us (411), 3.3 TB/s of codes.  At 18 columns the 16-bit call runs
+// at 0.80 of the measured copy rate, plan and merge included.  Over the 8-bit cache a stage of 128 tokens takes about 2000
+// cycles where its 32 KiB would take 1400, and a change of units 9000 more: a pipeline's chain (1300 cycles of weights, 1000 of
+// barriers between the roles, 1300 of widening and P.V) is what bounds it, two pipelines cannot hide all of it, and four
+// sets of softmax warps do not fit the register file.  Deep rings matter more than a second weight buffer: three K and V slots
+// instead of two, at its cost, were worth 5 us of 120.
 #pragma once
 #include <type_traits>
 
@@ -60,7 +61,6 @@ constexpr float kTokRaise = KV8 ? 14.f : 60.f;
 template <int NC, bool KV8>
 struct TokSmem {
   static constexpr int SB = NC <= 48 ? 2 : 1;                               // score buffers of a pipeline (tensor memory is full)
-  static constexpr int PB = 1;                                              // weight buffers of a pipeline
   static constexpr int kQBytes = NC * 256;                                  // [2][NC rows][128 bytes]
   static constexpr int kPBytes = 128 * 128;                                 // [128 tok][64 columns] f16
   static constexpr int kLandBytes = KV8 ? kTc2RawSlotBytes : kTc2SlotBytes; // K (or V) of one stage as TMA writes it
@@ -74,7 +74,7 @@ struct TokSmem {
   // the references at a unit's end (two sets take turns)
   static constexpr int kColumnBytes = NC * (2 * 8 + 4 + 2 * 4 * 4 + 2 * 4 + 4 * 4);
   __host__ __device__ static constexpr size_t total() {
-    return 1024 + (KV8 ? 2 : 1) * (size_t)kQBytes + 2 * PB * (size_t)kPBytes + (size_t)(NK + NV) * kLandBytes +
+    return 1024 + (KV8 ? 2 : 1) * (size_t)kQBytes + 2 * (size_t)kPBytes + (size_t)(NK + NV) * kLandBytes +
            (KV8 ? (size_t)NW * kTc2SlotBytes : 0) + kTokMeta * 32 + 2 * 16 + kTokDesc * sizeof(VStageDesc) + kColumnBytes + 672;
   }
   static constexpr size_t kMost = 227 * 1024;  // shared memory of a CTA
@@ -149,7 +149,7 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
                 const __grid_constant__ CUtensorMap tm_q, const DecodeParams p) {
   using L = TokSmem<NC, KV8>;
   constexpr int D = 128, TOK = kTc2StageTok;
-  constexpr int SB = L::SB, PB = L::PB, NK = L::NK, NV = L::NV, NW = L::NW;
+  constexpr int SB = L::SB, NK = L::NK, NV = L::NV, NW = L::NW;
   constexpr int kWarpK = 8, kWarpV = 9, kWarpM = 10, kWarpX = 12;
   static_assert(L::total() <= L::kMost, "shared memory");
   static_assert(NC % 16 == 0 && NC <= 64 && NC <= kTokMaxColumns<KV8>, "columns of an MMA with M = 128, and what shared memory holds");
@@ -159,8 +159,8 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
   uint8_t* gen = smem_raw + (base - raw);
   const uint32_t s_q = base;                                             // the unit's query rows as two terms
   const uint32_t s_qraw = s_q + (uint32_t)L::kQBytes;                    // ... in bf16
-  const uint32_t s_p = s_qraw + (KV8 ? (uint32_t)L::kQBytes : 0u);                   // [2 pipelines][PB] weights
-  const uint32_t s_k = s_p + 2u * PB * L::kPBytes;                       // [NK] K slots
+  const uint32_t s_p = s_qraw + (KV8 ? (uint32_t)L::kQBytes : 0u);       // [2 pipelines] weights
+  const uint32_t s_k = s_p + 2u * L::kPBytes;                            // [NK] K slots
   const uint32_t s_v = s_k + (uint32_t)NK * L::kLandBytes;               // [NV] V slots
   const uint32_t s_w = s_v + (uint32_t)NV * L::kLandBytes;               // [NW] widened V slots
   const uint32_t s_unit = s_w + (KV8 ? (uint32_t)NW * kTc2SlotBytes : 0u);  // [2] int4 {sequence, kv head}, 16-bit cache
@@ -187,9 +187,9 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
                                                      //     complete, both have read the columns' factors (4)
   const uint32_t s_sready = s_qfree + 8;             // [2 pipelines][2] the scores are in tensor memory (commit)
   const uint32_t s_sfree = s_sready + 32;            // [2][2] ... have been read                      (4 warps)
-  const uint32_t s_pready = s_sfree + 32;            // [2][2] weights written, O rescaled, V rows clean (4 warps)
-  const uint32_t s_pvdone = s_pready + 32;           // [2][2] the stage's P.V is complete             (commit)
-  const uint32_t s_wg = s_pvdone + 32;               // [2] the four warps of a pipeline meet          (4)
+  const uint32_t s_pready = s_sfree + 32;            // [2] weights written, O rescaled, V rows clean (4 warps)
+  const uint32_t s_pvdone = s_pready + 16;           // [2] the stage's P.V is complete             (commit)
+  const uint32_t s_wg = s_pvdone + 16;               // [2] the four warps of a pipeline meet          (4)
   const uint32_t s_both = s_wg + 16;                 // [1] the softmax warps of both pipelines meet   (8)
   const uint32_t s_qland = s_both + 8;               // the unit's bf16 query rows have landed         (TMA)
   const uint32_t s_qtaken = s_qland + 8;             // ... have been split                            (widening threads)
@@ -217,14 +217,14 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
     for (int i = 0; i < kTokMeta; ++i) mbar_init(s_mfull + 8 * i, 1);
     for (int i = 0; i < 2; ++i) {
       mbar_init(s_wg + 8 * i, 4);
+      mbar_init(s_pready + 8 * i, 4);
+      mbar_init(s_pvdone + 8 * i, 1);
       mbar_init(s_drain + 8 * i, 1);
       mbar_init(s_ufull + 8 * i, 1);
     }
     for (int i = 0; i < 4; ++i) {
       mbar_init(s_sready + 8 * i, 1);
       mbar_init(s_sfree + 8 * i, 4);
-      mbar_init(s_pready + 8 * i, 4);
-      mbar_init(s_pvdone + 8 * i, 1);
     }
     mbar_init(s_qready, KV8 ? 4 : 1);
     mbar_init(s_qfree, 4);
@@ -473,7 +473,7 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
               break;
             }
           }
-          if (now(s_pready + 8 * (2 * t + j % PB), (j / PB) & 1u)) {
+          if (now(s_pready + 8 * t, j & 1u)) {
             scores = false;
             break;
           }
@@ -541,7 +541,7 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
         const bool some = (meta.w & 0xffff) > 0, first = (meta.w >> 16) & 1;
         // (a unit's first P.V overwrites the accumulator that the softmax warps read at the end of the unit before)
         if (!tok_wait((KV8 ? s_wfull : s_vland) + 8 * (m % (2 * ring)), (m / (2 * ring)) & 1u, s_abort) ||
-            !tok_wait(s_pready + 8 * (2 * t + j % PB), (j / PB) & 1u, s_abort) ||
+            !tok_wait(s_pready + 8 * t, j & 1u, s_abort) ||
             (some && first && unit > 0 && !tok_wait(s_ofree, (uint32_t)(unit - 1) & 1u, s_abort))) {
           ok = false;
           break;
@@ -550,7 +550,7 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
         if (some) {
           tc_fence_after_sync();
           if (elect_one()) {
-            const uint64_t dp = umma_smem_desc(s_p + (uint32_t)(t * PB + j % PB) * L::kPBytes, 0, 1024);
+            const uint64_t dp = umma_smem_desc(s_p + (uint32_t)t * L::kPBytes, 0, 1024);
             const uint64_t dv = umma_smem_desc((KV8 ? s_w : s_v) + (uint32_t)vs * kTc2SlotBytes, kTc2HalfBytes, 1024);
 #pragma unroll
             for (int k = 0; k < TOK / 16; ++k)  // 16 tokens: 16 rows of 128 bytes of V and of P
@@ -558,12 +558,12 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
 #pragma unroll
             for (int k = 0; k < TOK / 16; ++k)  // the columns' sums of weights, in every lane
               umma_ts(tl, tmem + L::kColOne, dp + (uint64_t)(k * (2048 >> 4)), idesc_l, (first && k == 0) ? 0u : 1u);
-            umma_commit(s_pvdone + 8 * (2 * t + j % PB));
+            umma_commit(s_pvdone + 8 * t);
             umma_commit(freed);
           }
           issued = true;
         } else if (elect_one()) {
-          mbar_arrive(s_pvdone + 8 * (2 * t + j % PB));
+          mbar_arrive(s_pvdone + 8 * t);
           mbar_arrive(freed);
         }
         __syncwarp();
@@ -908,17 +908,13 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
           if (w4 == 0 && lane == 0) mbar_arrive(s_qfree);
         }
       }
-      // The weight buffer has to be free, and the accumulators complete where they are touched: by the P.V that used the
-      // buffer last, and of the pipeline's stage before.
-      bool values_seen = false;
-      auto wait_values = [&](uint32_t back) {
-        return i < back || tok_wait(s_pvdone + 8 * (2 * t + (i - back) % PB), ((i - back) / PB) & 1u, s_abort);
-      };
-      if (!wait_values(PB)) {
+      // The weight buffer has to be free, and the accumulators complete where they are touched: the P.V of the pipeline's
+      // stage before is complete.
+      if (i > 0 && !tok_wait(s_pvdone + 8 * t, (i - 1) & 1u, s_abort)) {
         ok = false;
         break;
       }
-      uint8_t* prow = gen + (s_p - base) + (size_t)(t * PB + i % PB) * L::kPBytes + (size_t)r * 128;  // this token's weights
+      uint8_t* prow = gen + (s_p - base) + (size_t)t * L::kPBytes + (size_t)r * 128;  // this token's weights
       for (bool formed = ntok == 0, raised = false;;) {
         if (!formed && !refs_due) {
           // ---- weights: 2^(score * factor - reference), into the second MMAs' operand
@@ -957,12 +953,9 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
             if (lane == 0) mbar_arrive(sfree);
           }
         }
-        if (!values_seen) {  // a unit that ended is written now
-          if (!wait_values(1) || (unit_open && !finish_unit())) {
-            ok = false;
-            break;
-          }
-          values_seen = true;
+        if (unit_open && !finish_unit()) {  // a unit that ended is written now
+          ok = false;
+          break;
         }
         if (formed) break;
         // ---- references: the columns' maxima over the stage, of the warp's tokens, then of the warps
@@ -1058,7 +1051,7 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
         if (lane == 0) mbar_arrive(sfree);
       }
       __syncwarp();
-      if (lane == 0) mbar_arrive(s_pready + 8 * (2 * t + i % PB));
+      if (lane == 0) mbar_arrive(s_pready + 8 * t);
 
       if (last) {  // the rest of the unit's work is put off (finish_unit)
         unit_open = true;
