@@ -35,7 +35,7 @@
 //
 // Measured, whole call (plan 10 us, this kernel, merge 12 us; 64 sequences of 256 to 8192 tokens, 8 kv heads; in brackets
 // the kernel with columns on M): 16-bit cache 18 columns 118 us (131), 32: 120 (134), 48: 129 (138), 64: 142 (141, hence the
-// limit); 8-bit cache 18: 114 (168), 32: 116 (171), 48: 127 (173), 64: 154 (176), 96: 267 with an earlier version (193).
+// limit); 8-bit cache 18: 107 (168), 32: 110 (171), 48: 127 (173), 64: 154 (176), 96: 267 with an earlier version (193).
 // 32 sequences of 4096 to 32768 tokens, 8-bit, 40 columns: 278 us (411), 3.3 TB/s of codes.  At 18 columns the 16-bit call runs
 // at 0.80 of the measured copy rate, plan and merge included.  Over the 8-bit cache a stage of 128 tokens takes about 2000
 // cycles where its 32 KiB would take 1400, and a change of units 9000 more: a pipeline's chain (1300 cycles of weights, 1000 of
@@ -65,6 +65,10 @@ struct TokSmem {
   static constexpr int kPBytes = 128 * 128;                                 // [128 tok][64 columns] f16
   static constexpr int kLandBytes = KV8 ? kTc2RawSlotBytes : kTc2SlotBytes; // K (or V) of one stage as TMA writes it
   static constexpr int NK = KV8 && NC <= 48 ? 3 : 2, NV = 3, NW = 2;        // K slots, V slots, widened V slots
+  // 8-bit cache: four warps widen V, together (48 columns: 278 us for the long batch above, 296 in two groups), or, where the
+  // softmax is short and the widening the longer chain, in a group for each pipeline, of which one works while the other
+  // waits (32 columns: 107 us, 114 together).
+  static constexpr int kWidenGroups = NC <= 32 ? 2 : 1, kWidenWarps = 4 / kWidenGroups;
   static constexpr int kWarps = KV8 ? 16 : 13;
   // tensor memory: scores [2 pipelines][SB], values [2], sums [2], the operand of ones
   static constexpr int kTmemCols = 512;
@@ -210,8 +214,8 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
     for (int i = 0; i < 2 * NK; ++i) mbar_init(s_kfull + 8 * i, 1);
     for (int i = 0; i < NK; ++i) mbar_init(s_kempty + 8 * i, 1);
     for (int i = 0; i < 2 * NV; ++i) mbar_init(s_vland + 8 * i, 1);
-    for (int i = 0; i < NV; ++i) mbar_init(s_vtaken + 8 * i, KV8 ? 4 : 1);
-    for (int i = 0; i < 2 * NW; ++i) mbar_init(s_wfull + 8 * i, 4);
+    for (int i = 0; i < NV; ++i) mbar_init(s_vtaken + 8 * i, KV8 ? L::kWidenWarps : 1);
+    for (int i = 0; i < 2 * NW; ++i) mbar_init(s_wfull + 8 * i, L::kWidenWarps);
     for (int i = 0; i < NW; ++i) mbar_init(s_wempty + 8 * i, 1);
     for (int i = 0; i < kTokDesc; ++i) mbar_init(s_vdfull + 8 * i, 1);
     for (int i = 0; i < kTokMeta; ++i) mbar_init(s_mfull + 8 * i, 1);
@@ -607,10 +611,11 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
     }
   } else if (KV8 && warp >= kWarpX) {
     // ================================================================= widening warps (8-bit cache)
-    const int tid_w = threadIdx.x & 127;
+    constexpr int kGroup = 32 * L::kWidenWarps;
+    const int tid_w = threadIdx.x & (kGroup - 1);
     bool ok = true;
     uint32_t u = 0;
-    for (uint32_t n = 0;; ++n) {
+    for (uint32_t n = L::kWidenGroups == 2 ? (threadIdx.x - 32 * kWarpX) / kGroup : 0u;; n += L::kWidenGroups) {
       const int vs = n % NV, ws = n % NW, ms = n % kTokMeta;
       if (!tok_wait(s_mfull + 8 * ms, (n / kTokMeta) & 1u, s_abort)) {
         ok = false;
@@ -619,7 +624,7 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
       const int4 meta = g_meta[2 * ms];
       if (meta.x < 0) break;
       const int ntok = meta.w & 0xffff;
-      if (!(n & 1) && ((meta.w >> 16) & 1)) {
+      if (((meta.w >> 16) & 1) && (L::kWidenGroups == 2 || !(n & 1))) {
         // ---- a unit starts: its query rows as hi + lo, scaled by a power of two that brings the row's largest magnitude
         // into [128, 256) (E4M3 goes up to 448).  A warp takes every fourth row, lane l dims 4 l .. 4 l + 3.
         if (!tok_wait(s_qland, u & 1u, s_abort) || !tok_wait(s_qfree, (u & 1u) ^ 1u, s_abort)) {
@@ -668,7 +673,8 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
         uint8_t* dst = gen + (s_w - base) + (size_t)ws * kTc2SlotBytes;
         // A unit of 16 codes (a 16-byte chunk of a row) becomes two chunks.  Eight lanes take four chunks of an even row and the
         // other four of the odd row behind it, so that neither their loads nor their stores meet at a bank.
-        const int cl = tid_w & 3, odd = (tid_w >> 2) & 1, r0 = 2 * (tid_w >> 3) + odd;  // rows r0 + 32 k
+        const int cl = tid_w & 3, odd = (tid_w >> 2) & 1, r0 = 2 * (tid_w >> 3) + odd;
+        constexpr int kStep = kGroup / 4;  // rows r0 + kStep k
         const uint8_t* s0 = src + (size_t)r0 * 128;
         const int sa = ((cl + 4 * odd) ^ (r0 & 7)) << 4, sb = sa ^ 64;
         uint8_t* da = dst + (size_t)odd * kTc2HalfBytes + (size_t)r0 * 128;
@@ -681,17 +687,17 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
                                                          e4m3x2_to_f16x2<kSelB0B1>(w.w), e4m3x2_to_f16x2<kSelB2B3>(w.w));
         };
 #pragma unroll 1
-        for (int k = 0; k < TOK; k += 64) {
+        for (int k = 0; k < TOK; k += 2 * kStep) {
           uint4 w[4];
 #pragma unroll
           for (int i = 0; i < 2; ++i) {  // (rows beyond the stage's tokens: stale, cleared by the softmax threads)
-            w[2 * i] = *reinterpret_cast<const uint4*>(s0 + (k + 32 * i) * 128 + sa);
-            w[2 * i + 1] = *reinterpret_cast<const uint4*>(s0 + (k + 32 * i) * 128 + sb);
+            w[2 * i] = *reinterpret_cast<const uint4*>(s0 + (k + kStep * i) * 128 + sa);
+            w[2 * i + 1] = *reinterpret_cast<const uint4*>(s0 + (k + kStep * i) * 128 + sb);
           }
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
-            widened(da + (k + 32 * i) * 128, w[2 * i]);
-            widened(db + (k + 32 * i) * 128, w[2 * i + 1]);
+            widened(da + (k + kStep * i) * 128, w[2 * i]);
+            widened(db + (k + kStep * i) * 128, w[2 * i + 1]);
           }
         }
         fence_proxy_async_smem();  // the widened slot is read by the MMAs through the async proxy
