@@ -207,7 +207,7 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
   volatile uint32_t* g_slot = reinterpret_cast<volatile uint32_t*>(gen + (s_slot - base));
   volatile int* s_abort = reinterpret_cast<volatile int*>(gen + (s_slot + 4 - base));
   volatile int* g_vote = reinterpret_cast<volatile int*>(gen + (s_slot + 8 - base));
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;  // (known to be the same in all lanes)
 
   if (threadIdx.x == 0) {
     *s_abort = 0;
@@ -615,7 +615,7 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
     const int tid_w = threadIdx.x & (kGroup - 1);
     bool ok = true;
     uint32_t u = 0;
-    for (uint32_t n = L::kWidenGroups == 2 ? (threadIdx.x - 32 * kWarpX) / kGroup : 0u;; n += L::kWidenGroups) {
+    for (uint32_t n = L::kWidenGroups == 2 ? (uint32_t)(warp - kWarpX) / L::kWidenWarps : 0u;; n += L::kWidenGroups) {
       const int vs = n % NV, ws = n % NW, ms = n % kTokMeta;
       if (!tok_wait(s_mfull + 8 * ms, (n / kTokMeta) & 1u, s_abort)) {
         ok = false;
