@@ -456,8 +456,7 @@ static int launch_tree_tok_nc(const CUtensorMap& tk, const CUtensorMap& tv, Deco
                               cudaStream_t st, int dev, bool dry) {
   if (p.GQ <= 32) return launch_tree_tok<32, KV8>(tk, tv, p, di, st, dev, dry);
   if (p.GQ <= 48) return launch_tree_tok<48, KV8>(tk, tv, p, di, st, dev, dry);
-  if constexpr (KV8) return launch_tree_tok<64, true>(tk, tv, p, di, st, dev, dry);
-  return OOCO_E_UNSUPPORTED;  // (not reached: kTokMaxColumns)
+  return launch_tree_tok<64, KV8>(tk, tv, p, di, st, dev, dry);
 }
 
 // Tree attention: the decode shapes that the rules of decode_core pick without a knob, compiled with the tree's mask.
@@ -466,8 +465,8 @@ static int launch_tree(int head_dim, bool kv8, bool chunk, bool tc2, bool row16,
                        const CUtensorMap& tv, DecodeParams& p, const DeviceInfo& di, int cps, cudaStream_t st, int dev,
                        bool dry) {
   if (chunk && head_dim == 128) {
-    if (kv8 && p.GQ <= kTokMaxColumns<true>) return launch_tree_tok_nc<true>(tk, tv, p, di, st, dev, dry);
-    if (!kv8 && p.GQ <= kTokMaxColumns<false>) return launch_tree_tok_nc<false>(tk, tv, p, di, st, dev, dry);
+    if (p.GQ <= kTokMaxColumns)
+      return kv8 ? launch_tree_tok_nc<true>(tk, tv, p, di, st, dev, dry) : launch_tree_tok_nc<false>(tk, tv, p, di, st, dev, dry);
     if (tc2)
       return kv8 ? launch_chunk_tc2<true, true>(tk, tv, p, di, st, dev, dry)
                  : launch_chunk_tc2<false, true>(tk, tv, p, di, st, dev, dry);
@@ -870,7 +869,7 @@ static int decode_core(const ooco_shape_t* s, const void* q, const void* k_cache
   p.items_per_cta = plan_items_per_cta(G_);
   // the 8-bit path widens codes to value / 256 (kE4m3WidenFactor): both scales carry the factor back (K's only
   // where K is widened: the tcgen05 score path multiplies the codes' own values)
-  const bool kv8_tc = (kv8 && tree && chunk && G_ <= kTokMaxColumns<true>) ||
+  const bool kv8_tc = (kv8 && tree && chunk && G_ <= kTokMaxColumns) ||
                       (kv8 && !chunk && ncw == 8 && (tree || g_knobs[kKnobKv8Tcgen05].load() != 0));
   p.scale_log2e = scale * 1.4426950408889634f * (kv8 ? kv8->k_scale * (kv8_tc ? 1.f : kE4m3WidenFactor) : 1.f);
   p.v_scale = kv8 ? kv8->v_scale * kE4m3WidenFactor : 1.f;

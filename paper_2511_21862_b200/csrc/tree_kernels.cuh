@@ -1,5 +1,4 @@
-// Tree attention of 17 to 48 (8-bit cache: 64) score columns per (sequence, kv head) at head_dim 128, with the TOKENS on the
-// MMA's M axis.
+// Tree attention of 17 to 64 score columns per (sequence, kv head) at head_dim 128, with the TOKENS on the MMA's M axis.
 //
 //   S^T[128 tok x NC]   = K_slot[128 tok x 128] . Q^T          tcgen05.mma M128, N = NC columns
 //   O^T[128 dim x NC] (+)= V_slot^T[128 dim x 128 tok] . P     tcgen05.mma M128, N = NC columns
@@ -34,14 +33,15 @@
 // the common exit, and the tensor memory is released after the MMAs in flight.
 //
 // Measured, whole call (plan 10 us, this kernel, merge 12 us; 64 sequences of 256 to 8192 tokens, 8 kv heads; in brackets
-// the kernel with columns on M): 16-bit cache 18 columns 118 us (131), 32: 120 (134), 48: 129 (138), 64: 142 (141, hence the
-// limit); 8-bit cache 18: 107 (168), 32: 110 (171), 48: 127 (173), 64: 154 (176), 96: 267 with an earlier version (193).
-// 32 sequences of 4096 to 32768 tokens, 8-bit, 40 columns: 278 us (411), 3.3 TB/s of codes.  At 18 columns the 16-bit call runs
-// at 0.80 of the measured copy rate, plan and merge included.  Over the 8-bit cache a stage of 128 tokens takes about 2000
-// cycles where its 32 KiB would take 1400, and a change of units 9000 more: a pipeline's chain (1300 cycles of weights, 1000 of
-// barriers between the roles, 1300 of widening and P.V) is what bounds it, two pipelines cannot hide all of it, and four
-// sets of softmax warps do not fit the register file.  Deep rings matter more than a second weight buffer: three K and V slots
-// instead of two, at its cost, were worth 5 us of 120.
+// the kernel with columns on M): 16-bit cache 18 columns 114 us (131), 32: 116 (134), 48: 123 (138), 64: 132 (136); 8-bit cache
+// 18: 104 (168), 32: 106 (171), 48: 119 (173), 64: 151 (176); beyond, with earlier versions of both: 8-bit 96: 267 (193), 16-bit 96:
+// 228 (156), since scores and accumulators fill tensor memory at 64.  32 sequences of 4096 to 32768 tokens, 8-bit, 40 columns:
+// 261 to 271 us (411), 3.4 TB/s of codes.  At 18 columns the 16-bit call runs at 0.82 of the measured copy rate, plan and merge
+// included.  Over the 8-bit cache a stage of 128 tokens takes about 1900 cycles where its 32 KiB would take 1400, and a change of
+// units some thousand more: a pipeline's chain (weights, barriers between the roles, widening, P.V) is what bounds it, two
+// pipelines cannot hide all of it, and four sets of softmax warps do not fit the register file.  What mattered: deep rings
+// (three K and V slots instead of two, at the price of a second weight buffer: 5 us of 120), and that the compiler knows
+// the warp's number to be the same in all lanes, so that addresses live in uniform registers (17 us of 278).
 #pragma once
 #include <type_traits>
 
@@ -50,9 +50,7 @@
 namespace ooco {
 
 constexpr int kTokMeta = 8, kTokDesc = 8;  // ring sizes: meta words, V descriptors
-// score columns that the kernel takes, from 17 (both sides measured above)
-template <bool KV8>
-constexpr int kTokMaxColumns = KV8 ? 64 : 48;
+constexpr int kTokMaxColumns = 64;         // score columns that the kernel takes, from 17 (both sides measured above)
 // A reference is raised when a score passes it by this much (log2 units): weights stay below 2^16 for f16 (the 8-bit
 // cache), where small ones lose bits below 2^-14; bf16 has the range of fp32, and a column's sum stays below 2^60 times its tokens.
 template <bool KV8>
@@ -156,7 +154,7 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
   constexpr int SB = L::SB, NK = L::NK, NV = L::NV, NW = L::NW;
   constexpr int kWarpK = 8, kWarpV = 9, kWarpM = 10, kWarpX = 12;
   static_assert(L::total() <= L::kMost, "shared memory");
-  static_assert(NC % 16 == 0 && NC <= 64 && NC <= kTokMaxColumns<KV8>, "columns of an MMA with M = 128, and what shared memory holds");
+  static_assert(NC % 16 == 0 && NC <= kTokMaxColumns, "columns of an MMA with M = 128, and what shared memory holds");
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw);
   const uint32_t base = (raw + 1023u) & ~1023u;
