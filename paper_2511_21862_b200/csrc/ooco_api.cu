@@ -454,6 +454,7 @@ static int launch_tree_tok(const CUtensorMap& tk, const CUtensorMap& tv, DecodeP
 template <bool KV8>
 static int launch_tree_tok_nc(const CUtensorMap& tk, const CUtensorMap& tv, DecodeParams& p, const DeviceInfo& di,
                               cudaStream_t st, int dev, bool dry) {
+  if (p.GQ <= 16) return launch_tree_tok<16, KV8>(tk, tv, p, di, st, dev, dry);
   if (p.GQ <= 32) return launch_tree_tok<32, KV8>(tk, tv, p, di, st, dev, dry);
   if (p.GQ <= 48) return launch_tree_tok<48, KV8>(tk, tv, p, di, st, dev, dry);
   return launch_tree_tok<64, KV8>(tk, tv, p, di, st, dev, dry);
@@ -473,12 +474,8 @@ static int launch_tree(int head_dim, bool kv8, bool chunk, bool tc2, bool row16,
     return launch_chunk_tc<true, true>(tk, tv, p, di, cps, st, dev, dry);
   }
   if (chunk) return launch_chunk_ncw<64, true>(ncw, tk, tv, p, di, cps, st, dev, dry);
-  if (row16)
-    return head_dim == 128 ? launch_row16<128, true>(tk, tv, p, di, cps, st, dev, dry)
-                           : launch_row16<64, true>(tk, tv, p, di, cps, st, dev, dry);
-  if (kv8)
-    return p.GQ > 8 ? launch_main<128, 8, 2, 1, 2, true>(tk, tv, p, di, cps, 0, st, dev, dry)
-                    : launch_main<128, 8, 1, 1, 2, true>(tk, tv, p, di, cps, 0, st, dev, dry);
+  if (row16) return launch_row16<64, true>(tk, tv, p, di, cps, st, dev, dry);
+  if (kv8) return launch_main<128, 8, 1, 1, 2, true>(tk, tv, p, di, cps, 0, st, dev, dry);
   return head_dim == 128 ? launch_main<128, 4, 1, 1, 0, true>(tk, tv, p, di, cps, 0, st, dev, dry)
                          : launch_main<64, 4, 1, 1, 0, true>(tk, tv, p, di, cps, 0, st, dev, dry);
 }
@@ -808,7 +805,9 @@ static int decode_core(const ooco_shape_t* s, const void* q, const void* k_cache
     tpw = 1;
   }
   // prefill chunk: 64-token stages; 8 warps (128 columns) x 1 CTA per SM, fewer columns: smaller CTAs x 2
-  const bool chunk = G_ > kDecodeMaxColumns;
+  // (trees of 9 to 64 columns at head_dim 128: tree_tok_kernel, whose items and stages are those of the chunk kernels)
+  const bool tree_tok = tree && s->head_dim == 128 && G_ >= kTokMinColumns && G_ <= kTokMaxColumns;
+  const bool chunk = G_ > kDecodeMaxColumns || tree_tok;
   // 9 .. 16 columns: the row layout with the tokens of a stage split over 4 warps x 2 CTAs per SM (the
   // column layout of the decode kernel needs a second MMA tile and a transposition per tile there)
   const bool row16 = !chunk && !kv8 && G_ > 8 && (tree || g_knobs[kKnobRowLayout16].load() != 0);
@@ -816,7 +815,7 @@ static int decode_core(const ooco_shape_t* s, const void* q, const void* k_cache
   // (knob 12: 0 = never; 1 = every prefill chunk, i.e. from 17 score columns; n >= 17 = from n columns)
   const int tc_knob = tree ? 1 : g_knobs[kKnobChunkTcgen05].load();
   const int tc_from = tc_knob == 1 ? 17 : tc_knob;
-  const bool chunk_tc = chunk && s->head_dim == 128 && (kv8 || (tc_knob != 0 && G_ >= tc_from));
+  const bool chunk_tc = chunk && s->head_dim == 128 && (kv8 || tree_tok || (tc_knob != 0 && G_ >= tc_from));
   // (more than one 128-row tile per item, bf16: the kernel that keeps two tiles per CTA on the tensor pipe in turns)
   const int two_tiles = tree ? 2 : g_knobs[kKnobChunkTwoTiles].load();  // 1: beyond 128 columns only; 2: its one-tile mode below, too
   // (8-bit cache: only the one-tile mode has a variant that widens the codes, so up to 128 columns)
@@ -866,10 +865,10 @@ static int decode_core(const ooco_shape_t* s, const void* q, const void* k_cache
   p.chunk_min = g_knobs[kKnobChunkMin].load();
   p.chunk_max = g_knobs[kKnobChunkMax].load();
   if (p.chunk_max < p.chunk_min) p.chunk_max = p.chunk_min;
-  p.items_per_cta = plan_items_per_cta(G_);
+  p.items_per_cta = plan_items_per_cta(tree_tok ? kDecodeMaxColumns + 1 : G_);  // (never more than the workspace is sized for)
   // the 8-bit path widens codes to value / 256 (kE4m3WidenFactor): both scales carry the factor back (K's only
   // where K is widened: the tcgen05 score path multiplies the codes' own values)
-  const bool kv8_tc = (kv8 && tree && chunk && G_ <= kTokMaxColumns) ||
+  const bool kv8_tc = (kv8 && tree_tok) ||
                       (kv8 && !chunk && ncw == 8 && (tree || g_knobs[kKnobKv8Tcgen05].load() != 0));
   p.scale_log2e = scale * 1.4426950408889634f * (kv8 ? kv8->k_scale * (kv8_tc ? 1.f : kE4m3WidenFactor) : 1.f);
   p.v_scale = kv8 ? kv8->v_scale * kE4m3WidenFactor : 1.f;

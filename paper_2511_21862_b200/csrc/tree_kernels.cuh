@@ -1,4 +1,4 @@
-// Tree attention of 17 to 64 score columns per (sequence, kv head) at head_dim 128, with the TOKENS on the MMA's M axis.
+// Tree attention of 9 to 64 score columns per (sequence, kv head) at head_dim 128, with the TOKENS on the MMA's M axis.
 //
 //   S^T[128 tok x NC]   = K_slot[128 tok x 128] . Q^T          tcgen05.mma M128, N = NC columns
 //   O^T[128 dim x NC] (+)= V_slot^T[128 dim x 128 tok] . P     tcgen05.mma M128, N = NC columns
@@ -33,8 +33,9 @@
 // the common exit, and the tensor memory is released after the MMAs in flight.
 //
 // Measured, whole call (plan 10 us, this kernel, merge 12 us; 64 sequences of 256 to 8192 tokens, 8 kv heads; in brackets
-// the kernel with columns on M): 16-bit cache 18 columns 114 us (131), 32: 116 (134), 48: 123 (138), 64: 132 (136); 8-bit cache
-// 18: 104 (168), 32: 106 (171), 48: 119 (173), 64: 151 (176); beyond, with earlier versions of both: 8-bit 96: 267 (193), 16-bit 96:
+// the kernels that served them before, from 17 columns that with columns on M): 16-bit cache 9 columns 111 us (119), 16: 112
+// (125), 18: 114 (131), 32: 116 (134), 48: 123 (138), 64: 132 (136); 8-bit cache
+// 9: 96 (132), 16: 97 (136), 18: 104 (168), 32: 106 (171), 48: 119 (173), 64: 151 (176); beyond, with earlier versions of both: 8-bit 96: 267 (193), 16-bit 96:
 // 228 (156), since scores and accumulators fill tensor memory at 64.  32 sequences of 4096 to 32768 tokens, 8-bit, 40 columns:
 // 261 to 271 us (411), 3.4 TB/s of codes.  At 18 columns the 16-bit call runs at 0.82 of the measured copy rate, plan and merge
 // included.  Over the 8-bit cache a stage of 128 tokens takes about 1900 cycles where its 32 KiB would take 1400, and a change of
@@ -50,7 +51,7 @@
 namespace ooco {
 
 constexpr int kTokMeta = 8, kTokDesc = 8;  // ring sizes: meta words, V descriptors
-constexpr int kTokMaxColumns = 64;         // score columns that the kernel takes, from 17 (both sides measured above)
+constexpr int kTokMinColumns = 9, kTokMaxColumns = 64;  // score columns that the kernel takes (both sides measured above)
 // A reference is raised when a score passes it by this much (log2 units): weights stay below 2^16 for f16 (the 8-bit
 // cache), where small ones lose bits below 2^-14; bf16 has the range of fp32, and a column's sum stays below 2^60 times its tokens.
 template <bool KV8>

@@ -381,9 +381,9 @@ def test_tree_attention(name):
 
 
 def test_tree_attention_chain_is_causal_attention():
-    """A chain over the same inputs is the causal operator, bit for bit where both run the same kernels (17 to 64 score
+    """A chain over the same inputs is the causal operator, bit for bit where both run the same kernels (9 to 64 score
     columns have a kernel of their own for trees)."""
-    for N, hq, hkv in ((2, 32, 8), (4, 32, 8), (40, 32, 8)):
+    for N, hq, hkv in ((2, 32, 8), (1, 64, 8), (40, 32, 8)):
         c = tree_case([N, 100, 300, 3000], hq, hkv, 128, 16, N, seed=N, kind="chain")
         got = run_tree(c)
         out = torch.empty_like(c["q"])
