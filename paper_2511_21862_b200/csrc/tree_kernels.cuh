@@ -730,10 +730,14 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
       ph_wg ^= 1u;
       return got;
     };
+    // Each pipeline's warps read the other's accumulators behind this: what the other's warps have waited for (its MMAs) or
+    // stored (a rescaling) is ordered before these reads by their fence before the barrier and this one's behind it.
     auto both_sync = [&]() {
+      tc_fence_before_sync();
       __syncwarp();
       if (lane == 0) mbar_arrive(s_both);
       const bool got = tok_wait(s_both, ph_both, s_abort);
+      tc_fence_after_sync();
       ph_both ^= 1u;
       return got;
     };
