@@ -95,8 +95,9 @@ enum {
                               original_len / w                                                          */
   OOCO_ROPE_RAMP = 4       /* by index: the frequencies that turn more than `high` times over
                               original_len are kept, those that turn less than `low` times divided by
-                              factor, a linear ramp over the index between; magnitude =
-                              0.1 ln(factor) + 1                                                         */
+                              factor, a linear ramp over the index between (its ends the whole indices
+                              around it, in [0, rot_dim - 1]: it may end beyond the last frequency);
+                              magnitude = 0.1 ln(factor) + 1                                             */
 };
 typedef struct {
   int32_t kind;          /* OOCO_ROPE_*                                        */

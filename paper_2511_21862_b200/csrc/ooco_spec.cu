@@ -228,9 +228,15 @@ int ooco_rope_frequencies(int32_t rot_dim, double base, const ooco_rope_scaling_
   auto index_of = [&](double turns) { return rot_dim * std::log(sc->original_len / (turns * 2 * pi)) / (2 * std::log(base)); };
   double lo = 0, hi = 0;
   if (kind == OOCO_ROPE_RAMP) {
+    // (the ramp may end beyond the last frequency: the slowest one turns more than `low` times then, and is divided by less)
     lo = std::fmax(std::floor(index_of(sc->high)), 0.0);
-    hi = std::fmin(std::ceil(index_of(sc->low)), (double)(half - 1));
-    if (hi <= lo) hi = lo + 1e-3;
+    hi = std::fmin(std::ceil(index_of(sc->low)), (double)(rot_dim - 1));
+    if (index_of(sc->low) < 0) {  // even the fastest turns less than `low` times
+      lo = -1;
+      hi = 0;
+    } else if (hi <= lo) {
+      hi = lo + 1e-3;
+    }
   }
   for (int j = 0; j < half; ++j) {
     double w = std::pow(base, -2.0 * j / rot_dim);
