@@ -85,16 +85,12 @@ def _shape(shape: Shape):
     if c is None:
         c = shape.c()
         object.__setattr__(shape, "_c_struct", c)
-        object.__setattr__(shape, "_c_address", ctypes.addressof(c))
     return c
 
 
 def _address(shape: Shape) -> int:
-    a = shape.__dict__.get("_c_address")
-    if a is None:
-        _shape(shape)
-        a = shape._c_address
-    return a
+    """Where this object's own struct lies: asked each time, since a copied or unpickled Shape has another."""
+    return ctypes.addressof(_shape(shape))
 
 
 def plan_slots_workspace_bytes(shape: Shape) -> int:
