@@ -175,10 +175,10 @@ PyObject* rope_kv_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded("rope_kv_append", n, 16, [&] {
     const bool kv8 = a[1] == Py_True;
     const ooco_shape_t& s = shape_at(a[2]);
-    const auto* rope = reinterpret_cast<const ooco_rope_t*>((uintptr_t)integer(a[3]));
+    ooco_rope_t r = *reinterpret_cast<const ooco_rope_t*>((uintptr_t)integer(a[3])), *const rope = &r;
     const at::Tensor& q_t = tensor(a[5], "q");
     const int dev = device_of(q_t, "q");
-    address(a[4], dev, kF32, "inv_freq", {rope->rot_dim / 2});
+    r.inv_freq = (const float*)address(a[4], dev, kF32, "inv_freq", {r.rot_dim / 2});
     const int64_t T = q_t.dim() ? q_t.size(0) : -1;
     const Rows q = rows(a[5], dev, T, s.num_q_heads, s.head_dim, "q"), k = rows(a[6], dev, T, s.num_kv_heads, s.head_dim, "k"),
                v = rows(a[7], dev, T, s.num_kv_heads, s.head_dim, "v");

@@ -133,16 +133,21 @@ class Rope:
     inv_freq: torch.Tensor
     magnitude: float = 1.0
     _c: object = field(default=None, init=False, repr=False, compare=False)
-    _address: int = field(default=0, init=False, repr=False, compare=False)
 
     def __post_init__(self):
         f = self.inv_freq
         if not f.is_cuda or f.dtype != torch.float32 or not f.is_contiguous() or f.numel() != self.rot_dim // 2:
             raise ValueError(f"inv_freq: expected a contiguous float32 CUDA tensor of {self.rot_dim // 2} elements, got "
                              f"{f.dtype} {tuple(f.shape)} on {f.device}")
-        c = ooco_rope_t(self.rot_dim, int(self.interleaved), self.magnitude, 0, f.data_ptr())
-        object.__setattr__(self, "_c", c)
-        object.__setattr__(self, "_address", ctypes.addressof(c))
+        # (the address of inv_freq is filled in by each call, from the tensor that it has then)
+        object.__setattr__(self, "_c", ooco_rope_t(self.rot_dim, int(self.interleaved), self.magnitude, 0, None))
+
+    def __reduce__(self):  # copies and pickles are made anew, with a struct of their own
+        return type(self), (self.rot_dim, self.interleaved, self.inv_freq, self.magnitude)
+
+    @property
+    def _address(self) -> int:
+        return ctypes.addressof(self._c)
 
 
 def rope_kv_append(shape: Shape, rope: Rope, q, k, v, positions, slot_map, q_out, k_cache, v_cache, stream=None):

@@ -58,3 +58,61 @@ def test_a_used_shape_in_another_process():
     out = subprocess.run([sys.executable, "-c", code], input=pickle.dumps(s), capture_output=True, timeout=300)
     assert out.returncode == 0, out.stderr.decode()
     assert out.stdout.split() == [str(spec.tree_workspace_bytes(s, 8)).encode(), b"64"]
+
+
+class FakeFrequencies:
+    """What a Rope asks of its tensor, without a GPU."""
+    is_cuda, device = True, "cuda:0"
+
+    def __init__(self, n):
+        import torch
+        self.n, self.dtype, self.shape = n, torch.float32, (n,)
+
+    def is_contiguous(self):
+        return True
+
+    def numel(self):
+        return self.n
+
+    def data_ptr(self):
+        return id(self)
+
+
+@pytest.mark.parametrize("how", [copy.copy, copy.deepcopy, lambda r: pickle.loads(pickle.dumps(r))],
+                         ids=["copy", "deepcopy", "pickle"])
+def test_copied_rotary_handles(how):
+    first = spec.Rope(32, True, FakeFrequencies(16), 1.25)
+    second = how(first)
+    assert (second.rot_dim, second.interleaved, second.magnitude) == (32, True, 1.25)
+    assert (second.inv_freq is first.inv_freq) == (how is copy.copy)
+    assert second._address == ctypes.addressof(second._c) != first._address
+    del first
+    gc.collect()
+    c = spec.ooco_rope_t.from_address(second._address)
+    assert (c.rot_dim, c.interleaved, c.magnitude, c.reserved) == (32, 1, 1.25, 0)
+
+
+@pytest.mark.gpu
+def test_a_rotary_handle_uses_the_tensor_it_has():
+    """Frequencies put elsewhere (a module moved, a tensor's data replaced) and copies of the handle give the same rows."""
+    import torch
+    T, hq, hkv, D = 5, 8, 2, 128
+    sh = binding.Shape(1, hq, hkv, D, 16, 2, 1, hkv * 16 * D, 16 * D, D)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    q, k, v = (torch.randn((T, h, D), generator=g, device="cuda").to(torch.bfloat16) for h in (hq, hkv, hkv))
+    pos, slots = (torch.arange(T, dtype=torch.int32, device="cuda") * s for s in (100, 3))
+    kc, vc = (torch.zeros((2, hkv, 16, D), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    inv = spec.rope_frequencies(D)[0].to("cuda")
+
+    def rotated(rope):
+        out = torch.empty_like(q)
+        spec.rope_kv_append(sh, rope, q, k, v, pos, slots, out, kc, vc)
+        return out
+
+    want = rotated(spec.Rope(D, False, inv))
+    held = torch.zeros_like(inv)
+    rope = spec.Rope(D, False, held)
+    assert not torch.equal(rotated(rope), want)           # no frequencies: nothing turns
+    held.data = inv
+    for handle in (rope, copy.deepcopy(rope), pickle.loads(pickle.dumps(rope))):
+        assert torch.equal(rotated(handle), want)
