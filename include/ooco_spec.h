@@ -200,7 +200,8 @@ typedef struct {
  * uniforms[c] * Z < w(x), and a refused one's token leaves w (w(x) <- 0, Z <- Z - w(x)).
  * Products, differences and sums are computed in 64 bits.
  *   target_probs, draft_probs   device, fp32, [B, N, V] with the strides of the struct; rows of leaves
- *                  (and of nodes not reached) are not read in draft_probs.  Rows sum to 1; a NaN counts as 0
+ *                  (and of nodes not reached) are not read in draft_probs.  Rows sum to 1; a NaN or negative
+ *                  value counts as 0, in either
  *   tokens         device, int32 [B, N]: the drafted tokens (entry 0 is not read); a token outside
  *                  [0, V) is never accepted
  *   parents        device, int32 [B, N]; NULL: a chain

@@ -118,6 +118,8 @@ def verify(p, q, tokens, parents, n, uniforms):
 
     cur, count = 0, 0
     path[0] = 0
+    if q is not None:
+        q = np.where(q > 0, q, np.float32(0))  # (NaN and negative values count as nothing)
     while True:
         w = np.where(p[cur] > 0, p[cur], 0).astype(np.float64)  # (NaN counts as nothing)
         mass, chosen = 1.0, None

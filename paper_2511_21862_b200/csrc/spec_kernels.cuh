@@ -435,6 +435,8 @@ __device__ __forceinline__ Df df_shfl(Df v, int src) {
 __device__ __forceinline__ Df df_shfl_up1(Df v) {
   return {__shfl_up_sync(0xffffffffu, v.hi, 1), __shfl_up_sync(0xffffffffu, v.lo, 1)};
 }
+// A draft probability: NaN counts as 0, like a negative value (of the target's, df_weight and the sums below see to that).
+__device__ __forceinline__ float draft_prob(float q) { return fmaxf(q, 0.f); }
 // max(p - s q, 0); NaN counts as 0
 __device__ __forceinline__ Df df_weight(float p, float q, Df s) {
   const float m = __fmul_rn(s.hi, q);                                  // s q = m + e
@@ -511,7 +513,7 @@ __global__ void __launch_bounds__(kVerifyThreads, 2) verify_kernel(const VerifyP
         if (par >= i || par < 0 || x < 0 || x >= V) par = -1;
         if (par >= 0) {
           pp = target[(int64_t)par * p.t_node + x];
-          if (draft) qq = draft[(int64_t)par * p.d_node + x];
+          if (draft) qq = draft_prob(draft[(int64_t)par * p.d_node + x]);
         }
       }
       s_parent[i] = par;
@@ -662,7 +664,7 @@ __global__ void __launch_bounds__(kVerifyThreads, 2) verify_kernel(const VerifyP
             for (int e = 0; e < 16; ++e) pv[e] = pr[v0 + 32 * e];
             if (kKind == 1 || kKind == 2) {
 #pragma unroll
-              for (int e = 0; e < 16; ++e) qv[e] = qr[v0 + 32 * e];
+              for (int e = 0; e < 16; ++e) qv[e] = draft_prob(qr[v0 + 32 * e]);
             }
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
@@ -683,7 +685,7 @@ __global__ void __launch_bounds__(kVerifyThreads, 2) verify_kernel(const VerifyP
               add_to(e & 1 ? s1 : s0, some ? w : Df{0.f, 0.f});
             }
           } else {
-            for (int v = v0; v < min(v_hi, v0 - lane + kVerifyTile); v += 32) add_to(s0, weight(v, pr[v], qr ? qr[v] : 0.f));
+            for (int v = v0; v < min(v_hi, v0 - lane + kVerifyTile); v += 32) add_to(s0, weight(v, pr[v], qr ? draft_prob(qr[v]) : 0.f));
           }
           Df s = df_add(s0, s1);
           for (int o = 16; o; o >>= 1) s = df_add(s, df_shfl_xor(s, o));
@@ -791,7 +793,7 @@ __global__ void __launch_bounds__(kVerifyThreads, 2) verify_kernel(const VerifyP
       for (int e = 0; e < 16; ++e) {
         const int v = v0 + 16 * lane + e;
         pv[e] = v < v_hi ? pr[v] : 0.f;
-        qv[e] = qr && v < v_hi ? qr[v] : 0.f;
+        qv[e] = qr && v < v_hi ? draft_prob(qr[v]) : 0.f;
       }
       s = Df{0.f, 0.f};
       Df s1 = {0.f, 0.f};
@@ -806,7 +808,7 @@ __global__ void __launch_bounds__(kVerifyThreads, 2) verify_kernel(const VerifyP
       src = first_over(upto, s.hi > 0.f);
       enter(upto, src);
       const int run_lo = v0 + 16 * src, v = run_lo + lane;
-      s = lane < 16 && v < v_hi ? weight(v, pr[v], qr ? qr[v] : 0.f) : Df{0.f, 0.f};
+      s = lane < 16 && v < v_hi ? weight(v, pr[v], qr ? draft_prob(qr[v]) : 0.f) : Df{0.f, 0.f};
       src = first_over(df_warp_scan(s, lane), s.hi > 0.f);
       if (lane == 0) p.out_tokens[(size_t)b * N + s_cmd.count] = min(run_lo + src, V - 1);
       return;
