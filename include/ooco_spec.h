@@ -198,10 +198,15 @@ typedef struct {
  * at the current node (w = p again where w's sum is 0; token 0 where that sum is 0, too, or not finite).
  * With draft_probs = NULL the drafts were not drawn but chosen: a child is accepted iff
  * uniforms[c] * Z < w(x), and a refused one's token leaves w (w(x) <- 0, Z <- Z - w(x)).
- * Products, differences and sums are computed in 64 bits.
- *   target_probs, draft_probs   device, fp32, [B, N, V] with the strides of the struct; rows of leaves
- *                  (and of nodes not reached) are not read in draft_probs.  Rows sum to 1; a NaN or negative
- *                  value counts as 0, in either
+ * Products, differences and sums are unevaluated pairs of fp32 values, which carry about 46 bits (24 where
+ * the pair's low part falls below fp32's range: products under about 2^-102).  So a decision is that of the
+ * exact formula unless the two sides of its comparison, or uniforms[0] * sum and the border of a cumulative
+ * sum, are nearer than about 2^-40 * (1 + S).
+ *   target_probs, draft_probs   device, fp32, [B, N, V] with the strides of the struct.  Rows sum to 1; a NaN or
+ *                  negative value counts as 0, in either.  Of every node with children one value per child is
+ *                  read in both, whether the walk reaches it or not (its value is used only then); whole rows are
+ *                  read of nodes that are reached: in draft_probs where a child was refused, in target_probs
+ *                  there and where the last token is drawn.  Rows of leaves in draft_probs are never read
  *   tokens         device, int32 [B, N]: the drafted tokens (entry 0 is not read); a token outside
  *                  [0, V) is never accepted
  *   parents        device, int32 [B, N]; NULL: a chain

@@ -46,3 +46,19 @@ def test_a_row_without_any_draft_probability(V):
     path, out, count = base.check_verify(p, q, tokens, par, u)
     assert [int(c) for c in count] == [1] * B
     assert path[0, 1] == 1 and path[1, 1] == (2 if tokens[1, 2] != tokens[1, 1] else path[1, 1])
+
+
+@pytest.mark.parametrize("drawn", [True, False])
+def test_rows_of_nodes_not_reached_do_not_matter(drawn):
+    """Whatever stands in the rows of nodes that the walk does not reach, and in the draft's rows of leaves."""
+    B, N, V = 12, 10, 900
+    p, q, tokens, par, u = base.verify_inputs(31, B, N, V, "tree", drawn)
+    want = base.run_verify(p, q, tokens, par, u, None)
+    for b in range(B):
+        for i in range(N):
+            if i not in want[0][b]:
+                p[b, i] = float("nan") if i % 2 else float("inf")
+            if drawn and (i not in want[0][b] or i not in par[b]):
+                q[b, i] = float("inf") if i % 2 else float("nan")
+    got = base.run_verify(p, q, tokens, par, u, None)
+    assert all(np.array_equal(a, b) for a, b in zip(got, want))
