@@ -75,7 +75,8 @@ extern "C" {
  *   granted_lens, total_lens device, int32 [B], written: new_lens or 0, and the context with them
  *   workspace      device, >= ooco_plan_slots_workspace_bytes(shape), 256-byte aligned
  *   status         device, int32 [1], may be NULL
- * One launch for few rows, two for many.
+ * Nothing written may share memory with an input or another output, but for the two in-place ones
+ * (OOCO_E_SHAPE).  One launch for few rows, two for many.
  */
 size_t ooco_plan_slots_workspace_bytes(const ooco_shape_t* shape);
 int ooco_plan_slots(const ooco_shape_t* shape, const int32_t* context_lens, const int32_t* new_lens,

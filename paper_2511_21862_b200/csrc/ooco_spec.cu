@@ -35,6 +35,15 @@ static int sm_count_of_current(int* sms) {
   return *sms > 0 ? OOCO_OK : fail_cuda("cudaDeviceGetAttribute", -1);
 }
 
+struct Range {
+  const void* p;
+  size_t bytes;
+};
+static bool overlap(const Range& a, const Range& b) {
+  const uintptr_t x = (uintptr_t)a.p, y = (uintptr_t)b.p;
+  return a.p && b.p && a.bytes && b.bytes && x < y + b.bytes && y < x + a.bytes;
+}
+
 // Up to this many rows the scanning CTA also writes the rows (one launch).
 constexpr int kSlotsOneLaunchRows = 4096;
 
@@ -173,6 +182,21 @@ int ooco_plan_slots(const ooco_shape_t* s, const int32_t* context_lens, const in
       !total_lens || !workspace || (num_free > 0 && !free_ids) || (num_rows > 0 && (!slot_map || !positions)))
     return OOCO_E_NULLPTR;
   if (workspace_bytes < ooco_plan_slots_workspace_bytes(s) || ((uintptr_t)workspace & 255)) return OOCO_E_WORKSPACE;
+  {  // rows are filled from the inputs after the per-sequence outputs are written: nothing written may share their memory
+    const size_t w = 4, n = (size_t)s->batch * w, rows = (size_t)num_rows * w;
+    const Range in[] = {{context_lens, n}, {new_lens, n}, {blocks_held, n}, {free_head, w}, {free_ids, num_free * w}, {parents, rows}};
+    const Range out[] = {{blocks_held_out == blocks_held ? nullptr : blocks_held_out, n},
+                         {free_head_out == free_head ? nullptr : free_head_out, w},
+                         {block_table, n * s->max_blocks_per_seq}, {slot_map, rows}, {positions, rows}, {first_token, n + w},
+                         {granted_lens, n}, {total_lens, n}, {workspace, ooco_plan_slots_workspace_bytes(s)}, {status, w}};
+    constexpr int kOut = sizeof out / sizeof *out;
+    for (int i = 0; i < kOut; ++i) {
+      for (const Range& r : in)
+        if (overlap(out[i], r)) return OOCO_E_SHAPE;
+      for (int j = 0; j < i; ++j)
+        if (overlap(out[i], out[j])) return OOCO_E_SHAPE;
+    }
+  }
   int sms = 0;
   if ((rc = sm_count_of_current(&sms))) return rc;
   SlotsParams p;

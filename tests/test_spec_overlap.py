@@ -1,0 +1,48 @@
+"""Calls whose outputs share memory with what is still to be read are refused before anything is enqueued (CPU).
+
+Every call here is one that must be refused: none may reach a GPU, the addresses are made up."""
+import ctypes
+
+import pytest
+
+from paper_2511_21862_b200 import build, spec
+
+from test_spec_host import SHAPE, shape
+
+B, MB, ROWS = 4, 8, 32
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _built():
+    build.build()
+
+
+def at(i):
+    """Address of made-up buffer i: 64 KiB apart."""
+    return (1 << 20) + (i << 16)
+
+
+SLOTS = dict(ctx=at(0), new=at(1), table=at(2), held=at(3), free=at(4), n_free=8, head=at(5), held_out=None, head_out=None,
+             row_len=0, rows=ROWS, parents=at(6), slot=at(7), pos=at(8), first=at(9), granted=at(10), total=at(11), ws=at(12),
+             ws_bytes=1 << 15, status=at(13))
+
+
+def slots(**kw):
+    a = dict(SLOTS, **kw)
+    return spec._lib().ooco_plan_slots(ctypes.byref(shape().c()), *a.values(), None)
+
+
+@pytest.mark.parametrize("out", ["slot", "pos", "first", "granted", "total", "held_out", "head_out", "table", "ws", "status"])
+@pytest.mark.parametrize("into", ["ctx", "new", "held", "free", "head", "parents"])
+def test_plan_slots_outputs_over_inputs(out, into):
+    if (out, into) in (("held_out", "held"), ("head_out", "head")):
+        pytest.skip("in place")
+    assert slots(**{out: SLOTS[into]}) == SHAPE
+
+
+def test_plan_slots_outputs_over_outputs_and_partly():
+    assert slots(granted=SLOTS["total"]) == SHAPE and slots(pos=SLOTS["slot"]) == SHAPE and slots(first=SLOTS["granted"]) == SHAPE
+    assert slots(total=SLOTS["ctx"] + 4 * (B - 1)) == SHAPE           # the last of the context's lengths
+    assert slots(pos=SLOTS["parents"] + 4 * (ROWS - 1)) == SHAPE
+    assert slots(slot=SLOTS["table"] + 4 * (B * MB - 1)) == SHAPE
+    assert slots(held_out=SLOTS["held"] + 4) == SHAPE                 # in place means in place
