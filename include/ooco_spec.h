@@ -234,7 +234,7 @@ int ooco_verify_drafts(const ooco_verify_t* shape, const float* target_probs, co
  *   num_accepted  device, int32 [B], clamped to [0, max_nodes - 1]
  *   base_lens     device, int32 [B]: context before the tree
  *   context_lens_out  device, int32 [B], written: base + 1 + accepted (base where nothing is kept);
- *                 may be NULL, may not be base_lens
+ *                 may be NULL; shares no memory with an input (OOCO_E_SHAPE)
  * A move whose token lies beyond the block table or in a block outside the pool is skipped.  The sequences'
  * blocks that hold nodes are distinct.  One launch; words are copied as they are (_fp8: bytes).
  */

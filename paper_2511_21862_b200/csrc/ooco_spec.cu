@@ -128,7 +128,10 @@ static int keep_path(const ooco_shape_t* s, int32_t max_nodes, void* k_cache, vo
   if (kv8 && (s->head_dim != 128 || ((s->kv_block_stride | s->kv_head_stride | s->kv_token_stride) & 15)))
     return OOCO_E_UNSUPPORTED;
   if (!k_cache || !v_cache || !block_table || !base_lens || !path || !num_accepted) return OOCO_E_NULLPTR;
-  if (context_lens_out == base_lens) return OOCO_E_SHAPE;
+  // (one CTA of a sequence writes its length while others may still read these)
+  const size_t w = 4, n = (size_t)s->batch * w;
+  for (const Range& r : {Range{base_lens, n}, Range{num_accepted, n}, Range{path, n * max_nodes}, Range{block_table, n * s->max_blocks_per_seq}})
+    if (overlap({context_lens_out, n}, r)) return OOCO_E_SHAPE;
   if (((uintptr_t)k_cache | (uintptr_t)v_cache) & 15) return OOCO_E_UNSUPPORTED;
   const int cell = kv8 ? 1 : 2;
   KeepParams p;

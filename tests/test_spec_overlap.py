@@ -46,3 +46,15 @@ def test_plan_slots_outputs_over_outputs_and_partly():
     assert slots(pos=SLOTS["parents"] + 4 * (ROWS - 1)) == SHAPE
     assert slots(slot=SLOTS["table"] + 4 * (B * MB - 1)) == SHAPE
     assert slots(held_out=SLOTS["held"] + 4) == SHAPE                 # in place means in place
+
+
+@pytest.mark.parametrize("name", ["ooco_kv_keep_path", "ooco_kv_keep_path_fp8"])
+def test_keep_path_lengths_over_inputs(name):
+    N = 8
+
+    def keep(out):
+        return getattr(spec._lib(), name)(ctypes.byref(shape().c()), N, at(0), at(1), at(2), at(3), at(4), at(5), out, None)
+
+    for out in (at(2), at(2) + 4 * (B * MB - 1), at(3), at(3) + 4 * (B - 1), at(3) - 4 * (B - 1), at(4), at(4) + 4 * (B * N - 1),
+                at(5), at(5) + 4):
+        assert keep(out) == SHAPE, hex(out)
