@@ -133,7 +133,8 @@ typedef struct {
  *                negative position is padding: nothing is written for it.  A row with a slot outside
  *                [0, num_blocks * block_size) leaves the cache alone (its q is still written).  No two
  *                rows may share a slot.
- *   q_out        device, bf16 rows q_out_stride apart, written; q itself is allowed (with its stride)
+ *   q_out        device, bf16 rows q_out_stride apart, written; q itself is allowed (with its stride), rows that
+ *                share memory with q's otherwise, with k's or with v's are not (OOCO_E_SHAPE)
  *   k_cache, v_cache      the pool of `shape`; word i of head h goes to
  *                block * kv_block_stride + h * kv_head_stride + offset * kv_token_stride + i
  * num_tokens = 0 launches nothing.  Strides are multiples of 8 elements, at least the row's length, and

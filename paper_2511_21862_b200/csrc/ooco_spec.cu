@@ -44,6 +44,15 @@ static bool overlap(const Range& a, const Range& b) {
   return a.p && b.p && a.bytes && b.bytes && x < y + b.bytes && y < x + a.bytes;
 }
 
+// Whether any of T rows of `la` bytes, `sa` apart from `a` on, shares memory with any of T rows of `lb` bytes, `sb` apart from
+// `b` on (rows of one spacing may lie in one another's gaps, as the parts of a projection do).
+static bool rows_overlap(const void* a, int64_t sa, int64_t la, const void* b, int64_t sb, int64_t lb, int64_t T) {
+  if (!overlap({a, (size_t)((T - 1) * sa + la)}, {b, (size_t)((T - 1) * sb + lb)})) return false;
+  if (T == 1 || sa != sb) return true;
+  const int64_t d = (int64_t)((uintptr_t)b - (uintptr_t)a) % sa, gap = d < 0 ? d + sa : d;  // b's row begins this far into a's period
+  return gap < la || gap + lb > sa;
+}
+
 // Up to this many rows the scanning CTA also writes the rows (one launch).
 constexpr int kSlotsOneLaunchRows = 4096;
 
@@ -73,6 +82,10 @@ static int rope_append(const ooco_shape_t* s, const ooco_rope_t* r, int32_t T, c
       ((uintptr_t)r->inv_freq & 3))
     return OOCO_E_UNSUPPORTED;
   if (T == 0) return OOCO_OK;
+  if (rows_overlap(q_out, 2 * q_out_stride, 2 * q_row, k, 2 * k_stride, 2 * kv_row, T) ||
+      rows_overlap(q_out, 2 * q_out_stride, 2 * q_row, v, 2 * v_stride, 2 * kv_row, T) ||
+      (q_out != q && rows_overlap(q_out, 2 * q_out_stride, 2 * q_row, q, 2 * q_stride, 2 * q_row, T)))
+    return OOCO_E_SHAPE;
   int sms = 0;
   if ((rc = sm_count_of_current(&sms))) return rc;
   RopeParams p;

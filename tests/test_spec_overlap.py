@@ -58,3 +58,21 @@ def test_keep_path_lengths_over_inputs(name):
     for out in (at(2), at(2) + 4 * (B * MB - 1), at(3), at(3) + 4 * (B - 1), at(3) - 4 * (B - 1), at(4), at(4) + 4 * (B * N - 1),
                 at(5), at(5) + 4):
         assert keep(out) == SHAPE, hex(out)
+
+
+@pytest.mark.parametrize("T", [1, 2, 50])
+def test_rotated_queries_over_other_rows(T):
+    """q, k, v as parts of one projection's rows (8, 2 and 2 heads of 128 in rows of 1536): q_out may be q or another buffer."""
+    stride, X = 1536, at(1)
+
+    def rope(q_out, q_out_stride=stride, q=X, k=X + 2 * 1024, v=X + 2 * 1280, ks=stride):
+        r = spec.ooco_rope_t(64, 0, 1.0, 0, at(0))
+        return spec._lib().ooco_rope_kv_append(ctypes.byref(shape().c()), ctypes.byref(r), T, q, stride, k, ks, v, stride, at(30),
+                                               at(31), q_out, q_out_stride, at(40), at(60), None)
+
+    for out in (X + 2 * 512, X + 2 * 1024, X + 2 * 1280, X + 2 * 1528, X - 2 * 512):
+        assert rope(out) == SHAPE, out - X
+    assert rope(X + 2 * 128) == SHAPE                                  # one head further
+    assert rope(X + 2 * stride * (T - 1) + 2 * 1016, 1024) == SHAPE    # begins in the last row
+    assert rope(at(20), 1024, k=at(20) + 2 * (1024 * T - 8), ks=256) == SHAPE
+    assert rope(at(20), 1024, v=at(20)) == SHAPE and rope(at(20), 1024, k=at(20), ks=256) == SHAPE
