@@ -298,4 +298,14 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_spec_calls", nullptr, -1, methods
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__spec_calls() { return PyModule_Create(&module); }
+#ifndef OOCO_BUILT_FOR
+#define OOCO_BUILT_FOR ""
+#endif
+PyMODINIT_FUNC PyInit__spec_calls() {
+  PyObject* m = PyModule_Create(&module);
+  if (m && PyModule_AddStringConstant(m, "built_for", OOCO_BUILT_FOR)) {
+    Py_DECREF(m);
+    return nullptr;
+  }
+  return m;
+}

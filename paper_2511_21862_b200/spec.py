@@ -49,10 +49,14 @@ def _load():
     if L is _L:
         return L
     if _calls is None:
+        from . import build
         try:
             from . import _spec_calls
         except ImportError as e:
             raise ImportError("_spec_calls.so is missing or unusable: run `python -m paper_2511_21862_b200.build`") from e
+        if _spec_calls.built_for != build._built_for():
+            raise ImportError(f"_spec_calls.so was built for {_spec_calls.built_for}, this is {build._built_for()}: run "
+                              "`python -m paper_2511_21862_b200.build`")
         _calls = _spec_calls
     sp, vp, i32, i64, f32, sz = (ctypes.POINTER(ooco_shape_t), ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64,
                                  ctypes.c_float, ctypes.c_size_t)
