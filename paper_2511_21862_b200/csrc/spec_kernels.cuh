@@ -513,13 +513,13 @@ __global__ void __launch_bounds__(kVerifyThreads, 2) verify_kernel(const VerifyP
         if (par >= i || par < 0 || x < 0 || x >= V) par = -1;
         if (par >= 0) {
           pp = target[(int64_t)par * p.t_node + x];
-          if (draft) qq = draft_prob(draft[(int64_t)par * p.d_node + x]);
+          if (draft) qq = draft[(int64_t)par * p.d_node + x];
         }
       }
       s_parent[i] = par;
       s_token[i] = x;
       s_p[i] = pp;
-      s_q[i] = qq;
+      s_q[i] = draft_prob(qq);
       s_u[i] = i < n ? p.uniforms[(size_t)b * N + i] : 0.f;
       s_drop[i] = 0;
       p.path[(size_t)b * N + i] = i == 0 && n > 0 ? 0 : -1;
@@ -664,7 +664,7 @@ __global__ void __launch_bounds__(kVerifyThreads, 2) verify_kernel(const VerifyP
             for (int e = 0; e < 16; ++e) pv[e] = pr[v0 + 32 * e];
             if (kKind == 1 || kKind == 2) {
 #pragma unroll
-              for (int e = 0; e < 16; ++e) qv[e] = draft_prob(qr[v0 + 32 * e]);
+              for (int e = 0; e < 16; ++e) qv[e] = qr[v0 + 32 * e];
             }
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
@@ -674,18 +674,18 @@ __global__ void __launch_bounds__(kVerifyThreads, 2) verify_kernel(const VerifyP
                 w = Df{pv[e], 0.f};
                 some = pv[e] > 0.f && !(kKind == 3 && (s_bits[(kVerifyTile / 32) * k + e] >> lane & 1u));
               } else if (kKind == 1) {
-                w = two_sum(pv[e], -qv[e]);
+                w = two_sum(pv[e], -draft_prob(qv[e]));
                 some = w.hi > 0.f;
               } else {
-                const float m = __fmul_rn(S.hi, qv[e]);
+                const float q = draft_prob(qv[e]), m = __fmul_rn(S.hi, q);
                 w = two_sum(pv[e], -m);
-                w.lo = __fsub_rn(w.lo, __fmaf_rn(S.lo, qv[e], __fmaf_rn(S.hi, qv[e], -m)));
+                w.lo = __fsub_rn(w.lo, __fmaf_rn(S.lo, q, __fmaf_rn(S.hi, q, -m)));
                 some = __fadd_rn(w.hi, w.lo) > 0.f;
               }
               add_to(e & 1 ? s1 : s0, some ? w : Df{0.f, 0.f});
             }
           } else {
-            for (int v = v0; v < min(v_hi, v0 - lane + kVerifyTile); v += 32) add_to(s0, weight(v, pr[v], qr ? draft_prob(qr[v]) : 0.f));
+            for (int v = v0; v < min(v_hi, v0 - lane + kVerifyTile); v += 32) add_to(s0, weight(v, pr[v], draft_prob(qr ? qr[v] : 0.f)));
           }
           Df s = df_add(s0, s1);
           for (int o = 16; o; o >>= 1) s = df_add(s, df_shfl_xor(s, o));
@@ -793,22 +793,22 @@ __global__ void __launch_bounds__(kVerifyThreads, 2) verify_kernel(const VerifyP
       for (int e = 0; e < 16; ++e) {
         const int v = v0 + 16 * lane + e;
         pv[e] = v < v_hi ? pr[v] : 0.f;
-        qv[e] = qr && v < v_hi ? draft_prob(qr[v]) : 0.f;
+        qv[e] = qr && v < v_hi ? qr[v] : 0.f;
       }
       s = Df{0.f, 0.f};
       Df s1 = {0.f, 0.f};
 #pragma unroll
       for (int e = 0; e < 16; e += 2) {
         const int v = v0 + 16 * lane + e;
-        if (v < v_hi) add_to(s, weight(v, pv[e], qv[e]));
-        if (v + 1 < v_hi) add_to(s1, weight(v + 1, pv[e + 1], qv[e + 1]));
+        if (v < v_hi) add_to(s, weight(v, pv[e], draft_prob(qv[e])));
+        if (v + 1 < v_hi) add_to(s1, weight(v + 1, pv[e + 1], draft_prob(qv[e + 1])));
       }
       s = df_add(s, s1);
       upto = df_warp_scan(s, lane);
       src = first_over(upto, s.hi > 0.f);
       enter(upto, src);
       const int run_lo = v0 + 16 * src, v = run_lo + lane;
-      s = lane < 16 && v < v_hi ? weight(v, pr[v], qr ? draft_prob(qr[v]) : 0.f) : Df{0.f, 0.f};
+      s = lane < 16 && v < v_hi ? weight(v, pr[v], draft_prob(qr ? qr[v] : 0.f)) : Df{0.f, 0.f};
       src = first_over(df_warp_scan(s, lane), s.hi > 0.f);
       if (lane == 0) p.out_tokens[(size_t)b * N + s_cmd.count] = min(run_lo + src, V - 1);
       return;
