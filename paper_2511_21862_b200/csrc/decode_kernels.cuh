@@ -240,7 +240,9 @@ __device__ __forceinline__ void host_stage_body(const HostStageParams& p, int bl
 // nodes' masks.)  The plan chooses the chunk
 // length from the total work, splits every sequence into near-equal chunks that are multiples of
 // `stage_tok`, and writes the item list.
-template <int kThreads>
+// kTree: tree attention has plan and merge kernels of its own, since the tests alone took 0.2 us of every call, and 4 us of a
+// call with 3000 short sequences.
+template <int kThreads, bool kTree = false>
 __global__ void __launch_bounds__(kThreads) plan_kernel(DecodeParams p, int stage_tok, int first_in_smem,
                                                         const AppendParams ap, int n_append,
                                                         const HostStageParams hs) {
@@ -251,7 +253,7 @@ __global__ void __launch_bounds__(kThreads) plan_kernel(DecodeParams p, int stag
   grid_dep_wait();
   grid_dep_launch();
   if (blockIdx.x > 0) {
-    if (p.tree_parents)
+    if (kTree)
       tree_mask_body(p, blockIdx.x - 1, gridDim.x - 1);
     else if ((int)blockIdx.x <= n_append)
       kv_append_body(ap, blockIdx.x - 1, n_append);
@@ -269,7 +271,7 @@ __global__ void __launch_bounds__(kThreads) plan_kernel(DecodeParams p, int stag
   int* s_len = s_first + p.B + 1;
   auto read_len = [&](int b) -> long long {  // context length clamped to [0, table capacity]
     const long long t = p.context_lens[b];
-    if (p.tree_parents && tree_nodes(p, b) == 0) return 0;  // no query token: nothing to read
+    if (kTree && tree_nodes(p, b) == 0) return 0;  // no query token: nothing to read
     return t < 0 ? 0 : (t > cap ? cap : t);
   };
   auto len_of = [&](int b) -> long long { return first_in_smem ? s_len[b] : read_len(b); };
@@ -410,7 +412,7 @@ __global__ void __launch_bounds__(kThreads) plan_kernel(DecodeParams p, int stag
   const int row = p.Sq * p.Hq * p.D;
   for (int b = wid; b < p.B; b += kThreads / 32) {
     if (len_of(b) > 0) continue;
-    const int used = p.tree_parents ? tree_nodes(p, b) * p.Hq * p.D : row;
+    const int used = kTree ? tree_nodes(p, b) * p.Hq * p.D : row;
     if (p.out_f32) {
       for (int i = lane; i < used; i += 32) reinterpret_cast<float*>(p.out)[(size_t)b * row + i] = 0.f;
     } else {
@@ -1501,7 +1503,7 @@ decode_main_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
 // and the first warp of the unit combines the shares through shared memory.  Units of unsplit
 // sequences have nothing to do.  The host picks wpu > 1 when there are too few units to fill the GPU
 // (a handful of very long sequences).
-template <int D>
+template <int D, bool kTree = false>
 __global__ void __launch_bounds__(256) lse_merge_kernel(const DecodeParams p, const int wpu_log2) {
   constexpr int V = D / 32;  // dims per lane
   __shared__ float s_part[8][D + 2];  // per warp: its share's accumulator, running maximum, denominator
@@ -1538,7 +1540,7 @@ __global__ void __launch_bounds__(256) lse_merge_kernel(const DecodeParams p, co
     // unsplit (or empty) sequence: the attention kernel wrote the row itself -- except with fp32 output, where
     // every row is a partial (an unsplit row passes through unchanged: one chunk of weight 1)
     bool work = live && (n > 1 || (p.out_f32 && n == 1));
-    if (p.tree_parents && work && qi >= tree_nodes(p, b)) work = false;  // a node that does not exist
+    if (kTree && work && qi >= tree_nodes(p, b)) work = false;  // a node that does not exist
     if (work && !checked(chk_index((long long)(first + n) * p.Hkv - 1, p.max_items) && first >= 0, &p.hdr->status,
                          kStatusBadIndex))
       work = false;

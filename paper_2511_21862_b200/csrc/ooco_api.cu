@@ -946,7 +946,7 @@ static int decode_core(const ooco_shape_t* s, const void* q, const void* k_cache
     const long long want = ((long long)p.B * q_len + 1023) / 1024;
     n_stage = (int)(want < di.sm_count ? want : di.sm_count);
   }
-  cudaError_t e = launch_ex(plan_kernel<1024>, dim3(1 + n_append + n_stage), dim3(1024),
+  cudaError_t e = launch_ex(tree ? plan_kernel<1024, true> : plan_kernel<1024>, dim3(1 + n_append + n_stage), dim3(1024),
                             first_in_smem ? first_bytes : 0, st, pdl_on, pp, stage_tok, first_in_smem, ap, n_append,
                             hs);
   if (e == cudaSuccess) e = cudaGetLastError();
@@ -963,9 +963,9 @@ static int decode_core(const ooco_shape_t* s, const void* q, const void* k_cache
     const int blocks = (int)(need < (long long)di.sm_count * 8 ? need : (long long)di.sm_count * 8);
     const bool pdl = g_knobs[kKnobPdl].load() != 0 && !pe;
     if (s->head_dim == 128)
-      e = launch_ex(lse_merge_kernel<128>, dim3(blocks), dim3(256), 0, st, pdl, p, wpu_log2);
+      e = launch_ex(tree ? lse_merge_kernel<128, true> : lse_merge_kernel<128>, dim3(blocks), dim3(256), 0, st, pdl, p, wpu_log2);
     else
-      e = launch_ex(lse_merge_kernel<64>, dim3(blocks), dim3(256), 0, st, pdl, p, wpu_log2);
+      e = launch_ex(tree ? lse_merge_kernel<64, true> : lse_merge_kernel<64>, dim3(blocks), dim3(256), 0, st, pdl, p, wpu_log2);
   }
   if (e == cudaSuccess) e = cudaGetLastError();
   if (e != cudaSuccess) return fail_cuda("launch of the merge kernel", (long)e);
