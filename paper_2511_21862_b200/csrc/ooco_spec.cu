@@ -345,11 +345,11 @@ int ooco_verify_drafts(const ooco_verify_t* s, const float* target_probs, const 
   p.N = s->max_nodes;
   p.V = s->vocab;
   // CTAs per sequence and their threads.  Few sequences (16 CTAs each do not fill the SMs twice): the largest cluster of
-  // large CTAs shortens the pass over the vocabulary (4 sequences of 152064 values: 11.3 us; with an earlier, slower pass
+  // large CTAs shortens the pass over the vocabulary (4 sequences of 152064 values: 11.7 us; with an earlier, slower pass
   // 13.3, and 17.8 with 8 x 256).  Else 8 CTAs of 256 threads, so that four CTAs per SM hide each other's serial phases (128
-  // sequences of 128256 values: 49.7 us, 58 with 4 x 512, 65 with 8 x 512), and fewer as the sequences alone give the GPU
-  // enough CTAs.  At least so many that a share's bit map fits shared memory (2^17 values), at most one per tile of the
-  // vocabulary.
+  // sequences of 128256 values: 50.5 us; when that was 49.7, 4 x 512 took 58 and 8 x 512 took 65), and fewer as the sequences
+  // alone give the GPU enough CTAs.  At least so many that a share's bit map fits shared memory (2^17 values), at most one per
+  // tile of the vocabulary.
   int cluster = kVerifyMaxCluster, threads = kVerifyThreads;
   if ((int64_t)s->batch * cluster > 2ll * sms) {
     threads = 256;

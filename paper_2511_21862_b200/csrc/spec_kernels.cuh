@@ -272,8 +272,8 @@ __device__ __forceinline__ void unpack8(const uint4 w, float (&x)[8]) {
 // with the halves layout the pieces of dims 8 c .. and rot / 2 + 8 c .. (the two members of eight pairs), else 32
 // consecutive bytes.  Bound by HBM (every q, k, v value is read and written once); the cosines and sines of a
 // token, the only costly arithmetic (one 64-bit product and reduction each), are formed once per token and shared
-// by all its heads through shared memory.  16384 tokens of 64 + 8 heads: 116 us, 5.8 TB/s (0.90 of the measured copy rate);
-// 40 tokens of 32 + 8 heads: 2.9 us, a launch and one trip to memory.
+// by all its heads through shared memory.  16384 tokens of 64 + 8 heads: 116 to 122 us, 5.5 to 5.8 TB/s (0.85 to 0.90 of
+// the measured copy rate), into the 8-bit cache 122; 40 tokens of 32 + 8 heads: 3 us (8-bit 3.5), a launch and one trip to memory.
 template <int D, bool KV8>
 __global__ void __launch_bounds__(kRopeThreads) rope_append_kernel(const RopeParams p, const int interleaved) {
   constexpr int UPH = D / 16;  // units per head
@@ -473,7 +473,7 @@ struct VerifyCommand {
 // through distributed shared memory.  Only rows that such a pass needs are read: one or two per sequence, however
 // many nodes there are.  Bound by HBM for many sequences (two rows of V fp32 values each), by latency for few
 // (gather, walk, pass and draw follow one another), which is why a sequence is spread over several CTAs then.  128
-// sequences of 16 nodes and 128256 values: 49.7 us, 4 of 5 nodes and 152064 values: 11.3 us.  The former reads 102 MB (16 us): a
+// sequences of 16 nodes and 128256 values: 50.5 us (chosen drafts 37.6), 4 of 5 nodes and 152064 values: 11.7 us (12.2).  The first reads 99 MB (15 us): a
 // third of a warp's time goes by at the cluster's barriers while CTA 0 gathers and walks, the issue slots are 46 % busy with
 // the two-float sums, and sequences that need a second pass are the tail.
 //
@@ -832,8 +832,8 @@ constexpr int kKeepThreads = 128, kKeepBatch = 8;
 // A thread owns one 16-byte column of a sequence (cache, head, piece of the row) through all moves: entries of the
 // path increase, so a move's source is never below its target, and a source that has not been read yet is never a
 // target of an earlier move; a batch of moves is read before it is written.  HBM-bound (each row read and written
-// once): 512 sequences, 8 heads, up to 31 moves of 256-byte rows, take 16.8 us, 4.7 TB/s; for few sequences the chain path ->
-// table -> rows is what it takes (8 sequences: 2.7 us).
+// once): 512 sequences, 8 heads, up to 31 moves of 256-byte rows, take 16.8 us, 4.7 TB/s (8-bit: 8.2); for few sequences the chain path ->
+// table -> rows is what it takes (8 sequences: 2.8 us).
 __global__ void __launch_bounds__(kKeepThreads) keep_path_kernel(const KeepParams p) {
   __shared__ int64_t s_src[kTreeMaxNodes], s_dst[kTreeMaxNodes];
   __shared__ int s_count, s_path[kTreeMaxNodes];

@@ -33,12 +33,14 @@
 // the common exit, and the tensor memory is released after the MMAs in flight.
 //
 // Measured, whole call (plan 10 us, this kernel, merge 12 us; 64 sequences of 256 to 8192 tokens, 8 kv heads; in brackets
-// the kernels that served them before, from 17 columns that with columns on M): 16-bit cache 9 columns 111 us (119), 16: 112
-// (125), 18: 114 (131), 32: 116 (134), 48: 123 (138), 64: 132 (136); 8-bit cache
-// 9: 96 (132), 16: 97 (136), 18: 104 (168), 32: 106 (171), 48: 119 (173), 64: 151 (176); beyond, with earlier versions of both: 8-bit 96: 267 (193), 16-bit 96:
-// 228 (156), since scores and accumulators fill tensor memory at 64.  32 sequences of 4096 to 32768 tokens, 8-bit, 40 columns:
-// 261 to 271 us (411), 3.4 TB/s of codes.  At 18 columns the 16-bit call runs at 0.82 of the measured copy rate, plan and merge
-// included.  Over the 8-bit cache a stage of 128 tokens takes about 1900 cycles where its 32 KiB would take 1400, and a change of
+// the causal operator over the same inputs, which has no mask to apply): 16-bit cache 9 columns 109 us (116), 16: 111 (123),
+// 18: 112 (116), 32: 115 (120), 48: 124 (125), 64: 132 (128); 8-bit cache 9: 95 (124), 16: 95 (129), 18: 103 (127), 32: 105
+// (129), 48: 120 (133), 64: 151 (136).  The rule's other side, the kernel with columns on M compiled with the tree's mask, in
+// the same run: 36 columns 120 us here, 130 there (8-bit 135, 169); 48: 122, 132 (122, 152); 64: 131 to 136, 135 to 140
+// (151, 152 to 155); 32 sequences of 4096 to 32768 tokens, 40 columns: 321, 337 (276, 365).  Beyond 64, with earlier versions
+// of both: 96: 228 here, 156 there (267, 193), since scores and accumulators fill tensor memory at 64.  That last batch over the
+// 8-bit cache takes 255 to 296 us from run to run, 3.1 to 3.6 TB/s of codes.  At 18 columns the 16-bit call runs at 0.85 of the
+// measured copy rate, plan and merge included.  Over the 8-bit cache a stage of 128 tokens takes about 1900 cycles where its 32 KiB would take 1400, and a change of
 // units some thousand more: a pipeline's chain (weights, barriers between the roles, widening, P.V) is what bounds it, two
 // pipelines cannot hide all of it, and four sets of softmax warps do not fit the register file.  What mattered: deep rings
 // (three K and V slots instead of two, at the price of a second weight buffer: 5 us of 120), and that the compiler knows
@@ -855,7 +857,7 @@ tree_tok_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
         const uint64_t* rows = p.tree_mask + (size_t)b * p.Sq;
         const uint64_t r0 = lane < p.Sq ? rows[lane] : 0ull, r1 = lane + 32 < p.Sq ? rows[lane + 32] : 0ull;
         const int node = tok0 + r - first_node;
-        const uint64_t mine = (1ull << p.G) - 1ull;
+        const uint64_t mine = (1ull << p.G) - 1ull;  // (G is at most 16, and qi * G below the 64 columns)
         uint64_t m = 0ull;
 #pragma unroll 1
         for (int qi = 0; qi < p.Sq; ++qi) {
