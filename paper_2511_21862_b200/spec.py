@@ -87,8 +87,7 @@ def _shape(shape: Shape):
     """The C struct of an (immutable) Shape, made once per object."""
     c = shape.__dict__.get("_c_struct")
     if c is None:
-        c = shape.c()
-        object.__setattr__(shape, "_c_struct", c)
+        c = shape.__dict__.setdefault("_c_struct", shape.c())   # (the first of several threads' stays)
     return c
 
 

@@ -60,6 +60,20 @@ def test_a_used_shape_in_another_process():
     assert out.stdout.split() == [str(spec.tree_workspace_bytes(s, 8)).encode(), b"64"]
 
 
+def test_threads_that_meet_a_shape_at_once_get_one_struct():
+    """A struct that another thread has put in meanwhile stays: a call may already hold its address."""
+    class Interrupted(binding.Shape):
+        def c(self):
+            if not hasattr(self, "others"):
+                object.__setattr__(self, "others", None)
+                object.__setattr__(self, "others", spec._shape(self))   # the other thread's whole turn
+            return super().c()
+
+    s = Interrupted(4, 8, 2, 128, 16, 64, 8, 2 * 16 * 128, 16 * 128, 128)
+    assert spec._shape(s) is s.others is spec._shape(s)
+    assert spec._address(s) == ctypes.addressof(s.others)
+
+
 class FakeFrequencies:
     """What a Rope asks of its tensor, without a GPU."""
     is_cuda, device = True, "cuda:0"
