@@ -107,7 +107,8 @@ def plan_slots(shape: Shape, context_lens, new_lens, block_table, blocks_held, f
                first_token, granted_lens, total_lens, workspace, *, row_len=0, parents=None, blocks_held_out=None,
                free_head_out=None, status=None, stream=None):
     """Blocks, cache slots and positions of the tokens that every sequence adds (`row_len` = 0: packed rows, else padded
-    rows of that length).  All tensors int32; `blocks_held` and `free_head` are updated in place unless outputs are given."""
+    rows of that length).  All tensors int32; `blocks_held` and `free_head` are updated in place unless outputs are given;
+    no other output may share memory with an input or another output."""
     _lib()
     rc = _calls.plan_slots(_at["ooco_plan_slots"], _address(shape), context_lens, new_lens, block_table, blocks_held, free_ids,
                            free_head, blocks_held_out, free_head_out, row_len, parents, slot_map, positions, first_token,
@@ -154,8 +155,8 @@ class Rope:
 
 
 def rope_kv_append(shape: Shape, rope: Rope, q, k, v, positions, slot_map, q_out, k_cache, v_cache, stream=None):
-    """q_out = rotated q (may be q); rotated k and v go to the bf16 caches' slots.  q, k, v: bf16 [T, heads, head_dim],
-    views with dense rows allowed; positions, slot_map: int32 [T]."""
+    """q_out = rotated q (q itself, or memory that neither q nor k nor v has); rotated k and v go to the bf16 caches' slots.
+    q, k, v: bf16 [T, heads, head_dim], views with dense rows allowed; positions, slot_map: int32 [T]."""
     _lib()
     rc = _calls.rope_kv_append(_at["ooco_rope_kv_append"], False, _address(shape), rope._address, rope.inv_freq, q, k, v,
                                positions, slot_map, q_out, k_cache, v_cache, 1.0, 1.0, stream)

@@ -2,6 +2,7 @@
 import copy
 import ctypes
 import gc
+import os
 import pickle
 import subprocess
 import sys
@@ -55,7 +56,8 @@ def test_a_used_shape_in_another_process():
             "assert spec._address(s) == ctypes.addressof(spec._shape(s))\n"
             "print(spec.tree_workspace_bytes(s, 8), spec._shape(s).num_blocks)\n")
     s = used()
-    out = subprocess.run([sys.executable, "-c", code], input=pickle.dumps(s), capture_output=True, timeout=300)
+    out = subprocess.run([sys.executable, "-c", code], input=pickle.dumps(s), capture_output=True, timeout=300,
+                         cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
     assert out.returncode == 0, out.stderr.decode()
     assert out.stdout.split() == [str(spec.tree_workspace_bytes(s, 8)).encode(), b"64"]
 
