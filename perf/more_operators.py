@@ -468,13 +468,13 @@ def _own(s):
         batch.fork_pages(s["shape"], s["parent"], s["child"], s["ctx"], s["table"], s["held"], s["free"], s["head"], s["shares"],
                          s["copy_src"], s["copy_dst"], s["granted"], s["workspace"], shared_lens=s["lens"], **s["outs"])
         o = s["outs"]
-        return dict(table=s["table"], ctx=o["context_lens_out"], held=o["blocks_held_out"], head=o["free_head_out"][0],
+        return dict(table=s["table"], ctx=o["context_lens_out"], held=o["blocks_held_out"], head=o["free_head_out"],
                     shares=o["shares_out"], copy_src=s["copy_src"], copy_dst=s["copy_dst"], granted=s["granted"])
     if op == "release":
         batch.release_pages(s["shape"], s["rows"], s["ctx"], s["table"], s["held"], s["free"], s["head"], s["shares"],
                             s["workspace"], keep_lens=s["keep"], **s["outs"])
         o = s["outs"]
-        return dict(free=s["free"], ctx=o["context_lens_out"], held=o["blocks_held_out"], head=o["free_head_out"][0],
+        return dict(free=s["free"], ctx=o["context_lens_out"], held=o["blocks_held_out"], head=o["free_head_out"],
                     shares=o["shares_out"])
     if op == "norm":
         if fp8:
