@@ -29,6 +29,10 @@ EXPORTS = (
     "ooco_plan_slots_workspace_bytes", "ooco_plan_slots", "ooco_rope_frequencies", "ooco_rope_kv_append",
     "ooco_rope_kv_append_fp8", "ooco_tree_workspace_bytes", "ooco_tree_attention", "ooco_tree_attention_fp8",
     "ooco_verify_drafts", "ooco_kv_keep_path", "ooco_kv_keep_path_fp8",
+    # a step of a continuous batch (bound in `batch`)
+    "ooco_pages_workspace_bytes", "ooco_fork_pages", "ooco_release_pages", "ooco_norm_rope_kv_append",
+    "ooco_norm_rope_kv_append_fp8", "ooco_shape_logits", "ooco_chunk_workspace_bytes", "ooco_chunk_attention",
+    "ooco_chunk_attention_fp8",
 )
 
 

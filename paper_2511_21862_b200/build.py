@@ -11,9 +11,10 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libooco.so")
 LIB_CHECKED = os.path.join(HERE, "libooco_checked.so")   # the same sources with -DOOCO_CHECKS
-SOURCES = ["ooco_api.cu", "ooco_spec.cu", "ooco_sched.cpp"]
-HEADERS = ["decode_kernels.cuh", "chunk_kernels.cuh", "chunk_tc_kernels.cuh", "chunk_tc2_kernels.cuh", "block_copy_kernels.cuh", "tree_kernels.cuh", "spec_kernels.cuh", "api_internal.h", "ptx.cuh", os.path.join("..", "..", "include", "ooco.h"),
-           os.path.join("..", "..", "include", "ooco_spec.h"),
+SOURCES = ["ooco_api.cu", "ooco_spec.cu", "ooco_batch.cu", "ooco_chunk.cu", "ooco_sched.cpp"]
+HEADERS = ["decode_kernels.cuh", "chunk_kernels.cuh", "chunk_tc_kernels.cuh", "chunk_tc2_kernels.cuh", "block_copy_kernels.cuh", "tree_kernels.cuh", "spec_kernels.cuh", "cta_util.cuh", "norm_rope_kernels.cuh",
+           "page_kernels.cuh", "logits_kernels.cuh", "packed_kernels.cuh", "api_internal.h", "ptx.cuh", os.path.join("..", "..", "include", "ooco.h"),
+           os.path.join("..", "..", "include", "ooco_spec.h"), os.path.join("..", "..", "include", "ooco_batch.h"),
            os.path.join("..", "..", "include", "ooco_sched.h")]
 
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-std=c++17", "-lineinfo",
@@ -21,8 +22,8 @@ NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-std=c++17",
 
 
 CALLS = os.path.join(HERE, "_spec_calls.so")             # CPython module, host code only
-CALLS_SOURCES = ["py_spec.cpp"]
-CALLS_HEADERS = [os.path.join("..", "..", "include", "ooco.h"), os.path.join("..", "..", "include", "ooco_spec.h")]
+CALLS_SOURCES = ["py_spec.cpp", "py_batch.cpp"]
+CALLS_HEADERS = ["py_calls.h"] + [os.path.join("..", "..", "include", f) for f in ("ooco.h", "ooco_spec.h", "ooco_batch.h")]
 
 
 def _built_for() -> str:

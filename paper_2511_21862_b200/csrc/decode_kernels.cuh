@@ -202,7 +202,7 @@ __device__ __forceinline__ void kv_append_body(const AppendParams& a, int block,
   }
 }
 
-__global__ void __launch_bounds__(256) kv_append_kernel(const AppendParams a) {
+static __global__ void __launch_bounds__(256) kv_append_kernel(const AppendParams a) {
   kv_append_body(a, blockIdx.x, gridDim.x);
 }
 

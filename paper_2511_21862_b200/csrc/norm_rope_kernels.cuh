@@ -1,0 +1,150 @@
+// Norms of the heads of q and k, rotary positions and the append to the paged cache, in one pass over q, k and v.
+#pragma once
+#include "cta_util.cuh"
+
+namespace ooco {
+
+struct HeadNormParams {
+  const uint16_t *q_weight, *k_weight;  // bf16 [D] or NULL
+  float eps, offset;
+};
+
+// The work is cut as in rope_append_kernel: a unit is 16 dims of one head of one token, two 16-byte pieces (with the halves
+// layout the two members of eight pairs).  Consecutive lanes hold the units of a head, so a head's sum of squares is the sum
+// over 16 values of a thread and a butterfly over its D / 16 lanes, in 32 bits; and since a thread keeps its place in the head
+// from unit to unit, it holds the weights of its 16 dims in registers.  Bound by HBM: q, k and v are read and written once.
+template <int D, bool KV8>
+__global__ void __launch_bounds__(kRopeThreads) norm_rope_append_kernel(const RopeParams p, const HeadNormParams hn,
+                                                                        const int interleaved) {
+  constexpr int UPH = D / 16;  // units (lanes) per head
+  __shared__ float2 s_cs[kRopeMaxTile][D / 2];
+  __shared__ int s_pos[kRopeMaxTile], s_slot[kRopeMaxTile];
+  grid_dep_wait();
+  grid_dep_launch();
+  const int heads = p.Hq + 2 * p.Hkv, per_tok = heads * UPH, rot_units = p.half / 8;
+  const int c = threadIdx.x % UPH;  // (the number of threads is a multiple of UPH)
+  const bool turned = c < rot_units, turned_halves = !interleaved && turned;
+  const int d_lo = turned_halves ? 8 * c : 16 * c, d_hi = turned_halves ? p.half + 8 * c : 16 * c + 8;
+  const uint4 none = make_uint4(0u, 0u, 0u, 0u);
+  uint4 qw[2] = {none, none}, kw[2] = {none, none};
+  if (hn.q_weight) {
+    qw[0] = *reinterpret_cast<const uint4*>(hn.q_weight + d_lo);
+    qw[1] = *reinterpret_cast<const uint4*>(hn.q_weight + d_hi);
+  }
+  if (hn.k_weight) {
+    kw[0] = *reinterpret_cast<const uint4*>(hn.k_weight + d_lo);
+    kw[1] = *reinterpret_cast<const uint4*>(hn.k_weight + d_hi);
+  }
+  for (int t0 = blockIdx.x * p.tile; t0 < p.T; t0 += gridDim.x * p.tile) {
+    const int nt = min(p.tile, p.T - t0);
+    for (int i = threadIdx.x; i < nt * p.half; i += kRopeThreads) {
+      const int tk = i / p.half, j = i - tk * p.half;
+      // angle / (2 pi) reduced to [-1/2, 1/2] in 64 bits: far positions lose nothing
+      const double turns = (double)p.positions[t0 + tk] * (double)p.inv_freq[j] * 0.15915494309189533577;
+      float s, co;
+      sincospif((float)(2.0 * (turns - rint(turns))), &s, &co);
+      s_cs[tk][j] = make_float2(co * p.magnitude, s * p.magnitude);
+    }
+    if ((int)threadIdx.x < nt) {
+      s_pos[threadIdx.x] = p.positions[t0 + threadIdx.x];
+      s_slot[threadIdx.x] = p.slots[t0 + threadIdx.x];
+    }
+    __syncthreads();
+    const int n = nt * per_tok;
+    for (int base = 0; base < n; base += kRopeThreads * kRopeBatch) {  // (the same trips for every thread: warps stay whole)
+      uint4 a[kRopeBatch], b[kRopeBatch];
+      int tk[kRopeBatch], head[kRopeBatch];
+#pragma unroll
+      for (int i = 0; i < kRopeBatch; ++i) {
+        const int u = base + i * kRopeThreads + threadIdx.x;
+        a[i] = b[i] = none;
+        tk[i] = -1;
+        head[i] = 0;
+        if (u >= n) continue;
+        const int tok = u / per_tok, e = u - tok * per_tok;
+        if (s_pos[tok] < 0) continue;  // padding
+        tk[i] = tok;
+        head[i] = e / UPH;
+        const size_t t = (size_t)(t0 + tok);
+        const uint16_t* src = head[i] < p.Hq           ? p.q + t * p.q_stride + (size_t)head[i] * D
+                              : head[i] < p.Hq + p.Hkv ? p.k + t * p.k_stride + (size_t)(head[i] - p.Hq) * D
+                                                       : p.v + t * p.v_stride + (size_t)(head[i] - p.Hq - p.Hkv) * D;
+        a[i] = *reinterpret_cast<const uint4*>(src + d_lo);
+        b[i] = *reinterpret_cast<const uint4*>(src + d_hi);
+      }
+#pragma unroll
+      for (int i = 0; i < kRopeBatch; ++i) {
+        const bool is_q = head[i] < p.Hq, is_v = head[i] >= p.Hq + p.Hkv;
+        float x[8], y[8];
+        unpack8(a[i], x);
+        unpack8(b[i], y);
+        float ss = 0.f;
+#pragma unroll
+        for (int m = 0; m < 8; ++m) ss = fmaf(x[m], x[m], fmaf(y[m], y[m], ss));
+#pragma unroll
+        for (int o = 1; o < UPH; o <<= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);  // (all lanes of a head take part alike)
+        if (tk[i] < 0) continue;
+        if (!is_v) {
+          const float r = __frsqrt_rn(ss * (1.f / D) + hn.eps);
+          if (is_q ? hn.q_weight != nullptr : hn.k_weight != nullptr) {
+            float w[8];
+            unpack8(is_q ? qw[0] : kw[0], w);
+#pragma unroll
+            for (int m = 0; m < 8; ++m) x[m] = x[m] * r * (w[m] + hn.offset);
+            unpack8(is_q ? qw[1] : kw[1], w);
+#pragma unroll
+            for (int m = 0; m < 8; ++m) y[m] = y[m] * r * (w[m] + hn.offset);
+          } else {
+#pragma unroll
+            for (int m = 0; m < 8; ++m) x[m] *= r, y[m] *= r;
+          }
+          if (turned) {
+            const float2* cs = &s_cs[tk[i]][8 * c];
+            if (interleaved) {
+#pragma unroll
+              for (int m = 0; m < 4; ++m) {
+                const float2 w0 = cs[m], w1 = cs[4 + m];
+                const float x0 = x[2 * m], y0 = y[2 * m];
+                x[2 * m] = x0 * w0.x - x[2 * m + 1] * w0.y;
+                x[2 * m + 1] = x[2 * m + 1] * w0.x + x0 * w0.y;
+                y[2 * m] = y0 * w1.x - y[2 * m + 1] * w1.y;
+                y[2 * m + 1] = y[2 * m + 1] * w1.x + y0 * w1.y;
+              }
+            } else {
+#pragma unroll
+              for (int m = 0; m < 8; ++m) {
+                const float2 w = cs[m];
+                const float x0 = x[m];
+                x[m] = x0 * w.x - y[m] * w.y;
+                y[m] = y[m] * w.x + x0 * w.y;
+              }
+            }
+          }
+        }
+        if (is_q) {
+          uint16_t* dst = p.q_out + (size_t)(t0 + tk[i]) * p.q_out_stride + (size_t)head[i] * D;
+          *reinterpret_cast<uint4*>(dst + d_lo) = pack8_bf16(x);
+          *reinterpret_cast<uint4*>(dst + d_hi) = pack8_bf16(y);
+        } else {
+          const int slot = s_slot[tk[i]];
+          if (slot < 0 || slot >= p.num_slots) continue;
+          const int h = head[i] - p.Hq - (is_v ? p.Hkv : 0);
+          const int64_t at = (int64_t)(slot >> p.bs_log2) * p.bstr + (int64_t)h * p.hstr +
+                             (int64_t)(slot & ((1 << p.bs_log2) - 1)) * p.tstr;
+          uint8_t* cache = is_v ? p.v_cache : p.k_cache;
+          if (KV8) {
+            const float sc = is_v ? p.v_scale : p.k_scale;
+            *reinterpret_cast<uint2*>(cache + at + d_lo) = pack8_e4m3(x, sc);
+            *reinterpret_cast<uint2*>(cache + at + d_hi) = pack8_e4m3(y, sc);
+          } else {
+            *reinterpret_cast<uint4*>(cache + 2 * (at + d_lo)) = is_v ? a[i] : pack8_bf16(x);
+            *reinterpret_cast<uint4*>(cache + 2 * (at + d_hi)) = is_v ? b[i] : pack8_bf16(y);
+          }
+        }
+      }
+    }
+    __syncthreads();  // the tile's cosines are consumed before the next tile's are written
+  }
+}
+
+}  // namespace ooco

@@ -143,7 +143,7 @@ static WsLayout ws_layout(const ooco_shape_t* s, int q_len = 1) {
   return w;
 }
 
-static int encode_kv_map(CUtensorMap* tm, const ooco_shape_t* s, const void* base, int tile_rows,
+int encode_kv_map(CUtensorMap* tm, const ooco_shape_t* s, const void* base, int tile_rows,
                          bool five_d) {
   EncodeTiledFn enc = encode_fn();
   if (!enc) return fail_cuda("cudaGetDriverEntryPoint(cuTensorMapEncodeTiled)", -1);
@@ -174,7 +174,7 @@ static int encode_kv_map(CUtensorMap* tm, const ooco_shape_t* s, const void* bas
 }
 
 // 8-bit pool: (128 bytes of a token row, token, head, block), one box = [tile_rows][128 B].
-static int encode_kv8_map(CUtensorMap* tm, const ooco_shape_t* s, const void* base, int tile_rows) {
+int encode_kv8_map(CUtensorMap* tm, const ooco_shape_t* s, const void* base, int tile_rows) {
   EncodeTiledFn enc = encode_fn();
   if (!enc) return fail_cuda("cudaGetDriverEntryPoint(cuTensorMapEncodeTiled)", -1);
   cuuint64_t dims[4] = {(cuuint64_t)s->head_dim, (cuuint64_t)s->block_size, (cuuint64_t)s->num_kv_heads,

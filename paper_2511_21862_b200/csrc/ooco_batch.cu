@@ -1,0 +1,295 @@
+// Host side of ooco_batch.h, except ooco_chunk_attention (ooco_chunk.cu): argument validation and launches.
+#include <cuda_runtime.h>
+
+#include <atomic>
+#include <cmath>
+#include <cstdint>
+#include <cstring>
+
+#include "../../include/ooco_batch.h"
+#include "api_internal.h"
+#include "logits_kernels.cuh"
+#include "page_kernels.cuh"
+
+namespace ooco {
+
+static_assert(kPagesStatusBadBlock == OOCO_STATUS_BAD_BLOCK && kPagesStatusRefused == OOCO_STATUS_REFUSED, "status bits");
+static_assert(kLogitsMaxBias == OOCO_MAX_BIAS, "bias limit");
+
+// Attributes of a kernel on the current device, set once: dynamic shared memory and clusters of 16 CTAs.
+static int configure(const void* kern, std::atomic<int>* done, int smem) {
+  int dev = 0;
+  if (current_device(&dev)) return fail_cuda("cudaGetDevice", -1);
+  if (dev < 64 && done[dev].load()) return OOCO_OK;
+  cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (e != cudaSuccess) return fail_cuda("cudaFuncSetAttribute", (long)e);
+  if (dev < 64) done[dev].store(1);
+  return OOCO_OK;
+}
+
+static int check_pages(const ooco_shape_t* s, int32_t n, int32_t num_free, const void* workspace, size_t workspace_bytes) {
+  int rc = validate_shape(s);
+  if (rc) return rc;
+  if (n < 0 || num_free < 0) return OOCO_E_SHAPE;
+  if (s->batch > OOCO_MAX_PAGE_ROWS || n > OOCO_MAX_PAGE_ROWS || (int64_t)n * s->max_blocks_per_seq > 1ll << 30)
+    return OOCO_E_UNSUPPORTED;
+  if (!workspace) return OOCO_E_NULLPTR;
+  if (workspace_bytes < ooco_pages_workspace_bytes(s, n) || ((uintptr_t)workspace & 255)) return OOCO_E_WORKSPACE;
+  return OOCO_OK;
+}
+
+// Nothing written shares memory with an input or another output.
+static bool disjoint(const Range* in, int n_in, const Range* out, int n_out) {
+  for (int i = 0; i < n_out; ++i) {
+    for (int j = 0; j < n_in; ++j)
+      if (overlap(out[i], in[j])) return false;
+    for (int j = 0; j < i; ++j)
+      if (overlap(out[i], out[j])) return false;
+  }
+  return true;
+}
+
+static PagesParams page_params(const ooco_shape_t* s, int32_t n, int32_t num_free, void* workspace) {
+  PagesParams p;
+  memset(&p, 0, sizeof p);
+  p.ws_a = (int32_t*)workspace;
+  p.ws_b = (int32_t*)((uint8_t*)workspace + up256((size_t)n * 4));
+  p.n = n;
+  p.B = s->batch;
+  p.NB = s->num_blocks;
+  p.MB = s->max_blocks_per_seq;
+  p.bs_log2 = log2_of(s->block_size);
+  p.num_free = num_free;
+  return p;
+}
+
+// CTAs of the call's cluster: one for a few table entries and a small pool, else as many as the entries keep busy.
+static int page_cluster(const PagesParams& p) {
+  const int64_t work = (int64_t)p.n * p.MB + p.NB / 2;
+  int c = 1;
+  while (c < kPagesMaxCluster && work > (int64_t)c * 4096) c *= 2;
+  return c;
+}
+
+template <typename K>
+static int launch_pages(K kern, std::atomic<int>* done, int maps, const PagesParams& p, cudaStream_t st, const char* where) {
+  const size_t most = 3 * OOCO_MAX_PAGE_ROWS / 8, smem = (size_t)maps * ((p.B + 31) / 32) * 4;
+  const int rc = configure((const void*)kern, done, (int)most);
+  if (rc) return rc;
+  const int cluster = page_cluster(p);
+  return finish(launch_clustered(kern, dim3(cluster), dim3(kPagesThreads), smem, st, pdl_enabled(), (unsigned)cluster, p, cluster),
+                where);
+}
+
+}  // namespace ooco
+
+using namespace ooco;
+
+extern "C" {
+
+size_t ooco_pages_workspace_bytes(const ooco_shape_t* s, int32_t num_rows) {
+  if (validate_shape(s) || num_rows < 0) return 0;
+  return 256 + 2 * up256((size_t)num_rows * 4);
+}
+
+int ooco_fork_pages(const ooco_shape_t* s, int32_t n, const int32_t* parents, const int32_t* children,
+                    const int32_t* shared_lens, int32_t* context_lens, int32_t* block_table, int32_t* blocks_held,
+                    const int32_t* free_ids, int32_t num_free, int32_t* free_head, int32_t* shares,
+                    int32_t* context_lens_out, int32_t* blocks_held_out, int32_t* free_head_out, int32_t* shares_out,
+                    int32_t* copy_src, int32_t* copy_dst, int32_t* granted, void* workspace, size_t workspace_bytes,
+                    int32_t* status, void* cuda_stream) {
+  int rc = check_pages(s, n, num_free, workspace, workspace_bytes);
+  if (rc) return rc;
+  if (!context_lens || !block_table || !blocks_held || !free_head || !shares || (num_free > 0 && !free_ids) ||
+      (n > 0 && (!parents || !children || !copy_src || !copy_dst || !granted)))
+    return OOCO_E_NULLPTR;
+  const size_t w = 4, rows = (size_t)s->batch * w, list = (size_t)n * w, pool = (size_t)s->num_blocks * w;
+  // (an output that is the input itself is in place, and then counts as written only)
+  const bool c_in = !context_lens_out || context_lens_out == context_lens, h_in = !blocks_held_out || blocks_held_out == blocks_held,
+             f_in = !free_head_out || free_head_out == free_head, s_in = !shares_out || shares_out == shares;
+  const Range in[] = {{parents, list}, {children, list}, {shared_lens, list}, {free_ids, num_free * w},
+                      {c_in ? nullptr : context_lens, rows}, {h_in ? nullptr : blocks_held, rows},
+                      {f_in ? nullptr : free_head, w}, {s_in ? nullptr : shares, pool}};
+  const Range out[] = {{c_in ? context_lens : context_lens_out, rows}, {h_in ? blocks_held : blocks_held_out, rows},
+                       {f_in ? free_head : free_head_out, w}, {s_in ? shares : shares_out, pool},
+                       {block_table, rows * s->max_blocks_per_seq}, {copy_src, list}, {copy_dst, list}, {granted, list},
+                       {workspace, ooco_pages_workspace_bytes(s, n)}, {status, w}};
+  if (!disjoint(in, sizeof in / sizeof *in, out, sizeof out / sizeof *out)) return OOCO_E_SHAPE;
+  PagesParams p = page_params(s, n, num_free, workspace);
+  p.parents = parents;
+  p.children = children;
+  p.lens = shared_lens;
+  p.context_lens = context_lens;
+  p.blocks_held = blocks_held;
+  p.free_head = free_head;
+  p.shares = shares;
+  p.block_table = block_table;
+  p.free_ids = const_cast<int32_t*>(free_ids);
+  p.context_lens_out = (int32_t*)out[0].p;
+  p.blocks_held_out = (int32_t*)out[1].p;
+  p.free_head_out = (int32_t*)out[2].p;
+  p.shares_out = (int32_t*)out[3].p;
+  p.copy_src = copy_src;
+  p.copy_dst = copy_dst;
+  p.granted = granted;
+  p.status = status;
+  static std::atomic<int> done[64];
+  return launch_pages(fork_pages_kernel, done, 3, p, (cudaStream_t)cuda_stream, "launch of the forking kernel");
+}
+
+int ooco_release_pages(const ooco_shape_t* s, int32_t n, const int32_t* rows_, const int32_t* keep_lens, int32_t* context_lens,
+                       const int32_t* block_table, int32_t* blocks_held, int32_t* free_ids, int32_t num_free,
+                       int32_t* free_head, int32_t* shares, int32_t* context_lens_out, int32_t* blocks_held_out,
+                       int32_t* free_head_out, int32_t* shares_out, void* workspace, size_t workspace_bytes,
+                       int32_t* status, void* cuda_stream) {
+  int rc = check_pages(s, n, num_free, workspace, workspace_bytes);
+  if (rc) return rc;
+  if (!context_lens || !block_table || !blocks_held || !free_head || !shares || (num_free > 0 && !free_ids) || (n > 0 && !rows_))
+    return OOCO_E_NULLPTR;
+  const size_t w = 4, rows = (size_t)s->batch * w, list = (size_t)n * w, pool = (size_t)s->num_blocks * w;
+  const bool c_in = !context_lens_out || context_lens_out == context_lens, h_in = !blocks_held_out || blocks_held_out == blocks_held,
+             f_in = !free_head_out || free_head_out == free_head, s_in = !shares_out || shares_out == shares;
+  const Range in[] = {{rows_, list}, {keep_lens, list}, {block_table, rows * s->max_blocks_per_seq},
+                      {c_in ? nullptr : context_lens, rows}, {h_in ? nullptr : blocks_held, rows},
+                      {f_in ? nullptr : free_head, w}, {s_in ? nullptr : shares, pool}};
+  const Range out[] = {{c_in ? context_lens : context_lens_out, rows}, {h_in ? blocks_held : blocks_held_out, rows},
+                       {f_in ? free_head : free_head_out, w}, {s_in ? shares : shares_out, pool}, {free_ids, num_free * w},
+                       {workspace, ooco_pages_workspace_bytes(s, n)}, {status, w}};
+  if (!disjoint(in, sizeof in / sizeof *in, out, sizeof out / sizeof *out)) return OOCO_E_SHAPE;
+  PagesParams p = page_params(s, n, num_free, workspace);
+  p.parents = rows_;
+  p.lens = keep_lens;
+  p.context_lens = context_lens;
+  p.blocks_held = blocks_held;
+  p.free_head = free_head;
+  p.shares = shares;
+  p.block_table = const_cast<int32_t*>(block_table);
+  p.free_ids = free_ids;
+  p.context_lens_out = (int32_t*)out[0].p;
+  p.blocks_held_out = (int32_t*)out[1].p;
+  p.free_head_out = (int32_t*)out[2].p;
+  p.shares_out = (int32_t*)out[3].p;
+  p.status = status;
+  static std::atomic<int> done[64];
+  return launch_pages(release_pages_kernel, done, 2, p, (cudaStream_t)cuda_stream, "launch of the releasing kernel");
+}
+
+int ooco_norm_rope_kv_append(const ooco_shape_t* shape, const ooco_rope_t* rope, const ooco_head_norm_t* norm,
+                             int32_t num_tokens, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                             const void* v, int64_t v_stride, const int32_t* positions, const int32_t* slot_map, void* q_out,
+                             int64_t q_out_stride, void* k_cache, void* v_cache, void* cuda_stream) {
+  if (!norm) return OOCO_E_NULLPTR;
+  return rope_append(shape, rope, norm, num_tokens, q, q_stride, k, k_stride, v, v_stride, positions, slot_map, q_out,
+                     q_out_stride, k_cache, v_cache, false, 1.f, 1.f, cuda_stream);
+}
+
+int ooco_norm_rope_kv_append_fp8(const ooco_shape_t* shape, const ooco_rope_t* rope, const ooco_head_norm_t* norm,
+                                 int32_t num_tokens, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                                 const void* v, int64_t v_stride, const int32_t* positions, const int32_t* slot_map,
+                                 void* q_out, int64_t q_out_stride, void* k_cache, void* v_cache, float k_scale,
+                                 float v_scale, void* cuda_stream) {
+  if (!norm) return OOCO_E_NULLPTR;
+  return rope_append(shape, rope, norm, num_tokens, q, q_stride, k, k_stride, v, v_stride, positions, slot_map, q_out,
+                     q_out_stride, k_cache, v_cache, true, k_scale, v_scale, cuda_stream);
+}
+
+int ooco_shape_logits(const ooco_logits_t* s, const void* logits, const float* temperature, const float* repetition,
+                      const float* frequency, const float* presence, const int32_t* history, const int32_t* history_lens,
+                      const int32_t* prompt_lens, const int32_t* tokens, const int32_t* parents, const int32_t* tree_sizes,
+                      const int32_t* bias_tokens, const float* bias_values, const int32_t* mask, float* out_logits,
+                      float* out_probs, void* cuda_stream) {
+  if (!s) return OOCO_E_NULLPTR;
+  if (s->batch <= 0 || s->max_nodes <= 0 || s->vocab <= 0 || (s->logits_fp32 != 0 && s->logits_fp32 != 1) ||
+      s->history_width < 0 || s->max_bias < 0)
+    return OOCO_E_SHAPE;
+  if (s->batch > (1 << 24) || s->max_nodes > OOCO_TREE_MAX_NODES || s->vocab > OOCO_MAX_SHAPED_VOCAB || s->max_bias > OOCO_MAX_BIAS ||
+      (int64_t)s->batch * s->max_nodes * kLogitsMaxCluster > INT32_MAX)
+    return OOCO_E_UNSUPPORTED;
+  const bool penalties = repetition || frequency || presence;
+  if (!logits || (!out_logits && !out_probs)) return OOCO_E_NULLPTR;
+  if (penalties && (!history_lens || (s->history_width > 0 && !history))) return OOCO_E_NULLPTR;
+  if (!bias_tokens != !bias_values || (s->max_bias > 0 && !bias_tokens)) return OOCO_E_NULLPTR;
+  const int64_t B = s->batch, N = s->max_nodes, V = s->vocab, cell = s->logits_fp32 ? 4 : 2;
+  // rows of an output must not meet one another; masks may be shared
+  auto rows_ok = [&](int64_t seq, int64_t node) {
+    return seq >= 0 && node >= 0 && (N == 1 || node >= V) && (B == 1 || seq >= (N - 1) * node + V);
+  };
+  if (s->logits_seq_stride < 0 || s->logits_node_stride < 0 || (mask && (s->mask_seq_stride < 0 || s->mask_node_stride < 0)) ||
+      (out_logits && !rows_ok(s->out_seq_stride, s->out_node_stride)) ||
+      (out_probs && !rows_ok(s->probs_seq_stride, s->probs_node_stride)))
+    return OOCO_E_SHAPE;
+  if (((uintptr_t)logits & (cell - 1)) || (((uintptr_t)out_logits | (uintptr_t)out_probs | (uintptr_t)mask) & 3)) return OOCO_E_UNSUPPORTED;
+  {
+    auto span = [&](int64_t seq, int64_t node, int64_t last, int64_t bytes) {
+      return (size_t)(((B - 1) * seq + (N - 1) * node + last) * bytes);
+    };
+    const size_t lb = span(s->logits_seq_stride, s->logits_node_stride, V, cell), w = 4, b1 = (size_t)B * w;
+    auto same = [&](const float* o, int64_t seq, int64_t node) {
+      return (const void*)o == logits && s->logits_fp32 && (B == 1 || seq == s->logits_seq_stride) && (N == 1 || node == s->logits_node_stride);
+    };
+    const Range out[] = {{out_logits, span(s->out_seq_stride, s->out_node_stride, V, 4)},
+                         {out_probs, span(s->probs_seq_stride, s->probs_node_stride, V, 4)}};
+    if (overlap(out[0], out[1])) return OOCO_E_SHAPE;
+    if (overlap(out[0], {logits, lb}) && !same(out_logits, s->out_seq_stride, s->out_node_stride)) return OOCO_E_SHAPE;
+    if (overlap(out[1], {logits, lb}) && !same(out_probs, s->probs_seq_stride, s->probs_node_stride)) return OOCO_E_SHAPE;
+    const Range in[] = {{temperature, b1}, {repetition, b1}, {frequency, b1}, {presence, b1}, {history, b1 * s->history_width},
+                        {history_lens, b1}, {prompt_lens, b1}, {tokens, b1 * N}, {parents, b1 * N}, {tree_sizes, b1},
+                        {bias_tokens, b1 * s->max_bias}, {bias_values, b1 * s->max_bias},
+                        {mask, span(s->mask_seq_stride, s->mask_node_stride, (V + 31) / 32, 4)}};
+    for (const Range& r : in)
+      if (overlap(out[0], r) || overlap(out[1], r)) return OOCO_E_SHAPE;
+  }
+  int dev = 0, rc;
+  if ((rc = current_device(&dev))) return rc;
+  const int sms = device_info(dev).sm_count;
+  if (sms <= 0) return fail_cuda("cudaDeviceGetAttribute", -1);
+  LogitsParams p;
+  memset(&p, 0, sizeof p);
+  p.logits = logits;
+  p.temperature = temperature;
+  p.repetition = repetition;
+  p.frequency = frequency;
+  p.presence = presence;
+  p.history = history;
+  p.history_lens = history_lens;
+  p.prompt_lens = prompt_lens;
+  p.tokens = tokens;
+  p.parents = parents;
+  p.tree_sizes = tree_sizes;
+  p.bias_tokens = bias_tokens;
+  p.bias_values = bias_values;
+  p.mask = (const uint32_t*)mask;
+  p.out = out_logits;
+  p.probs = out_probs;
+  p.l_seq = s->logits_seq_stride;
+  p.l_node = s->logits_node_stride;
+  p.o_seq = s->out_seq_stride;
+  p.o_node = s->out_node_stride;
+  p.p_seq = s->probs_seq_stride;
+  p.p_node = s->probs_node_stride;
+  p.m_seq = s->mask_seq_stride;
+  p.m_node = s->mask_node_stride;
+  p.B = s->batch;
+  p.N = s->max_nodes;
+  p.V = s->vocab;
+  p.L = s->history_width;
+  p.M = s->max_bias;
+  p.penalties = penalties;
+  // CTAs per row: as many as shares of at least 4096 tokens allow while the rows alone do not fill the SMs twice, else the
+  // fewest whose share (one word a token) lets two CTAs share an SM
+  const int64_t rows = B * N;
+  int cluster = 1;
+  while (cluster < kLogitsMaxCluster && (V > cluster * 26 * 1024ll || (rows * cluster < 2ll * sms && V > cluster * 4096ll))) cluster *= 2;
+  p.share = (int)(((V + cluster - 1) / cluster + 255) / 256 * 256);
+  const size_t smem = (size_t)p.share * 4;
+  cudaStream_t st = (cudaStream_t)cuda_stream;
+  static std::atomic<int> done[2][64];
+  auto kern = s->logits_fp32 ? shape_logits_kernel<float> : shape_logits_kernel<__nv_bfloat16>;
+  if ((rc = configure((const void*)kern, done[s->logits_fp32], (OOCO_MAX_SHAPED_VOCAB / kLogitsMaxCluster) * 4))) return rc;
+  return finish(launch_clustered(kern, dim3((unsigned)(rows * cluster)), dim3(kLogitsThreads), smem, st, pdl_enabled(),
+                                 (unsigned)cluster, p, cluster),
+                "launch of the logits kernel");
+}
+
+}  // extern "C"

@@ -8,25 +8,13 @@
 
 #include "../../include/ooco_spec.h"
 #include "api_internal.h"
+#include "norm_rope_kernels.cuh"
 #include "spec_kernels.cuh"
 
 namespace ooco {
 
 static_assert(kTreeMaxNodes == OOCO_TREE_MAX_NODES, "node limit");
 static_assert(kSlotsStatusBadBlock == OOCO_STATUS_BAD_BLOCK && kSlotsStatusRefused == OOCO_STATUS_REFUSED, "status bits");
-
-static int log2_of(int x) {  // x: a power of two
-  int k = 0;
-  while ((1 << k) < x) ++k;
-  return k;
-}
-
-static size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
-
-static int finish(cudaError_t e, const char* where) {
-  if (e == cudaSuccess) e = cudaGetLastError();
-  return e == cudaSuccess ? OOCO_OK : fail_cuda(where, (long)e);
-}
 
 static int sm_count_of_current(int* sms) {
   int dev = 0;
@@ -35,31 +23,13 @@ static int sm_count_of_current(int* sms) {
   return *sms > 0 ? OOCO_OK : fail_cuda("cudaDeviceGetAttribute", -1);
 }
 
-struct Range {
-  const void* p;
-  size_t bytes;
-};
-static bool overlap(const Range& a, const Range& b) {
-  const uintptr_t x = (uintptr_t)a.p, y = (uintptr_t)b.p;
-  return a.p && b.p && a.bytes && b.bytes && x < y + b.bytes && y < x + a.bytes;
-}
-
-// Whether any of T rows of `la` bytes, `sa` apart from `a` on, shares memory with any of T rows of `lb` bytes, `sb` apart from
-// `b` on (rows of one spacing may lie in one another's gaps, as the parts of a projection do).
-static bool rows_overlap(const void* a, int64_t sa, int64_t la, const void* b, int64_t sb, int64_t lb, int64_t T) {
-  if (!overlap({a, (size_t)((T - 1) * sa + la)}, {b, (size_t)((T - 1) * sb + lb)})) return false;
-  if (T == 1 || sa != sb) return true;
-  const int64_t d = (int64_t)((uintptr_t)b - (uintptr_t)a) % sa, gap = d < 0 ? d + sa : d;  // b's row begins this far into a's period
-  return gap < la || gap + lb > sa;
-}
-
 // Up to this many rows the scanning CTA also writes the rows (one launch).
 constexpr int kSlotsOneLaunchRows = 4096;
 
-static int rope_append(const ooco_shape_t* s, const ooco_rope_t* r, int32_t T, const void* q, int64_t q_stride,
-                       const void* k, int64_t k_stride, const void* v, int64_t v_stride, const int32_t* positions,
-                       const int32_t* slot_map, void* q_out, int64_t q_out_stride, void* k_cache, void* v_cache,
-                       bool kv8, float k_scale, float v_scale, void* cuda_stream) {
+int rope_append(const ooco_shape_t* s, const ooco_rope_t* r, const ooco_head_norm_t* norm, int32_t T, const void* q,
+                int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride, const int32_t* positions,
+                const int32_t* slot_map, void* q_out, int64_t q_out_stride, void* k_cache, void* v_cache, bool kv8,
+                float k_scale, float v_scale, void* cuda_stream) {
   int rc = validate_shape(s);
   if (rc) return rc;
   if (!r) return OOCO_E_NULLPTR;
@@ -67,6 +37,10 @@ static int rope_append(const ooco_shape_t* s, const ooco_rope_t* r, int32_t T, c
       !std::isfinite(r->magnitude) || T < 0)
     return OOCO_E_SHAPE;
   if (r->rot_dim % 16) return OOCO_E_UNSUPPORTED;
+  if (norm) {
+    if (!(norm->eps >= 0.f) || !std::isfinite(norm->eps) || !std::isfinite(norm->weight_offset)) return OOCO_E_SHAPE;
+    if (((uintptr_t)norm->q_weight | (uintptr_t)norm->k_weight) & 15) return OOCO_E_UNSUPPORTED;
+  }
   if (kv8) {
     if (!(k_scale > 0.f) || !(v_scale > 0.f)) return OOCO_E_SHAPE;
     if (s->head_dim != 128 || ((s->kv_block_stride | s->kv_head_stride | s->kv_token_stride) & 15)) return OOCO_E_UNSUPPORTED;
@@ -76,7 +50,7 @@ static int rope_append(const ooco_shape_t* s, const ooco_rope_t* r, int32_t T, c
   if (T > 0 && (!q || !k || !v || !positions || !slot_map || !q_out)) return OOCO_E_NULLPTR;
   const int64_t q_row = (int64_t)s->num_q_heads * s->head_dim, kv_row = (int64_t)s->num_kv_heads * s->head_dim;
   if (q_stride < q_row || q_out_stride < q_row || k_stride < kv_row || v_stride < kv_row) return OOCO_E_SHAPE;
-  if (q == q_out && q_stride != q_out_stride) return OOCO_E_SHAPE;
+  if (T > 0 && q == q_out && q_stride != q_out_stride) return OOCO_E_SHAPE;
   if (((q_stride | q_out_stride | k_stride | v_stride) & 7) ||
       (((uintptr_t)q | (uintptr_t)k | (uintptr_t)v | (uintptr_t)q_out | (uintptr_t)k_cache | (uintptr_t)v_cache) & 15) ||
       ((uintptr_t)r->inv_freq & 3))
@@ -122,6 +96,14 @@ static int rope_append(const ooco_shape_t* s, const ooco_rope_t* r, int32_t T, c
   cudaStream_t st = (cudaStream_t)cuda_stream;
   const bool pdl = pdl_enabled();
   cudaError_t e;
+  if (norm) {
+    const HeadNormParams hn = {(const uint16_t*)norm->q_weight, (const uint16_t*)norm->k_weight, norm->eps, norm->weight_offset};
+    e = kv8 ? launch_ex(norm_rope_append_kernel<128, true>, grid, block, 0, st, pdl, p, hn, (int)r->interleaved)
+        : s->head_dim == 128
+            ? launch_ex(norm_rope_append_kernel<128, false>, grid, block, 0, st, pdl, p, hn, (int)r->interleaved)
+            : launch_ex(norm_rope_append_kernel<64, false>, grid, block, 0, st, pdl, p, hn, (int)r->interleaved);
+    return finish(e, "launch of the rotary append kernel with norms");
+  }
   if (kv8)
     e = launch_ex(rope_append_kernel<128, true>, grid, block, 0, st, pdl, p, (int)r->interleaved);
   else if (s->head_dim == 128)
@@ -302,7 +284,7 @@ int ooco_rope_kv_append(const ooco_shape_t* shape, const ooco_rope_t* rope, int3
                         int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
                         const int32_t* positions, const int32_t* slot_map, void* q_out, int64_t q_out_stride,
                         void* k_cache, void* v_cache, void* cuda_stream) {
-  return rope_append(shape, rope, num_tokens, q, q_stride, k, k_stride, v, v_stride, positions, slot_map, q_out,
+  return rope_append(shape, rope, nullptr, num_tokens, q, q_stride, k, k_stride, v, v_stride, positions, slot_map, q_out,
                      q_out_stride, k_cache, v_cache, false, 1.f, 1.f, cuda_stream);
 }
 
@@ -310,7 +292,7 @@ int ooco_rope_kv_append_fp8(const ooco_shape_t* shape, const ooco_rope_t* rope, 
                             int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
                             const int32_t* positions, const int32_t* slot_map, void* q_out, int64_t q_out_stride,
                             void* k_cache, void* v_cache, float k_scale, float v_scale, void* cuda_stream) {
-  return rope_append(shape, rope, num_tokens, q, q_stride, k, k_stride, v, v_stride, positions, slot_map, q_out,
+  return rope_append(shape, rope, nullptr, num_tokens, q, q_stride, k, k_stride, v, v_stride, positions, slot_map, q_out,
                      q_out_stride, k_cache, v_cache, true, k_scale, v_scale, cuda_stream);
 }
 

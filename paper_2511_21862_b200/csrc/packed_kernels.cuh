@@ -1,0 +1,1127 @@
+// Attention of the new tokens of all sequences over the paged cache, rows packed: plan -> tiles on tcgen05 -> merge.
+//
+// The G n_b score columns (query x head of the group) of a (sequence, kv head) pair are cut into units of 128 columns, or of
+// 256 where there are more than 128: two kernels, one list of items each, because what bounds them differs.
+//   packed_tc_kernel<.., one tile>   at most 128 columns: the cache is read once for few columns, HBM-bound.  The scores of a
+//                                    stage run while the softmax threads still work on the stage before.
+//   packed_tc_kernel<.., two tiles>  a piece of a prompt: two 128-row tiles share every K / V slot and take turns on the
+//                                    tensor pipe, tensor-bound.
+// The CTA is that of chunk_tc2_kernel (chunk_tc2_kernels.cuh), which has one number of query tokens for all sequences; there
+// also stands why its MMAs, slots and warps are as they are.  What differs: a unit carries its sequence's rows, columns and
+// partial rows with it (an item is 32 bytes, a stage's meta words are three), so that sequences of any lengths share a launch;
+// head_dim 64 has half the slot, twice the slots and half the MMAs; an 8-bit cache runs every column on the one-tile kernel.
+#pragma once
+#include "chunk_tc2_kernels.cuh"
+#include "cta_util.cuh"
+
+namespace ooco {
+
+constexpr int kPackedEnd = 1 << 18;          // flag of a stage's meta words: the end marker
+constexpr int kPackedGridCap = 160;          // most CTAs of an attention kernel (bounds the workspace)
+// items the plan aims at per CTA
+__host__ __device__ constexpr int packed_items_per_cta(int list) { return list ? 2 : 4; }  // (0: one-tile list, 1: two-tile list)
+constexpr int kPackedMinStages = 2;          // shortest chunk: 256 tokens
+constexpr int kPackedStatusRefused = 128;
+
+template <int D>
+struct PackedSmem {
+  static constexpr int NK = D == 128 ? kTc2KSlots : 4, NV = D == 128 ? kTc2VSlots : 6;  // (the meta ring is longer than either)
+  static constexpr int kSlotBytes = (D / 64) * kTc2HalfBytes, kQBytes = (D / 64) * kTcRows * 128;
+  __host__ __device__ static size_t total() {
+    return 1024 + 2 * (size_t)kQBytes + (size_t)(NK + NV) * kSlotBytes + kTc2MetaRing * 48 + NV * sizeof(VStageDesc) + 512;
+  }
+};
+
+struct PackedHeader {  // first 256 bytes of the workspace
+  int32_t status;
+  int32_t n_items[2];    // of the one-tile and of the two-tile list, which follow one another in `items`
+  int32_t next_item[2];  // next unit (item x kv head) that no CTA has taken
+  int32_t n_merge;       // tiles whose tokens are cut into several items
+  int32_t merge_rows;    // their rows (x kv head)
+  int32_t pad[57];
+};
+static_assert(sizeof(PackedHeader) == 256, "header is 256 bytes");
+
+struct PackedParams {
+  const __nv_bfloat16* q;
+  __nv_bfloat16* out;
+  const int32_t *block_table, *context_lens, *first_row, *chunk_lens;
+  PackedHeader* hdr;
+  int32_t* tile_first;   // [B + 1]
+  int4* items;           // [2 max_items] {b, first column, t0, t1}, {first partial row or -1, first row of q, n, T}
+  int4* merge;           // [max_merge] {first row of q, first column, chunks, first partial row}
+  int32_t* merge_first;  // [max_merge + 1] row number of each
+  float* part_o;         // [max_part_rows, D] normalised partial rows
+  float* part_lse;       // [max_part_rows] log2-domain log-sum-exp of each
+  int64_t q_stride, out_stride;
+  int32_t B, Hq, Hkv, G, bs, MB, NB, num_rows, max_chunk;
+  int32_t two_tiles;     // 1: more than 128 columns go to the two-tile list
+  int32_t grid, max_tiles, max_items, max_merge, max_part_rows, tile_rows;
+  float scale_log2e, v_scale;
+};
+
+// ------------------------------------------------------------------------------------ plan
+struct PackedSeq {
+  int r0, n, T;  // first row, query tokens, context
+};
+__device__ __forceinline__ PackedSeq packed_seq(const PackedParams& p, int b, bool* refused = nullptr) {
+  PackedSeq s;
+  s.r0 = p.first_row[b];
+  long long n = (long long)p.first_row[b + 1] - s.r0;
+  if (p.chunk_lens) n = min(n, (long long)p.chunk_lens[b]);
+  if (s.r0 < 0 || n < 0) n = 0;
+  n = min(n, (long long)p.num_rows - s.r0);
+  if (n > p.max_chunk) {
+    n = 0;
+    if (refused) *refused = true;
+  }
+  s.n = n < 0 ? 0 : (int)n;
+  const long long cap = (long long)p.MB * p.bs, t = p.context_lens[b];
+  s.T = (int)(t < 0 ? 0 : (t > cap ? cap : t));
+  return s;
+}
+__device__ __forceinline__ bool packed_two(const PackedParams& p, int n) { return p.two_tiles && p.G * n > kTcRows; }
+
+// One CTA.  A tile is a unit's columns of one sequence (for all kv heads); its length is what its last column sees, in stages
+// of 128 tokens.  Every list gets a chunk length from its total of stages, tiles that are longer are cut into near-equal
+// chunks, and the items are sorted by length, longest first, so that the dynamic schedule ends evenly.  Latency-bound: a few
+// block-wide scans.
+__global__ void __launch_bounds__(1024) packed_plan_kernel(const PackedParams p, const int first_in_smem) {
+  extern __shared__ int s_first[];  // [B + 1] when they fit
+  __shared__ long long s_warp[32];
+  __shared__ int s_hist[1024];      // 512 lengths for each list
+  __shared__ long long s_sum[2];
+  const int tid = threadIdx.x;
+  grid_dep_wait();
+  grid_dep_launch();
+  int* first = first_in_smem ? s_first : p.tile_first;
+  s_hist[tid] = 0;
+  if (tid < 2) s_sum[tid] = 0;
+  bool refused = false;
+  long long tiles = 0;
+  for (int b0 = 0; b0 < p.B; b0 += 1024) {
+    const int b = b0 + tid;
+    long long nt = 0, total;
+    if (b < p.B) {
+      const int n = packed_seq(p, b, &refused).n, per = packed_two(p, n) ? kTc2Rows : kTcRows;
+      nt = ((long long)p.G * n + per - 1) / per;
+    }
+    const long long upto = tiles + block_scan(nt, s_warp, &total);
+    if (b < p.B) first[b] = (int)min(upto - nt, (long long)INT32_MAX);
+    tiles += total;
+  }
+  const bool overflow = tiles > p.max_tiles;  // (rows that overlap)
+  const int NT = overflow ? 0 : (int)tiles;
+  if (tid == 0) first[p.B] = NT;
+  refused = __syncthreads_or(refused);
+  struct Tile {
+    int b, c0, cols, stages, list;
+    PackedSeq s;
+  };
+  auto tile_of = [&](int i) {
+    int lo = 0, hi = p.B;  // largest b with first[b] <= i
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (first[mid] <= i) lo = mid; else hi = mid;
+    }
+    Tile t;
+    t.b = lo;
+    t.s = packed_seq(p, lo);
+    t.list = packed_two(p, t.s.n);
+    const int per = t.list ? kTc2Rows : kTcRows;
+    t.c0 = (i - first[lo]) * per;
+    t.cols = min(per, p.G * t.s.n - t.c0);
+    const int seen = min(t.s.T, max(0, t.s.T - t.s.n + 1 + (t.c0 + t.cols - 1) / p.G));
+    t.stages = (seen + kTc2StageTok - 1) / kTc2StageTok;
+    return t;
+  };
+  long long sum[2] = {0, 0};
+  for (int i = tid; i < NT; i += 1024) {
+    const Tile t = tile_of(i);
+    sum[t.list] += max(1, t.stages);
+  }
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    for (int o = 16; o; o >>= 1) sum[k] += __shfl_xor_sync(0xffffffffu, sum[k], o);
+    if ((tid & 31) == 0 && sum[k]) atomicAdd((unsigned long long*)&s_sum[k], (unsigned long long)sum[k]);
+  }
+  __syncthreads();
+  int longest[2];
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const long long ctas = (long long)p.grid * packed_items_per_cta(k);
+    longest[k] = max(kPackedMinStages, (int)((s_sum[k] * p.Hkv + ctas - 1) / ctas));
+  }
+  // chunks of a tile: `len` stages each but the last
+  auto cut = [&](const Tile& t, int& nch, int& len) {
+    const int s = max(1, t.stages);
+    nch = (s + longest[t.list] - 1) / longest[t.list];
+    len = (s + nch - 1) / nch;
+    nch = (s + len - 1) / len;
+  };
+  auto bucket = [](int list, int len) { return 512 * list + 511 - min(len, 511); };
+  long long parts = 0, merges = 0;  // rows of partial results; (rows << 32 | tiles) to be merged
+  for (int i0 = 0; i0 < NT; i0 += 1024) {
+    const int i = i0 + tid;
+    Tile t = {};
+    int nch = 1, len = 0;
+    long long rows = 0, total;
+    if (i < NT) {
+      t = tile_of(i);
+      cut(t, nch, len);
+      if (nch > 1) rows = (long long)nch * p.Hkv * t.cols;
+    }
+    const long long slot = parts + block_scan(rows, s_warp, &total) - rows;
+    parts += total;
+    if (rows && slot + rows > p.max_part_rows) nch = 1;  // (not met: the workspace bound covers the cuts)
+    const long long m1 = nch > 1 ? ((long long)p.Hkv * t.cols << 32) | 1 : 0;
+    const long long m = merges + block_scan(m1, s_warp, &total) - m1;
+    merges += total;
+    const int at = (int)(m & 0xffffffff);
+    if (nch > 1 && at < p.max_merge) {
+      p.merge[at] = make_int4(t.s.r0, t.c0, nch, (int)slot);
+      p.merge_first[at] = (int)(m >> 32);
+    }
+    if (i < NT) {
+      if (nch > 1) {
+        atomicAdd(&s_hist[bucket(t.list, len)], nch - 1);
+        atomicAdd(&s_hist[bucket(t.list, t.stages - (nch - 1) * len)], 1);
+      } else {
+        atomicAdd(&s_hist[bucket(t.list, t.stages)], 1);
+      }
+    }
+  }
+  const int n_merge = min((int)(merges & 0xffffffff), p.max_merge);
+  __syncthreads();
+  long long all, one = 0;
+  const int mine = s_hist[tid];
+  const long long before = block_scan(mine, s_warp, &all) - mine;
+  s_hist[tid] = (int)before;  // cursors
+  if (tid == 512) s_sum[0] = before;
+  __syncthreads();
+  one = s_sum[0];
+  if (tid == 0) {
+    p.hdr->status = (overflow ? kStatusPlanOverflow : 0) | (refused ? kPackedStatusRefused : 0);
+    p.hdr->n_items[0] = (int)one;
+    p.hdr->n_items[1] = (int)(all - one);
+    p.hdr->next_item[0] = p.hdr->next_item[1] = p.grid;
+    p.hdr->n_merge = n_merge;
+    p.hdr->merge_rows = (int)(merges >> 32);
+    p.merge_first[n_merge] = (int)(merges >> 32);
+  }
+  parts = 0;
+  for (int i0 = 0; i0 < NT; i0 += 1024) {  // (the same scan as above gives every tile its partial rows again)
+    const int i = i0 + tid;
+    Tile t = {};
+    int nch = 1, len = 0;
+    long long rows = 0, total;
+    if (i < NT) {
+      t = tile_of(i);
+      cut(t, nch, len);
+      if (nch > 1) rows = (long long)nch * p.Hkv * t.cols;
+    }
+    const long long slot = parts + block_scan(rows, s_warp, &total) - rows;
+    parts += total;
+    if (i >= NT) continue;
+    if (rows && slot + rows > p.max_part_rows) nch = 1, rows = 0, len = max(1, t.stages);
+    const int seen = t.stages ? min(t.s.T, t.s.T - t.s.n + 1 + (t.c0 + t.cols - 1) / p.G) : 0;
+    for (int c = 0; c < nch; ++c) {
+      const int st = nch > 1 ? min(len, t.stages - c * len) : t.stages;
+      const int at = atomicAdd(&s_hist[bucket(t.list, st)], 1);
+      if (!checked(chk_index(at, p.max_items), &p.hdr->status, kStatusBadIndex) || at >= p.max_items) continue;
+      const int t0 = c * len * kTc2StageTok;
+      p.items[2 * at] = make_int4(t.b, t.c0, t0, min(seen, t0 + st * kTc2StageTok));
+      p.items[2 * at + 1] = make_int4(nch > 1 ? (int)slot + c * p.Hkv * t.cols : -1, t.s.r0, t.s.n, t.s.T);
+    }
+  }
+}
+
+// ------------------------------------------------------------------------------------ merge
+// One warp per (column, kv head) of a tile that was cut: the partial rows, normalised, are averaged with the weights of their
+// log-sum-exps, in the order of the chunks.
+template <int D>
+__global__ void __launch_bounds__(256) packed_merge_kernel(const PackedParams p) {
+  constexpr int V = D / 32;  // dims per lane
+  const int lane = threadIdx.x & 31;
+  grid_dep_launch();
+  grid_dep_wait();
+  const int rows = p.hdr->merge_rows, n_merge = p.hdr->n_merge;
+  for (int r = blockIdx.x * 8 + (threadIdx.x >> 5); r < rows; r += gridDim.x * 8) {
+    int lo = 0, hi = n_merge;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (p.merge_first[mid] <= r) lo = mid; else hi = mid;
+    }
+    const int4 m = p.merge[lo];
+    const int per = p.merge_first[lo + 1] - p.merge_first[lo];  // rows of a chunk: kv heads x columns
+    const int cols = per / p.Hkv, idx = r - p.merge_first[lo], h = idx / cols, col = m.y + idx - h * cols;
+    if (!checked(chk_index((long long)m.w + (long long)m.z * per - 1, p.max_part_rows), &p.hdr->status, kStatusBadIndex)) continue;
+    const float* lses = p.part_lse + m.w + idx;
+    const float* src = p.part_o + (int64_t)(m.w + idx) * D + lane * V;
+    float M = -INFINITY, den = 0.f, acc[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) acc[i] = 0.f;
+    for (int c0 = 0; c0 < m.z; c0 += 32) {
+      const int cnt = min(32, m.z - c0);
+      const float lse = lane < cnt ? lses[(int64_t)(c0 + lane) * per] : -INFINITY;
+      float gm = lse;
+#pragma unroll
+      for (int o = 16; o; o >>= 1) gm = fmaxf(gm, __shfl_xor_sync(0xffffffffu, gm, o));
+      const float Mn = fmaxf(M, gm), Ms = Mn == -INFINITY ? 0.f : Mn;
+      const float resc = exp2f(M - Ms), w_lane = exp2f(lse - Ms);
+      M = Mn;
+      float ws = w_lane;
+#pragma unroll
+      for (int o = 16; o; o >>= 1) ws += __shfl_xor_sync(0xffffffffu, ws, o);
+      den = den * resc + ws;
+#pragma unroll
+      for (int i = 0; i < V; ++i) acc[i] *= resc;
+#pragma unroll 8
+      for (int j = 0; j < cnt; ++j) {
+        const float w = __shfl_sync(0xffffffffu, w_lane, j);
+        const float* o = src + (int64_t)(c0 + j) * per * D;
+        if (V == 4) {
+          const float4 x = *reinterpret_cast<const float4*>(o);
+          acc[0] += w * x.x; acc[1] += w * x.y; acc[V - 2] += w * x.z; acc[V - 1] += w * x.w;
+        } else {
+          const float2 x = *reinterpret_cast<const float2*>(o);
+          acc[0] += w * x.x; acc[V - 1] += w * x.y;
+        }
+      }
+    }
+    const float inv = den > 0.f ? 1.f / den : 0.f;
+    __nv_bfloat16* dst = p.out + (int64_t)(m.x + col / p.G) * p.out_stride + (int64_t)(h * p.G + col % p.G) * D + lane * V;
+#pragma unroll
+    for (int i = 0; i < V; i += 2)
+      *reinterpret_cast<uint32_t*>(dst + i) = pack_bf16x2(acc[i] * inv, acc[i + 1] * inv);
+  }
+}
+
+// ------------------------------------------------------------------------------------ tiles
+// Barriers: stage number n (counted over the whole kernel, bookkeeping stages and the end marker included) uses K slot n % NK,
+// V slot n % NV, meta entry n % 8 and, for each tile, barrier n & 1 of the pairs [2] below with phase parity (n >> 1) & 1;
+// every tile takes a turn of its barriers on every stage, with or without work.  The meta ring is longer than the slots that a
+// stage must find free, so an entry is rewritten only after all readers of its stage.
+template <int D, bool KV8, bool kOne>
+__global__ void __launch_bounds__(kTc2Threads, 1)
+packed_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
+                 const PackedParams p) {
+  using L = PackedSmem<D>;
+  constexpr int NH = D / 64;                               // 64-dim halves of a row
+  constexpr int NK = L::NK, NV = KV8 ? 2 : L::NV, NM = kTc2MetaRing;
+  constexpr int kTile = kOne ? kTcRows : kTc2Rows;         // score columns of a unit
+  constexpr int kSlotBytes = L::kSlotBytes, kQBytes = L::kQBytes;
+  constexpr int kWarpK = 16, kWarpV = 17, kWarpM = 18;  // warps 0 .. 15: softmax; 18, 19: MMA of tile 0, 1
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t raw = smem_u32(smem_raw);
+  const uint32_t base = (raw + 1023u) & ~1023u;
+  uint8_t* gen = smem_raw + (base - raw);
+  const uint32_t s_q = base;                                       // [2] Q tiles
+  const uint32_t s_k = s_q + 2u * kQBytes;                      // [NK] K slots
+  const uint32_t s_v = s_k + (uint32_t)NK * kSlotBytes;         // [NV] V slots
+  const uint32_t s_rk = s_q + kQBytes;                          // KV8: [NK] 8-bit K slots (tile 1's Q region)
+  const uint32_t s_rv = s_v + (uint32_t)NV * kSlotBytes;        // KV8: [NV] 8-bit V slots (the third V slot's place)
+  const uint32_t s_meta = s_v + (uint32_t)L::NV * kSlotBytes;  // [NM] three int4 per stage
+  const uint32_t s_vdesc = s_meta + (uint32_t)NM * 48;             // [NV] VStageDesc
+  const uint32_t s_bar = s_vdesc + (uint32_t)L::NV * sizeof(VStageDesc);
+  const uint32_t s_kfull = s_bar;                  // [NK] the K slot has landed                          (TMA)
+  const uint32_t s_kempty = s_kfull + NK * 8;      // [NK] the score MMAs that read it are complete       (MMA commit)
+  const uint32_t s_vfull = s_kempty + NK * 8;      // [NV] the V slot has landed                          (TMA)
+  const uint32_t s_vempty = s_vfull + NV * 8;      // [NV] the P.V MMAs that read it are complete         (MMA commit)
+  const uint32_t s_vdfull = s_vempty + NV * 8;     // [NV] the stage's V descriptor is posted             (K producer)
+  const uint32_t s_mfull = s_vdfull + NV * 8;      // [NM] the stage's meta words are posted              (K producer)
+  const uint32_t s_sready = s_mfull + NM * 8;      // [2 tiles][2] S_t holds the stage's scores            (MMA commit)
+  const uint32_t s_pready = s_sready + 32;         // [2 tiles][2] P_t written, O_t rescaled, V rows clean (256 threads)
+  const uint32_t s_pvdone = s_pready + 32;         // [2 tiles] the unit's last P.V_t is complete          (MMA commit)
+  const uint32_t s_qready = s_pvdone + 16;         // [2 tiles] Q_t of the unit is in shared memory        (256 threads)
+  const uint32_t s_pvstage = s_qready + 16;       // [2] one-tile mode: the stage's P.V is complete              (MMA commit)
+  const uint32_t s_rkfull = s_pvstage + 16;       // KV8 [NK] the 8-bit K slot has landed                         (TMA)
+  const uint32_t s_rkempty = s_rkfull + 16;       // KV8 [NK] the 8-bit K slot has been widened                   (256 threads)
+  const uint32_t s_rvfull = s_rkempty + 16;       // KV8 [NV] the 8-bit V slot has landed                         (TMA)
+  const uint32_t s_rvempty = s_rvfull + 16;       // KV8 [NV] the 8-bit V slot has been widened                   (256 threads)
+  const uint32_t s_drain = s_rvempty + 16;
+  const uint32_t s_slot = s_drain + 16;
+  int4* g_meta = reinterpret_cast<int4*>(gen + (s_meta - base));
+  VStageDesc* g_vdesc = reinterpret_cast<VStageDesc*>(gen + (s_vdesc - base));
+  volatile uint32_t* g_slot = reinterpret_cast<volatile uint32_t*>(gen + (s_slot - base));
+  volatile int* s_abort = reinterpret_cast<volatile int*>(gen + (s_slot + 4 - base));
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;  // (known to be uniform)
+
+  if (threadIdx.x == 0) {
+    *s_abort = 0;
+    for (int i = 0; i < NK; ++i) {
+      mbar_init(s_kfull + 8 * i, KV8 ? 256 : 1);  // (KV8: filled by the widening threads, not by TMA)
+      mbar_init(s_kempty + 8 * i, kOne ? 1 : 2);  // one arrival per MMA warp that reads K
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(s_rkfull + 8 * i, 1);
+      mbar_init(s_rkempty + 8 * i, 256);
+      mbar_init(s_rvfull + 8 * i, 1);
+      mbar_init(s_rvempty + 8 * i, 256);
+    }
+    for (int i = 0; i < NV; ++i) {
+      mbar_init(s_vfull + 8 * i, KV8 ? 256 : 1);
+      mbar_init(s_vempty + 8 * i, kOne ? 1 : 2);
+      mbar_init(s_vdfull + 8 * i, 1);
+    }
+    for (int i = 0; i < NM; ++i) mbar_init(s_mfull + 8 * i, 1);
+    for (int i = 0; i < 4; ++i) {
+      mbar_init(s_sready + 8 * i, 1);
+      mbar_init(s_pready + 8 * i, 256);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(s_pvdone + 8 * i, 1);
+      mbar_init(s_qready + 8 * i, 256);
+      mbar_init(s_pvstage + 8 * i, 1);
+    }
+    mbar_init(s_drain, 1);
+    mbar_init(s_drain + 8, 1);
+    fence_mbar_init();
+  }
+  if (warp == kWarpM) tmem_alloc(s_slot, kTc2TmemCols);
+  tc_fence_before_sync();
+  __syncthreads();
+  tc_fence_after_sync();
+  const uint32_t tmem = *g_slot;
+  grid_dep_wait();    // the plan must have completed
+  grid_dep_launch();  // the next kernel of the call may queue up behind this grid
+
+  constexpr int kList = kOne ? 0 : 1;  // which of the plan's two item lists
+  const long long cap_tokens = (long long)p.MB * p.bs;
+
+  if (warp == kWarpK) {
+    // ================================================================= K producer (and the walk over the units)
+    if (lane == 0) prefetch_tmap(&tm_k);
+    const long long n_units = (long long)p.hdr->n_items[kList] * p.Hkv;
+    const int4* items = p.items + (kOne ? 0 : 2 * (size_t)p.hdr->n_items[0]);
+    const int boxes_per_stage = kTc2StageTok / p.tile_rows;   // at most 8 (blocks of 16 tokens)
+    const uint32_t box_rows_bytes = (uint32_t)p.tile_rows * 128;
+    int it = 0;
+    bool ok = true, violated = false;
+    long long unit = blockIdx.x;
+    auto table_entry = [&](const int32_t* e) {
+      const int v = *e;
+      return checked(chk_table_entry(v, p.NB), &p.hdr->status, kStatusBadTableEntry) ? v : p.NB;
+    };
+    // waits until K slot, V slot (and with it the V descriptor) of stage `it` are free; false when a wait gave up
+    auto acquire = [&]() {
+      // (KV8: the slots the copies land in are the 8-bit ones, free once they have been widened)
+      return warp_wait((KV8 ? s_rkempty : s_kempty) + 8 * (it % NK), (((uint32_t)(it / NK)) & 1u) ^ 1u, s_abort) &&
+             warp_wait((KV8 ? s_rvempty : s_vempty) + 8 * (it % NV), (((uint32_t)(it / NV)) & 1u) ^ 1u, s_abort);
+    };
+    while (unit < n_units && ok) {
+      int nxt = 0;
+      if (lane == 0) nxt = atomicAdd(&p.hdr->next_item[kList], 1);
+      nxt = __shfl_sync(0xffffffffu, nxt, 0);
+      const int item = (int)(unit / p.Hkv), h = (int)(unit - (long long)item * p.Hkv);
+      const int4 d = items[2 * item], d2 = items[2 * item + 1];  // {b, first column, t0, t1}, {partial row or -1, first row of q, n, T}
+      if (!checked(chk_item(d.x, 0, d.z, d.w, p.B, 1, cap_tokens) && chk_span(d2.y, d2.z, 0, p.num_rows) &&
+                       (d2.x < 0 || chk_index(d2.x, p.max_part_rows)), &p.hdr->status, kStatusBadItem)) {
+        *s_abort = 1;
+        violated = true;
+        ok = false;
+        break;
+      }
+      const int b = d.x, c0 = d.y, t0 = d.z, t1 = d.w;
+      const int lim_base = d2.w - d2.z + 1;                         // tokens the first query token sees
+      const int columns = p.G * d2.z;                               // of the (sequence, kv head) pair
+      const int col_hi = min(columns, c0 + kTile) - 1;
+      const int part = d2.x < 0 ? -1 : d2.x + h * (col_hi + 1 - c0);
+      const int t1e = min(t1, lim_base + col_hi / p.G);             // nothing beyond is visible to this unit
+      const int nstage = t1e > t0 ? (t1e - t0 + kTc2StageTok - 1) / kTc2StageTok : 0;
+      const int32_t* row = p.block_table + (size_t)b * p.MB;
+      int blk_cur = 0;
+      {
+        const int tb = t0 + lane * p.tile_rows;
+        if (lane < boxes_per_stage && tb < t1e) blk_cur = table_entry(row + tb / p.bs);
+      }
+      // a pair that sees nothing of this chunk passes one stage without tokens, which carries the bookkeeping
+      for (int s = 0; s < (nstage > 0 ? nstage : 1); ++s, ++it) {
+        const int tok0 = t0 + s * kTc2StageTok;
+        const int ntok = nstage > 0 ? min(kTc2StageTok, t1e - tok0) : 0;
+        const int nbox = (ntok + p.tile_rows - 1) / p.tile_rows;
+        int blk_n = 0;  // table entries of the following stage, one stage ahead of their use
+        {
+          const int tb = tok0 + kTc2StageTok + lane * p.tile_rows;
+          if (s + 1 < nstage && lane < boxes_per_stage && tb < t1e) blk_n = table_entry(row + tb / p.bs);
+        }
+        if (!acquire()) {
+          ok = false;
+          break;
+        }
+        const int ks = it % NK, vs = it % NV, ms = it % NM;
+        const uint32_t kfull = (KV8 ? s_rkfull : s_kfull) + 8 * ks;
+        if (lane == 0) {
+          const int flags = (s == 0 ? 1 : 0) | (s == (nstage > 0 ? nstage : 1) - 1 ? 2 : 0);
+          g_meta[3 * ms] = make_int4(part, d2.y, h, ntok | (flags << 16));
+          g_meta[3 * ms + 1] = make_int4(tok0, lim_base, t1, c0);
+          g_meta[3 * ms + 2] = make_int4(columns, 0, 0, 0);
+          g_vdesc[vs].nbox = nbox;
+          g_vdesc[vs].h = h;
+          if (nbox > 0)
+            mbar_arrive_expect_tx(kfull, (KV8 ? 1u : (uint32_t)NH) * (uint32_t)nbox * box_rows_bytes);
+          else
+            mbar_arrive(kfull);
+        }
+        __syncwarp();
+        bool span_ok = true;
+        if (lane < nbox) {
+          const int tb = tok0 + lane * p.tile_rows;
+          const int c_tok = tb % p.bs;
+          const uint32_t k0 = KV8 ? s_rk + (uint32_t)ks * kTc2RawSlotBytes : s_k + (uint32_t)ks * kSlotBytes;
+          const uint32_t dk = k0 + (uint32_t)lane * box_rows_bytes;
+          span_ok = checked(chk_span(dk, box_rows_bytes, k0, (long long)k0 + kTc2HalfBytes) && chk_span(lane, 1, 0, 8),
+                            &p.hdr->status, kStatusBadSmem);
+          if (span_ok) {
+            tma_load_4d(dk, &tm_k, kfull, 0, c_tok, h, blk_cur);  // (KV8: the row's 128 codes; else its first 64 dims)
+            if (!KV8 && NH > 1) tma_load_4d(dk + kTc2HalfBytes, &tm_k, kfull, 64, c_tok, h, blk_cur);
+            g_vdesc[vs].blk[lane & 7] = blk_cur;
+            g_vdesc[vs].c_tok[lane & 7] = c_tok;
+          }
+        }
+        if (kChecked && !__all_sync(0xffffffffu, span_ok)) {  // a skipped copy leaves the stage incomplete: stop
+          *s_abort = 1;
+          violated = true;
+          ok = false;
+          break;
+        }
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive(s_vdfull + 8 * vs);  // the V producer takes over the stage's V boxes
+          mbar_arrive(s_mfull + 8 * ms);   // the softmax threads may read the meta words
+        }
+        blk_cur = blk_n;
+      }
+      unit = nxt;
+    }
+    if (ok) {  // end marker: one more stage, seen by every other warp
+      if (acquire()) {
+        if (lane == 0) {
+          g_meta[3 * (it % NM)] = make_int4(0, 0, 0, kPackedEnd);
+          g_vdesc[it % NV].nbox = -1;
+          mbar_arrive((KV8 ? s_rkfull : s_kfull) + 8 * (it % NK));
+          mbar_arrive(s_vdfull + 8 * (it % NV));
+          mbar_arrive(s_mfull + 8 * (it % NM));
+        }
+        ++it;
+      } else {
+        ok = false;
+      }
+    }
+    if (!ok) {  // stop path: record it, then wait (bounded) until every K copy already issued has landed
+      if (lane == 0 && !violated) atomicOr(&p.hdr->status, kStatusWaitTimeout);
+      int dummy_abort = 0;
+      for (int k = 0; k < (it < NK ? it : NK); ++k) {
+        const int j = it - 1 - k;
+        mbar_wait_bounded((KV8 ? s_rkfull : s_kfull) + 8 * (j % NK), (uint32_t)(j / NK) & 1u, &dummy_abort, kWaitLimitNs / 8);
+      }
+    }
+  } else if (warp == kWarpV) {
+    // ================================================================= V producer
+    if (lane == 0) prefetch_tmap(&tm_v);
+    const uint32_t box_rows_bytes = (uint32_t)p.tile_rows * 128;
+    int it = 0;
+    bool ok = true;
+    for (;; ++it) {
+      const int vs = it % NV;
+      if (!warp_wait(s_vdfull + 8 * vs, (uint32_t)(it / NV) & 1u, s_abort)) {
+        ok = false;
+        break;
+      }
+      const VStageDesc& vd = g_vdesc[vs];
+      const int nbox = vd.nbox;
+      const uint32_t vfull = (KV8 ? s_rvfull : s_vfull) + 8 * vs;
+      if (nbox <= 0) {  // a stage without tokens, or the end marker
+        if (lane == 0) mbar_arrive(vfull);
+        if (nbox < 0) break;
+        continue;
+      }
+      if (lane == 0) mbar_arrive_expect_tx(vfull, (KV8 ? 1u : (uint32_t)NH) * (uint32_t)nbox * box_rows_bytes);
+      __syncwarp();
+      if (lane < nbox && lane < 8) {
+        const uint32_t dv = (KV8 ? s_rv + (uint32_t)vs * kTc2RawSlotBytes : s_v + (uint32_t)vs * kSlotBytes) +
+                            (uint32_t)lane * box_rows_bytes;
+        tma_load_4d(dv, &tm_v, vfull, 0, vd.c_tok[lane], vd.h, vd.blk[lane]);
+        if (!KV8 && NH > 1) tma_load_4d(dv + kTc2HalfBytes, &tm_v, vfull, 64, vd.c_tok[lane], vd.h, vd.blk[lane]);
+      }
+    }
+    if (!ok) {
+      if (lane == 0) atomicOr(&p.hdr->status, kStatusWaitTimeout);
+      int dummy_abort = 0;
+      for (int k = 0; k < (it < NV ? it : NV); ++k) {
+        const int j = it - 1 - k;
+        mbar_wait_bounded((KV8 ? s_rvfull : s_vfull) + 8 * (j % NV), (uint32_t)(j / NV) & 1u, &dummy_abort, kWaitLimitNs / 8);
+      }
+    }
+  } else if (warp >= kWarpM && kOne) {
+    // ================================================================= MMA warps, one-tile mode
+    // One thread issues an MMA about every 100 cycles, so a single issuing thread needs longer for the 16 MMAs of a
+    // stage than HBM needs for the stage's bytes.  With one tile the two issuing warps split the stage instead: warp
+    // kWarpM issues the scores S(n) = Q . K_slot^T into S buffer n & 1 (columns 256 (n & 1); buffer 1 is what tile 1's
+    // scores would occupy), warp kWarpM + 1 the values O += P(n) . V_slot.  The pipe keeps no order between two
+    // threads' MMAs, so each hand-over has a barrier: S(n) overwrites P(n - 2), hence waits for P.V(n - 2) to be
+    // complete (s_pvstage, one completion per stage, with or without tokens); P.V(n) waits for the softmax threads'
+    // P(n).  The scores of a stage are thus computed while the softmax threads still work on the one before.
+    const int t = warp - kWarpM;
+    bool issued = false, ok = true;
+    if (t == 0) {
+      const uint32_t idesc_s = umma_idesc_16bit(kTcRows, kTc2StageTok, 0, !KV8);  // (KV8: f16 operands)
+      const uint64_t dq = umma_smem_desc(s_q, 0, 1024);
+      uint32_t n_q = 0;  // units with tokens (uses of the q-ready barrier)
+      for (uint32_t n = 0;; ++n) {
+        const int ks = n % NK, ms = n % NM;
+        if (!warp_wait(s_kfull + 8 * ks, (n / NK) & 1u, s_abort)) {
+          ok = false;
+          break;
+        }
+        const int4 meta = g_meta[3 * ms];
+        const bool end = meta.w & kPackedEnd;
+        const int ntok = end ? 0 : (meta.w & 0xffff);
+        const bool first = !end && ((meta.w >> 16) & 1);
+        // The buffer's previous contents, P(n - 2), have been consumed.  Waited for on every stage, with or without
+        // tokens (the end marker included): it also means that the softmax threads are past their wait for S(n - 2),
+        // so this stage's completion of the score barrier n & 1 cannot overtake them.
+        if (n >= 2 && !warp_wait(s_pvstage + 8 * (n & 1), ((n - 2) >> 1) & 1u, s_abort)) {
+          ok = false;
+          break;
+        }
+        if (ntok > 0) {
+          if (first) {
+            if (!warp_wait(s_qready, n_q & 1u, s_abort)) {
+              ok = false;
+              break;
+            }
+            ++n_q;
+          }
+          tc_fence_after_sync();
+          if (lane == 0) {
+            const uint64_t dk = umma_smem_desc(s_k + (uint32_t)ks * kSlotBytes, 0, 1024);
+            const uint32_t ts = tmem + 256u * (n & 1);
+#pragma unroll
+            for (int hh = 0; hh < NH; ++hh)
+#pragma unroll
+              for (int k = 0; k < 4; ++k) {  // 16 dims = 32 bytes further along the rows; the second 64 dims = the next half
+                const uint64_t off = (uint64_t)((hh * kTc2HalfBytes + k * 32) >> 4);
+                umma_ss(ts, dq + off, dk + off, idesc_s, (hh | k) ? 1u : 0u);
+              }
+            umma_commit(s_sready + 8 * (n & 1));
+            umma_commit(s_kempty + 8 * ks);
+          }
+          __syncwarp();
+          issued = true;
+        } else {
+          // no scores: the turn of the barriers is taken all the same (also wakes the softmax threads for the end marker)
+          if (lane == 0) {
+            mbar_arrive(s_sready + 8 * (n & 1));
+            mbar_arrive(s_kempty + 8 * ks);
+          }
+          __syncwarp();
+        }
+        if (end) break;
+      }
+    } else {
+      const uint32_t idesc_o = umma_idesc_16bit(kTcRows, D, 1, !KV8);
+      for (uint32_t n = 0;; ++n) {
+        const int vs = n % NV, ms = n % NM;
+        if (!warp_wait(s_mfull + 8 * ms, (n / NM) & 1u, s_abort)) {
+          ok = false;
+          break;
+        }
+        const int4 meta = g_meta[3 * ms];
+        if (meta.w & kPackedEnd) break;
+        const int ntok = meta.w & 0xffff;
+        const bool first = (meta.w >> 16) & 1, last = (meta.w >> 17) & 1;
+        // the V slot first (normally there already), so that nothing but the MMAs follows the softmax threads' hand-over
+        if ((ntok > 0 && !warp_wait(s_vfull + 8 * vs, (n / NV) & 1u, s_abort)) ||
+            !warp_wait(s_pready + 8 * (n & 1), (n >> 1) & 1u, s_abort)) {
+          ok = false;
+          break;
+        }
+        if (ntok > 0) {
+          tc_fence_after_sync();
+          if (lane == 0) {
+            const uint64_t dv = umma_smem_desc(s_v + (uint32_t)vs * kSlotBytes, kTc2HalfBytes, 1024);
+            const uint32_t tp = tmem + 256u * (n & 1);
+#pragma unroll
+            for (int k = 0; k < kTc2StageTok / 16; ++k)  // 16 tokens: 8 columns of P, 16 rows of 128 bytes of V in either half
+              umma_ts(tmem + 128, tp + 8 * k, dv + (uint64_t)(k * (2048 >> 4)), idesc_o, (first && k == 0) ? 0u : 1u);
+            if (last) umma_commit(s_pvdone);
+            umma_commit(s_pvstage + 8 * (n & 1));
+            umma_commit(s_vempty + 8 * vs);
+          }
+          __syncwarp();
+          issued = true;
+        } else {
+          if (lane == 0) {
+            if (last) mbar_arrive(s_pvdone);  // a unit without tokens: nothing to wait for
+            mbar_arrive(s_pvstage + 8 * (n & 1));
+            mbar_arrive(s_vempty + 8 * vs);
+          }
+          __syncwarp();
+        }
+      }
+    }
+    if (!ok && lane == 0) atomicOr(&p.hdr->status, kStatusWaitTimeout);
+    if (!ok && issued) {  // the tensor memory must not be released under MMAs in flight
+      if (lane == 0) umma_commit(s_drain + 8 * t);
+      __syncwarp();
+      int dummy = 0;
+      mbar_wait_bounded(s_drain + 8 * t, 0u, &dummy, kWaitLimitNs / 8);
+    }
+  } else if (warp >= kWarpM) {
+    // ================================================================= MMA warps: warp kWarpM + t issues tile t's MMAs
+    // One thread issues an MMA about every 110 to 130 cycles whatever its size (measured: M128 N64 or N128 K16, either
+    // operand source), twice what the pipe needs for N = 128, and the pipe overlaps the MMAs of two threads (two
+    // issuers: one N = 128 MMA per 70 cycles).  So each tile has an issuing warp of its own; the order inside a tile,
+    // P.V_t(n - 1) before S_t(n), is the program order of its thread, and the tiles need no order between them.
+    const int t = warp - kWarpM;
+    const uint32_t idesc_s = umma_idesc_16bit(kTcRows, kTc2StageTok, 0, true);
+    const uint32_t idesc_o = umma_idesc_16bit(kTcRows, D, 1, true);
+    const uint32_t ts = tmem + 256u * t;
+    const uint64_t dq = umma_smem_desc(s_q + (uint32_t)t * kQBytes, 0, 1024);
+    uint32_t n_q = 0;  // units in which the tile had rows and tokens (uses of its q-ready barrier)
+    bool issued = false, ok = true;
+    // what is known about the stage whose P.V MMAs are still to be issued
+    bool p_valid = false, p_act = false, p_first = false, p_last = false;
+    int p_ntok = 0;
+    uint32_t p_n = 0;
+    for (uint32_t n = 0;; ++n) {
+      const int ks = n % NK, ms = n % NM;
+      if (!warp_wait(s_kfull + 8 * ks, (n / NK) & 1u, s_abort)) {
+        ok = false;
+        break;
+      }
+      const int4 meta = g_meta[3 * ms], meta2 = g_meta[3 * ms + 1];
+      const int columns = g_meta[3 * ms + 2].x;
+      const bool end = meta.w & kPackedEnd;
+      const int ntok = end ? 0 : (meta.w & 0xffff);
+      const bool first = !end && ((meta.w >> 16) & 1), last = !end && ((meta.w >> 17) & 1);
+      const bool act = !end && (t == 0 || meta2.w + kTcRows < columns);  // a unit always has rows in its first tile
+      // Everything that is normally there already is waited for first (the pending stage's V slot, the other tile's
+      // turn: see below), so that nothing but the MMAs themselves follows the softmax threads' hand-over.
+      if (p_valid && p_act && p_ntok > 0 && !warp_wait(s_vfull + 8 * (p_n % NV), (p_n / NV) & 1u, s_abort)) {
+        ok = false;
+        break;
+      }
+      // The tiles take turns, half a stage apart: S_0(n), S_1(n), S_0(n + 1), ... in this order, so that one tile's
+      // softmax runs beside the other tile's MMAs (P.V of the stage before, then these scores) instead of both tiles
+      // doing the same thing at once.  Tile 1 waits for tile 0's scores of this stage, tile 0 for tile 1's of the
+      // stage before -- on every stage, with or without work, so that neither warp can get two turns ahead of the
+      // other on a barrier pair.
+      if (t == 1 ? !warp_wait(s_sready + 8 * (n & 1), (n >> 1) & 1u, s_abort)
+                 : (n > 0 && !warp_wait(s_sready + 8 * (2 + ((n - 1) & 1)), ((n - 1) >> 1) & 1u, s_abort))) {
+        ok = false;
+        break;
+      }
+      // ---- P.V of the pending stage: waits for the tile's softmax threads, then issues (or just takes the turn)
+      if (p_valid) {
+        const int vs = p_n % NV;
+        if (!warp_wait(s_pready + 8 * (2 * t + (p_n & 1)), (p_n >> 1) & 1u, s_abort)) {
+          ok = false;
+          break;
+        }
+        if (p_act && p_ntok > 0) {
+          tc_fence_after_sync();
+          if (lane == 0) {
+            const uint64_t dv = umma_smem_desc(s_v + (uint32_t)vs * kSlotBytes, kTc2HalfBytes, 1024);
+#pragma unroll
+            for (int k = 0; k < kTc2StageTok / 16; ++k)  // 16 tokens: 8 columns of P, 16 rows of 128 bytes of V in either half
+              umma_ts(ts + 128, ts + 8 * k, dv + (uint64_t)(k * (2048 >> 4)), idesc_o, (p_first && k == 0) ? 0u : 1u);
+            if (p_last) umma_commit(s_pvdone + 8 * t);
+            umma_commit(s_vempty + 8 * vs);  // (one of the two arrivals that free the V slot)
+          }
+          __syncwarp();
+          issued = true;
+        } else {
+          if (lane == 0) {
+            if (p_act && p_last) mbar_arrive(s_pvdone + 8 * t);  // a unit without tokens: nothing to wait for
+            mbar_arrive(s_vempty + 8 * vs);
+          }
+          __syncwarp();
+        }
+      }
+      // ---- scores of this stage
+      if (act && ntok > 0) {
+        if (first) {
+          if (!warp_wait(s_qready + 8 * t, n_q & 1u, s_abort)) {
+            ok = false;
+            break;
+          }
+          ++n_q;
+        }
+        tc_fence_after_sync();
+        if (lane == 0) {
+          const uint64_t dk = umma_smem_desc(s_k + (uint32_t)ks * kSlotBytes, 0, 1024);
+#pragma unroll
+          for (int hh = 0; hh < NH; ++hh)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {  // 16 dims = 32 bytes further along the rows; the second 64 dims = the next half
+              const uint64_t off = (uint64_t)((hh * kTc2HalfBytes + k * 32) >> 4);
+              umma_ss(ts, dq + off, dk + off, idesc_s, (hh | k) ? 1u : 0u);
+            }
+          umma_commit(s_sready + 8 * (2 * t + (n & 1)));
+          umma_commit(s_kempty + 8 * ks);  // (one of the two arrivals that free the K slot)
+        }
+        __syncwarp();
+        issued = true;
+      } else {
+        // no scores for this tile: the turn of its barriers is taken all the same (also wakes the softmax threads
+        // for the end marker)
+        if (lane == 0) {
+          mbar_arrive(s_sready + 8 * (2 * t + (n & 1)));
+          mbar_arrive(s_kempty + 8 * ks);
+        }
+        __syncwarp();
+      }
+      if (end) break;
+      p_valid = true;
+      p_act = act;
+      p_first = first;
+      p_last = last;
+      p_ntok = ntok;
+      p_n = n;
+    }
+    if (!ok && lane == 0) atomicOr(&p.hdr->status, kStatusWaitTimeout);
+    if (!ok && issued) {  // the tensor memory must not be released under MMAs in flight
+      if (lane == 0) umma_commit(s_drain + 8 * t);
+      __syncwarp();
+      int dummy = 0;
+      mbar_wait_bounded(s_drain + 8 * t, 0u, &dummy, kWaitLimitNs / 8);
+    }
+  } else {
+    // ================================================================= softmax warps
+    // Tile t = warps 8 t .. 8 t + 7.  Warp (q = warp & 3, hf = (warp >> 2) & 1) owns the 16 score rows
+    // 32 q + 16 hf .. + 15 of the tile (a warp reaches the 32 tensor-memory lanes of its quarter q only) and reads
+    // them in the 16-lane shape: lane (g, tq) holds rows g and g + 8, columns 8 i + 2 tq, + 1 -- two threads would be
+    // too few per row to hide the latency of the row's chain, four share it here and combine with quad shuffles.
+    const int t = warp >> 3, q4 = warp & 3, hf = (warp >> 2) & 1;
+    const int g = lane >> 2, tq = lane & 3;
+    const int row0 = 32 * q4 + 16 * hf + g;  // this thread's rows of the tile: row0 and row0 + 8
+    const uint32_t trow = tmem + ((uint32_t)(32 * q4 + 16 * hf) << 16) + 256u * t;  // the warp's lanes, the tile's columns
+    const int tid_t = threadIdx.x & 255;     // index among the tile's 256 threads
+    // Score column (query token x head) of a tile's row r: column 4 (r % 32) + r / 32 of the tile, so that the columns
+    // of a tile that is not full spread over the four lane quarters -- the warps with hf = 0 take rows before those with
+    // hf = 1, one busy warp per scheduler -- and a warp none of whose rows is a column skips the stage's arithmetic.
+    auto tile_col = [](int r) { return 4 * (r & 31) + (r >> 5); };
+    uint8_t* q_gen = gen + (size_t)t * kQBytes;
+    float m_ref[2] = {-INFINITY, -INFINITY};  // reference maximum per row (scaled, log2 domain)
+    float l_part[2] = {0.f, 0.f};             // this thread's share of the row's sum of weights
+    int lim_row[2] = {0, 0};
+    uint32_t n_unit = 0;  // units in which this tile had rows
+    bool ok = true;
+    bool q_ahead = false;  // the Q rows of the unit that starts with the next stage are in shared memory already
+    // Q of the tile's columns from c0_ on, of a sequence whose rows of q begin at row0_, into the swizzled K-major tile
+    // ([half][row][64 dims], 16-byte chunk ^= row & 7): thread i of the tile writes half of row i >> 1; then the q-ready
+    // arrival
+    auto load_q = [&](int row0_, int h_, int c0_, int columns_) {
+      const int r_ = tid_t >> 1, part_ = tid_t & 1;
+      const int col_ = c0_ + t * kTcRows + tile_col(r_);
+      const int qi_ = col_ / p.G, head_ = col_ - qi_ * p.G;
+      const bool real_ = col_ < columns_;
+      const uint4* src = reinterpret_cast<const uint4*>(p.q + (int64_t)(row0_ + (real_ ? qi_ : 0)) * p.q_stride +
+                                                        (int64_t)(h_ * p.G + (real_ ? head_ : 0)) * D + part_ * (D / 2));
+#pragma unroll
+      for (int c = 0; c < D / 16; ++c) {
+        uint4 v = real_ ? src[c] : make_uint4(0u, 0u, 0u, 0u);
+        if (KV8) v = make_uint4(bf16x2_to_f16x2(v.x), bf16x2_to_f16x2(v.y), bf16x2_to_f16x2(v.z), bf16x2_to_f16x2(v.w));
+        const int cc = part_ * (D / 16) + c;
+        *reinterpret_cast<uint4*>(q_gen + (size_t)(cc >> 3) * kTc2HalfBytes + (size_t)r_ * 128 + (((cc & 7) ^ (r_ & 7)) << 4)) = v;
+      }
+      fence_proxy_async_smem();  // the tile is read by the MMAs through the async proxy
+      mbar_arrive(s_qready + 8 * t);
+    };
+    if (KV8 && t == 1) {
+      // ================================================================= widening warps (8-bit cache, one-tile mode)
+      // Stage n of the 8-bit rings becomes stage n of the 16-bit slots (stages without tokens and the end marker take
+      // their turns too).  A unit of work is (token row r, 16-byte chunk c of the row's 128 codes): one 16-byte load,
+      // sixteen codes widened, two 16-byte stores into the row's 64-dim half c / 4; 1024 units per slot, four per
+      // thread.  K first: the scores need it a stage earlier than P.V needs V.
+      auto widen = [&](const uint8_t* rsrc, uint8_t* sdst, int ntok_) {
+#pragma unroll
+        for (int i = 0; i < kTc2StageTok * 8 / 256; ++i) {
+          const int u = i * 256 + tid_t;
+          const int r = u >> 3, c = u & 7;
+          if (r >= ntok_) continue;  // rows beyond the stage's tokens are never used (masked scores, cleared V rows)
+          const uint4 w = *reinterpret_cast<const uint4*>(rsrc + (size_t)r * 128 + ((c ^ (r & 7)) << 4));
+          uint8_t* drow = sdst + (size_t)(c >> 2) * kTc2HalfBytes + (size_t)r * 128;
+          *reinterpret_cast<uint4*>(drow + (((2 * (c & 3)) ^ (r & 7)) << 4)) =
+              make_uint4(e4m3x2_to_f16x2<kSelB0B1>(w.x), e4m3x2_to_f16x2<kSelB2B3>(w.x), e4m3x2_to_f16x2<kSelB0B1>(w.y),
+                         e4m3x2_to_f16x2<kSelB2B3>(w.y));
+          *reinterpret_cast<uint4*>(drow + (((2 * (c & 3) + 1) ^ (r & 7)) << 4)) =
+              make_uint4(e4m3x2_to_f16x2<kSelB0B1>(w.z), e4m3x2_to_f16x2<kSelB2B3>(w.z), e4m3x2_to_f16x2<kSelB0B1>(w.w),
+                         e4m3x2_to_f16x2<kSelB2B3>(w.w));
+        }
+      };
+      for (uint32_t n = 0;; ++n) {
+        const int ks = n % NK, vs = n % NV, ms = n % NM;
+        // the 8-bit K slot has landed (its meta words were written before its barrier was armed), the 16-bit one is free
+        if (!warp_wait(s_rkfull + 8 * ks, (n / NK) & 1u, s_abort) ||
+            !warp_wait(s_kempty + 8 * ks, ((n / NK) & 1u) ^ 1u, s_abort)) {
+          ok = false;
+          break;
+        }
+        const int4 meta = g_meta[3 * ms];
+        const bool end = meta.w & kPackedEnd;
+        const int ntok = end ? 0 : (meta.w & 0xffff);
+        if (ntok > 0) {
+          widen(gen + (s_rk - base) + (size_t)ks * kTc2RawSlotBytes, gen + (s_k - base) + (size_t)ks * kSlotBytes, ntok);
+          fence_proxy_async_smem();  // the widened slot is read by the MMAs through the async proxy
+        }
+        mbar_arrive(s_kfull + 8 * ks);
+        mbar_arrive(s_rkempty + 8 * ks);
+        if (end) break;
+        if (!warp_wait(s_rvfull + 8 * vs, (n / NV) & 1u, s_abort) ||
+            !warp_wait(s_vempty + 8 * vs, ((n / NV) & 1u) ^ 1u, s_abort)) {
+          ok = false;
+          break;
+        }
+        if (ntok > 0) {
+          widen(gen + (s_rv - base) + (size_t)vs * kTc2RawSlotBytes, gen + (s_v - base) + (size_t)vs * kSlotBytes, ntok);
+          fence_proxy_async_smem();
+        }
+        mbar_arrive(s_vfull + 8 * vs);
+        mbar_arrive(s_rvempty + 8 * vs);
+      }
+    }
+    for (uint32_t n = 0; !(kOne && t == 1); ++n) {  // (one-tile mode: the warps of tile 1 have nothing else to do)
+      const int ms = n % NM;
+      if (!warp_wait(s_mfull + 8 * ms, (n / NM) & 1u, s_abort)) {
+        ok = false;
+        break;
+      }
+      const int4 meta = g_meta[3 * ms], meta2 = g_meta[3 * ms + 1];
+      const int columns = g_meta[3 * ms + 2].x;
+      const bool end = meta.w & kPackedEnd;
+      const int ntok = end ? 0 : (meta.w & 0xffff);
+      const bool first = !end && ((meta.w >> 16) & 1), last = !end && ((meta.w >> 17) & 1);
+      const int h = meta.z, c0 = meta2.w, lim_base = meta2.y;
+      const bool act = !end && (t == 0 || c0 + kTcRows < columns);
+      const int col0 = c0 + t * kTcRows + tile_col(row0);  // score column of row0; that of row0 + 8: col0 + 32
+      const bool warp_rows = c0 + t * kTcRows + tile_col(32 * q4 + 16 * hf) < columns;  // the warp's first column exists
+      if (first && act) {
+#pragma unroll
+        for (int rr = 0; rr < 2; ++rr) {
+          m_ref[rr] = -INFINITY;
+          l_part[rr] = 0.f;
+          lim_row[rr] = lim_base + (col0 + 32 * rr) / p.G;
+        }
+        if (ntok > 0 && !q_ahead) load_q(meta.y, h, c0, columns);
+        q_ahead = false;
+        ++n_unit;
+      }
+      if (!warp_wait(s_sready + 8 * (2 * t + (n & 1)), (n >> 1) & 1u, s_abort)) {
+        ok = false;
+        break;
+      }
+      if (end) break;
+      if (act && ntok > 0 && warp_rows) {
+        tc_fence_after_sync();
+        // Two passes over the stage's scores, 64 tokens at a time (32 registers): the row maxima first, then, with the
+        // reference maxima known, the weights.  Reading the scores twice costs little (tensor memory is close) and
+        // keeps the threads clear of spills.  sh[4 i + 2 rr + c] = score of row (row0 + 8 rr), token 64 h2 + 8 i + 2 tq + c.
+        // tokens [0, e) of the stage are visible to the row
+        const int e0 = min(min(meta2.z, lim_row[0]) - meta2.x, ntok), e1 = min(min(meta2.z, lim_row[1]) - meta2.x, ntok);
+        const bool masked = __any_sync(0xffffffffu, min(e0, e1) < kTc2StageTok);
+        const uint32_t srow = trow + (kOne ? 256u * (n & 1) : 0u);  // the stage's S (and P) columns
+        auto load_half = [&](int h2, uint32_t (&sh)[32]) {
+          tmem_ld_16x256b_x8(srow + 64 * h2, sh);
+          tmem_ld_wait();
+          if (masked) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+#pragma unroll
+              for (int c = 0; c < 2; ++c) {
+                const int j = 64 * h2 + 8 * i + 2 * tq + c;
+                if (j >= e0) sh[4 * i + c] = 0xff800000u;  // -inf
+                if (j >= e1) sh[4 * i + 2 + c] = 0xff800000u;
+              }
+          }
+        };
+        float mxr[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+        for (int h2 = 0; h2 < 2; ++h2) {
+          uint32_t sh[32];
+          load_half(h2, sh);
+#pragma unroll
+          for (int rr = 0; rr < 2; ++rr) {
+            float ma = mxr[rr], mb = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < 8; i += 2) {  // three-input maximum: two scores per instruction, two chains
+              ma = fmax3(ma, __uint_as_float(sh[4 * i + 2 * rr]), __uint_as_float(sh[4 * i + 2 * rr + 1]));
+              mb = fmax3(mb, __uint_as_float(sh[4 * i + 4 + 2 * rr]), __uint_as_float(sh[4 * i + 4 + 2 * rr + 1]));
+            }
+            mxr[rr] = fmaxf(ma, mb);
+          }
+        }
+        float alpha[2] = {1.f, 1.f}, neg_mu[2];
+        bool raise_any = false;
+#pragma unroll
+        for (int rr = 0; rr < 2; ++rr) {
+          float mx = mxr[rr];
+          mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+          mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+          mx *= p.scale_log2e;  // the scale is positive
+          // reference maximum: raised only when the row maximum is more than kTcRescaleStep above it
+          const bool raise = m_ref[rr] != -INFINITY && mx > m_ref[rr] + kTcRescaleStep;
+          if (m_ref[rr] == -INFINITY) {
+            m_ref[rr] = mx;  // nothing accumulated for this row so far
+          } else if (raise) {
+            alpha[rr] = ex2(m_ref[rr] - mx);
+            m_ref[rr] = mx;
+          }
+          raise_any |= raise;
+          neg_mu[rr] = m_ref[rr] == -INFINITY ? 0.f : -m_ref[rr];
+        }
+        if (__any_sync(0xffffffffu, raise_any)) {
+          // P.V of the previous stage was issued before this stage's score MMAs, so it is complete: O may be rescaled
+          // (one-tile mode: another thread issues it, so its own barrier is waited on; never on a unit's first stage)
+          if (kOne && !warp_wait(s_pvstage + 8 * ((n - 1) & 1), ((n - 1) >> 1) & 1u, s_abort)) {
+            ok = false;
+            break;
+          }
+          if (kOne) tc_fence_after_sync();
+#pragma unroll 1
+          for (int c2 = 0; c2 < NH; ++c2) {
+            uint32_t o[32];
+            tmem_ld_16x256b_x8(trow + 128 + 64 * c2, o);
+            tmem_ld_wait();
+#pragma unroll
+            for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * alpha[(j >> 1) & 1]);
+            tmem_st_16x256b_x8(trow + 128 + 64 * c2, o);
+          }
+          tmem_st_wait();
+          l_part[0] *= alpha[0];
+          l_part[1] *= alpha[1];
+        }
+        const float2 scale2 = make_float2(p.scale_log2e, p.scale_log2e);
+        const float2 nm0 = make_float2(neg_mu[0], neg_mu[0]), nm1 = make_float2(neg_mu[1], neg_mu[1]);
+        float2 add0 = {0.f, 0.f}, add1 = {0.f, 0.f};
+#pragma unroll
+        for (int h2 = 0; h2 < 2; ++h2) {  // 64 tokens at a time: 16 packed words of P per thread
+          uint32_t sh[32];
+          load_half(h2, sh);
+          // (P of the first 64 tokens lands on score columns 0 .. 31, read by now; the second 64 tokens' scores, still
+          // to be read, are columns 64 .. 127)
+          uint32_t pw[16];  // pw[2 i + rr]: row (row0 + 8 rr), tokens 64 h2 + 8 i + 2 tq, + 1 = P column 32 h2 + 4 i + tq
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const int r = 4 * i;
+            const float2 x0 = ffma2(make_float2(__uint_as_float(sh[r]), __uint_as_float(sh[r + 1])), scale2, nm0);
+            const float2 x1 = ffma2(make_float2(__uint_as_float(sh[r + 2]), __uint_as_float(sh[r + 3])), scale2, nm1);
+            const float2 w0 = make_float2(ex2(x0.x), ex2(x0.y)), w1 = make_float2(ex2(x1.x), ex2(x1.y));
+            add0 = fadd2(add0, w0);
+            add1 = fadd2(add1, w1);
+            pw[2 * i] = KV8 ? pack_f16x2(w0.x, w0.y) : pack_bf16x2(w0.x, w0.y);
+            pw[2 * i + 1] = KV8 ? pack_f16x2(w1.x, w1.y) : pack_bf16x2(w1.x, w1.y);
+          }
+          tmem_st_16x128b_x8(srow + 32 * h2, pw);
+        }
+        l_part[0] += add0.x + add0.y;
+        l_part[1] += add1.x + add1.y;
+        tmem_st_wait();
+      }
+      if (act && ntok > 0) {
+        if (ntok < kTc2StageTok) {
+          // V rows beyond the stage's tokens may hold anything (NaN included): clear them once the slot has landed
+          const int vs = n % NV;
+          if (!warp_wait(s_vfull + 8 * vs, (n / NV) & 1u, s_abort)) {
+            ok = false;
+            break;
+          }
+          uint8_t* vgen = gen + (s_v - base) + (size_t)vs * kSlotBytes;
+          for (int idx = tid_t; idx < (kTc2StageTok - ntok) * (D / 8); idx += 256) {
+            const int r = ntok + idx / (D / 8), c = idx % (D / 8);
+            *reinterpret_cast<uint4*>(vgen + (size_t)(c >> 3) * kTc2HalfBytes + (size_t)r * 128 + ((c & 7) << 4)) =
+                make_uint4(0u, 0u, 0u, 0u);
+          }
+          fence_proxy_async_smem();  // the cleared rows are read by the MMA through the async proxy
+        }
+        tc_fence_before_sync();
+        __syncwarp();
+      }
+      mbar_arrive(s_pready + 8 * (2 * t + (n & 1)));
+
+      if (last && act) {
+        // The unit's last score MMAs are complete, so the tile's Q rows are free: when the next stage opens a unit
+        // with rows in this tile, its Q goes to shared memory now and the score MMAs of that stage need not wait
+        // for the epilogue below.
+        {
+          const int ms1 = (n + 1) % NM;
+          if (!warp_wait(s_mfull + 8 * ms1, ((n + 1) / NM) & 1u, s_abort)) {
+            ok = false;
+            break;
+          }
+          const int4 nm = g_meta[3 * ms1], nm2 = g_meta[3 * ms1 + 1];
+          const int ncol = g_meta[3 * ms1 + 2].x;
+          if (!(nm.w & kPackedEnd) && (nm.w & 0xffff) > 0 && (t == 0 || nm2.w + kTcRows < ncol)) {
+            load_q(nm.y, nm.z, nm2.w, ncol);
+            q_ahead = true;
+          }
+        }
+        // ---- the unit is complete: normalise the rows of O and write them
+        const int part = meta.x;  // first partial row of the unit, or -1: the rows are complete
+        // use number n_unit - 1 of the tile's pv-done barrier
+        if (!warp_wait(s_pvdone + 8 * t, (n_unit - 1) & 1u, s_abort)) {
+          ok = false;
+          break;
+        }
+        tc_fence_after_sync();
+        const bool unit_has_tokens = ntok > 0;  // (a unit without tokens is one stage: nothing is in O)
+        float inv[2], lse[2];
+        __nv_bfloat16* orow[2];
+        float* prow[2];
+        bool write_row[2];
+#pragma unroll
+        for (int rr = 0; rr < 2; ++rr) {
+          float l = l_part[rr];
+          l += __shfl_xor_sync(0xffffffffu, l, 1);
+          l += __shfl_xor_sync(0xffffffffu, l, 2);
+          // l = 0: the row saw no token of this chunk; the 8-bit cache's V scale (and widening factor) comes in here
+          inv[rr] = (l > 0.f ? 1.f / l : 0.f) * (KV8 ? p.v_scale : 1.f);
+          lse[rr] = l > 0.f ? m_ref[rr] + lg2(l) : -INFINITY;
+          const int col = col0 + 32 * rr;
+          const int qi = col / p.G, head = col - qi * p.G;
+          write_row[rr] = col < columns &&
+                          checked(part < 0 || chk_index(part + col - c0, p.max_part_rows), &p.hdr->status, kStatusBadIndex);
+          orow[rr] = p.out + (int64_t)(meta.y + qi) * p.out_stride + (int64_t)(h * p.G + head) * D;
+          prow[rr] = p.part_o + (int64_t)(part + col - c0) * D;
+          if (write_row[rr] && tq == 0 && part >= 0) p.part_lse[part + col - c0] = lse[rr];
+        }
+#pragma unroll 1
+        for (int c2 = 0; c2 < (warp_rows ? NH : 0); ++c2) {
+          uint32_t o[32];  // o[4 i + 2 rr + c] = row (row0 + 8 rr), dim 64 c2 + 8 i + 2 tq + c
+          if (unit_has_tokens) {
+            tmem_ld_16x256b_x8(trow + 128 + 64 * c2, o);
+            tmem_ld_wait();
+          } else {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) o[j] = 0u;
+          }
+#pragma unroll
+          for (int rr = 0; rr < 2; ++rr) {
+            if (!write_row[rr]) continue;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const float a = __uint_as_float(o[4 * i + 2 * rr]) * inv[rr], c = __uint_as_float(o[4 * i + 2 * rr + 1]) * inv[rr];
+              const int dim = 64 * c2 + 8 * i + 2 * tq;
+              if (part < 0)
+                *reinterpret_cast<uint32_t*>(orow[rr] + dim) = pack_bf16x2(a, c);
+              else
+                *reinterpret_cast<float2*>(prow[rr] + dim) = make_float2(a, c);
+            }
+          }
+          __syncwarp();  // the tensor-memory loads are warp-wide: reconverge before the next one
+        }
+        tc_fence_before_sync();  // the next unit's first P.V overwrites O: ordered behind these reads by p-ready
+      }
+    }
+    if (!ok && lane == 0) atomicOr(&p.hdr->status, kStatusWaitTimeout);
+  }
+  // ---- common exit: release the tensor memory once every warp is done with it
+  tc_fence_before_sync();
+  __syncthreads();
+  if (warp == kWarpM) tmem_dealloc(tmem, kTc2TmemCols);
+}
+
+
+}  // namespace ooco
