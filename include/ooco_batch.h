@@ -112,15 +112,16 @@ typedef struct {
   int32_t max_nodes;        /* N rows per sequence, 1 .. OOCO_TREE_MAX_NODES                           */
   int32_t vocab;            /* V, 1 .. OOCO_MAX_SHAPED_VOCAB                                           */
   int32_t logits_fp32;      /* 0: bf16 logits, 1: fp32                                                 */
-  int32_t history_width;    /* row width of `history`                                                  */
+  int32_t history_width;    /* row width of `history`, 0 .. OOCO_MAX_HISTORY                            */
   int32_t max_bias;         /* entries per sequence of bias_tokens, 0 .. OOCO_MAX_BIAS                 */
   int64_t logits_seq_stride, logits_node_stride;  /* elements; rows of V consecutive values            */
   int64_t out_seq_stride, out_node_stride;
   int64_t probs_seq_stride, probs_node_stride;
   int64_t mask_seq_stride, mask_node_stride;      /* 32-bit words; 0 = one mask for all                */
 } ooco_logits_t;
-#define OOCO_MAX_SHAPED_VOCAB (1 << 19)
+#define OOCO_MAX_SHAPED_VOCAB 409600
 #define OOCO_MAX_BIAS 1024
+#define OOCO_MAX_HISTORY (1 << 30)
 
 /*
  * From logits to what a sampler, or ooco_verify_drafts, takes: for every row (sequence b, node i) and token v

@@ -18,7 +18,7 @@ from .binding import OocoError, Shape, ooco_shape_t
 from .spec import Rope, ooco_rope_t
 
 MAX_PAGE_ROWS = 1 << 18
-MAX_SHAPED_VOCAB = 1 << 19
+MAX_SHAPED_VOCAB = 409600
 MAX_BIAS = 1024
 
 

@@ -4,13 +4,17 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "cta_util.cuh"
 #include "ptx.cuh"
 
 namespace ooco {
 
-constexpr int kLogitsThreads = 512, kLogitsMaxCluster = 16, kLogitsMaxBias = 1024;
-constexpr uint32_t kSeenBit = 0x80000000u;  // of a counter: the token stands in the prompt
+constexpr int kLogitsThreads = 256, kLogitsWarps = kLogitsThreads / 32, kLogitsMaxCluster = 16, kLogitsMaxBias = 1024;
+constexpr int kLogitsList = 1024;   // tokens of a share, with a text that names them, that are listed
+constexpr int kLogitsBlock = 256;   // neighbouring tokens that one CTA of a row has
+constexpr int kLogitsAhead = 10;    // groups of a thread whose loads run ahead of their use
 
 struct LogitsParams {
   const void* logits;
@@ -20,204 +24,444 @@ struct LogitsParams {
   float *out, *probs;
   int64_t l_seq, l_node, o_seq, o_node, p_seq, p_node, m_seq, m_node;
   int32_t B, N, V, L, M;   // L = history width, M = bias entries
-  int32_t share;           // values per CTA, a multiple of 256
   int32_t penalties;       // any of the three is given
+  int32_t share;           // tokens of a CTA, a multiple of kLogitsBlock
+  int32_t cluster_log2;    // CTAs of a row
+  int32_t run;             // nodes of a sequence that a cluster works on, one after the other
 };
 
-__device__ __forceinline__ void add_cluster(uint32_t addr, uint32_t v) {
-  asm volatile("red.relaxed.cluster.shared::cluster.add.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
-}
-__device__ __forceinline__ void or_cluster(uint32_t addr, uint32_t v) {
-  asm volatile("red.relaxed.cluster.shared::cluster.or.b32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
-}
 __device__ __forceinline__ float logit(const __nv_bfloat16* p) { return __bfloat162float(*p); }
 __device__ __forceinline__ float logit(const float* p) { return *p; }
-__device__ __forceinline__ float no_nan(float x) { return x == x ? x : -INFINITY; }
 
 struct Penalties {
   float rep, freq, pres;
 };
 // Every operation is rounded to fp32, none contracted, so that equal logits stay equal and near ones keep their order.
-__device__ __forceinline__ float penalised(float x, uint32_t count, const Penalties& w) {
+__device__ __forceinline__ float penalised(float x, uint32_t made, const Penalties& w) {
   x = x > 0.f ? __fdiv_rn(x, w.rep) : __fmul_rn(x, w.rep);
-  const uint32_t n = count & ~kSeenBit;
-  if (n) x = __fsub_rn(__fsub_rn(x, __fmul_rn(w.freq, (float)n)), w.pres);
+  if (made) x = __fsub_rn(__fsub_rn(x, __fmul_rn(w.freq, (float)made)), w.pres);
   return x;
 }
 
-// Reduction over the CTA, then over the cluster through distributed shared memory; every thread gets the result.  The order of
-// a sum depends on the launch shape alone.
-template <typename Op>
-__device__ __forceinline__ float cluster_reduce(float v, Op op, float* s_warp, float* s_rank, int rank, int cluster) {
-  const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
-  for (int o = 16; o; o >>= 1) v = op(v, __shfl_xor_sync(0xffffffffu, v, o));
-  if (lane == 0) s_warp[wid] = v;
-  __syncthreads();
-  if (wid == 0) {
-    v = s_warp[lane % (kLogitsThreads / 32)];
-    for (int o = kLogitsThreads / 64; o; o >>= 1) v = op(v, __shfl_xor_sync(0xffffffffu, v, o));
-    if (cluster > 1) {
-      if (lane < cluster) st_cluster(map_cluster(smem_u32(s_rank + rank), lane), v);
-    } else if (lane == 0) {
-      s_rank[0] = v;
-    }
-  }
-  if (cluster > 1) {
-    cluster_arrive();
-    cluster_wait();
-  } else {
-    __syncthreads();
-  }
-  v = s_rank[0];
-  for (int r = 1; r < cluster; ++r) v = op(v, s_rank[r]);
-  return v;
-}
+// A reference r, and the sum of exp((x - r) / T) (or, where the temperature asks for the largest logit, its lowest index).
+struct Softmax {
+  float top, sum;
+};
 
-// A cluster of CTAs per row.  Each CTA holds its share of the vocabulary in shared memory as one word per token: first the
-// token's count (the history is read once, split over the CTAs, which count in one another's shared memory), then the shaped
-// logit, then its weight.  So logits are read once and probabilities written once, which is what bounds the kernel: HBM for
-// many rows, the chain of passes and cluster barriers for few.  Sums are fp32: 2^-24 relative a term and step of a tree of
-// about 16 levels and the 40 to 130 values of a thread.
-template <typename T>
-__global__ void __launch_bounds__(kLogitsThreads, 2) shape_logits_kernel(const LogitsParams p, const int cluster) {
-  extern __shared__ uint32_t s_word[];  // [share]
-  __shared__ float s_warp[2][kLogitsThreads / 32], s_rank[2][kLogitsMaxCluster];
-  __shared__ int s_parent[kTreeMaxNodes], s_bias_token[kLogitsMaxBias];
-  const int tid = threadIdx.x;
-  const int rank = cluster > 1 ? (int)cluster_rank() : 0;
-  const int row = blockIdx.x / cluster, b = row / p.N, node = row - b * p.N;
+__device__ __forceinline__ void prefetch_l2(const void* ptr) { asm volatile("prefetch.global.L2 [%0];" ::"l"(ptr)); }
+
+// A thread's neighbouring tokens.
+template <int W>
+struct Group {
+  float x[W];
+  __device__ float& operator[](int j) { return x[j]; }
+  __device__ const float& operator[](int j) const { return x[j]; }
+};
+
+// What a token's text says: a bit for the prompt above the number of generated occurrences.  Half a word where the history is
+// short enough (two tokens share a word of shared memory, and their fields cannot run into one another), else a word.
+template <bool kHalf>
+struct Counter {
+  static constexpr uint32_t kPrompt = kHalf ? 0x8000u : 0x80000000u;
+  __device__ static uint32_t read(const uint32_t* s, int at) {
+    return kHalf ? (s[at >> 1] >> (16 * (at & 1))) & 0xffffu : s[at];
+  }
+  __device__ static uint32_t add(uint32_t* s, int at, uint32_t v) {  // returns what was there
+    return kHalf ? (atomicAdd(&s[at >> 1], v << (16 * (at & 1))) >> (16 * (at & 1))) & 0xffffu : atomicAdd(&s[at], v);
+  }
+  __device__ static void take(uint32_t* s, int at) { kHalf ? atomicSub(&s[at >> 1], 1u << (16 * (at & 1))) : atomicSub(&s[at], 1u); }
+  __device__ static uint32_t mark(uint32_t* s, int at) {
+    return kHalf ? (atomicOr(&s[at >> 1], kPrompt << (16 * (at & 1))) >> (16 * (at & 1))) & 0xffffu : atomicOr(&s[at], kPrompt);
+  }
+};
+
+// A cluster of CTAs works on `run` nodes of a sequence (one, without drafts).  Blocks of 256 neighbouring tokens go to its CTAs in
+// turn, so that the low token numbers, which tokenisers give to frequent pieces, do not all fall to one.  The text is read and
+// counted once for all the nodes: every CTA reads the whole history (from L2 but for the first) and counts what falls into its
+// share, which is cheaper than sending counts through the cluster; tokens that it meets are listed, so that the arithmetic of the
+// penalties runs with full warps.  Then, for each node: the masked logits to shared memory, one word a token; penalties and
+// biases on the tokens concerned; the largest; weights and their sum; one exchange in the cluster; probabilities.  So logits are
+// read once and probabilities written once, which is what bounds the kernel for many rows, beside the instructions (about 15 a
+// token); few rows are bound by the chain of loads, reductions and the exchange.
+// Sums are fp32: 2^-24 relative a step, over the 20 to 64 values of a thread, a tree of 8 levels, and a tree over the CTAs.
+// kWide: rows of logits and outputs begin on boundaries of four values, so a thread has groups of four neighbours, which every
+// access to shared and global memory moves without conflicts or partial sectors; else single tokens, side by side across the lanes.
+template <typename T, bool kWide, bool kHalf>
+__global__ void __launch_bounds__(kLogitsThreads, 3) shape_logits_kernel(const LogitsParams p) {
+  using C = Counter<kHalf>;
+  constexpr int W = kWide ? 4 : 1;
+  using G = Group<W>;
+  extern __shared__ uint4 s_dyn[];  // values [share]; with penalties: counters [share], ancestors of the nodes
+  float* s_val = reinterpret_cast<float*>(s_dyn);
+  uint32_t* s_count = reinterpret_cast<uint32_t*>(s_val + p.share);
+  uint32_t* s_above = s_count + (kHalf ? p.share / 2 : p.share);  // [N][words]
+  __shared__ float s_warp[2][kLogitsWarps], s_factor;
+  __shared__ Softmax s_rank[2][kLogitsMaxCluster];
+  __shared__ int s_token[kTreeMaxNodes], s_parent[kTreeMaxNodes], s_bias_at[kLogitsMaxBias], s_bias_token[kLogitsMaxBias], s_listed;
+  __shared__ uint16_t s_list[kLogitsList];
+  const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
+  const int cluster = 1 << p.cluster_log2, runs = (p.N + p.run - 1) / p.run;
+  const uint32_t rank = cluster > 1 ? cluster_rank() : 0;
+  const int unit = blockIdx.x >> p.cluster_log2, b = unit / runs, node0 = (unit - b * runs) * p.run;
   grid_dep_wait();
   grid_dep_launch();
-  if (p.tree_sizes && node >= p.tree_sizes[b]) return;  // (the whole cluster)
-  const int lo = min(p.V, rank * p.share), hi = min(p.V, lo + p.share), n = hi - lo;
-  const T* src = reinterpret_cast<const T*>(p.logits) + (int64_t)b * p.l_seq + (int64_t)node * p.l_node + lo;
-  const uint32_t* mask = p.mask ? p.mask + (int64_t)b * p.m_seq + (int64_t)node * p.m_node + (lo >> 5) : nullptr;
-  float* s_val = reinterpret_cast<float*>(s_word);
+  const int nodes = p.tree_sizes ? min(p.N, p.tree_sizes[b]) : p.N, node1 = min(nodes, node0 + p.run);
+  if (node0 >= node1) return;  // (the whole cluster)
+  const bool exchange = cluster > 1 && p.probs;
+  if (exchange) cluster_arrive();  // (waited for before the first write to another CTA's memory)
+  // the token at place i of the share, and the place of a token, or -1
+  auto token = [&](uint32_t i) {
+    return (int)((((i / kLogitsBlock) << p.cluster_log2) + rank) * kLogitsBlock + i % kLogitsBlock);
+  };
+  auto place = [&](uint32_t tok) {
+    const uint32_t block = tok / kLogitsBlock;
+    return tok < (uint32_t)p.V && (block & (cluster - 1)) == rank
+               ? (int)((block >> p.cluster_log2) * kLogitsBlock + tok % kLogitsBlock) : -1;
+  };
+  const T* src0 = reinterpret_cast<const T*>(p.logits) + (int64_t)b * p.l_seq;
+  const uint32_t* mask0 = p.mask ? p.mask + (int64_t)b * p.m_seq : nullptr;
+  auto prefetch = [&](int node) {
+    constexpr int kLine = 128 / (int)sizeof(T);
+    const T* src = src0 + (int64_t)node * p.l_node;
+    for (int i = tid * kLine; i < p.share; i += kLogitsThreads * kLine)
+      if (token(i) < p.V) prefetch_l2(src + token(i));
+    if (mask0)
+      for (int i = tid * kLogitsBlock; i < p.share; i += kLogitsThreads * kLogitsBlock)
+        if (token(i) < p.V) prefetch_l2(mask0 + (int64_t)node * p.m_node + (token(i) >> 5));
+  };
+  // ---- once: the text, the biases
+  const float t = p.temperature ? p.temperature[b] : 1.f;
+  const bool soft = t > 0.f;
+  if (tid == 0) {
+    s_listed = 0;
+    if (soft) s_factor = (float)(1.4426950408889634 / (double)t);  // (one rounding)
+  }
   Penalties w = {1.f, 0.f, 0.f};
+  const bool drafts = p.penalties && p.tokens && p.N > 1;
+  const int words = (p.N + 31) / 32;
+  auto list = [&](int at) {  // a token whose counter was 0
+    const int i = atomicAdd(&s_listed, 1);
+    if (i < kLogitsList) s_list[i] = (uint16_t)at;
+  };
+  if (p.M > 0)
+    for (int j = tid; j < p.M; j += kLogitsThreads) s_bias_token[j] = p.bias_tokens[(int64_t)b * p.M + j];
   if (p.penalties) {
+    const int len = min(max(0, p.history_lens[b]), p.L), prompt = p.prompt_lens ? min(max(0, p.prompt_lens[b]), len) : 0;
     if (p.repetition) w.rep = p.repetition[b] > 0.f ? p.repetition[b] : 1.f;
     if (p.frequency) w.freq = p.frequency[b];
     if (p.presence) w.pres = p.presence[b];
-    for (int i = tid; i < p.share / 4; i += kLogitsThreads) reinterpret_cast<uint4*>(s_word)[i] = make_uint4(0u, 0u, 0u, 0u);
-    const int len = min(max(0, p.history_lens[b]), p.L), prompt = p.prompt_lens ? min(max(0, p.prompt_lens[b]), len) : 0;
-    const bool drafts = p.tokens && node > 0;
-    if (rank == 0 && drafts)
-      for (int i = tid; i <= node; i += kLogitsThreads) s_parent[i] = p.parents ? p.parents[(int64_t)b * p.N + i] : i - 1;
-    if (cluster > 1) {
-      cluster_arrive();
-      cluster_wait();
-    } else {
-      __syncthreads();
-    }
-    const uint32_t base = smem_u32(s_word);
-    auto count = [&](int tok, bool generated) {
-      if (tok < 0 || tok >= p.V) return;
-      const int owner = tok / p.share;
-      const uint32_t at = base + 4u * (uint32_t)(tok - owner * p.share);
-      if (cluster > 1) {
-        const uint32_t far = map_cluster(at, owner);
-        if (generated) add_cluster(far, 1u); else or_cluster(far, kSeenBit);
-      } else {
-        if (generated) atomicAdd(&s_word[tok], 1u); else atomicOr(&s_word[tok], kSeenBit);
+    prefetch(node0);
+    if (node0 + 1 < node1) prefetch(node0 + 1);
+    for (int i = tid; i < (kHalf ? p.share / 8 : p.share / 4); i += kLogitsThreads)
+      reinterpret_cast<uint4*>(s_count)[i] = make_uint4(0u, 0u, 0u, 0u);
+    if (drafts)
+      for (int i = tid; i < p.N; i += kLogitsThreads) {
+        const int up = p.parents ? p.parents[(int64_t)b * p.N + i] : i - 1;
+        s_parent[i] = up < i ? up : -1;
+        s_token[i] = p.tokens[(int64_t)b * p.N + i];
       }
+    __syncthreads();
+    if (drafts && wid == kLogitsWarps - 1)  // the nodes of every branch but the root, parents first
+      for (int i = 0; i < node1; ++i) {
+        const int up = s_parent[i];
+        if (lane < words) {
+          const uint32_t own = i > 0 && (i >> 5) == lane ? 1u << (i & 31) : 0u;
+          s_above[i * words + lane] = (up >= 0 ? s_above[up * words + lane] : 0u) | own;
+        }
+        __syncwarp();
+      }
+    auto count = [&](int tok, bool generated) {
+      const int at = place(tok);
+      if (at >= 0 && !(generated ? C::add(s_count, at, 1u) : C::mark(s_count, at))) list(at);
     };
     const int32_t* text = p.history + (int64_t)b * p.L;
-    for (int i = rank * kLogitsThreads + tid; i < len; i += cluster * kLogitsThreads) count(text[i], i >= prompt);
-    if (rank == 0 && drafts && tid == 0)
-      for (int k = node; k > 0;) {
-        count(p.tokens[(int64_t)b * p.N + k], true);
-        const int up = s_parent[k];
-        k = up < k ? up : -1;
+    const int whole = ((uintptr_t)text & 15) ? 0 : len / 4;
+    for (int i0 = tid; i0 < whole; i0 += 4 * kLogitsThreads) {  // four loads in flight
+      int4 u[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int i = i0 + k * kLogitsThreads;
+        u[k] = i < whole ? reinterpret_cast<const int4*>(text)[i] : make_int4(-1, -1, -1, -1);
       }
-    if (cluster > 1) {
-      cluster_arrive();
-      cluster_wait();
-    } else {
-      __syncthreads();
-    }
-  } else if (cluster > 1 && p.probs) {
-    cluster_arrive();  // (waited for before the first write to another CTA's memory)
-  }
-  // ---- the shaped logits but for the biases
-  constexpr int W = 8;
-  const bool wide = !((uintptr_t)src & 15);
-  const int groups = wide ? n / W : 0;
-  for (int g = tid; g < groups; g += kLogitsThreads) {
-    float x[W];
-    if (sizeof(T) == 2) {
-      unpack8(reinterpret_cast<const uint4*>(src)[g], x);
-    } else {
-      const float4 lo4 = reinterpret_cast<const float4*>(src)[2 * g], hi4 = reinterpret_cast<const float4*>(src)[2 * g + 1];
-      x[0] = lo4.x, x[1] = lo4.y, x[2] = lo4.z, x[3] = lo4.w, x[4] = hi4.x, x[5] = hi4.y, x[6] = hi4.z, x[7] = hi4.w;
-    }
-    const uint32_t allowed = mask ? mask[g >> 2] >> (8 * (g & 3)) : 0xffu;
-    if (p.penalties) {
-      const uint4 c0 = reinterpret_cast<const uint4*>(s_word)[2 * g], c1 = reinterpret_cast<const uint4*>(s_word)[2 * g + 1];
-      const uint32_t c[W] = {c0.x, c0.y, c0.z, c0.w, c1.x, c1.y, c1.z, c1.w};
 #pragma unroll
-      for (int k = 0; k < W; ++k)
-        if (c[k]) x[k] = penalised(x[k], c[k], w);
+      for (int k = 0; k < 4; ++k) {
+        const int i = 4 * (i0 + k * kLogitsThreads);
+        count(u[k].x, i >= prompt);
+        count(u[k].y, i + 1 >= prompt);
+        count(u[k].z, i + 2 >= prompt);
+        count(u[k].w, i + 3 >= prompt);
+      }
     }
-#pragma unroll
-    for (int k = 0; k < W; ++k) x[k] = (allowed >> k) & 1u ? no_nan(x[k]) : -INFINITY;
-    reinterpret_cast<float4*>(s_val)[2 * g] = make_float4(x[0], x[1], x[2], x[3]);
-    reinterpret_cast<float4*>(s_val)[2 * g + 1] = make_float4(x[4], x[5], x[6], x[7]);
-  }
-  for (int i = groups * W + tid; i < n; i += kLogitsThreads) {
-    float x = logit(src + i);
-    if (p.penalties && s_word[i]) x = penalised(x, s_word[i], w);
-    s_val[i] = !mask || ((mask[i >> 5] >> (i & 31)) & 1u) ? no_nan(x) : -INFINITY;
+    for (int i = 4 * whole + tid; i < len; i += kLogitsThreads) count(text[i], i >= prompt);
   }
   __syncthreads();
-  if (p.M > 0) {  // a token may be listed more than once: the thread of its first entry adds them all, in their order
-    for (int j = tid; j < p.M; j += kLogitsThreads) s_bias_token[j] = p.bias_tokens[(int64_t)b * p.M + j];
-    __syncthreads();
-    for (int j = tid; j < p.M; j += kLogitsThreads) {
-      const int tok = s_bias_token[j];
-      if (tok < lo || tok >= hi) continue;
-      bool first = true;
-      for (int k = 0; k < j; ++k) first &= s_bias_token[k] != tok;
-      if (!first || s_val[tok - lo] == -INFINITY) continue;
-      float x = s_val[tok - lo];
-      for (int k = j; k < p.M; ++k)
-        if (s_bias_token[k] == tok) x = __fadd_rn(x, p.bias_values[(int64_t)b * p.M + k]);
-      s_val[tok - lo] = no_nan(x);
-    }
-    __syncthreads();
+  for (int j = tid; j < p.M; j += kLogitsThreads) {  // a token's first entry stands for all of them
+    int at = place(s_bias_token[j]);
+    for (int k = 0; k < j && at >= 0; ++k)
+      if (s_bias_token[k] == s_bias_token[j]) at = -1;
+    s_bias_at[j] = at;
   }
-  float* out = p.out ? p.out + (int64_t)b * p.o_seq + (int64_t)node * p.o_node + lo : nullptr;
-  if (out)
-    for (int i = tid; i < n; i += kLogitsThreads) out[i] = s_val[i];
-  if (!p.probs) return;  // (the whole grid)
-  float* probs = p.probs + (int64_t)b * p.p_seq + (int64_t)node * p.p_node + lo;
-  if (cluster > 1 && !p.penalties) cluster_wait();
-  // ---- softmax
-  float top = -INFINITY;
-  for (int i = tid; i < n; i += kLogitsThreads) top = fmaxf(top, s_val[i]);
-  top = cluster_reduce(top, [](float a, float c) { return fmaxf(a, c); }, s_warp[0], s_rank[0], rank, cluster);
-  const float t = p.temperature ? p.temperature[b] : 1.f;
-  if (top == -INFINITY) {
-    for (int i = tid; i < n; i += kLogitsThreads) probs[i] = 0.f;
-  } else if (t > 0.f) {
-    const float inv = __fdiv_rn(1.f, t);
-    float sum = 0.f;
-    for (int i = tid; i < n; i += kLogitsThreads) {
-      const float x = s_val[i];
-      const float e = x == top ? 1.f : (x == -INFINITY ? 0.f : expf((x - top) * inv));
-      s_val[i] = e;
-      sum += e;
+  const int listed0 = s_listed;  // (of the text; the drafts of a node come behind)
+  const float factor = soft ? s_factor : 0.f;
+  __syncthreads();  // (before a draft is listed)
+  // ---- a thread's groups of W tokens: places and tokens move on by fixed steps, since a step is whole blocks
+  constexpr int kStep = kLogitsThreads * W;
+  const int i_first = tid * W, v_first = token(i_first), v_step = kStep << p.cluster_log2;
+  // f(place, token) for the groups in the vocabulary (a row's last one may end behind it: kEnd)
+  const int blocks_in = max(0, (p.V / kLogitsBlock - (int)rank + cluster - 1) >> p.cluster_log2);  // blocks wholly inside
+  const int steps_in = blocks_in * kLogitsBlock / kStep;                                          // ... and steps
+  auto groups = [&](auto f) {
+    int i = i_first, v = v_first;
+#pragma unroll 4
+    for (int k = 0; k < steps_in; ++k, i += kStep, v += v_step) f(i, v, std::false_type{});
+    for (; i < p.share; i += kStep, v += v_step)
+      if (v < p.V) f(i, v, std::true_type{});
+  };
+  auto store = [&](float* dst, int v, const G& x, auto end) {
+    if constexpr (kWide) {
+      if (!decltype(end)::value || v + W <= p.V) {
+        *reinterpret_cast<float4*>(dst + v) = make_float4(x[0], x[1], x[2], x[3]);
+      } else {
+#pragma unroll
+        for (int j = 0; j < W; ++j)
+          if (v + j < p.V) dst[v + j] = x[j];
+      }
+    } else {
+      dst[v] = x[0];
     }
-    sum = cluster_reduce(sum, [](float a, float c) { return a + c; }, s_warp[1], s_rank[1], rank, cluster);
-    const float scale = __fdiv_rn(1.f, sum);
-    for (int i = tid; i < n; i += kLogitsThreads) probs[i] = s_val[i] * scale;
-  } else {  // the lowest index of the largest logit
-    float at = INFINITY;  // (indices are below 2^24: exact)
-    for (int i = tid; i < n; i += kLogitsThreads)
-      if (s_val[i] == top) at = fminf(at, (float)(lo + i));
-    at = cluster_reduce(at, [](float a, float c) { return fminf(a, c); }, s_warp[1], s_rank[1], rank, cluster);
-    for (int i = tid; i < n; i += kLogitsThreads) probs[i] = (float)(lo + i) == at ? 1.f : 0.f;
+  };
+  auto get = [&](int i, G& x) {
+    if constexpr (kWide) {
+      const float4 u = *reinterpret_cast<const float4*>(s_val + i);
+      x[0] = u.x, x[1] = u.y, x[2] = u.z, x[3] = u.w;
+    } else {
+      x[0] = s_val[i];
+    }
+  };
+  auto put = [&](int i, const G& x) {
+    if constexpr (kWide)
+      *reinterpret_cast<float4*>(s_val + i) = make_float4(x[0], x[1], x[2], x[3]);
+    else
+      s_val[i] = x[0];
+  };
+  auto reduce = [&](float v, float* s, auto op) {
+#pragma unroll
+    for (int o = 16; o; o >>= 1) v = op(v, __shfl_xor_sync(0xffffffffu, v, o));
+    if (lane == 0) s[wid] = v;
+    __syncthreads();
+    v = s[lane & (kLogitsWarps - 1)];
+#pragma unroll
+    for (int o = kLogitsWarps / 2; o; o >>= 1) v = op(v, __shfl_xor_sync(0xffffffffu, v, o));
+    return v;
+  };
+  // the weight of a logit beside a reference; equal infinite logits have a weight of 1 each, whatever the temperature
+  auto weight = [&](float v, float ref) { return v == ref ? 1.f : (v == -INFINITY ? 0.f : ex2((v - ref) * factor)); };
+
+  // a group's logits as they are loaded, and as values (the maximum with -inf turns a NaN into it)
+  using Raw = std::conditional_t<kWide, std::conditional_t<sizeof(T) == 2, uint2, float4>, T>;
+  auto values = [&](const Raw& r, G& x) {
+    if constexpr (!kWide) {
+      x[0] = logit(&r);
+    } else if constexpr (sizeof(T) == 2) {
+      x[0] = bf16_lo(r.x), x[1] = bf16_hi(r.x), x[2] = bf16_lo(r.y), x[3] = bf16_hi(r.y);
+    } else {
+      x[0] = r.x, x[1] = r.y, x[2] = r.z, x[3] = r.w;
+    }
+  };
+  Raw ahead[kLogitsAhead];          // the next node's first groups
+  uint32_t ahead_mask[kLogitsAhead];
+  auto load_ahead = [&](int node) {
+    const T* src = src0 + (int64_t)node * p.l_node;
+    const uint32_t* mask = mask0 ? mask0 + (int64_t)node * p.m_node : nullptr;
+#pragma unroll
+    for (int k = 0; k < kLogitsAhead; ++k) {
+      const int i = i_first + k * kStep, v = v_first + k * v_step;
+      if (i < p.share && v + W <= p.V) {
+        ahead[k] = *reinterpret_cast<const Raw*>(src + v);
+        ahead_mask[k] = mask ? mask[v >> 5] : ~0u;
+      }
+    }
+  };
+  load_ahead(node0);
+
+  for (int node = node0; node < node1; ++node) {
+    // ---- masked logits to shared memory
+    auto finish = [&](int i, G& x, uint32_t allowed) {
+#pragma unroll
+      for (int j = 0; j < W; ++j) x[j] = (allowed >> j) & 1u ? fmaxf(x[j], -INFINITY) : -INFINITY;
+      put(i, x);
+    };
+#pragma unroll
+    for (int k = 0; k < kLogitsAhead; ++k) {
+      const int i = i_first + k * kStep, v = v_first + k * v_step;
+      if (i < p.share && v + W <= p.V) {
+        G x;
+        values(ahead[k], x);
+        finish(i, x, ahead_mask[k] >> (v & 31));
+      }
+    }
+    {  // what is left: steps that were not loaded ahead, the group across the end of the vocabulary
+      const T* src = src0 + (int64_t)node * p.l_node;
+      const uint32_t* mask = mask0 ? mask0 + (int64_t)node * p.m_node : nullptr;
+      for (int i = i_first, v = v_first, k = 0; i < p.share && v < p.V; i += kStep, v += v_step, ++k) {
+        if (k < kLogitsAhead && v + W <= p.V) continue;
+        G x;
+        if (v + W <= p.V) {
+          values(*reinterpret_cast<const Raw*>(src + v), x);
+        } else {
+#pragma unroll
+          for (int j = 0; j < W; ++j) x[j] = v + j < p.V ? logit(src + v + j) : -INFINITY;
+        }
+        finish(i, x, mask ? mask[v >> 5] >> (v & 31) : ~0u);
+      }
+    }
+    if (node + 1 < node1) load_ahead(node + 1);
+    if (node + 2 < node1) prefetch(node + 2);
+    // ---- penalties and biases
+    if (drafts && tid > 0 && tid <= node && ((s_above[node * words + (tid >> 5)] >> (tid & 31)) & 1u)) {
+      const int at = place(s_token[tid]);
+      if (at >= 0 && !C::add(s_count, at, 1u)) list(at);
+    }
+    if (p.penalties || p.M > 0) __syncthreads();
+    if (p.penalties) {
+      const int listed = s_listed;
+      const bool all = listed > kLogitsList;  // a share with more tokens than the list holds is walked through
+      for (int i = tid; i < (all ? p.share : listed); i += kLogitsThreads) {
+        const int at = all ? i : s_list[i];
+        const uint32_t word = C::read(s_count, at);
+        if (!word || (all && token(at) >= p.V)) continue;
+        const float x = s_val[at];
+        if (x != -INFINITY) s_val[at] = fmaxf(penalised(x, word & (C::kPrompt - 1), w), -INFINITY);
+      }
+      __syncthreads();
+      if (tid == 0) s_listed = listed0;
+      if (drafts && tid > 0 && tid <= node && ((s_above[node * words + (tid >> 5)] >> (tid & 31)) & 1u)) {
+        const int at = place(s_token[tid]);
+        if (at >= 0) C::take(s_count, at);  // back to what the text says
+      }
+    }
+    if (p.M > 0) {
+      for (int j = tid; j < p.M; j += kLogitsThreads) {
+        const int at = s_bias_at[j];
+        if (at < 0 || s_val[at] == -INFINITY) continue;
+        float x = s_val[at];
+        for (int k = j; k < p.M; ++k)
+          if (s_bias_token[k] == s_bias_token[j]) x = __fadd_rn(x, p.bias_values[(int64_t)b * p.M + k]);
+        s_val[at] = fmaxf(x, -INFINITY);
+      }
+      __syncthreads();
+    }
+    float* out = p.out ? p.out + (int64_t)b * p.o_seq + (int64_t)node * p.o_node : nullptr;
+    if (!p.probs) {
+      groups([&](int i, int v, auto end) {
+        G x;
+        get(i, x);
+        store(out, v, x, end);
+      });
+      __syncthreads();
+      continue;
+    }
+    // ---- softmax: the CTA's own largest logit is its reference, so one exchange between the CTAs does
+    float top = -INFINITY;
+    groups([&](int i, int, auto) {
+      G x;
+      get(i, x);
+#pragma unroll
+      for (int j = 0; j < W; ++j) top = fmaxf(top, x[j]);
+    });
+    top = reduce(top, s_warp[0], [](float a, float c) { return fmaxf(a, c); });
+    float sum;
+    if (soft) {
+      sum = 0.f;
+      const bool plain = fabsf(top) < INFINITY && factor > 0.f && factor < INFINITY;
+      if (out)
+        groups([&](int i, int v, auto end) {
+          G x;
+          get(i, x);
+          store(out, v, x, end);
+        });
+      if (plain) {
+        groups([&](int i, int, auto) {
+          G x;
+          get(i, x);
+#pragma unroll
+          for (int j = 0; j < W; ++j) {
+            x[j] = ex2((x[j] - top) * factor);
+            sum += x[j];
+          }
+          put(i, x);
+        });
+      } else {
+        groups([&](int i, int, auto) {
+          G x;
+          get(i, x);
+#pragma unroll
+          for (int j = 0; j < W; ++j) {
+            x[j] = top == -INFINITY ? 0.f : weight(x[j], top);
+            sum += x[j];
+          }
+          put(i, x);
+        });
+      }
+      sum = reduce(sum, s_warp[1], [](float a, float c) { return a + c; });
+    } else {
+      sum = INFINITY;  // the lowest index (below 2^24: exact) of the CTA's largest logit
+      groups([&](int i, int v, auto end) {
+        G x;
+        get(i, x);
+        if (out) store(out, v, x, end);
+#pragma unroll
+        for (int j = 0; j < W; ++j)
+          if (x[j] == top && v + j < p.V) sum = fminf(sum, (float)(v + j));
+      });
+      sum = reduce(sum, s_warp[1], [](float a, float c) { return fminf(a, c); });
+    }
+    Softmax all = {top, sum};
+    if (exchange) {
+      Softmax* ranks = s_rank[node & 1];  // (one of two: a CTA may still read the node before's)
+      if (node == node0) cluster_wait();  // every CTA of the cluster has started
+      if (wid == 0 && lane < cluster) {
+        const uint32_t at = map_cluster(smem_u32(&ranks[rank]), lane);
+        st_cluster(at, top);
+        st_cluster(at + 4, sum);
+      }
+      cluster_arrive();
+      cluster_wait();
+      Softmax o = {-INFINITY, soft ? 0.f : INFINITY};
+      if (lane < cluster) o = ranks[lane];
+      all.top = o.top;
+#pragma unroll
+      for (int k = kLogitsMaxCluster / 2; k; k >>= 1) all.top = fmaxf(all.top, __shfl_xor_sync(0xffffffffu, all.top, k));
+      all.top = __shfl_sync(0xffffffffu, all.top, 0);
+      all.sum = soft ? o.sum * weight(o.top, all.top) : (o.top == all.top ? o.sum : INFINITY);
+#pragma unroll
+      for (int k = kLogitsMaxCluster / 2; k; k >>= 1) {
+        const float other = __shfl_xor_sync(0xffffffffu, all.sum, k);
+        all.sum = soft ? all.sum + other : fminf(all.sum, other);
+      }
+      all.sum = __shfl_sync(0xffffffffu, all.sum, 0);
+    }
+    float* probs = p.probs + (int64_t)b * p.p_seq + (int64_t)node * p.p_node;
+    if (soft) {
+      const float scale = all.top == -INFINITY ? 0.f : weight(top, all.top) * __fdiv_rn(1.f, all.sum);
+      groups([&](int i, int v, auto end) {
+        G x;
+        get(i, x);
+#pragma unroll
+        for (int j = 0; j < W; ++j) x[j] *= scale;
+        store(probs, v, x, end);
+      });
+    } else {
+      groups([&](int, int v, auto end) {
+        G x;
+#pragma unroll
+        for (int j = 0; j < W; ++j) x[j] = all.top != -INFINITY && (float)(v + j) == all.sum ? 1.f : 0.f;
+        store(probs, v, x, end);
+      });
+    }
+    // (a thread's groups are its own: the next node's logits may overwrite them.  The counters are back to the text's behind the
+    // barriers of the reductions)
   }
-  // (every write to another CTA's memory lies before a barrier that this CTA has passed)
 }
 
 }  // namespace ooco

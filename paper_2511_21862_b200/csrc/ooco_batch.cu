@@ -14,7 +14,7 @@
 namespace ooco {
 
 static_assert(kPagesStatusBadBlock == OOCO_STATUS_BAD_BLOCK && kPagesStatusRefused == OOCO_STATUS_REFUSED, "status bits");
-static_assert(kLogitsMaxBias == OOCO_MAX_BIAS, "bias limit");
+static_assert(kLogitsMaxBias == OOCO_MAX_BIAS && OOCO_MAX_SHAPED_VOCAB % (kLogitsMaxCluster * kLogitsBlock) == 0, "limits");
 
 // Attributes of a kernel on the current device, set once: dynamic shared memory and clusters of 16 CTAs.
 static int configure(const void* kern, std::atomic<int>* done, int smem) {
@@ -204,6 +204,7 @@ int ooco_shape_logits(const ooco_logits_t* s, const void* logits, const float* t
       s->history_width < 0 || s->max_bias < 0)
     return OOCO_E_SHAPE;
   if (s->batch > (1 << 24) || s->max_nodes > OOCO_TREE_MAX_NODES || s->vocab > OOCO_MAX_SHAPED_VOCAB || s->max_bias > OOCO_MAX_BIAS ||
+      s->history_width > OOCO_MAX_HISTORY ||
       (int64_t)s->batch * s->max_nodes * kLogitsMaxCluster > INT32_MAX)
     return OOCO_E_UNSUPPORTED;
   const bool penalties = repetition || frequency || presence;
@@ -276,19 +277,40 @@ int ooco_shape_logits(const ooco_logits_t* s, const void* logits, const float* t
   p.L = s->history_width;
   p.M = s->max_bias;
   p.penalties = penalties;
-  // CTAs per row: as many as shares of at least 4096 tokens allow while the rows alone do not fill the SMs twice, else the
-  // fewest whose share (one word a token) lets two CTAs share an SM
-  const int64_t rows = B * N;
+  // CTAs per row: shares of at most 10240 tokens, so that three CTAs fit an SM (256 rows of 152064 tokens in trees of 16: 150 us;
+  // with shares of 20480: 350), and more while the rows alone do not fill the SMs twice and shares of more than 4096 tokens can
+  // be halved.  Nodes per cluster: up to 8 share the counting of their text (the same rows: 220 us with 1, 160 with 4, 155 with
+  // 16), as long as there are enough clusters for three CTAs an SM.
+  const int64_t blocks = (V + kLogitsBlock - 1) / kLogitsBlock;
   int cluster = 1;
-  while (cluster < kLogitsMaxCluster && (V > cluster * 26 * 1024ll || (rows * cluster < 2ll * sms && V > cluster * 4096ll))) cluster *= 2;
-  p.share = (int)(((V + cluster - 1) / cluster + 255) / 256 * 256);
-  const size_t smem = (size_t)p.share * 4;
-  cudaStream_t st = (cudaStream_t)cuda_stream;
-  static std::atomic<int> done[2][64];
-  auto kern = s->logits_fp32 ? shape_logits_kernel<float> : shape_logits_kernel<__nv_bfloat16>;
-  if ((rc = configure((const void*)kern, done[s->logits_fp32], (OOCO_MAX_SHAPED_VOCAB / kLogitsMaxCluster) * 4))) return rc;
-  return finish(launch_clustered(kern, dim3((unsigned)(rows * cluster)), dim3(kLogitsThreads), smem, st, pdl_enabled(),
-                                 (unsigned)cluster, p, cluster),
+  while (cluster < kLogitsMaxCluster && (V > cluster * 10240ll || (B * N * cluster < 2ll * sms && V > cluster * 4096ll))) {
+    cluster *= 2;
+    ++p.cluster_log2;
+  }
+  p.share = (int)((blocks + cluster - 1) / cluster * kLogitsBlock);
+  p.run = 1;
+  while (p.run < 8 && p.run < N && B * ((N + 2 * p.run - 1) / (2 * p.run)) * cluster >= 3ll * sms) p.run *= 2;
+  const bool half = s->history_width + N < 32768;
+  const size_t smem = (size_t)p.share * 4 + (penalties ? (size_t)p.share * (half ? 2 : 4) + N * ((N + 31) / 32) * 4 : 0);
+  auto aligned = [&](const void* ptr, int64_t seq, int64_t node, int64_t bytes) {
+    const int64_t rest = 4 * bytes - 1;
+    return !ptr || (!((uintptr_t)ptr & rest) && (B == 1 || !(seq & 3)) && (N == 1 || !(node & 3)));
+  };
+  const bool wide = aligned(logits, s->logits_seq_stride, s->logits_node_stride, cell) &&
+                    aligned(out_logits, s->out_seq_stride, s->out_node_stride, 4) &&
+                    aligned(out_probs, s->probs_seq_stride, s->probs_node_stride, 4);
+  static std::atomic<int> done[8][64];
+  const int which = (s->logits_fp32 ? 4 : 0) + (wide ? 2 : 0) + (half ? 1 : 0);
+  using K = void (*)(LogitsParams);
+  static const K kernels[8] = {shape_logits_kernel<__nv_bfloat16, false, false>, shape_logits_kernel<__nv_bfloat16, false, true>,
+                               shape_logits_kernel<__nv_bfloat16, true, false>, shape_logits_kernel<__nv_bfloat16, true, true>,
+                               shape_logits_kernel<float, false, false>, shape_logits_kernel<float, false, true>,
+                               shape_logits_kernel<float, true, false>, shape_logits_kernel<float, true, true>};
+  // the most that any call takes: a share's values and whole-word counters, the ancestors of a full tree
+  if ((rc = configure((const void*)kernels[which], done[which], OOCO_MAX_SHAPED_VOCAB / kLogitsMaxCluster * 8 + 8192))) return rc;
+  const int64_t runs = (N + p.run - 1) / p.run;
+  return finish(launch_clustered(kernels[which], dim3((unsigned)(B * runs * cluster)), dim3(kLogitsThreads), smem,
+                                 (cudaStream_t)cuda_stream, pdl_enabled(), (unsigned)cluster, p),
                 "launch of the logits kernel");
 }
 

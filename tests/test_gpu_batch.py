@@ -538,7 +538,7 @@ def run_logits(B, N, V, *, dtype=torch.bfloat16, pen=True, bias=0, mask=True, tr
     (2, 16, 32000, dict(sizes=[16, 3])), (1, 1, 128256, dict(L=9000, bias=300)), (2, 1, 152064, dict(dtype=torch.float32, bias=5)),
     (3, 2, 50257, dict(special=True)), (2, 3, 1000, dict(pen=False)), (2, 3, 1000, dict(pen=False, mask=False, temperature=False)),
     (2, 3, 4099, dict(out=False)), (2, 3, 4099, dict(probs=False)), (3, 1, 4096, dict(pad=5)), (3, 1, 4096, dict(pad=8, L=1)),
-    (1, 2, 300000, dict(L=100)), (1, 1, 1 << 19, dict(mask=False, bias=3)), (320, 1, 200, dict(bias=1, dtype=torch.float32)),
+    (1, 2, 300000, dict(L=100)), (1, 1, 409600, dict(mask=False, bias=3, L=40000)), (320, 1, 200, dict(bias=1, dtype=torch.float32)),
     (2, 4, 777, dict(dtype=torch.float32, in_place="out", probs=True)), (2, 4, 1024, dict(dtype=torch.float32, in_place="probs"))])
 def test_logits(B, N, V, kw):
     run_logits(B, N, V, seed=B + V, **kw)
