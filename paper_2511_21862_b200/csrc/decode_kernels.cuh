@@ -99,6 +99,9 @@ struct DecodeParams {
   const int32_t* tree_sizes;    // [B] nodes that exist, or NULL: Sq of them
   uint64_t* tree_mask;          // [B, Sq, tree_words] bit j of row i: node j is node i or one of its ancestors
   int32_t tree_words;
+  // Packed rows (one query token per sequence, that of sequence b in row first_row[b], rows a stride of elements apart).
+  const int32_t* first_row;
+  int64_t q_stride, out_stride;
 };
 
 // Nodes of sequence b's tree.
@@ -808,7 +811,7 @@ static_assert(sizeof(VStageDesc) == 96, "descriptor slot is 96 bytes");
 // shared memory, K as the TMA wrote it) into the stage's own tensor-memory columns.  The consumer warps load their
 // 16-token tile of S in the mma.sync accumulator layout and go on with the softmax and the value MMAs as in KVM 1;
 // the codes of K are never widened.
-template <int D, int NCW, int NT, int TPW, int KVM, bool kTree>
+template <int D, int NCW, int NT, int TPW, int KVM, bool kTree, bool kPacked>
 __device__ __forceinline__ uint32_t decode_main_body(const CUtensorMap& tm_k, const CUtensorMap& tm_v,
                                                      const DecodeParams& p, uint8_t* smem_raw) {
   constexpr bool KV8 = KVM != 0, KVTC = KVM == 2;
@@ -1166,7 +1169,8 @@ __device__ __forceinline__ uint32_t decode_main_body(const CUtensorMap& tm_k, co
           const uint32_t dq = s_q + (uint32_t)kslot * qslot + (uint32_t)lane * p.G * D * 2;
           if (checked(chk_span(dq, (long long)p.G * D * 2, s_q + (long long)kslot * qslot, s_q + (long long)(kslot + 1) * qslot),
                       &p.hdr->status, kStatusBadSmem))
-            bulk_g2s(dq, p.q + (((size_t)b * p.Sq + lane) * p.Hq + (size_t)h * p.G) * D, (uint32_t)p.G * D * 2, kfull);
+            bulk_g2s(dq, kPacked ? p.q + (int64_t)p.first_row[b] * p.q_stride + (size_t)h * p.G * D
+                                 : p.q + (((size_t)b * p.Sq + lane) * p.Hq + (size_t)h * p.G) * D, (uint32_t)p.G * D * 2, kfull);
           else
             span_ok = false;
         }
@@ -1465,7 +1469,10 @@ __device__ __forceinline__ uint32_t decode_main_body(const CUtensorMap& tm_k, co
           if (kChecked && !dst_ok) continue;
           if (n_chunks == 1 && !p.out_f32) {
             const int qi = p.Sq > 1 ? col / p.G : 0, head = col - qi * p.G;
-            p.out[(((size_t)b * p.Sq + qi) * p.Hq + (size_t)h * p.G + head) * D + dim] = __float2bfloat16_rn(o);
+            if (kPacked)
+              p.out[(int64_t)p.first_row[b] * p.out_stride + ((size_t)h * p.G + head) * D + dim] = __float2bfloat16_rn(o);
+            else
+              p.out[(((size_t)b * p.Sq + qi) * p.Hq + (size_t)h * p.G + head) * D + dim] = __float2bfloat16_rn(o);
           } else {
             p.part_o[((size_t)item * p.GQ + col) * D + dim] = o;
             if (dim == 0) p.part_lse[(size_t)item * p.GQ + col] = den > 0.f ? M + lg2(den) : -INFINITY;
@@ -1479,12 +1486,12 @@ __device__ __forceinline__ uint32_t decode_main_body(const CUtensorMap& tm_k, co
   return tmem;
 }
 
-template <int D, int NCW, int NT, int TPW, int KVM = 0, bool kTree = false>
+template <int D, int NCW, int NT, int TPW, int KVM = 0, bool kTree = false, bool kPacked = false>
 __global__ void __launch_bounds__(SmemLayout<D, NCW, NT, TPW, KVM>::kWarps * 32, (KVM && NCW == 8 && NT == 1) ? 2 : 1)
 decode_main_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
                    const DecodeParams p) {
   extern __shared__ uint8_t smem_raw[];
-  const uint32_t tmem = decode_main_body<D, NCW, NT, TPW, KVM, kTree>(tm_k, tm_v, p, smem_raw);
+  const uint32_t tmem = decode_main_body<D, NCW, NT, TPW, KVM, kTree, kPacked>(tm_k, tm_v, p, smem_raw);
   if (KVM == 2) {  // common exit: release the tensor memory once every warp is done with it
     tc_fence_before_sync();
     __syncthreads();

@@ -15,30 +15,44 @@ namespace ooco {
 static_assert(kPackedStatusRefused == OOCO_STATUS_REFUSED, "status bit");
 
 struct PackedLayout {
-  size_t off_tiles, off_items, off_merge, off_merge_first, off_lse, off_o, total;
-  int max_tiles, max_items, max_merge, max_part_rows;
+  size_t off_tiles, off_items, off_dec_first, off_dec_items, off_merge, off_merge_first, off_lse, off_o, total;
+  int max_tiles, max_items, max_merge, max_dec_chunks, dec_rows, max_part_rows;
 };
+
+// CTAs an SM of the decode kernel, as the decode operators launch it.
+static int decode_ctas_per_sm(int head_dim, bool kv8, int64_t G) { return kv8 ? (G > 8 ? 1 : 2) : (head_dim == 64 ? 4 : 2); }
+// Which calls have a decode list: bf16 caches up to 8 heads a group (one MMA tile of columns), 8-bit ones all.
+static bool has_decode(bool kv8, int64_t G) { return kv8 || G <= 8; }
 
 // Bounds that hold for any lengths.  A tile of s stages is cut into at most 2 s / L chunks, where L >= S / (CTAs x items per
 // CTA), S the list's stages over all kv heads: 2 CTAs x items per CTA chunks (x heads) in all, of at most a tile's columns.
-static PackedLayout packed_layout(const ooco_shape_t* s, int64_t num_rows, int64_t max_chunk, bool two_tiles) {
+static PackedLayout packed_layout(const ooco_shape_t* s, int64_t num_rows, int64_t max_chunk) {
   const int64_t G = s->num_q_heads / s->num_kv_heads, cols = G * max_chunk;
   const int64_t cuts[2] = {2ll * kPackedGridCap * packed_items_per_cta(0), 2ll * kPackedGridCap * packed_items_per_cta(1)};
+  const int64_t dec_cuts = 4ll * kPackedGridCap * packed_items_per_cta(2);  // (CTAs x items per CTA / kv heads, at most)
   const int64_t longest = ((int64_t)s->max_blocks_per_seq * s->block_size + kPackedMinStages * kTc2StageTok - 1) / (kPackedMinStages * kTc2StageTok);
   PackedLayout w;
   const int64_t tiles = s->batch + num_rows * G / kTcRows + 1;
-  int64_t rows = cuts[0] * (cols < kTcRows ? cols : kTcRows);
-  if (two_tiles && cols > kTcRows) rows += cuts[1] * kTc2Rows;
+  int64_t rows = max_chunk > 1 || G > 8 ? cuts[0] * (cols < kTcRows ? cols : kTcRows) : 0;
+  if (cols > kTcRows) rows += cuts[1] * kTc2Rows;
   const int64_t most = num_rows * s->num_q_heads * (longest + 1);  // every row in as many chunks as its context allows
   if (rows > most) rows = most;
   auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
   w.max_tiles = (int)(tiles > INT32_MAX / 4 ? INT32_MAX / 4 : tiles);
   w.max_items = w.max_tiles + (int)(cuts[0] + cuts[1]);
   w.max_merge = (int)(tiles < cuts[0] + cuts[1] ? tiles : cuts[0] + cuts[1]);
-  w.max_part_rows = (int)rows;
+  const int64_t decodes = s->batch < num_rows ? s->batch : num_rows;
+  int64_t chunks = decodes + dec_cuts / s->num_kv_heads + 1;
+  if (chunks > decodes * (longest + 1)) chunks = decodes * (longest + 1);
+  w.max_dec_chunks = (int)chunks;
+  w.dec_rows = (int)(chunks * s->num_q_heads);
+  w.max_part_rows = (int)(w.dec_rows + rows);
+  w.max_merge += (int)decodes;
   w.off_tiles = sizeof(PackedHeader);
   w.off_items = w.off_tiles + up(((size_t)s->batch + 1) * 4);
-  w.off_merge = w.off_items + up((size_t)w.max_items * 32);
+  w.off_dec_first = w.off_items + up((size_t)w.max_items * 32);
+  w.off_dec_items = w.off_dec_first + up(((size_t)s->batch + 1) * 4);
+  w.off_merge = w.off_dec_items + up((size_t)w.max_dec_chunks * s->num_kv_heads * 16);
   w.off_merge_first = w.off_merge + up((size_t)w.max_merge * 16);
   w.off_lse = w.off_merge_first + up(((size_t)w.max_merge + 1) * 4);
   w.off_o = w.off_lse + up((size_t)w.max_part_rows * 4);
@@ -62,6 +76,30 @@ static int launch_packed(const CUtensorMap& tk, const CUtensorMap& tv, const Pac
   cudaError_t e = launch_ex(kern, dim3(p.grid), dim3(kTc2Threads), smem, st, pdl_enabled(), tk, tv, p);
   if (e == cudaSuccess) e = cudaGetLastError();
   return e == cudaSuccess ? OOCO_OK : fail_cuda("launch of the packed attention kernel", (long)e);
+}
+
+// The decode list: decode_main_kernel in the launch shape of the decode operators, one query token per sequence.
+template <int D, int NCW, int NT, int KVM>
+static int launch_decodes(const CUtensorMap& tk, const CUtensorMap& tv, DecodeParams& p, const DeviceInfo& di, int ctas_per_sm,
+                          cudaStream_t st, int dev, bool dry) {
+  using L = SmemLayout<D, NCW, NT, 1, KVM>;
+  auto kern = decode_main_kernel<D, NCW, NT, 1, KVM, false, true>;
+  const size_t budget = ((size_t)di.smem_optin + 1024) / ctas_per_sm - 1024;
+  int nst = KVM == 2 ? 8 : 32;
+  while (nst > 2 && L::total(nst, p.GQ) > budget) --nst;
+  const size_t smem = L::total(nst, p.GQ);
+  if (smem > (size_t)di.smem_optin) return OOCO_E_UNSUPPORTED;
+  p.nstages = nst;
+  static std::atomic<int> configured[64];
+  if (dev < 0 || dev >= 64 || !configured[dev].load()) {
+    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, di.smem_optin);
+    if (e != cudaSuccess) return fail_cuda("cudaFuncSetAttribute(max dynamic smem)", (long)e);
+    if (dev >= 0 && dev < 64) configured[dev].store(1);
+  }
+  if (dry) return OOCO_OK;
+  cudaError_t e = launch_ex(kern, dim3(p.next_item_init), dim3(L::kWarps * 32), smem, st, pdl_enabled(), tk, tv, p);
+  if (e == cudaSuccess) e = cudaGetLastError();
+  return e == cudaSuccess ? OOCO_OK : fail_cuda("launch of the decode attention kernel", (long)e);
 }
 
 static int check_rows(int64_t num_rows, int64_t max_chunk) {
@@ -90,7 +128,7 @@ static int chunk_core(const ooco_shape_t* s, int32_t num_rows, int32_t max_chunk
     return OOCO_E_UNSUPPORTED;
   if (num_rows > 0 && rows_overlap(q, 2 * q_stride, 2 * row, out, 2 * out_stride, 2 * row, num_rows)) return OOCO_E_SHAPE;
   const bool two = !kv8;
-  const PackedLayout w = packed_layout(s, num_rows, max_chunk, two);
+  const PackedLayout w = packed_layout(s, num_rows, max_chunk);
   if (workspace_bytes < w.total || ((uintptr_t)workspace & 255)) return OOCO_E_WORKSPACE;
   if (num_rows == 0 || max_chunk == 0) return OOCO_OK;
   int dev = 0;
@@ -119,6 +157,7 @@ static int chunk_core(const ooco_shape_t* s, int32_t num_rows, int32_t max_chunk
   p.Hq = s->num_q_heads;
   p.Hkv = s->num_kv_heads;
   p.G = (int)G;
+  p.D = s->head_dim;
   p.bs = s->block_size;
   p.MB = s->max_blocks_per_seq;
   p.NB = s->num_blocks;
@@ -126,6 +165,13 @@ static int chunk_core(const ooco_shape_t* s, int32_t num_rows, int32_t max_chunk
   p.max_chunk = max_chunk;
   p.two_tiles = two && G * max_chunk > kTcRows;
   p.grid = di.sm_count < kPackedGridCap ? di.sm_count : kPackedGridCap;
+  p.dec_first = (int32_t*)(ws + w.off_dec_first);
+  p.dec_items = (int4*)(ws + w.off_dec_items);
+  p.max_dec_chunks = w.max_dec_chunks;
+  p.dec_rows = w.dec_rows;
+  p.decode = has_decode(kv8, G);
+  p.dec_grid = di.sm_count * decode_ctas_per_sm(s->head_dim, kv8, G);
+  if (p.dec_grid > 4 * kPackedGridCap) p.dec_grid = 4 * kPackedGridCap;
   p.max_tiles = w.max_tiles;
   p.max_items = w.max_items;
   p.max_merge = w.max_merge;
@@ -140,13 +186,64 @@ static int chunk_core(const ooco_shape_t* s, int32_t num_rows, int32_t max_chunk
     if ((rc = encode_kv_map(&tk, s, k_cache, p.tile_rows, false)) || (rc = encode_kv_map(&tv, s, v_cache, p.tile_rows, false)))
       return rc;
   }
+  // the decode list's view of the same workspace; 128-byte boxes of at most a stage's tokens
+  DecodeParams d;
+  memset(&d, 0, sizeof d);
+  const bool wide = kv8 && G > 8;
+  const int dec_stage = kv8 ? 128 : 64;
+  CUtensorMap dk, dv;
+  if (p.decode) {
+    d.q = p.q;
+    d.out = p.out;
+    d.block_table = block_table;
+    d.context_lens = context_lens;
+    d.hdr = &p.hdr->dec;
+    d.items = p.dec_items;
+    d.seq_first = p.dec_first;
+    d.part_o = p.part_o;
+    d.part_lse = p.part_lse;
+    d.B = p.B;
+    d.Hq = p.Hq;
+    d.Hkv = p.Hkv;
+    d.G = d.GQ = p.G;
+    d.Sq = 1;
+    d.D = s->head_dim;
+    d.bs = p.bs;
+    d.MB = p.MB;
+    d.NB = p.NB;
+    d.max_items = w.max_dec_chunks * p.Hkv;
+    d.tile_rows = s->block_size < dec_stage ? s->block_size : dec_stage;
+    d.next_item_init = p.dec_grid;
+    d.first_row = first_row;
+    d.q_stride = q_stride;
+    d.out_stride = out_stride;
+    // (scores come from the codes' own values here: only V carries the widening factor)
+    d.scale_log2e = scale * 1.4426950408889634f * k_scale;
+    d.v_scale = p.v_scale;
+    bool five_d = !kv8 && s->head_dim == 128 && encode_kv_map(&dk, s, k_cache, d.tile_rows, true) == OOCO_OK;
+    d.split_halves = five_d ? 0 : 1;
+    if (kv8)
+      rc = encode_kv8_map(&dk, s, k_cache, d.tile_rows);
+    else if (!five_d)
+      rc = encode_kv_map(&dk, s, k_cache, d.tile_rows, false);
+    if (!rc) rc = kv8 ? encode_kv8_map(&dv, s, v_cache, d.tile_rows) : encode_kv_map(&dv, s, v_cache, d.tile_rows, five_d);
+    if (rc) return rc;
+  }
+  const int cps = decode_ctas_per_sm(s->head_dim, kv8, G);
   cudaStream_t st = (cudaStream_t)cuda_stream;
+  auto decodes = [&](bool dry) -> int {
+    if (kv8) return wide ? launch_decodes<128, 8, 2, 2>(dk, dv, d, di, cps, st, dev, dry) : launch_decodes<128, 8, 1, 2>(dk, dv, d, di, cps, st, dev, dry);
+    return s->head_dim == 128 ? launch_decodes<128, 4, 1, 0>(dk, dv, d, di, cps, st, dev, dry)
+                              : launch_decodes<64, 4, 1, 0>(dk, dv, d, di, cps, st, dev, dry);
+  };
+  const bool tiles = !p.decode || max_chunk > 1;
   auto attention = [&](bool dry) -> int {
     int r = OOCO_OK;
     if (p.two_tiles)
       r = s->head_dim == 128 ? launch_packed<128, false, false>(tk, tv, p, di, dev, st, dry)
                              : launch_packed<64, false, false>(tk, tv, p, di, dev, st, dry);
-    if (r) return r;
+    if (!r && p.decode) r = decodes(dry);
+    if (r || !tiles) return r;
     if (kv8) return launch_packed<128, true, true>(tk, tv, p, di, dev, st, dry);
     return s->head_dim == 128 ? launch_packed<128, false, true>(tk, tv, p, di, dev, st, dry)
                               : launch_packed<64, false, true>(tk, tv, p, di, dev, st, dry);
@@ -176,7 +273,7 @@ size_t ooco_chunk_workspace_bytes(const ooco_shape_t* s, int32_t num_rows, int32
   if (validate_shape(s) || check_rows(num_rows, max_chunk) ||
       (int64_t)(s->num_q_heads / s->num_kv_heads) * num_rows > INT32_MAX / 2)
     return 0;
-  return packed_layout(s, num_rows, max_chunk, true).total;
+  return packed_layout(s, num_rows, max_chunk).total;
 }
 
 int ooco_chunk_attention(const ooco_shape_t* shape, int32_t num_rows, int32_t max_chunk, const void* q, int64_t q_stride,

@@ -1,16 +1,19 @@
 // Attention of the new tokens of all sequences over the paged cache, rows packed: plan -> tiles on tcgen05 -> merge.
 //
-// The G n_b score columns (query x head of the group) of a (sequence, kv head) pair are cut into units of 128 columns, or of
-// 256 where there are more than 128: two kernels, one list of items each, because what bounds them differs.
-//   packed_tc_kernel<.., one tile>   at most 128 columns: the cache is read once for few columns, HBM-bound.  The scores of a
+// The G n_b score columns (query x head of the group) of a (sequence, kv head) pair go, by their number, to one of three lists of
+// items, each with a kernel of its own, because what bounds them differs:
+//   decode_main_kernel               one query token (a decode): as the decode operators, HBM-bound
+//   packed_tc_kernel<.., one tile>   else at most 128 columns: the cache is read once for few columns, HBM-bound.  The scores of a
 //                                    stage run while the softmax threads still work on the stage before.
-//   packed_tc_kernel<.., two tiles>  a piece of a prompt: two 128-row tiles share every K / V slot and take turns on the
-//                                    tensor pipe, tensor-bound.
+//   packed_tc_kernel<.., two tiles>  a piece of a prompt, units of 256 columns: two 128-row tiles share every K / V slot and take
+//                                    turns on the tensor pipe, tensor-bound
 // The CTA is that of chunk_tc2_kernel (chunk_tc2_kernels.cuh), which has one number of query tokens for all sequences; there
 // also stands why its MMAs, slots and warps are as they are.  What differs: a unit carries its sequence's rows, columns and
 // partial rows with it (an item is 32 bytes, a stage's meta words are three), so that sequences of any lengths share a launch;
 // head_dim 64 has half the slot, twice the slots and half the MMAs; an 8-bit cache runs every column on the one-tile kernel.
 #pragma once
+#include <cstddef>
+
 #include "chunk_tc2_kernels.cuh"
 #include "cta_util.cuh"
 
@@ -18,8 +21,8 @@ namespace ooco {
 
 constexpr int kPackedEnd = 1 << 18;          // flag of a stage's meta words: the end marker
 constexpr int kPackedGridCap = 160;          // most CTAs of an attention kernel (bounds the workspace)
-// items the plan aims at per CTA
-__host__ __device__ constexpr int packed_items_per_cta(int list) { return list ? 2 : 4; }  // (0: one-tile list, 1: two-tile list)
+// Lists: 0 = one tile, 1 = two tiles, 2 = decodes.  Items the plan aims at per CTA:
+__host__ __device__ constexpr int packed_items_per_cta(int list) { return list == 0 ? 4 : (list == 1 ? 2 : 6); }
 constexpr int kPackedMinStages = 2;          // shortest chunk: 256 tokens
 constexpr int kPackedStatusRefused = 128;
 
@@ -32,15 +35,15 @@ struct PackedSmem {
   }
 };
 
-struct PackedHeader {  // first 256 bytes of the workspace
-  int32_t status;
-  int32_t n_items[2];    // of the one-tile and of the two-tile list, which follow one another in `items`
-  int32_t next_item[2];  // next unit (item x kv head) that no CTA has taken
+struct PackedHeader {  // first bytes of the workspace
+  WsHeader dec;          // status word; work units (item x kv head) of the decode list and the next one that no CTA has taken
   int32_t n_merge;       // tiles whose tokens are cut into several items
   int32_t merge_rows;    // their rows (x kv head)
-  int32_t pad[57];
+  int32_t n_items[2];    // of the one-tile and of the two-tile list, which follow one another in `items`
+  int32_t next_item[2];  // next unit (item x kv head) that no CTA has taken
+  int32_t pad[58];
 };
-static_assert(sizeof(PackedHeader) == 256, "header is 256 bytes");
+static_assert(sizeof(PackedHeader) == 512 && offsetof(PackedHeader, dec) == 0, "the status word leads the workspace");
 
 struct PackedParams {
   const __nv_bfloat16* q;
@@ -54,9 +57,12 @@ struct PackedParams {
   float* part_o;         // [max_part_rows, D] normalised partial rows
   float* part_lse;       // [max_part_rows] log2-domain log-sum-exp of each
   int64_t q_stride, out_stride;
-  int32_t B, Hq, Hkv, G, bs, MB, NB, num_rows, max_chunk;
+  int32_t B, Hq, Hkv, G, D, bs, MB, NB, num_rows, max_chunk;
+  int4* dec_items;       // [max_dec_chunks, Hkv] items of decode_main_kernel
+  int32_t* dec_first;    // [B + 1] their chunks, counted over the sequences
   int32_t two_tiles;     // 1: more than 128 columns go to the two-tile list
-  int32_t grid, max_tiles, max_items, max_merge, max_part_rows, tile_rows;
+  int32_t decode;        // 1: sequences with one query token go to the decode list
+  int32_t grid, dec_grid, max_tiles, max_items, max_merge, max_part_rows, max_dec_chunks, dec_rows, tile_rows;
   float scale_log2e, v_scale;
 };
 
@@ -80,7 +86,10 @@ __device__ __forceinline__ PackedSeq packed_seq(const PackedParams& p, int b, bo
   s.T = (int)(t < 0 ? 0 : (t > cap ? cap : t));
   return s;
 }
-__device__ __forceinline__ bool packed_two(const PackedParams& p, int n) { return p.two_tiles && p.G * n > kTcRows; }
+__device__ __forceinline__ int packed_list(const PackedParams& p, const PackedSeq& s) {
+  if (p.decode && s.n == 1) return 2;
+  return p.two_tiles && p.G * s.n > kTcRows ? 1 : 0;
+}
 
 // One CTA.  A tile is a unit's columns of one sequence (for all kv heads); its length is what its last column sees, in stages
 // of 128 tokens.  Every list gets a chunk length from its total of stages, tiles that are longer are cut into near-equal
@@ -89,22 +98,23 @@ __device__ __forceinline__ bool packed_two(const PackedParams& p, int n) { retur
 __global__ void __launch_bounds__(1024) packed_plan_kernel(const PackedParams p, const int first_in_smem) {
   extern __shared__ int s_first[];  // [B + 1] when they fit
   __shared__ long long s_warp[32];
-  __shared__ int s_hist[1024];      // 512 lengths for each list
-  __shared__ long long s_sum[2];
+  __shared__ int s_hist[1024];      // 340 lengths for each list
+  __shared__ long long s_sum[3];
   const int tid = threadIdx.x;
   grid_dep_wait();
   grid_dep_launch();
   int* first = first_in_smem ? s_first : p.tile_first;
   s_hist[tid] = 0;
-  if (tid < 2) s_sum[tid] = 0;
+  if (tid < 3) s_sum[tid] = 0;
   bool refused = false;
   long long tiles = 0;
   for (int b0 = 0; b0 < p.B; b0 += 1024) {
     const int b = b0 + tid;
     long long nt = 0, total;
     if (b < p.B) {
-      const int n = packed_seq(p, b, &refused).n, per = packed_two(p, n) ? kTc2Rows : kTcRows;
-      nt = ((long long)p.G * n + per - 1) / per;
+      const PackedSeq q = packed_seq(p, b, &refused);
+      const int per = packed_list(p, q) == 1 ? kTc2Rows : kTcRows;
+      if (q.T > 0) nt = ((long long)p.G * q.n + per - 1) / per;  // (without a context: zeros, below)
     }
     const long long upto = tiles + block_scan(nt, s_warp, &total);
     if (b < p.B) first[b] = (int)min(upto - nt, (long long)INT32_MAX);
@@ -127,40 +137,48 @@ __global__ void __launch_bounds__(1024) packed_plan_kernel(const PackedParams p,
     Tile t;
     t.b = lo;
     t.s = packed_seq(p, lo);
-    t.list = packed_two(p, t.s.n);
-    const int per = t.list ? kTc2Rows : kTcRows;
+    t.list = packed_list(p, t.s);
+    const int per = t.list == 1 ? kTc2Rows : kTcRows;
     t.c0 = (i - first[lo]) * per;
     t.cols = min(per, p.G * t.s.n - t.c0);
     const int seen = min(t.s.T, max(0, t.s.T - t.s.n + 1 + (t.c0 + t.cols - 1) / p.G));
     t.stages = (seen + kTc2StageTok - 1) / kTc2StageTok;
     return t;
   };
-  long long sum[2] = {0, 0};
+  long long sum[3] = {0, 0, 0};
   for (int i = tid; i < NT; i += 1024) {
     const Tile t = tile_of(i);
-    sum[t.list] += max(1, t.stages);
+#pragma unroll
+    for (int k = 0; k < 3; ++k) sum[k] += t.list == k ? max(1, t.stages) : 0;
   }
 #pragma unroll
-  for (int k = 0; k < 2; ++k) {
+  for (int k = 0; k < 3; ++k) {
     for (int o = 16; o; o >>= 1) sum[k] += __shfl_xor_sync(0xffffffffu, sum[k], o);
     if ((tid & 31) == 0 && sum[k]) atomicAdd((unsigned long long*)&s_sum[k], (unsigned long long)sum[k]);
   }
   __syncthreads();
-  int longest[2];
+  int longest[3];
 #pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    const long long ctas = (long long)p.grid * packed_items_per_cta(k);
+  for (int k = 0; k < 3; ++k) {
+    const long long ctas = (long long)(k == 2 ? p.dec_grid : p.grid) * packed_items_per_cta(k);
     longest[k] = max(kPackedMinStages, (int)((s_sum[k] * p.Hkv + ctas - 1) / ctas));
   }
   // chunks of a tile: `len` stages each but the last
   auto cut = [&](const Tile& t, int& nch, int& len) {
     const int s = max(1, t.stages);
-    nch = (s + longest[t.list] - 1) / longest[t.list];
+    const int most = t.list == 0 ? longest[0] : (t.list == 1 ? longest[1] : longest[2]);
+    nch = (s + most - 1) / most;
     len = (s + nch - 1) / nch;
     nch = (s + len - 1) / len;
   };
-  auto bucket = [](int list, int len) { return 512 * list + 511 - min(len, 511); };
-  long long parts = 0, merges = 0;  // rows of partial results; (rows << 32 | tiles) to be merged
+  auto bucket = [](int list, int len) { return 340 * list + 339 - min(len, 339); };
+  // What a tile needs, summed over the tiles before it: (chunks of the decode list << 32 | rows of partial results of the others);
+  // every chunk of the decode list has partial rows, in front of the others', by its number.
+  auto needs = [&](const Tile& t, int nch) -> long long {
+    if (t.list == 2) return (long long)nch << 32;
+    return nch > 1 ? (long long)nch * p.Hkv * t.cols : 0;
+  };
+  long long parts = 0, merges = 0;  // (rows << 32 | tiles) to be merged
   for (int i0 = 0; i0 < NT; i0 += 1024) {
     const int i = i0 + tid;
     Tile t = {};
@@ -169,11 +187,13 @@ __global__ void __launch_bounds__(1024) packed_plan_kernel(const PackedParams p,
     if (i < NT) {
       t = tile_of(i);
       cut(t, nch, len);
-      if (nch > 1) rows = (long long)nch * p.Hkv * t.cols;
+      rows = needs(t, nch);
     }
-    const long long slot = parts + block_scan(rows, s_warp, &total) - rows;
+    const long long from = parts + block_scan(rows, s_warp, &total) - rows;
     parts += total;
-    if (rows && slot + rows > p.max_part_rows) nch = 1;  // (not met: the workspace bound covers the cuts)
+    const int chunk = (int)(from >> 32);
+    const long long slot = t.list == 2 ? (long long)chunk * p.Hkv * p.G : p.dec_rows + (from & 0xffffffff);
+    if (t.list != 2 && slot + rows > p.max_part_rows) nch = 1;  // (not met: the workspace bound covers the cuts)
     const long long m1 = nch > 1 ? ((long long)p.Hkv * t.cols << 32) | 1 : 0;
     const long long m = merges + block_scan(m1, s_warp, &total) - m1;
     merges += total;
@@ -183,6 +203,10 @@ __global__ void __launch_bounds__(1024) packed_plan_kernel(const PackedParams p,
       p.merge_first[at] = (int)(m >> 32);
     }
     if (i < NT) {
+      if (t.list == 2) {
+        p.dec_first[t.b] = chunk;
+        p.dec_first[t.b + 1] = chunk + nch;  // (what the next sequence writes there, if it is one of the list)
+      }
       if (nch > 1) {
         atomicAdd(&s_hist[bucket(t.list, len)], nch - 1);
         atomicAdd(&s_hist[bucket(t.list, t.stages - (nch - 1) * len)], 1);
@@ -193,17 +217,20 @@ __global__ void __launch_bounds__(1024) packed_plan_kernel(const PackedParams p,
   }
   const int n_merge = min((int)(merges & 0xffffffff), p.max_merge);
   __syncthreads();
-  long long all, one = 0;
+  long long all;
   const int mine = s_hist[tid];
   const long long before = block_scan(mine, s_warp, &all) - mine;
   s_hist[tid] = (int)before;  // cursors
-  if (tid == 512) s_sum[0] = before;
+  if (tid == 340) s_sum[0] = before;
+  if (tid == 680) s_sum[1] = before;
   __syncthreads();
-  one = s_sum[0];
+  const int one = (int)s_sum[0], two = (int)s_sum[1];  // items of the first list, of the first two
   if (tid == 0) {
-    p.hdr->status = (overflow ? kStatusPlanOverflow : 0) | (refused ? kPackedStatusRefused : 0);
-    p.hdr->n_items[0] = (int)one;
-    p.hdr->n_items[1] = (int)(all - one);
+    p.hdr->dec.status = (overflow ? kStatusPlanOverflow : 0) | (refused ? kPackedStatusRefused : 0);
+    p.hdr->dec.n_items = (int)(all - two) * p.Hkv;
+    p.hdr->dec.next_item = p.dec_grid;
+    p.hdr->n_items[0] = one;
+    p.hdr->n_items[1] = two - one;
     p.hdr->next_item[0] = p.hdr->next_item[1] = p.grid;
     p.hdr->n_merge = n_merge;
     p.hdr->merge_rows = (int)(merges >> 32);
@@ -218,21 +245,37 @@ __global__ void __launch_bounds__(1024) packed_plan_kernel(const PackedParams p,
     if (i < NT) {
       t = tile_of(i);
       cut(t, nch, len);
-      if (nch > 1) rows = (long long)nch * p.Hkv * t.cols;
+      rows = needs(t, nch);
     }
-    const long long slot = parts + block_scan(rows, s_warp, &total) - rows;
+    const long long from = parts + block_scan(rows, s_warp, &total) - rows;
     parts += total;
+    const int chunk = (int)(from >> 32);
+    const long long slot = t.list == 2 ? (long long)chunk * p.Hkv * p.G : p.dec_rows + (from & 0xffffffff);
     if (i >= NT) continue;
-    if (rows && slot + rows > p.max_part_rows) nch = 1, rows = 0, len = max(1, t.stages);
+    if (t.list != 2 && slot + rows > p.max_part_rows) nch = 1, len = max(1, t.stages);
     const int seen = t.stages ? min(t.s.T, t.s.T - t.s.n + 1 + (t.c0 + t.cols - 1) / p.G) : 0;
     for (int c = 0; c < nch; ++c) {
       const int st = nch > 1 ? min(len, t.stages - c * len) : t.stages;
       const int at = atomicAdd(&s_hist[bucket(t.list, st)], 1);
-      if (!checked(chk_index(at, p.max_items), &p.hdr->status, kStatusBadIndex) || at >= p.max_items) continue;
+      if (t.list == 2) {
+        if (!checked(chk_index(at - two, p.max_dec_chunks), &p.hdr->dec.status, kStatusBadIndex) || at - two >= p.max_dec_chunks) continue;
+        const int t0 = c * len * kTc2StageTok;
+        for (int h = 0; h < p.Hkv; ++h)
+          p.dec_items[(size_t)(at - two) * p.Hkv + h] = make_int4(t.b, (chunk + c) * p.Hkv + h, t0, min(seen, t0 + st * kTc2StageTok));
+        continue;
+      }
+      if (!checked(chk_index(at, p.max_items), &p.hdr->dec.status, kStatusBadIndex) || at >= p.max_items) continue;
       const int t0 = c * len * kTc2StageTok;
       p.items[2 * at] = make_int4(t.b, t.c0, t0, min(seen, t0 + st * kTc2StageTok));
       p.items[2 * at + 1] = make_int4(nch > 1 ? (int)slot + c * p.Hkv * t.cols : -1, t.s.r0, t.s.n, t.s.T);
     }
+  }
+  for (int b = tid >> 5; b < p.B; b += 32) {  // query tokens of a sequence without a context
+    const PackedSeq q = packed_seq(p, b);
+    if (q.T > 0) continue;
+    const int vecs = p.Hq * p.D / 8;
+    for (long long i = tid & 31; i < (long long)q.n * vecs; i += 32)
+      *reinterpret_cast<uint4*>(p.out + (q.r0 + i / vecs) * p.out_stride + 8 * (i % vecs)) = make_uint4(0u, 0u, 0u, 0u);
   }
 }
 
@@ -255,7 +298,7 @@ __global__ void __launch_bounds__(256) packed_merge_kernel(const PackedParams p)
     const int4 m = p.merge[lo];
     const int per = p.merge_first[lo + 1] - p.merge_first[lo];  // rows of a chunk: kv heads x columns
     const int cols = per / p.Hkv, idx = r - p.merge_first[lo], h = idx / cols, col = m.y + idx - h * cols;
-    if (!checked(chk_index((long long)m.w + (long long)m.z * per - 1, p.max_part_rows), &p.hdr->status, kStatusBadIndex)) continue;
+    if (!checked(chk_index((long long)m.w + (long long)m.z * per - 1, p.max_part_rows), &p.hdr->dec.status, kStatusBadIndex)) continue;
     const float* lses = p.part_lse + m.w + idx;
     const float* src = p.part_o + (int64_t)(m.w + idx) * D + lane * V;
     float M = -INFINITY, den = 0.f, acc[V];
@@ -401,7 +444,7 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
     long long unit = blockIdx.x;
     auto table_entry = [&](const int32_t* e) {
       const int v = *e;
-      return checked(chk_table_entry(v, p.NB), &p.hdr->status, kStatusBadTableEntry) ? v : p.NB;
+      return checked(chk_table_entry(v, p.NB), &p.hdr->dec.status, kStatusBadTableEntry) ? v : p.NB;
     };
     // waits until K slot, V slot (and with it the V descriptor) of stage `it` are free; false when a wait gave up
     auto acquire = [&]() {
@@ -416,7 +459,7 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
       const int item = (int)(unit / p.Hkv), h = (int)(unit - (long long)item * p.Hkv);
       const int4 d = items[2 * item], d2 = items[2 * item + 1];  // {b, first column, t0, t1}, {partial row or -1, first row of q, n, T}
       if (!checked(chk_item(d.x, 0, d.z, d.w, p.B, 1, cap_tokens) && chk_span(d2.y, d2.z, 0, p.num_rows) &&
-                       (d2.x < 0 || chk_index(d2.x, p.max_part_rows)), &p.hdr->status, kStatusBadItem)) {
+                       (d2.x < 0 || chk_index(d2.x, p.max_part_rows)), &p.hdr->dec.status, kStatusBadItem)) {
         *s_abort = 1;
         violated = true;
         ok = false;
@@ -471,7 +514,7 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
           const uint32_t k0 = KV8 ? s_rk + (uint32_t)ks * kTc2RawSlotBytes : s_k + (uint32_t)ks * kSlotBytes;
           const uint32_t dk = k0 + (uint32_t)lane * box_rows_bytes;
           span_ok = checked(chk_span(dk, box_rows_bytes, k0, (long long)k0 + kTc2HalfBytes) && chk_span(lane, 1, 0, 8),
-                            &p.hdr->status, kStatusBadSmem);
+                            &p.hdr->dec.status, kStatusBadSmem);
           if (span_ok) {
             tma_load_4d(dk, &tm_k, kfull, 0, c_tok, h, blk_cur);  // (KV8: the row's 128 codes; else its first 64 dims)
             if (!KV8 && NH > 1) tma_load_4d(dk + kTc2HalfBytes, &tm_k, kfull, 64, c_tok, h, blk_cur);
@@ -509,7 +552,7 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
       }
     }
     if (!ok) {  // stop path: record it, then wait (bounded) until every K copy already issued has landed
-      if (lane == 0 && !violated) atomicOr(&p.hdr->status, kStatusWaitTimeout);
+      if (lane == 0 && !violated) atomicOr(&p.hdr->dec.status, kStatusWaitTimeout);
       int dummy_abort = 0;
       for (int k = 0; k < (it < NK ? it : NK); ++k) {
         const int j = it - 1 - k;
@@ -546,7 +589,7 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
       }
     }
     if (!ok) {
-      if (lane == 0) atomicOr(&p.hdr->status, kStatusWaitTimeout);
+      if (lane == 0) atomicOr(&p.hdr->dec.status, kStatusWaitTimeout);
       int dummy_abort = 0;
       for (int k = 0; k < (it < NV ? it : NV); ++k) {
         const int j = it - 1 - k;
@@ -661,7 +704,7 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
         }
       }
     }
-    if (!ok && lane == 0) atomicOr(&p.hdr->status, kStatusWaitTimeout);
+    if (!ok && lane == 0) atomicOr(&p.hdr->dec.status, kStatusWaitTimeout);
     if (!ok && issued) {  // the tensor memory must not be released under MMAs in flight
       if (lane == 0) umma_commit(s_drain + 8 * t);
       __syncwarp();
@@ -781,7 +824,7 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
       p_ntok = ntok;
       p_n = n;
     }
-    if (!ok && lane == 0) atomicOr(&p.hdr->status, kStatusWaitTimeout);
+    if (!ok && lane == 0) atomicOr(&p.hdr->dec.status, kStatusWaitTimeout);
     if (!ok && issued) {  // the tensor memory must not be released under MMAs in flight
       if (lane == 0) umma_commit(s_drain + 8 * t);
       __syncwarp();
@@ -1082,7 +1125,7 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
           const int col = col0 + 32 * rr;
           const int qi = col / p.G, head = col - qi * p.G;
           write_row[rr] = col < columns &&
-                          checked(part < 0 || chk_index(part + col - c0, p.max_part_rows), &p.hdr->status, kStatusBadIndex);
+                          checked(part < 0 || chk_index(part + col - c0, p.max_part_rows), &p.hdr->dec.status, kStatusBadIndex);
           orow[rr] = p.out + (int64_t)(meta.y + qi) * p.out_stride + (int64_t)(h * p.G + head) * D;
           prow[rr] = p.part_o + (int64_t)(part + col - c0) * D;
           if (write_row[rr] && tq == 0 && part >= 0) p.part_lse[part + col - c0] = lse[rr];
@@ -1115,7 +1158,7 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
         tc_fence_before_sync();  // the next unit's first P.V overwrites O: ordered behind these reads by p-ready
       }
     }
-    if (!ok && lane == 0) atomicOr(&p.hdr->status, kStatusWaitTimeout);
+    if (!ok && lane == 0) atomicOr(&p.hdr->dec.status, kStatusWaitTimeout);
   }
   // ---- common exit: release the tensor memory once every warp is done with it
   tc_fence_before_sync();
