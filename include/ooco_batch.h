@@ -58,7 +58,7 @@ extern "C" {
  *   status         device, int32 [1], may be NULL: OOCO_STATUS_REFUSED, OOCO_STATUS_BAD_BLOCK (an id outside the
  *                  pool: it is handed on, but not counted and not copied)
  * Nothing written may share memory with an input or another output, but for the in-place ones
- * (OOCO_E_SHAPE).  One launch.
+ * (OOCO_E_SHAPE).  One launch for few table entries, two for many.
  *
  * ooco_release_pages: row rows[c] keeps its first keep_lens[c] tokens (NULL: none) and gives back the blocks
  * behind the last one that these need: a block with other holders loses one of them, a block without becomes
@@ -67,7 +67,7 @@ extern "C" {
  * ending at free_head; ids for which the list has no room are dropped with OOCO_STATUS_REFUSED.  context_lens
  * becomes the smaller of itself and keep_lens, blocks_held the blocks kept; table entries stay.  A row outside
  * [0, batch) or named twice is refused; a row's blocks_held is clamped to [0, max_blocks_per_seq].
- *   free_ids is written in [new free_head, free_head); the rest as above.
+ *   free_ids is written in [new free_head, free_head); the rest as above.  One launch, or five for many table entries.
  */
 #define OOCO_MAX_PAGE_ROWS (1 << 18)
 size_t ooco_pages_workspace_bytes(const ooco_shape_t* shape, int32_t num_rows);

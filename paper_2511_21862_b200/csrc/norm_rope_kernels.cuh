@@ -12,11 +12,13 @@ struct HeadNormParams {
 // The work is cut as in rope_append_kernel: a unit is 16 dims of one head of one token, two 16-byte pieces (with the halves
 // layout the two members of eight pairs).  Consecutive lanes hold the units of a head, so a head's sum of squares is the sum
 // over 16 values of a thread and a butterfly over its D / 16 lanes, in 32 bits; and since a thread keeps its place in the head
-// from unit to unit, it holds the weights of its 16 dims in registers.  Bound by HBM: q, k and v are read and written once.
+// from unit to unit, it finds the weights of its 16 dims at a place of its own.  Bound by HBM: q, k and v are read and written once.
 template <int D, bool KV8>
-__global__ void __launch_bounds__(kRopeThreads) norm_rope_append_kernel(const RopeParams p, const HeadNormParams hn,
+__global__ void __launch_bounds__(kRopeThreads, 4) norm_rope_append_kernel(const RopeParams p, const HeadNormParams hn,
                                                                         const int interleaved) {
   constexpr int UPH = D / 16;  // units (lanes) per head
+  __shared__ float4 s_w4[2][D / 4];  // weights with their offset, of q and of k
+  float(*s_w)[D] = reinterpret_cast<float(*)[D]>(s_w4);
   __shared__ float2 s_cs[kRopeMaxTile][D / 2];
   __shared__ int s_pos[kRopeMaxTile], s_slot[kRopeMaxTile];
   grid_dep_wait();
@@ -26,14 +28,9 @@ __global__ void __launch_bounds__(kRopeThreads) norm_rope_append_kernel(const Ro
   const bool turned = c < rot_units, turned_halves = !interleaved && turned;
   const int d_lo = turned_halves ? 8 * c : 16 * c, d_hi = turned_halves ? p.half + 8 * c : 16 * c + 8;
   const uint4 none = make_uint4(0u, 0u, 0u, 0u);
-  uint4 qw[2] = {none, none}, kw[2] = {none, none};
-  if (hn.q_weight) {
-    qw[0] = *reinterpret_cast<const uint4*>(hn.q_weight + d_lo);
-    qw[1] = *reinterpret_cast<const uint4*>(hn.q_weight + d_hi);
-  }
-  if (hn.k_weight) {
-    kw[0] = *reinterpret_cast<const uint4*>(hn.k_weight + d_lo);
-    kw[1] = *reinterpret_cast<const uint4*>(hn.k_weight + d_hi);
+  for (int i = threadIdx.x; i < 2 * D; i += kRopeThreads) {
+    const uint16_t* w = i < D ? hn.q_weight : hn.k_weight;
+    s_w[i / D][i % D] = w ? __uint_as_float((uint32_t)w[i % D] << 16) + hn.offset : 1.f;
   }
   for (int t0 = blockIdx.x * p.tile; t0 < p.T; t0 += gridDim.x * p.tile) {
     const int nt = min(p.tile, p.T - t0);
@@ -86,17 +83,12 @@ __global__ void __launch_bounds__(kRopeThreads) norm_rope_append_kernel(const Ro
         if (tk[i] < 0) continue;
         if (!is_v) {
           const float r = __frsqrt_rn(ss * (1.f / D) + hn.eps);
-          if (is_q ? hn.q_weight != nullptr : hn.k_weight != nullptr) {
-            float w[8];
-            unpack8(is_q ? qw[0] : kw[0], w);
+          const float4* w = reinterpret_cast<const float4*>(s_w[is_q ? 0 : 1]);
 #pragma unroll
-            for (int m = 0; m < 8; ++m) x[m] = x[m] * r * (w[m] + hn.offset);
-            unpack8(is_q ? qw[1] : kw[1], w);
-#pragma unroll
-            for (int m = 0; m < 8; ++m) y[m] = y[m] * r * (w[m] + hn.offset);
-          } else {
-#pragma unroll
-            for (int m = 0; m < 8; ++m) x[m] *= r, y[m] *= r;
+          for (int m = 0; m < 2; ++m) {
+            const float4 u = w[d_lo / 4 + m], z = w[d_hi / 4 + m];
+            x[4 * m] *= r * u.x, x[4 * m + 1] *= r * u.y, x[4 * m + 2] *= r * u.z, x[4 * m + 3] *= r * u.w;
+            y[4 * m] *= r * z.x, y[4 * m + 1] *= r * z.y, y[4 * m + 2] *= r * z.z, y[4 * m + 3] *= r * z.w;
           }
           if (turned) {
             const float2* cs = &s_cs[tk[i]][8 * c];

@@ -53,8 +53,9 @@ static bool disjoint(const Range* in, int n_in, const Range* out, int n_out) {
 static PagesParams page_params(const ooco_shape_t* s, int32_t n, int32_t num_free, void* workspace) {
   PagesParams p;
   memset(&p, 0, sizeof p);
-  p.ws_a = (int32_t*)workspace;
-  p.ws_b = (int32_t*)((uint8_t*)workspace + up256((size_t)n * 4));
+  p.ws_off = (int32_t*)workspace;
+  p.ws_from = (int32_t*)((uint8_t*)workspace + up256(((size_t)n + 1) * 4));
+  p.ws_total = (int32_t*)((uint8_t*)workspace + 2 * up256(((size_t)n + 1) * 4));
   p.n = n;
   p.B = s->batch;
   p.NB = s->num_blocks;
@@ -64,22 +65,29 @@ static PagesParams page_params(const ooco_shape_t* s, int32_t n, int32_t num_fre
   return p;
 }
 
-// CTAs of the call's cluster: one for a few table entries and a small pool, else as many as the entries keep busy.
-static int page_cluster(const PagesParams& p) {
-  const int64_t work = (int64_t)p.n * p.MB + p.NB / 2;
-  int c = 1;
-  while (c < kPagesMaxCluster && work > (int64_t)c * 4096) c *= 2;
-  return c;
-}
-
+// One launch of a cluster for few table entries and a small pool (one CTA up to 4096 entries, four a thread: a barrier of a cluster
+// costs about as much as they do), a launch per phase on all SMs for more than 65536 (16 CTAs of 4 a thread: from there on the
+// cluster's phases take longer than launches).
 template <typename K>
-static int launch_pages(K kern, std::atomic<int>* done, int maps, const PagesParams& p, cudaStream_t st, const char* where) {
-  const size_t most = 3 * OOCO_MAX_PAGE_ROWS / 8, smem = (size_t)maps * ((p.B + 31) / 32) * 4;
-  const int rc = configure((const void*)kern, done, (int)most);
+static int launch_pages(K kern, std::atomic<int>* done, int maps, int phases, PagesParams& p, cudaStream_t st, const char* where) {
+  const size_t most = 3 * OOCO_MAX_PAGE_ROWS / 8, list = p.n <= kPagesListInSmem ? ((size_t)3 * p.n + 1) * 4 : 0;
+  const size_t map = (size_t)maps * ((p.B + 31) / 32) * 4, smem = map > list ? map : list;
+  int rc = configure((const void*)kern, done, (int)most), dev = 0;
   if (rc) return rc;
-  const int cluster = page_cluster(p);
-  return finish(launch_clustered(kern, dim3(cluster), dim3(kPagesThreads), smem, st, pdl_enabled(), (unsigned)cluster, p, cluster),
-                where);
+  const int64_t work = (int64_t)p.n * p.MB + p.NB / 4;
+  if (work <= 65536) {
+    int cluster = 1;
+    while (cluster < kPagesMaxCluster && work > (int64_t)cluster * 4096) cluster *= 2;
+    p.phase = -1;
+    return finish(launch_clustered(kern, dim3(cluster), dim3(kPagesThreads), smem, st, pdl_enabled(), (unsigned)cluster, p), where);
+  }
+  if ((rc = current_device(&dev))) return rc;
+  int grid = device_info(dev).sm_count;
+  if (grid <= 0) return fail_cuda("cudaDeviceGetAttribute", -1);
+  if (grid > kPagesThreads) grid = kPagesThreads;
+  for (p.phase = 1; p.phase <= phases; ++p.phase)
+    if ((rc = finish(launch_ex(kern, dim3(grid), dim3(kPagesThreads), smem, st, pdl_enabled(), p), where))) return rc;
+  return OOCO_OK;
 }
 
 }  // namespace ooco
@@ -90,7 +98,7 @@ extern "C" {
 
 size_t ooco_pages_workspace_bytes(const ooco_shape_t* s, int32_t num_rows) {
   if (validate_shape(s) || num_rows < 0) return 0;
-  return 256 + 2 * up256((size_t)num_rows * 4);
+  return 2 * up256(((size_t)num_rows + 1) * 4) + kPagesThreads * 4;
 }
 
 int ooco_fork_pages(const ooco_shape_t* s, int32_t n, const int32_t* parents, const int32_t* children,
@@ -135,7 +143,7 @@ int ooco_fork_pages(const ooco_shape_t* s, int32_t n, const int32_t* parents, co
   p.granted = granted;
   p.status = status;
   static std::atomic<int> done[64];
-  return launch_pages(fork_pages_kernel, done, 3, p, (cudaStream_t)cuda_stream, "launch of the forking kernel");
+  return launch_pages(fork_pages_kernel, done, 3, 2, p, (cudaStream_t)cuda_stream, "launch of the forking kernel");
 }
 
 int ooco_release_pages(const ooco_shape_t* s, int32_t n, const int32_t* rows_, const int32_t* keep_lens, int32_t* context_lens,
@@ -172,7 +180,7 @@ int ooco_release_pages(const ooco_shape_t* s, int32_t n, const int32_t* rows_, c
   p.shares_out = (int32_t*)out[3].p;
   p.status = status;
   static std::atomic<int> done[64];
-  return launch_pages(release_pages_kernel, done, 2, p, (cudaStream_t)cuda_stream, "launch of the releasing kernel");
+  return launch_pages(release_pages_kernel, done, 2, 5, p, (cudaStream_t)cuda_stream, "launch of the releasing kernel");
 }
 
 int ooco_norm_rope_kv_append(const ooco_shape_t* shape, const ooco_rope_t* rope, const ooco_head_norm_t* norm,
