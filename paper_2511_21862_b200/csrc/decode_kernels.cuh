@@ -102,6 +102,7 @@ struct DecodeParams {
   // Packed rows (one query token per sequence, that of sequence b in row first_row[b], rows a stride of elements apart).
   const int32_t* first_row;
   int64_t q_stride, out_stride;
+  int32_t early;  // the kernel in front of this one has waited for the plan: this one waits for that one's end, at its own
 };
 
 // Nodes of sequence b's tree.
@@ -894,8 +895,8 @@ __device__ __forceinline__ uint32_t decode_main_body(const CUtensorMap& tm_k, co
     tc_fence_after_sync();
     tmem = *reinterpret_cast<volatile uint32_t*>(gen + (s_tslot - base));
   }
-  grid_dep_wait();    // the plan (and a fused append) must have completed
-  grid_dep_launch();  // the merge kernel may queue up behind this grid
+  if (!kPacked || !p.early) grid_dep_wait();  // the plan (and a fused append) must have completed
+  grid_dep_launch();                          // the merge kernel may queue up behind this grid
   const int n_items = p.hdr->n_items;
 
   if (KVTC && warp == NCW + 1) {
@@ -1500,6 +1501,7 @@ decode_main_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
       tmem_dealloc(tmem, L::kTcSBuffers * L::kTcSColumns);
     }
   }
+  if (kPacked && p.early) grid_dep_wait();
 }
 
 // ------------------------------------------------------------------------------------ merge

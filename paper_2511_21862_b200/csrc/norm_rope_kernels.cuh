@@ -23,7 +23,8 @@ __global__ void __launch_bounds__(kRopeThreads, 4) norm_rope_append_kernel(const
   __shared__ int s_pos[kRopeMaxTile], s_slot[kRopeMaxTile];
   grid_dep_wait();
   grid_dep_launch();
-  const int heads = p.Hq + 2 * p.Hkv, per_tok = heads * UPH, rot_units = p.half / 8;
+  constexpr int GROUPS = kRopeThreads / UPH;  // heads at a time
+  const int heads = p.Hq + 2 * p.Hkv, rot_units = p.half / 8;
   const int c = threadIdx.x % UPH;  // (the number of threads is a multiple of UPH)
   const bool turned = c < rot_units, turned_halves = !interleaved && turned;
   const int d_lo = turned_halves ? 8 * c : 16 * c, d_hi = turned_halves ? p.half + 8 * c : 16 * c + 8;
@@ -47,21 +48,24 @@ __global__ void __launch_bounds__(kRopeThreads, 4) norm_rope_append_kernel(const
       s_slot[threadIdx.x] = p.slots[t0 + threadIdx.x];
     }
     __syncthreads();
-    const int n = nt * per_tok;
-    for (int base = 0; base < n; base += kRopeThreads * kRopeBatch) {  // (the same trips for every thread: warps stay whole)
+    // the heads of all tokens of the tile in a row, GROUPS at a time (the same trips for every thread: warps stay whole)
+    const int n = (nt * heads + GROUPS * kRopeBatch - 1) / (GROUPS * kRopeBatch);
+    int tok = 0, next = threadIdx.x / UPH;
+    for (int trip = 0; trip < n; ++trip) {
       uint4 a[kRopeBatch], b[kRopeBatch];
       int tk[kRopeBatch], head[kRopeBatch];
 #pragma unroll
       for (int i = 0; i < kRopeBatch; ++i) {
-        const int u = base + i * kRopeThreads + threadIdx.x;
+        while (next >= heads) {
+          next -= heads;
+          ++tok;
+        }
         a[i] = b[i] = none;
         tk[i] = -1;
-        head[i] = 0;
-        if (u >= n) continue;
-        const int tok = u / per_tok, e = u - tok * per_tok;
-        if (s_pos[tok] < 0) continue;  // padding
+        head[i] = next;
+        next += GROUPS;
+        if (tok >= nt || s_pos[tok] < 0) continue;  // (padding)
         tk[i] = tok;
-        head[i] = e / UPH;
         const size_t t = (size_t)(t0 + tok);
         const uint16_t* src = head[i] < p.Hq           ? p.q + t * p.q_stride + (size_t)head[i] * D
                               : head[i] < p.Hq + p.Hkv ? p.k + t * p.k_stride + (size_t)(head[i] - p.Hq) * D

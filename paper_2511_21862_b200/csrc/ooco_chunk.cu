@@ -15,8 +15,8 @@ namespace ooco {
 static_assert(kPackedStatusRefused == OOCO_STATUS_REFUSED, "status bit");
 
 struct PackedLayout {
-  size_t off_tiles, off_items, off_dec_first, off_dec_items, off_merge, off_merge_first, off_lse, off_o, total;
-  int max_tiles, max_items, max_merge, max_dec_chunks, dec_rows, max_part_rows;
+  size_t off_first, off_tiles, off_before[2], off_start[2], off_order[2], off_dec_first, off_dec_items, off_merge, off_lse, off_o, total;
+  int max_tiles, max_merge, max_dec_chunks, max_part_rows, part_rows[2];
 };
 
 // CTAs an SM of the decode kernel, as the decode operators launch it.
@@ -24,39 +24,43 @@ static int decode_ctas_per_sm(int head_dim, bool kv8, int64_t G) { return kv8 ? 
 // Which calls have a decode list: bf16 caches up to 8 heads a group (one MMA tile of columns), 8-bit ones all.
 static bool has_decode(bool kv8, int64_t G) { return kv8 || G <= 8; }
 
-// Bounds that hold for any lengths.  A tile of s stages is cut into at most 2 s / L chunks, where L >= S / (CTAs x items per
-// CTA), S the list's stages over all kv heads: 2 CTAs x items per CTA chunks (x heads) in all, of at most a tile's columns.
+// Bounds that hold for any lengths.  A decode of s stages is cut into at most s / L + 1 items, where L >= S / (CTAs x items per CTA),
+// S the list's stages over all kv heads: (CTAs x items per CTA) / heads items beside one a sequence.  Of a tile list every CTA has at
+// most two units whose rows are merged.
 static PackedLayout packed_layout(const ooco_shape_t* s, int64_t num_rows, int64_t max_chunk) {
   const int64_t G = s->num_q_heads / s->num_kv_heads, cols = G * max_chunk;
-  const int64_t cuts[2] = {2ll * kPackedGridCap * packed_items_per_cta(0), 2ll * kPackedGridCap * packed_items_per_cta(1)};
-  const int64_t dec_cuts = 4ll * kPackedGridCap * packed_items_per_cta(2);  // (CTAs x items per CTA / kv heads, at most)
   const int64_t longest = ((int64_t)s->max_blocks_per_seq * s->block_size + kPackedMinStages * kTc2StageTok - 1) / (kPackedMinStages * kTc2StageTok);
   PackedLayout w;
   const int64_t tiles = s->batch + num_rows * G / kTcRows + 1;
-  int64_t rows = max_chunk > 1 || G > 8 ? cuts[0] * (cols < kTcRows ? cols : kTcRows) : 0;
-  if (cols > kTcRows) rows += cuts[1] * kTc2Rows;
-  const int64_t most = num_rows * s->num_q_heads * (longest + 1);  // every row in as many chunks as its context allows
-  if (rows > most) rows = most;
-  auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
-  w.max_tiles = (int)(tiles > INT32_MAX / 4 ? INT32_MAX / 4 : tiles);
-  w.max_items = w.max_tiles + (int)(cuts[0] + cuts[1]);
-  w.max_merge = (int)(tiles < cuts[0] + cuts[1] ? tiles : cuts[0] + cuts[1]);
   const int64_t decodes = s->batch < num_rows ? s->batch : num_rows;
-  int64_t chunks = decodes + dec_cuts / s->num_kv_heads + 1;
+  int64_t chunks = decodes + 4ll * kPackedGridCap * kPackedDecodeItems / s->num_kv_heads + 1;
   if (chunks > decodes * (longest + 1)) chunks = decodes * (longest + 1);
+  w.max_tiles = (int)(tiles > INT32_MAX / 4 ? INT32_MAX / 4 : tiles);
+  w.max_merge = (int)decodes;
   w.max_dec_chunks = (int)chunks;
-  w.dec_rows = (int)(chunks * s->num_q_heads);
-  w.max_part_rows = (int)(w.dec_rows + rows);
-  w.max_merge += (int)decodes;
-  w.off_tiles = sizeof(PackedHeader);
-  w.off_items = w.off_tiles + up(((size_t)s->batch + 1) * 4);
-  w.off_dec_first = w.off_items + up((size_t)w.max_items * 32);
-  w.off_dec_items = w.off_dec_first + up(((size_t)s->batch + 1) * 4);
-  w.off_merge = w.off_dec_items + up((size_t)w.max_dec_chunks * s->num_kv_heads * 16);
-  w.off_merge_first = w.off_merge + up((size_t)w.max_merge * 16);
-  w.off_lse = w.off_merge_first + up(((size_t)w.max_merge + 1) * 4);
-  w.off_o = w.off_lse + up((size_t)w.max_part_rows * 4);
-  w.total = w.off_o + up((size_t)w.max_part_rows * s->head_dim * 4);
+  w.part_rows[0] = (int)(chunks * s->num_q_heads);
+  w.part_rows[1] = w.part_rows[0] + 2 * kPackedGridCap * kTcRows;
+  w.max_part_rows = w.part_rows[1] + (cols > kTcRows ? 2 * kPackedGridCap * kTc2Rows : 0);
+  auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
+  size_t at = sizeof(PackedHeader);
+  auto put = [&](size_t bytes) {
+    const size_t here = at;
+    at += up(bytes);
+    return here;
+  };
+  w.off_first = put(((size_t)s->batch + 1) * 4);
+  w.off_tiles = put((size_t)w.max_tiles * sizeof(PackedTile));
+  for (int k = 0; k < 2; ++k) {
+    w.off_before[k] = put(((size_t)w.max_tiles + 1) * 8);
+    w.off_start[k] = put((size_t)kPackedGridCap * 16);
+    w.off_order[k] = put((size_t)w.max_tiles * 4);
+  }
+  w.off_dec_first = put(((size_t)s->batch + 1) * 4);
+  w.off_dec_items = put((size_t)w.max_dec_chunks * s->num_kv_heads * 16);
+  w.off_merge = put((size_t)w.max_merge * 16);
+  w.off_lse = put((size_t)w.max_part_rows * 4);
+  w.off_o = put((size_t)w.max_part_rows * s->head_dim * 4);
+  w.total = at;
   return w;
 }
 
@@ -145,10 +149,15 @@ static int chunk_core(const ooco_shape_t* s, int32_t num_rows, int32_t max_chunk
   p.first_row = first_row;
   p.chunk_lens = chunk_lens;
   p.hdr = (PackedHeader*)ws;
-  p.tile_first = (int32_t*)(ws + w.off_tiles);
-  p.items = (int4*)(ws + w.off_items);
+  p.tile_first = (int32_t*)(ws + w.off_first);
+  p.tiles = (PackedTile*)(ws + w.off_tiles);
+  for (int k = 0; k < 2; ++k) {
+    p.before[k] = (int64_t*)(ws + w.off_before[k]);
+    p.start[k] = (int4*)(ws + w.off_start[k]);
+    p.order[k] = (int32_t*)(ws + w.off_order[k]);
+    p.part_rows[k] = w.part_rows[k];
+  }
   p.merge = (int4*)(ws + w.off_merge);
-  p.merge_first = (int32_t*)(ws + w.off_merge_first);
   p.part_lse = (float*)(ws + w.off_lse);
   p.part_o = (float*)(ws + w.off_o);
   p.q_stride = q_stride;
@@ -168,14 +177,14 @@ static int chunk_core(const ooco_shape_t* s, int32_t num_rows, int32_t max_chunk
   p.dec_first = (int32_t*)(ws + w.off_dec_first);
   p.dec_items = (int4*)(ws + w.off_dec_items);
   p.max_dec_chunks = w.max_dec_chunks;
-  p.dec_rows = w.dec_rows;
   p.decode = has_decode(kv8, G);
   p.dec_grid = di.sm_count * decode_ctas_per_sm(s->head_dim, kv8, G);
   if (p.dec_grid > 4 * kPackedGridCap) p.dec_grid = 4 * kPackedGridCap;
   p.max_tiles = w.max_tiles;
-  p.max_items = w.max_items;
   p.max_merge = w.max_merge;
   p.max_part_rows = w.max_part_rows;
+  p.early = p.decode || p.two_tiles;
+  p.dec_stage_bytes = 2.f * kTc2StageTok * s->head_dim * (kv8 ? 1 : 2);
   p.tile_rows = s->block_size < kTc2StageTok ? s->block_size : kTc2StageTok;
   p.scale_log2e = scale * 1.4426950408889634f * (kv8 ? k_scale * kE4m3WidenFactor : 1.f);
   p.v_scale = kv8 ? v_scale * kE4m3WidenFactor : 1.f;
@@ -217,6 +226,7 @@ static int chunk_core(const ooco_shape_t* s, int32_t num_rows, int32_t max_chunk
     d.first_row = first_row;
     d.q_stride = q_stride;
     d.out_stride = out_stride;
+    d.early = p.two_tiles;
     // (scores come from the codes' own values here: only V carries the widening factor)
     d.scale_log2e = scale * 1.4426950408889634f * k_scale;
     d.v_scale = p.v_scale;
@@ -249,16 +259,18 @@ static int chunk_core(const ooco_shape_t* s, int32_t num_rows, int32_t max_chunk
                               : launch_packed<64, false, true>(tk, tv, p, di, dev, st, dry);
   };
   if ((rc = attention(true))) return rc;  // everything that can refuse the call, before the first launch
-  const size_t first_bytes = ((size_t)p.B + 1) * 4;
-  const int first_in_smem = first_bytes <= 32 * 1024;
-  cudaError_t e = launch_ex(packed_plan_kernel, dim3(1), dim3(1024), first_in_smem ? first_bytes : 0, st, pdl_enabled(), p, first_in_smem);
+  const size_t seq_bytes = (size_t)p.B * 20 + 4;
+  const int in_smem = seq_bytes <= 26 * 1024;  // (with the static part under 48 KiB)
+  cudaError_t e = launch_ex(packed_plan_kernel, dim3(1), dim3(1024), in_smem ? seq_bytes : 0, st, pdl_enabled(), p, in_smem);
   if (e == cudaSuccess) e = cudaGetLastError();
   if (e != cudaSuccess) return fail_cuda("launch of the packed plan kernel", (long)e);
   if ((rc = attention(false))) return rc;
-  int64_t blocks = ((int64_t)num_rows * p.Hq + 7) / 8;
-  if (blocks > 8ll * di.sm_count) blocks = 8ll * di.sm_count;
-  e = launch_ex(s->head_dim == 128 ? packed_merge_kernel<128> : packed_merge_kernel<64>, dim3((unsigned)blocks), dim3(256), 0, st,
-                pdl_enabled(), p);
+  // merging: the cuts of the tile lists that were launched, and the rows of the decode list
+  const int lists = (tiles ? 1 : 0) | (p.two_tiles ? 2 : 0), cut_ctas = (p.grid - 1) * kMergeSplit * (lists == 3 ? 2 : (lists ? 1 : 0));
+  int64_t blocks = p.decode ? ((int64_t)(w.max_merge) * p.Hq + 7) / 8 : 0;
+  if (blocks > 4ll * di.sm_count) blocks = 4ll * di.sm_count;
+  e = launch_ex(s->head_dim == 128 ? packed_merge_kernel<128> : packed_merge_kernel<64>, dim3((unsigned)(cut_ctas + blocks)), dim3(256),
+                0, st, pdl_enabled(), p, lists, cut_ctas);
   if (e == cudaSuccess) e = cudaGetLastError();
   return e == cudaSuccess ? OOCO_OK : fail_cuda("launch of the packed merge kernel", (long)e);
 }

@@ -1,16 +1,23 @@
 // Attention of the new tokens of all sequences over the paged cache, rows packed: plan -> tiles on tcgen05 -> merge.
 //
-// The G n_b score columns (query x head of the group) of a (sequence, kv head) pair go, by their number, to one of three lists of
-// items, each with a kernel of its own, because what bounds them differs:
+// The G n_b score columns (query x head of the group) of a (sequence, kv head) pair go, by their number, to one of three lists,
+// each with a kernel of its own, because what bounds them differs:
 //   decode_main_kernel               one query token (a decode): as the decode operators, HBM-bound
 //   packed_tc_kernel<.., one tile>   else at most 128 columns: the cache is read once for few columns, HBM-bound.  The scores of a
 //                                    stage run while the softmax threads still work on the stage before.
-//   packed_tc_kernel<.., two tiles>  a piece of a prompt, units of 256 columns: two 128-row tiles share every K / V slot and take
+//   packed_tc_kernel<.., two tiles>  a piece of a prompt, tiles of 256 columns: two 128-row halves share every K / V slot and take
 //                                    turns on the tensor pipe, tensor-bound
+// How the CTAs of a tile kernel share the (tile, kv head) pairs of their list is the plan's choice.  Many short pairs: the CTAs
+// pull whole pairs, the longest first.  Few or long ones (the longest is more than a quarter of a CTA's share): all their stages
+// (128 tokens) stand in a row, which is cut into as many equal pieces as there are CTAs; a pair that a cut goes through becomes
+// two or more units, whose rows are merged, at most two of them per CTA.  Measured: 4 pieces of prompts beside 60 decodes, 240
+// pairs of up to 64 stages: pieces 154 us, whole or halved pairs 193 and 175 (a CTA gets one or two of them); 5 prompts, 4500
+// pairs of up to 125: whole pairs 2.7 ms, pieces 3.9 (neighbouring pairs, which read the same K and V, run at the same time
+// only when they are pulled in turn: else they come from HBM again).
 // The CTA is that of chunk_tc2_kernel (chunk_tc2_kernels.cuh), which has one number of query tokens for all sequences; there
-// also stands why its MMAs, slots and warps are as they are.  What differs: a unit carries its sequence's rows, columns and
-// partial rows with it (an item is 32 bytes, a stage's meta words are three), so that sequences of any lengths share a launch;
-// head_dim 64 has half the slot, twice the slots and half the MMAs; an 8-bit cache runs every column on the one-tile kernel.
+// also stands why its MMAs, slots and warps are as they are.  What differs: a stage's meta words say all about its unit (rows,
+// columns, partial rows), so that sequences of any lengths share a launch; head_dim 64 has half the slot, twice the slots and half
+// the MMAs; an 8-bit cache runs every column on the one-tile kernel.
 #pragma once
 #include <cstddef>
 
@@ -21,9 +28,10 @@ namespace ooco {
 
 constexpr int kPackedEnd = 1 << 18;          // flag of a stage's meta words: the end marker
 constexpr int kPackedGridCap = 160;          // most CTAs of an attention kernel (bounds the workspace)
-// Lists: 0 = one tile, 1 = two tiles, 2 = decodes.  Items the plan aims at per CTA:
-__host__ __device__ constexpr int packed_items_per_cta(int list) { return list == 0 ? 4 : (list == 1 ? 2 : 6); }
-constexpr int kPackedMinStages = 2;          // shortest chunk: 256 tokens
+// Lists: 0 = one tile, 1 = two tiles, 2 = decodes.
+constexpr int kPackedDecodeItems = 6;        // items of the decode list that the plan aims at per CTA
+constexpr int kPackedMinStages = 2;          // shortest item, and shortest piece of a tile list: 256 tokens
+__host__ __device__ constexpr int packed_tile(int list) { return list == 1 ? kTc2Rows : kTcRows; }  // columns of a tile
 constexpr int kPackedStatusRefused = 128;
 
 template <int D>
@@ -37,34 +45,68 @@ struct PackedSmem {
 
 struct PackedHeader {  // first bytes of the workspace
   WsHeader dec;          // status word; work units (item x kv head) of the decode list and the next one that no CTA has taken
-  int32_t n_merge;       // tiles whose tokens are cut into several items
-  int32_t merge_rows;    // their rows (x kv head)
-  int32_t n_items[2];    // of the one-tile and of the two-tile list, which follow one another in `items`
-  int32_t next_item[2];  // next unit (item x kv head) that no CTA has taken
-  int32_t pad[58];
+  int32_t merge_rows;    // rows of the sequences of the decode list whose tokens are cut into several items
+  int64_t stages[2];     // of the tile lists, over all kv heads
+  int32_t pull[2];       // whether their CTAs pull whole pairs
+  int32_t pairs[2];      // (tile, kv head) pairs of the lists, and the next one to be pulled
+  int32_t next[2];
+  int32_t pieces[2];     // else: pieces of the list's row of stages
+  int32_t pad[50];
 };
 static_assert(sizeof(PackedHeader) == 512 && offsetof(PackedHeader, dec) == 0, "the status word leads the workspace");
+
+struct alignas(16) PackedTile {
+  int32_t b, c0, stages, first;  // sequence; first column; stages of 128 tokens that its last column sees (at least 1); first tile of
+  int32_t r0, n, T, end;         // the sequence; first row of q, query tokens, context; end of the sequence's tiles
+};
+static_assert(sizeof(PackedTile) == 32, "two vectors");
 
 struct PackedParams {
   const __nv_bfloat16* q;
   __nv_bfloat16* out;
   const int32_t *block_table, *context_lens, *first_row, *chunk_lens;
   PackedHeader* hdr;
-  int32_t* tile_first;   // [B + 1]
-  int4* items;           // [2 max_items] {b, first column, t0, t1}, {first partial row or -1, first row of q, n, T}
-  int4* merge;           // [max_merge] {first row of q, first column, chunks, first partial row}
-  int32_t* merge_first;  // [max_merge + 1] row number of each
-  float* part_o;         // [max_part_rows, D] normalised partial rows
+  int32_t* tile_first;   // [B + 1] first tile of each sequence
+  PackedTile* tiles;     // [max_tiles]
+  int64_t* before[2];    // [max_tiles + 1] stages of the list's tiles before each tile (one kv head)
+  int4* start[2];        // [grid] where each piece of the list begins: {tile, kv head, stage of the pair, -}
+  int32_t* order[2];     // [max_tiles] the list's tiles, longest first (where pairs are pulled)
+  int4* merge;           // [max_merge] decode list: {row of q, -, chunks, first partial row}
+  float* part_o;         // [max_part_rows, D] normalised partial rows: the decode list's, then two units of every CTA for each tile list
   float* part_lse;       // [max_part_rows] log2-domain log-sum-exp of each
   int64_t q_stride, out_stride;
-  int32_t B, Hq, Hkv, G, D, bs, MB, NB, num_rows, max_chunk;
   int4* dec_items;       // [max_dec_chunks, Hkv] items of decode_main_kernel
   int32_t* dec_first;    // [B + 1] their chunks, counted over the sequences
+  int32_t B, Hq, Hkv, G, D, bs, MB, NB, num_rows, max_chunk;
   int32_t two_tiles;     // 1: more than 128 columns go to the two-tile list
   int32_t decode;        // 1: sequences with one query token go to the decode list
-  int32_t grid, dec_grid, max_tiles, max_items, max_merge, max_part_rows, max_dec_chunks, dec_rows, tile_rows;
+  int32_t early;         // one-tile kernel: it may start before the kernel in front of it has ended (see packed_plan_kernel)
+  int32_t grid, dec_grid, max_tiles, max_merge, max_part_rows, max_dec_chunks, tile_rows;
+  int32_t part_rows[2];  // first partial row of each tile list
   float scale_log2e, v_scale;
+  float dec_stage_bytes; // K and V of 128 tokens of one kv head
 };
+
+// Columns of a tile, and tokens that the last of them sees.
+__device__ __forceinline__ int packed_cols(const PackedParams& p, const PackedTile& t, int list) {
+  return min(packed_tile(list), p.G * t.n - t.c0);
+}
+__device__ __forceinline__ int packed_seen(const PackedParams& p, const PackedTile& t, int list) {
+  return min(t.T, max(0, t.T - t.n + 1 + (t.c0 + packed_cols(p, t, list) - 1) / p.G));
+}
+// A list's row of stages: sequence by sequence, kv head by kv head, tile by tile (neighbours read the same K and V).
+// How many pieces a list's row of stages is cut into (none shorter than kPackedMinStages, unless it is the only one), and where
+// piece k begins: piece k is CTA k's.
+__device__ __forceinline__ int packed_pieces(int64_t stages, int grid) {
+  return (int)max((int64_t)1, min(stages / kPackedMinStages, (int64_t)grid));
+}
+__device__ __forceinline__ int64_t packed_cut(int64_t stages, int k, int pieces) {
+  return stages / pieces * k + stages % pieces * k / pieces;
+}
+// First partial row of a unit of CTA k: its pair begins in its piece (then it goes on in the next), or it began before.
+__device__ __forceinline__ int packed_part(const PackedParams& p, int list, int k, bool begins) {
+  return p.part_rows[list] + (2 * k + (begins ? 1 : 0)) * packed_tile(list);
+}
 
 // ------------------------------------------------------------------------------------ plan
 struct PackedSeq {
@@ -91,30 +133,39 @@ __device__ __forceinline__ int packed_list(const PackedParams& p, const PackedSe
   return p.two_tiles && p.G * s.n > kTcRows ? 1 : 0;
 }
 
-// One CTA.  A tile is a unit's columns of one sequence (for all kv heads); its length is what its last column sees, in stages
-// of 128 tokens.  Every list gets a chunk length from its total of stages, tiles that are longer are cut into near-equal
-// chunks, and the items are sorted by length, longest first, so that the dynamic schedule ends evenly.  Latency-bound: a few
-// block-wide scans.
-__global__ void __launch_bounds__(1024) packed_plan_kernel(const PackedParams p, const int first_in_smem) {
-  extern __shared__ int s_first[];  // [B + 1] when they fit
-  __shared__ long long s_warp[32];
-  __shared__ int s_hist[1024];      // 340 lengths for each list
-  __shared__ long long s_sum[3];
+// One CTA.  Tiles of all sequences in their order, the stages before each (one sum for each tile list), the tile with which every
+// CTA's piece begins; and the decode list: items of near-equal length, longest first, so that its dynamic schedule ends evenly.
+// Latency-bound: a few block-wide scans; up to 1024 tiles are kept by the threads.
+// The kernels behind the plan run side by side where SMs are free: each waits for the plan only, in that it can start only when all
+// CTAs of the one in front of it have waited (for the plan), and ends by waiting for the end of that one.
+__global__ void __launch_bounds__(1024) packed_plan_kernel(const PackedParams p, const int in_smem) {
+  extern __shared__ int4 s_seq[];   // when they fit: [B] first row, query tokens, context, then [B + 1] first tile
+  __shared__ long long s_warp[32], s_sum;
+  __shared__ long long s_before[2][1025];
+  __shared__ int s_hist[1024], s_most[4], s_share;
+  __shared__ unsigned long long s_best;
   const int tid = threadIdx.x;
   grid_dep_wait();
   grid_dep_launch();
-  int* first = first_in_smem ? s_first : p.tile_first;
+  int* first = in_smem ? reinterpret_cast<int*>(s_seq + p.B) : p.tile_first;
+  auto seq = [&](int b) {
+    if (!in_smem) return packed_seq(p, b);
+    const int4 v = s_seq[b];
+    return PackedSeq{v.x, v.y, v.z};
+  };
   s_hist[tid] = 0;
-  if (tid < 3) s_sum[tid] = 0;
-  bool refused = false;
+  if (tid == 0) s_sum = 0, s_best = ~0ull;
+  bool refused = false, decodes = false;
   long long tiles = 0;
   for (int b0 = 0; b0 < p.B; b0 += 1024) {
     const int b = b0 + tid;
     long long nt = 0, total;
     if (b < p.B) {
       const PackedSeq q = packed_seq(p, b, &refused);
-      const int per = packed_list(p, q) == 1 ? kTc2Rows : kTcRows;
+      if (in_smem) s_seq[b] = make_int4(q.r0, q.n, q.T, 0);
+      const int list = packed_list(p, q), per = packed_tile(list);
       if (q.T > 0) nt = ((long long)p.G * q.n + per - 1) / per;  // (without a context: zeros, below)
+      decodes |= list == 2 && nt > 0;
     }
     const long long upto = tiles + block_scan(nt, s_warp, &total);
     if (b < p.B) first[b] = (int)min(upto - nt, (long long)INT32_MAX);
@@ -124,154 +175,217 @@ __global__ void __launch_bounds__(1024) packed_plan_kernel(const PackedParams p,
   const int NT = overflow ? 0 : (int)tiles;
   if (tid == 0) first[p.B] = NT;
   refused = __syncthreads_or(refused);
-  struct Tile {
-    int b, c0, cols, stages, list;
-    PackedSeq s;
-  };
-  auto tile_of = [&](int i) {
+  decodes = __syncthreads_or(decodes);
+  auto tile_of = [&](int i, int& list) {
     int lo = 0, hi = p.B;  // largest b with first[b] <= i
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
       if (first[mid] <= i) lo = mid; else hi = mid;
     }
-    Tile t;
+    const PackedSeq q = seq(lo);
+    list = packed_list(p, q);
+    const int per = packed_tile(list);
+    PackedTile t;
     t.b = lo;
-    t.s = packed_seq(p, lo);
-    t.list = packed_list(p, t.s);
-    const int per = t.list == 1 ? kTc2Rows : kTcRows;
     t.c0 = (i - first[lo]) * per;
-    t.cols = min(per, p.G * t.s.n - t.c0);
-    const int seen = min(t.s.T, max(0, t.s.T - t.s.n + 1 + (t.c0 + t.cols - 1) / p.G));
-    t.stages = (seen + kTc2StageTok - 1) / kTc2StageTok;
+    t.first = first[lo];
+    t.end = first[lo + 1];
+    t.r0 = q.r0;
+    t.n = q.n;
+    t.T = q.T;
+    t.stages = max(1, (packed_seen(p, t, list) + kTc2StageTok - 1) / kTc2StageTok);
     return t;
   };
-  long long sum[3] = {0, 0, 0};
-  for (int i = tid; i < NT; i += 1024) {
-    const Tile t = tile_of(i);
-#pragma unroll
-    for (int k = 0; k < 3; ++k) sum[k] += t.list == k ? max(1, t.stages) : 0;
-  }
-#pragma unroll
-  for (int k = 0; k < 3; ++k) {
-    for (int o = 16; o; o >>= 1) sum[k] += __shfl_xor_sync(0xffffffffu, sum[k], o);
-    if ((tid & 31) == 0 && sum[k]) atomicAdd((unsigned long long*)&s_sum[k], (unsigned long long)sum[k]);
-  }
-  __syncthreads();
-  int longest[3];
-#pragma unroll
-  for (int k = 0; k < 3; ++k) {
-    const long long ctas = (long long)(k == 2 ? p.dec_grid : p.grid) * packed_items_per_cta(k);
-    longest[k] = max(kPackedMinStages, (int)((s_sum[k] * p.Hkv + ctas - 1) / ctas));
-  }
-  // chunks of a tile: `len` stages each but the last
-  auto cut = [&](const Tile& t, int& nch, int& len) {
-    const int s = max(1, t.stages);
-    const int most = t.list == 0 ? longest[0] : (t.list == 1 ? longest[1] : longest[2]);
-    nch = (s + most - 1) / most;
-    len = (s + nch - 1) / nch;
-    nch = (s + len - 1) / len;
+  const bool single = NT <= 1024;
+  PackedTile kept = {};
+  int kept_list = -1;
+  if (single && tid < NT) kept = tile_of(tid, kept_list);
+  auto tile_at = [&](int i, int& list) {
+    if (!single) return tile_of(i, list);
+    list = kept_list;
+    return kept;
   };
-  auto bucket = [](int list, int len) { return 340 * list + 339 - min(len, 339); };
-  // What a tile needs, summed over the tiles before it: (chunks of the decode list << 32 | rows of partial results of the others);
-  // every chunk of the decode list has partial rows, in front of the others', by its number.
-  auto needs = [&](const Tile& t, int nch) -> long long {
-    if (t.list == 2) return (long long)nch << 32;
-    return nch > 1 ? (long long)nch * p.Hkv * t.cols : 0;
-  };
-  long long parts = 0, merges = 0;  // (rows << 32 | tiles) to be merged
+  // ---- tile lists
+  long long sums[2] = {0, 0};
+  long long dec_sum = 0;
+  int longest_tile[2] = {0, 0}, list_tiles[2] = {0, 0};
   for (int i0 = 0; i0 < NT; i0 += 1024) {
     const int i = i0 + tid;
-    Tile t = {};
-    int nch = 1, len = 0;
-    long long rows = 0, total;
-    if (i < NT) {
-      t = tile_of(i);
-      cut(t, nch, len);
-      rows = needs(t, nch);
-    }
-    const long long from = parts + block_scan(rows, s_warp, &total) - rows;
-    parts += total;
-    const int chunk = (int)(from >> 32);
-    const long long slot = t.list == 2 ? (long long)chunk * p.Hkv * p.G : p.dec_rows + (from & 0xffffffff);
-    if (t.list != 2 && slot + rows > p.max_part_rows) nch = 1;  // (not met: the workspace bound covers the cuts)
-    const long long m1 = nch > 1 ? ((long long)p.Hkv * t.cols << 32) | 1 : 0;
-    const long long m = merges + block_scan(m1, s_warp, &total) - m1;
-    merges += total;
-    const int at = (int)(m & 0xffffffff);
-    if (nch > 1 && at < p.max_merge) {
-      p.merge[at] = make_int4(t.s.r0, t.c0, nch, (int)slot);
-      p.merge_first[at] = (int)(m >> 32);
-    }
-    if (i < NT) {
-      if (t.list == 2) {
-        p.dec_first[t.b] = chunk;
-        p.dec_first[t.b + 1] = chunk + nch;  // (what the next sequence writes there, if it is one of the list)
-      }
-      if (nch > 1) {
-        atomicAdd(&s_hist[bucket(t.list, len)], nch - 1);
-        atomicAdd(&s_hist[bucket(t.list, t.stages - (nch - 1) * len)], 1);
-      } else {
-        atomicAdd(&s_hist[bucket(t.list, t.stages)], 1);
+    int list = -1;
+    PackedTile t = {};
+    if (i < NT) t = tile_at(i, list);
+    if (list == 2) dec_sum += t.stages;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      if (k == 1 && !p.two_tiles) continue;
+      const long long v = list == k ? t.stages : 0;
+      long long total;
+      const long long at = sums[k] + block_scan(v, s_warp, &total) - v;
+      sums[k] += total;
+      if (i < NT) {
+        p.before[k][i] = at;
+        if (single) s_before[k][i] = at;
       }
     }
+    if (i < NT && list != 2) p.tiles[i] = t;
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+      if (list == k) {
+        longest_tile[k] = max(longest_tile[k], t.stages);
+        ++list_tiles[k];
+      }
   }
-  const int n_merge = min((int)(merges & 0xffffffff), p.max_merge);
-  __syncthreads();
-  long long all;
-  const int mine = s_hist[tid];
-  const long long before = block_scan(mine, s_warp, &all) - mine;
-  s_hist[tid] = (int)before;  // cursors
-  if (tid == 340) s_sum[0] = before;
-  if (tid == 680) s_sum[1] = before;
-  __syncthreads();
-  const int one = (int)s_sum[0], two = (int)s_sum[1];  // items of the first list, of the first two
-  if (tid == 0) {
-    p.hdr->dec.status = (overflow ? kStatusPlanOverflow : 0) | (refused ? kPackedStatusRefused : 0);
-    p.hdr->dec.n_items = (int)(all - two) * p.Hkv;
-    p.hdr->dec.next_item = p.dec_grid;
-    p.hdr->n_items[0] = one;
-    p.hdr->n_items[1] = two - one;
-    p.hdr->next_item[0] = p.hdr->next_item[1] = p.grid;
-    p.hdr->n_merge = n_merge;
-    p.hdr->merge_rows = (int)(merges >> 32);
-    p.merge_first[n_merge] = (int)(merges >> 32);
-  }
-  parts = 0;
-  for (int i0 = 0; i0 < NT; i0 += 1024) {  // (the same scan as above gives every tile its partial rows again)
-    const int i = i0 + tid;
-    Tile t = {};
-    int nch = 1, len = 0;
-    long long rows = 0, total;
-    if (i < NT) {
-      t = tile_of(i);
-      cut(t, nch, len);
-      rows = needs(t, nch);
+  if (tid < 4) s_most[tid] = 0;
+  if (tid == 0)
+    for (int k = 0; k < 2; ++k) {
+      p.hdr->stages[k] = sums[k] * p.Hkv;
+      p.before[k][NT] = sums[k];
+      if (single) s_before[k][NT] = sums[k];
     }
-    const long long from = parts + block_scan(rows, s_warp, &total) - rows;
-    parts += total;
-    const int chunk = (int)(from >> 32);
-    const long long slot = t.list == 2 ? (long long)chunk * p.Hkv * p.G : p.dec_rows + (from & 0xffffffff);
-    if (i >= NT) continue;
-    if (t.list != 2 && slot + rows > p.max_part_rows) nch = 1, len = max(1, t.stages);
-    const int seen = t.stages ? min(t.s.T, t.s.T - t.s.n + 1 + (t.c0 + t.cols - 1) / p.G) : 0;
-    for (int c = 0; c < nch; ++c) {
-      const int st = nch > 1 ? min(len, t.stages - c * len) : t.stages;
-      const int at = atomicAdd(&s_hist[bucket(t.list, st)], 1);
-      if (t.list == 2) {
-        if (!checked(chk_index(at - two, p.max_dec_chunks), &p.hdr->dec.status, kStatusBadIndex) || at - two >= p.max_dec_chunks) continue;
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < 2; ++k)
+    if (list_tiles[k]) {
+      atomicMax(&s_most[k], longest_tile[k]);
+      atomicAdd(&s_most[2 + k], list_tiles[k]);
+    }
+  __syncthreads();
+  auto bucket = [](int len) { return 1023 - min(len, 1023); };
+  // s_hist (numbers of things of a bucket) becomes the first place of each bucket; the user clears it for the next
+  auto places = [&] {
+    __syncthreads();
+    long long all;
+    const int mine = s_hist[tid];
+    const long long before = block_scan(mine, s_warp, &all) - mine;
+    s_hist[tid] = (int)before;
+    __syncthreads();
+  };
+  if (decodes) {
+    for (int o = 16; o; o >>= 1) dec_sum += __shfl_xor_sync(0xffffffffu, dec_sum, o);
+    if ((tid & 31) == 0 && dec_sum) atomicAdd((unsigned long long*)&s_sum, (unsigned long long)dec_sum);
+    __syncthreads();
+    // Pieces of prompts beside decodes: the first are bound by the tensor pipe, the others by HBM, which fewer SMs can keep busy.  So
+    // the two-tile kernel leaves some SMs to the decode kernel, which starts there at once: the number that lets both end
+    // soonest, by the time of a stage on an SM (kStageUs) and the rates of HBM and of an SM's decodes (bytes a us).
+    constexpr float kHbm = 6.9e6f, kSm = 75e3f;
+    const float stage_us = p.D == 128 ? 2.3f : 1.5f, bytes = (float)s_sum * p.Hkv * p.dec_stage_bytes;
+    if (sums[1] > 0 && tid < p.grid) {
+      const int c = tid + 1, rest = p.grid - c;
+      const float two = (float)sums[1] * p.Hkv * stage_us / c;
+      const float t = rest ? fmaxf(two, fmaxf(bytes / kHbm, bytes / (kSm * rest))) : two + bytes / kHbm;
+      atomicMin((unsigned long long*)&s_best, (unsigned long long)__float_as_uint(t) << 32 | c);
+    }
+    __syncthreads();
+    if (tid == 0) s_share = sums[1] > 0 ? (int)(s_best & 0xffffffff) : p.grid;
+    __syncthreads();
+  }
+  for (int k = 0; k < 2; ++k) {
+    const bool pull = (long long)s_most[k] * 4 * p.grid <= sums[k] * p.Hkv;
+    if (tid == 0) {
+      p.hdr->pull[k] = pull;
+      p.hdr->pairs[k] = s_most[2 + k] * p.Hkv;
+      p.hdr->next[k] = p.grid;
+    }
+    if (sums[k] == 0) continue;
+    if (pull) {
+      for (int i = tid; i < NT; i += 1024) {
+        int list;
+        const PackedTile t = tile_at(i, list);
+        if (list == k) atomicAdd(&s_hist[bucket(t.stages)], 1);
+      }
+      places();
+      for (int i = tid; i < NT; i += 1024) {
+        int list;
+        const PackedTile t = tile_at(i, list);
+        if (list == k) p.order[k][atomicAdd(&s_hist[bucket(t.stages)], 1)] = i;
+      }
+      __syncthreads();
+      s_hist[tid] = 0;
+      __syncthreads();
+      continue;
+    }
+    auto before = [&](int i) { return single ? s_before[k][i] : p.before[k][i]; };
+    const int pieces = packed_pieces(sums[k] * p.Hkv, k == 1 && decodes ? s_share : p.grid);
+    if (tid == 0) p.hdr->pieces[k] = pieces;
+    for (int c = tid; c < pieces; c += 1024) {
+      const long long x = packed_cut(sums[k] * p.Hkv, c, pieces);
+      int lo = 0, hi = p.B;  // the sequence: largest b whose stages before it, of all heads, are no more than x
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (before(first[mid]) * p.Hkv <= x) lo = mid; else hi = mid;
+      }
+      const int t0 = first[lo], t1 = first[lo + 1];
+      const long long base = before(t0), per_head = before(t1) - base, rest = x - base * p.Hkv;
+      const int h = (int)(rest / per_head);
+      const long long at = base + rest - h * per_head;
+      lo = t0;
+      hi = t1;  // the tile
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (before(mid) <= at) lo = mid; else hi = mid;
+      }
+      p.start[k][c] = make_int4(lo, h, (int)(at - before(lo)), 0);
+    }
+  }
+  // ---- decode list
+  int n_merge = 0, merge_rows = 0, n_items = 0;
+  if (decodes) {
+    const long long ctas = (long long)p.dec_grid * kPackedDecodeItems;
+    const int longest = max(kPackedMinStages, (int)((s_sum * p.Hkv + ctas - 1) / ctas));
+    auto cut = [&](int stages, int& nch, int& len) {  // chunks of `len` stages each but the last
+      nch = (stages + longest - 1) / longest;
+      len = (stages + nch - 1) / nch;
+      nch = (stages + len - 1) / len;
+    };
+    long long run = 0, kept_at = 0;  // (chunks << 32 | sequences in several chunks) so far
+    auto visit = [&](bool again, auto f) {
+      run = 0;
+      for (int i0 = 0; i0 < NT; i0 += 1024) {
+        const int i = i0 + tid;
+        int list = -1, nch = 0, len = 1;
+        PackedTile t = {};
+        if (i < NT) t = tile_at(i, list);
+        if (list == 2) cut(t.stages, nch, len);
+        long long at = kept_at;
+        if (!(again && single)) {
+          const long long v = list == 2 ? ((long long)nch << 32) | (nch > 1 ? 1 : 0) : 0;
+          long long total;
+          at = run + block_scan(v, s_warp, &total) - v;
+          run += total;
+          kept_at = at;
+        }
+        if (list == 2) f(t, nch, len, (int)(at >> 32), (int)(at & 0xffffffff));
+      }
+    };
+    visit(false, [&](const PackedTile& t, int nch, int len, int chunk, int m) {
+      p.dec_first[t.b] = chunk;
+      p.dec_first[t.b + 1] = chunk + nch;  // (what the next sequence writes there, if it is one of the list)
+      atomicAdd(&s_hist[bucket(len)], nch - 1);
+      atomicAdd(&s_hist[bucket(t.stages - (nch - 1) * len)], 1);
+      if (nch > 1 && m < p.max_merge) p.merge[m] = make_int4(t.r0, 0, nch, chunk * p.Hq);
+    });
+    n_items = (int)(run >> 32);
+    n_merge = min((int)(run & 0xffffffff), p.max_merge);
+    merge_rows = n_merge * p.Hq;
+    places();
+    visit(true, [&](const PackedTile& t, int nch, int len, int chunk, int) {
+      for (int c = 0; c < nch; ++c) {
+        const int at = atomicAdd(&s_hist[bucket(min(len, t.stages - c * len))], 1);
+        if (!checked(chk_index(at, p.max_dec_chunks), &p.hdr->dec.status, kStatusBadIndex) || at >= p.max_dec_chunks) continue;
         const int t0 = c * len * kTc2StageTok;
         for (int h = 0; h < p.Hkv; ++h)
-          p.dec_items[(size_t)(at - two) * p.Hkv + h] = make_int4(t.b, (chunk + c) * p.Hkv + h, t0, min(seen, t0 + st * kTc2StageTok));
-        continue;
+          p.dec_items[(size_t)at * p.Hkv + h] = make_int4(t.b, (chunk + c) * p.Hkv + h, t0, min(t.T, t0 + len * kTc2StageTok));
       }
-      if (!checked(chk_index(at, p.max_items), &p.hdr->dec.status, kStatusBadIndex) || at >= p.max_items) continue;
-      const int t0 = c * len * kTc2StageTok;
-      p.items[2 * at] = make_int4(t.b, t.c0, t0, min(seen, t0 + st * kTc2StageTok));
-      p.items[2 * at + 1] = make_int4(nch > 1 ? (int)slot + c * p.Hkv * t.cols : -1, t.s.r0, t.s.n, t.s.T);
-    }
+    });
+  }
+  if (tid == 0) {
+    p.hdr->dec.status = (overflow ? kStatusPlanOverflow : 0) | (refused ? kPackedStatusRefused : 0);
+    p.hdr->dec.n_items = min(n_items, p.max_dec_chunks) * p.Hkv;
+    p.hdr->dec.next_item = p.dec_grid;
+    p.hdr->merge_rows = merge_rows;
   }
   for (int b = tid >> 5; b < p.B; b += 32) {  // query tokens of a sequence without a context
-    const PackedSeq q = packed_seq(p, b);
+    const PackedSeq q = seq(b);
     if (q.T > 0) continue;
     const int vecs = p.Hq * p.D / 8;
     for (long long i = tid & 31; i < (long long)q.n * vecs; i += 32)
@@ -280,63 +394,83 @@ __global__ void __launch_bounds__(1024) packed_plan_kernel(const PackedParams p,
 }
 
 // ------------------------------------------------------------------------------------ merge
-// One warp per (column, kv head) of a tile that was cut: the partial rows, normalised, are averaged with the weights of their
-// log-sum-exps, in the order of the chunks.
-template <int D>
-__global__ void __launch_bounds__(256) packed_merge_kernel(const PackedParams p) {
+// One warp per row (a column of a (tile, kv head) pair): the partial rows, normalised, are averaged with the weights of their
+// log-sum-exps, in the order of the tokens.  part(c) = partial row of piece c.
+template <int D, typename F>
+__device__ __forceinline__ void merge_row(const PackedParams& p, int pieces, F part, __nv_bfloat16* dst) {
   constexpr int V = D / 32;  // dims per lane
   const int lane = threadIdx.x & 31;
-  grid_dep_launch();
-  grid_dep_wait();
-  const int rows = p.hdr->merge_rows, n_merge = p.hdr->n_merge;
-  for (int r = blockIdx.x * 8 + (threadIdx.x >> 5); r < rows; r += gridDim.x * 8) {
-    int lo = 0, hi = n_merge;
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (p.merge_first[mid] <= r) lo = mid; else hi = mid;
-    }
-    const int4 m = p.merge[lo];
-    const int per = p.merge_first[lo + 1] - p.merge_first[lo];  // rows of a chunk: kv heads x columns
-    const int cols = per / p.Hkv, idx = r - p.merge_first[lo], h = idx / cols, col = m.y + idx - h * cols;
-    if (!checked(chk_index((long long)m.w + (long long)m.z * per - 1, p.max_part_rows), &p.hdr->dec.status, kStatusBadIndex)) continue;
-    const float* lses = p.part_lse + m.w + idx;
-    const float* src = p.part_o + (int64_t)(m.w + idx) * D + lane * V;
-    float M = -INFINITY, den = 0.f, acc[V];
+  float M = -INFINITY, den = 0.f, acc[V];
 #pragma unroll
-    for (int i = 0; i < V; ++i) acc[i] = 0.f;
-    for (int c0 = 0; c0 < m.z; c0 += 32) {
-      const int cnt = min(32, m.z - c0);
-      const float lse = lane < cnt ? lses[(int64_t)(c0 + lane) * per] : -INFINITY;
-      float gm = lse;
+  for (int i = 0; i < V; ++i) acc[i] = 0.f;
+  for (int c0 = 0; c0 < pieces; c0 += 32) {
+    const int cnt = min(32, pieces - c0);
+    const float lse = lane < cnt ? p.part_lse[part(c0 + lane)] : -INFINITY;
+    float gm = lse;
 #pragma unroll
-      for (int o = 16; o; o >>= 1) gm = fmaxf(gm, __shfl_xor_sync(0xffffffffu, gm, o));
-      const float Mn = fmaxf(M, gm), Ms = Mn == -INFINITY ? 0.f : Mn;
-      const float resc = exp2f(M - Ms), w_lane = exp2f(lse - Ms);
-      M = Mn;
-      float ws = w_lane;
+    for (int o = 16; o; o >>= 1) gm = fmaxf(gm, __shfl_xor_sync(0xffffffffu, gm, o));
+    const float Mn = fmaxf(M, gm), Ms = Mn == -INFINITY ? 0.f : Mn;
+    const float resc = exp2f(M - Ms), w_lane = exp2f(lse - Ms);
+    M = Mn;
+    float ws = w_lane;
 #pragma unroll
-      for (int o = 16; o; o >>= 1) ws += __shfl_xor_sync(0xffffffffu, ws, o);
-      den = den * resc + ws;
+    for (int o = 16; o; o >>= 1) ws += __shfl_xor_sync(0xffffffffu, ws, o);
+    den = den * resc + ws;
 #pragma unroll
-      for (int i = 0; i < V; ++i) acc[i] *= resc;
+    for (int i = 0; i < V; ++i) acc[i] *= resc;
 #pragma unroll 8
-      for (int j = 0; j < cnt; ++j) {
-        const float w = __shfl_sync(0xffffffffu, w_lane, j);
-        const float* o = src + (int64_t)(c0 + j) * per * D;
-        if (V == 4) {
-          const float4 x = *reinterpret_cast<const float4*>(o);
-          acc[0] += w * x.x; acc[1] += w * x.y; acc[V - 2] += w * x.z; acc[V - 1] += w * x.w;
-        } else {
-          const float2 x = *reinterpret_cast<const float2*>(o);
-          acc[0] += w * x.x; acc[V - 1] += w * x.y;
-        }
+    for (int j = 0; j < cnt; ++j) {
+      const float w = __shfl_sync(0xffffffffu, w_lane, j);
+      const float* o = p.part_o + (int64_t)part(c0 + j) * D + lane * V;
+      if (V == 4) {
+        const float4 x = *reinterpret_cast<const float4*>(o);
+        acc[0] += w * x.x; acc[1] += w * x.y; acc[V - 2] += w * x.z; acc[V - 1] += w * x.w;
+      } else {
+        const float2 x = *reinterpret_cast<const float2*>(o);
+        acc[0] += w * x.x; acc[V - 1] += w * x.y;
       }
     }
-    const float inv = den > 0.f ? 1.f / den : 0.f;
-    __nv_bfloat16* dst = p.out + (int64_t)(m.x + col / p.G) * p.out_stride + (int64_t)(h * p.G + col % p.G) * D + lane * V;
+  }
+  const float inv = den > 0.f ? 1.f / den : 0.f;
 #pragma unroll
-    for (int i = 0; i < V; i += 2)
-      *reinterpret_cast<uint32_t*>(dst + i) = pack_bf16x2(acc[i] * inv, acc[i + 1] * inv);
+  for (int i = 0; i < V; i += 2) *reinterpret_cast<uint32_t*>(dst + lane * V + i) = pack_bf16x2(acc[i] * inv, acc[i + 1] * inv);
+}
+
+constexpr int kMergeSplit = 16;  // CTAs that share the rows of a pair (147 pairs of 256 rows in two: 7 us, with 4 CTAs each 21)
+
+// The first CTAs: for each tile list and cut, the pair that it goes through (if it is the pair's first cut), by kMergeSplit CTAs
+// each.  The others: the decode list.
+template <int D>
+__global__ void __launch_bounds__(256) packed_merge_kernel(const PackedParams p, const int lists, const int cut_ctas) {
+  const int warp = threadIdx.x >> 5;
+  grid_dep_launch();
+  grid_dep_wait();
+  if ((int)blockIdx.x < cut_ctas) {
+    const int u = blockIdx.x / kMergeSplit, list = lists == 3 ? u & 1 : (lists == 2 ? 1 : 0), k = 1 + (lists == 3 ? u >> 1 : u);
+    const int64_t stages = p.hdr->stages[list];
+    const int pieces = p.hdr->pieces[list];
+    if (stages == 0 || p.hdr->pull[list] || k >= pieces) return;
+    const int4 at = p.start[list][k];
+    if (at.z == 0) return;  // between two pairs
+    const PackedTile t = p.tiles[at.x];
+    const int h = at.y, cols = packed_cols(p, t, list);
+    const int64_t begin = packed_cut(stages, k, pieces) - at.z, end = begin + t.stages;
+    if (packed_cut(stages, k - 1, pieces) > begin) return;  // not the pair's first cut
+    int last = k;  // the piece that holds the pair's last stage
+    while (last + 1 < pieces && packed_cut(stages, last + 1, pieces) < end) ++last;
+    for (int col = (blockIdx.x % kMergeSplit) * 8 + warp; col < cols; col += 8 * kMergeSplit) {
+      const int column = t.c0 + col;
+      merge_row<D>(p, last - k + 2, [&](int c) { return packed_part(p, list, k - 1 + c, c == 0) + col; },
+                   p.out + (int64_t)(t.r0 + column / p.G) * p.out_stride + (int64_t)(h * p.G + column % p.G) * D);
+    }
+    return;
+  }
+  const int rows = p.hdr->merge_rows;
+  for (int r = (blockIdx.x - cut_ctas) * 8 + warp; r < rows; r += (gridDim.x - cut_ctas) * 8) {
+    const int4 m = p.merge[r / p.Hq];
+    const int hq = r % p.Hq;
+    if (!checked(chk_index((long long)m.w + (long long)m.z * p.Hq - 1, p.max_part_rows), &p.hdr->dec.status, kStatusBadIndex)) continue;
+    merge_row<D>(p, m.z, [&](int c) { return m.w + c * p.Hq + hq; }, p.out + (int64_t)m.x * p.out_stride + (int64_t)hq * D);
   }
 }
 
@@ -352,7 +486,6 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
   using L = PackedSmem<D>;
   constexpr int NH = D / 64;                               // 64-dim halves of a row
   constexpr int NK = L::NK, NV = KV8 ? 2 : L::NV, NM = kTc2MetaRing;
-  constexpr int kTile = kOne ? kTcRows : kTc2Rows;         // score columns of a unit
   constexpr int kSlotBytes = L::kSlotBytes, kQBytes = L::kQBytes;
   constexpr int kWarpK = 16, kWarpV = 17, kWarpM = 18;  // warps 0 .. 15: softmax; 18, 19: MMA of tile 0, 1
   extern __shared__ uint8_t smem_raw[];
@@ -426,22 +559,30 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
   __syncthreads();
   tc_fence_after_sync();
   const uint32_t tmem = *g_slot;
-  grid_dep_wait();    // the plan must have completed
-  grid_dep_launch();  // the next kernel of the call may queue up behind this grid
+  if (!kOne || !p.early) grid_dep_wait();  // the plan must have completed
+  grid_dep_launch();                       // the next kernel of the call may queue up behind this grid
 
-  constexpr int kList = kOne ? 0 : 1;  // which of the plan's two item lists
+  constexpr int kList = kOne ? 0 : 1;
   const long long cap_tokens = (long long)p.MB * p.bs;
 
   if (warp == kWarpK) {
     // ================================================================= K producer (and the walk over the units)
     if (lane == 0) prefetch_tmap(&tm_k);
-    const long long n_units = (long long)p.hdr->n_items[kList] * p.Hkv;
-    const int4* items = p.items + (kOne ? 0 : 2 * (size_t)p.hdr->n_items[0]);
     const int boxes_per_stage = kTc2StageTok / p.tile_rows;   // at most 8 (blocks of 16 tokens)
     const uint32_t box_rows_bytes = (uint32_t)p.tile_rows * 128;
     int it = 0;
     bool ok = true, violated = false;
-    long long unit = blockIdx.x;
+    const int64_t stages_all = p.hdr->stages[kList];
+    const bool pull = p.hdr->pull[kList];
+    const int pieces = pull || stages_all == 0 ? 0 : p.hdr->pieces[kList];
+    int unit = blockIdx.x;  // where pairs are pulled: the next one
+    int64_t left = 0;       // else: stages left of the CTA's piece,
+    int4 at = make_int4(0, 0, 0, 0);  // and the next one's tile, kv head and number in its pair
+    if ((int)blockIdx.x < pieces) {
+      left = packed_cut(stages_all, blockIdx.x + 1, pieces) - packed_cut(stages_all, blockIdx.x, pieces);
+      at = p.start[kList][blockIdx.x];
+    }
+    const int n_pairs = pull ? p.hdr->pairs[kList] : 0;
     auto table_entry = [&](const int32_t* e) {
       const int v = *e;
       return checked(chk_table_entry(v, p.NB), &p.hdr->dec.status, kStatusBadTableEntry) ? v : p.NB;
@@ -452,26 +593,28 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
       return warp_wait((KV8 ? s_rkempty : s_kempty) + 8 * (it % NK), (((uint32_t)(it / NK)) & 1u) ^ 1u, s_abort) &&
              warp_wait((KV8 ? s_rvempty : s_vempty) + 8 * (it % NV), (((uint32_t)(it / NV)) & 1u) ^ 1u, s_abort);
     };
-    while (unit < n_units && ok) {
+    while ((pull ? unit < n_pairs : left > 0) && ok) {
       int nxt = 0;
-      if (lane == 0) nxt = atomicAdd(&p.hdr->next_item[kList], 1);
-      nxt = __shfl_sync(0xffffffffu, nxt, 0);
-      const int item = (int)(unit / p.Hkv), h = (int)(unit - (long long)item * p.Hkv);
-      const int4 d = items[2 * item], d2 = items[2 * item + 1];  // {b, first column, t0, t1}, {partial row or -1, first row of q, n, T}
-      if (!checked(chk_item(d.x, 0, d.z, d.w, p.B, 1, cap_tokens) && chk_span(d2.y, d2.z, 0, p.num_rows) &&
-                       (d2.x < 0 || chk_index(d2.x, p.max_part_rows)), &p.hdr->dec.status, kStatusBadItem)) {
+      if (pull) {
+        if (lane == 0) nxt = atomicAdd(&p.hdr->next[kList], 1);
+        nxt = __shfl_sync(0xffffffffu, nxt, 0);
+        at = make_int4(p.order[kList][unit / p.Hkv], unit % p.Hkv, 0, 0);
+      }
+      const PackedTile tile = p.tiles[at.x];
+      if (!checked(chk_item(tile.b, 0, 0, tile.T, p.B, 1, cap_tokens) && chk_span(tile.r0, tile.n, 0, p.num_rows) && tile.stages > 0 &&
+                       chk_index(at.x, p.max_tiles), &p.hdr->dec.status, kStatusBadItem)) {
         *s_abort = 1;
         violated = true;
         ok = false;
         break;
       }
-      const int b = d.x, c0 = d.y, t0 = d.z, t1 = d.w;
-      const int lim_base = d2.w - d2.z + 1;                         // tokens the first query token sees
-      const int columns = p.G * d2.z;                               // of the (sequence, kv head) pair
-      const int col_hi = min(columns, c0 + kTile) - 1;
-      const int part = d2.x < 0 ? -1 : d2.x + h * (col_hi + 1 - c0);
-      const int t1e = min(t1, lim_base + col_hi / p.G);             // nothing beyond is visible to this unit
-      const int nstage = t1e > t0 ? (t1e - t0 + kTc2StageTok - 1) / kTc2StageTok : 0;
+      const int h = at.y, s0 = at.z, s1 = pull ? tile.stages : (int)min((int64_t)tile.stages, s0 + left);
+      const int b = tile.b, c0 = tile.c0, t0 = s0 * kTc2StageTok, t1 = min(packed_seen(p, tile, kList), s1 * kTc2StageTok);
+      const int lim_base = tile.T - tile.n + 1;                     // tokens the first query token sees
+      const int columns = p.G * tile.n;                             // of the (sequence, kv head) pair
+      const int part = s0 == 0 && s1 == tile.stages ? -1 : packed_part(p, kList, blockIdx.x, s0 == 0);
+      const int t1e = t1;                                           // (the plan counts only what the last column sees)
+      const int nstage = t1e > t0 ? s1 - s0 : 0;
       const int32_t* row = p.block_table + (size_t)b * p.MB;
       int blk_cur = 0;
       {
@@ -496,7 +639,7 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
         const uint32_t kfull = (KV8 ? s_rkfull : s_kfull) + 8 * ks;
         if (lane == 0) {
           const int flags = (s == 0 ? 1 : 0) | (s == (nstage > 0 ? nstage : 1) - 1 ? 2 : 0);
-          g_meta[3 * ms] = make_int4(part, d2.y, h, ntok | (flags << 16));
+          g_meta[3 * ms] = make_int4(part, tile.r0, h, ntok | (flags << 16));
           g_meta[3 * ms + 1] = make_int4(tok0, lim_base, t1, c0);
           g_meta[3 * ms + 2] = make_int4(columns, 0, 0, 0);
           g_vdesc[vs].nbox = nbox;
@@ -535,7 +678,20 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
         }
         blk_cur = blk_n;
       }
-      unit = nxt;
+      if (pull) {
+        unit = nxt;
+      } else {
+        left -= s1 - s0;
+        at.z = 0;
+        if (++at.x == tile.end) {
+          if (++at.y < p.Hkv) {
+            at.x = tile.first;
+          } else {
+            at.y = 0;
+            while (left > 0 && p.before[kList][at.x + 1] == p.before[kList][at.x]) ++at.x;  // (tiles of the other lists)
+          }
+        }
+      }
     }
     if (ok) {  // end marker: one more stage, seen by every other warp
       if (acquire()) {
@@ -1164,6 +1320,7 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
   tc_fence_before_sync();
   __syncthreads();
   if (warp == kWarpM) tmem_dealloc(tmem, kTc2TmemCols);
+  if (kOne && p.early) grid_dep_wait();  // (this grid's end says that the one in front of it has ended, too)
 }
 
 
