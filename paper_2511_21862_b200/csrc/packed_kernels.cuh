@@ -7,13 +7,12 @@
 //                                    stage run while the softmax threads still work on the stage before.
 //   packed_tc_kernel<.., two tiles>  a piece of a prompt, tiles of 256 columns: two 128-row halves share every K / V slot and take
 //                                    turns on the tensor pipe, tensor-bound
-// How the CTAs of a tile kernel share the (tile, kv head) pairs of their list is the plan's choice.  Many short pairs: the CTAs
-// pull whole pairs, the longest first.  Few or long ones (the longest is more than a quarter of a CTA's share): all their stages
-// (128 tokens) stand in a row, which is cut into as many equal pieces as there are CTAs; a pair that a cut goes through becomes
-// two or more units, whose rows are merged, at most two of them per CTA.  Measured: 4 pieces of prompts beside 60 decodes, 240
-// pairs of up to 64 stages: pieces 154 us, whole or halved pairs 193 and 175 (a CTA gets one or two of them); 5 prompts, 4500
-// pairs of up to 125: whole pairs 2.7 ms, pieces 3.9 (neighbouring pairs, which read the same K and V, run at the same time
-// only when they are pulled in turn: else they come from HBM again).
+// How the CTAs of a tile kernel share the (tile, kv head) pairs of their list is the plan's choice.  Many or short pairs: the CTAs
+// pull whole pairs, the longest first; what ends early leaves its SM to the decode kernel.  Few long ones (the longest is more than
+// half of a CTA's share, or three quarters of it and the decodes' time together): all their stages (128 tokens) stand in a row,
+// which is cut into as many pieces of equal length as there are CTAs; a pair that a cut goes through becomes two or more units,
+// whose rows are merged, at most two of them per CTA.  Measured, pulled and cut: 16 or 4 pieces of 480 tokens of prompts beside 48
+// or 60 decodes 432 and 481, 240 and 260 us; one piece of 1024 or 128 tokens of a prompt of 8192, 64 q heads 293 and 284, 164 and 86.
 // The CTA is that of chunk_tc2_kernel (chunk_tc2_kernels.cuh), which has one number of query tokens for all sequences; there
 // also stands why its MMAs, slots and warps are as they are.  What differs: a stage's meta words say all about its unit (rows,
 // columns, partial rows), so that sequences of any lengths share a launch; head_dim 64 has half the slot, twice the slots and half
@@ -30,7 +29,11 @@ constexpr int kPackedEnd = 1 << 18;          // flag of a stage's meta words: th
 constexpr int kPackedGridCap = 160;          // most CTAs of an attention kernel (bounds the workspace)
 // Lists: 0 = one tile, 1 = two tiles, 2 = decodes.
 constexpr int kPackedDecodeItems = 6;        // items of the decode list that the plan aims at per CTA
-constexpr int kPackedMinStages = 2;          // shortest item, and shortest piece of a tile list: 256 tokens
+constexpr int kPackedMinStages = 2;          // shortest item: 256 tokens
+// What a unit of a tile list costs beside its stages (its last products, writing its rows, the next one's queries), in stages: 64
+// sequences of 480 new tokens, CTAs of 10 and of 150 units for 479 stages took 1050 and 1970 us.
+constexpr int kPackedUnitCost = 3;
+constexpr int kPackedMinPiece = 6;           // shortest piece of a tile list, in stages
 __host__ __device__ constexpr int packed_tile(int list) { return list == 1 ? kTc2Rows : kTcRows; }  // columns of a tile
 constexpr int kPackedStatusRefused = 128;
 
@@ -46,7 +49,7 @@ struct PackedSmem {
 struct PackedHeader {  // first bytes of the workspace
   WsHeader dec;          // status word; work units (item x kv head) of the decode list and the next one that no CTA has taken
   int32_t merge_rows;    // rows of the sequences of the decode list whose tokens are cut into several items
-  int64_t stages[2];     // of the tile lists, over all kv heads
+  int64_t stages[2];     // length of the tile lists' rows, over all kv heads
   int32_t pull[2];       // whether their CTAs pull whole pairs
   int32_t pairs[2];      // (tile, kv head) pairs of the lists, and the next one to be pulled
   int32_t next[2];
@@ -68,8 +71,8 @@ struct PackedParams {
   PackedHeader* hdr;
   int32_t* tile_first;   // [B + 1] first tile of each sequence
   PackedTile* tiles;     // [max_tiles]
-  int64_t* before[2];    // [max_tiles + 1] stages of the list's tiles before each tile (one kv head)
-  int4* start[2];        // [grid] where each piece of the list begins: {tile, kv head, stage of the pair, -}
+  int64_t* before[2];    // [max_tiles + 1] length of the list's row before each tile (one kv head)
+  int4* start[2];        // [grid] where each piece of the list begins: {tile, kv head, place in the pair, -}
   int32_t* order[2];     // [max_tiles] the list's tiles, longest first (where pairs are pulled)
   int4* merge;           // [max_merge] decode list: {row of q, -, chunks, first partial row}
   float* part_o;         // [max_part_rows, D] normalised partial rows: the decode list's, then two units of every CTA for each tile list
@@ -94,11 +97,12 @@ __device__ __forceinline__ int packed_cols(const PackedParams& p, const PackedTi
 __device__ __forceinline__ int packed_seen(const PackedParams& p, const PackedTile& t, int list) {
   return min(t.T, max(0, t.T - t.n + 1 + (t.c0 + packed_cols(p, t, list) - 1) / p.G));
 }
-// A list's row of stages: sequence by sequence, kv head by kv head, tile by tile (neighbours read the same K and V).
-// How many pieces a list's row of stages is cut into (none shorter than kPackedMinStages, unless it is the only one), and where
-// piece k begins: piece k is CTA k's.
+// A list's row: the stages of every pair behind kPackedUnitCost more for the pair itself, sequence by sequence, kv head by kv head,
+// tile by tile (neighbours read the same K and V).  A cut in front of or inside the additional ones lies between two pairs.
+// How many pieces the row is cut into (none shorter than kPackedMinPiece, unless it is the only one), and where piece k, which is
+// CTA k's, begins.
 __device__ __forceinline__ int packed_pieces(int64_t stages, int grid) {
-  return (int)max((int64_t)1, min(stages / kPackedMinStages, (int64_t)grid));
+  return (int)max((int64_t)1, min(stages / kPackedMinPiece, (int64_t)grid));
 }
 __device__ __forceinline__ int64_t packed_cut(int64_t stages, int k, int pieces) {
   return stages / pieces * k + stages % pieces * k / pieces;
@@ -144,6 +148,7 @@ __global__ void __launch_bounds__(1024) packed_plan_kernel(const PackedParams p,
   __shared__ long long s_before[2][1025];
   __shared__ int s_hist[1024], s_most[4], s_share;
   __shared__ unsigned long long s_best;
+  __shared__ float s_beside;  // what the decodes take, in stages of the two-tile kernel
   const int tid = threadIdx.x;
   grid_dep_wait();
   grid_dep_launch();
@@ -218,7 +223,7 @@ __global__ void __launch_bounds__(1024) packed_plan_kernel(const PackedParams p,
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
       if (k == 1 && !p.two_tiles) continue;
-      const long long v = list == k ? t.stages : 0;
+      const long long v = list == k ? t.stages + kPackedUnitCost : 0;
       long long total;
       const long long at = sums[k] + block_scan(v, s_warp, &total) - v;
       sums[k] += total;
@@ -276,11 +281,12 @@ __global__ void __launch_bounds__(1024) packed_plan_kernel(const PackedParams p,
       atomicMin((unsigned long long*)&s_best, (unsigned long long)__float_as_uint(t) << 32 | c);
     }
     __syncthreads();
-    if (tid == 0) s_share = sums[1] > 0 ? (int)(s_best & 0xffffffff) : p.grid;
+    if (tid == 0) s_share = sums[1] > 0 ? (int)(s_best & 0xffffffff) : p.grid, s_beside = bytes / kHbm / stage_us;
     __syncthreads();
   }
   for (int k = 0; k < 2; ++k) {
-    const bool pull = (long long)s_most[k] * 4 * p.grid <= sums[k] * p.Hkv;
+    const float share = (float)sums[k] * p.Hkv / p.grid, longest = (float)(s_most[k] + kPackedUnitCost);
+    const bool pull = k == 1 && decodes ? longest <= 0.75f * (share + s_beside) : longest <= 0.5f * share;
     if (tid == 0) {
       p.hdr->pull[k] = pull;
       p.hdr->pairs[k] = s_most[2 + k] * p.Hkv;
@@ -451,10 +457,10 @@ __global__ void __launch_bounds__(256) packed_merge_kernel(const PackedParams p,
     const int pieces = p.hdr->pieces[list];
     if (stages == 0 || p.hdr->pull[list] || k >= pieces) return;
     const int4 at = p.start[list][k];
-    if (at.z == 0) return;  // between two pairs
+    if (at.z <= kPackedUnitCost) return;  // between two pairs
     const PackedTile t = p.tiles[at.x];
     const int h = at.y, cols = packed_cols(p, t, list);
-    const int64_t begin = packed_cut(stages, k, pieces) - at.z, end = begin + t.stages;
+    const int64_t begin = packed_cut(stages, k, pieces) - at.z + kPackedUnitCost, end = begin + t.stages;
     if (packed_cut(stages, k - 1, pieces) > begin) return;  // not the pair's first cut
     int last = k;  // the piece that holds the pair's last stage
     while (last + 1 < pieces && packed_cut(stages, last + 1, pieces) < end) ++last;
@@ -576,8 +582,8 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
     const bool pull = p.hdr->pull[kList];
     const int pieces = pull || stages_all == 0 ? 0 : p.hdr->pieces[kList];
     int unit = blockIdx.x;  // where pairs are pulled: the next one
-    int64_t left = 0;       // else: stages left of the CTA's piece,
-    int4 at = make_int4(0, 0, 0, 0);  // and the next one's tile, kv head and number in its pair
+    int64_t left = 0;       // else: what is left of the CTA's piece,
+    int4 at = make_int4(0, 0, 0, 0);  // and its next tile, kv head and place in the pair
     if ((int)blockIdx.x < pieces) {
       left = packed_cut(stages_all, blockIdx.x + 1, pieces) - packed_cut(stages_all, blockIdx.x, pieces);
       at = p.start[kList][blockIdx.x];
@@ -608,7 +614,8 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
         ok = false;
         break;
       }
-      const int h = at.y, s0 = at.z, s1 = pull ? tile.stages : (int)min((int64_t)tile.stages, s0 + left);
+      const int h = at.y, s0 = max(0, at.z - kPackedUnitCost);
+      const int s1 = pull ? tile.stages : max(s0, (int)min((int64_t)tile.stages, at.z + left - kPackedUnitCost));
       const int b = tile.b, c0 = tile.c0, t0 = s0 * kTc2StageTok, t1 = min(packed_seen(p, tile, kList), s1 * kTc2StageTok);
       const int lim_base = tile.T - tile.n + 1;                     // tokens the first query token sees
       const int columns = p.G * tile.n;                             // of the (sequence, kv head) pair
@@ -622,7 +629,8 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
         if (lane < boxes_per_stage && tb < t1e) blk_cur = table_entry(row + tb / p.bs);
       }
       // a pair that sees nothing of this chunk passes one stage without tokens, which carries the bookkeeping
-      for (int s = 0; s < (nstage > 0 ? nstage : 1); ++s, ++it) {
+      // (a piece that ends in front of a pair's stages leaves the whole pair to the next one)
+      for (int s = 0; s < (nstage > 0 ? nstage : (s1 > s0 ? 1 : 0)); ++s, ++it) {
         const int tok0 = t0 + s * kTc2StageTok;
         const int ntok = nstage > 0 ? min(kTc2StageTok, t1e - tok0) : 0;
         const int nbox = (ntok + p.tile_rows - 1) / p.tile_rows;
@@ -681,7 +689,7 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
       if (pull) {
         unit = nxt;
       } else {
-        left -= s1 - s0;
+        left -= tile.stages + kPackedUnitCost - at.z;  // (below 0 where the pair goes on in the next piece)
         at.z = 0;
         if (++at.x == tile.end) {
           if (++at.y < p.Hkv) {
