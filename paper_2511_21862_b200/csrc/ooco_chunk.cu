@@ -183,7 +183,7 @@ static int chunk_core(const ooco_shape_t* s, int32_t num_rows, int32_t max_chunk
   p.max_tiles = w.max_tiles;
   p.max_merge = w.max_merge;
   p.max_part_rows = w.max_part_rows;
-  p.early = p.decode || p.two_tiles;
+  p.early = !kv8 && (p.decode || p.two_tiles);
   p.dec_stage_bytes = 2.f * kTc2StageTok * s->head_dim * (kv8 ? 1 : 2);
   p.tile_rows = s->block_size < kTc2StageTok ? s->block_size : kTc2StageTok;
   p.scale_log2e = scale * 1.4426950408889634f * (kv8 ? k_scale * kE4m3WidenFactor : 1.f);
@@ -226,7 +226,7 @@ static int chunk_core(const ooco_shape_t* s, int32_t num_rows, int32_t max_chunk
     d.first_row = first_row;
     d.q_stride = q_stride;
     d.out_stride = out_stride;
-    d.early = p.two_tiles;
+    d.early = p.two_tiles || (kv8 && max_chunk > 1);
     // (scores come from the codes' own values here: only V carries the widening factor)
     d.scale_log2e = scale * 1.4426950408889634f * k_scale;
     d.v_scale = p.v_scale;
@@ -252,9 +252,12 @@ static int chunk_core(const ooco_shape_t* s, int32_t num_rows, int32_t max_chunk
     if (p.two_tiles)
       r = s->head_dim == 128 ? launch_packed<128, false, false>(tk, tv, p, di, dev, st, dry)
                              : launch_packed<64, false, false>(tk, tv, p, di, dev, st, dry);
+    if (kv8) {
+      if (tiles) r = launch_packed<128, true, true>(tk, tv, p, di, dev, st, dry);
+      return r ? r : decodes(dry);
+    }
     if (!r && p.decode) r = decodes(dry);
     if (r || !tiles) return r;
-    if (kv8) return launch_packed<128, true, true>(tk, tv, p, di, dev, st, dry);
     return s->head_dim == 128 ? launch_packed<128, false, true>(tk, tv, p, di, dev, st, dry)
                               : launch_packed<64, false, true>(tk, tv, p, di, dev, st, dry);
   };
@@ -265,12 +268,8 @@ static int chunk_core(const ooco_shape_t* s, int32_t num_rows, int32_t max_chunk
   if (e == cudaSuccess) e = cudaGetLastError();
   if (e != cudaSuccess) return fail_cuda("launch of the packed plan kernel", (long)e);
   if ((rc = attention(false))) return rc;
-  // merging: the cuts of the tile lists that were launched, and the rows of the decode list
-  const int lists = (tiles ? 1 : 0) | (p.two_tiles ? 2 : 0), cut_ctas = (p.grid - 1) * kMergeSplit * (lists == 3 ? 2 : (lists ? 1 : 0));
-  int64_t blocks = p.decode ? ((int64_t)(w.max_merge) * p.Hq + 7) / 8 : 0;
-  if (blocks > 4ll * di.sm_count) blocks = 4ll * di.sm_count;
-  e = launch_ex(s->head_dim == 128 ? packed_merge_kernel<128> : packed_merge_kernel<64>, dim3((unsigned)(cut_ctas + blocks)), dim3(256),
-                0, st, pdl_enabled(), p, lists, cut_ctas);
+  e = launch_ex(s->head_dim == 128 ? packed_merge_kernel<128> : packed_merge_kernel<64>, dim3((unsigned)(4 * di.sm_count)), dim3(256), 0,
+                st, pdl_enabled(), p);
   if (e == cudaSuccess) e = cudaGetLastError();
   return e == cudaSuccess ? OOCO_OK : fail_cuda("launch of the packed merge kernel", (long)e);
 }

@@ -270,8 +270,9 @@ __global__ void __launch_bounds__(1024) packed_plan_kernel(const PackedParams p,
     if ((tid & 31) == 0 && dec_sum) atomicAdd((unsigned long long*)&s_sum, (unsigned long long)dec_sum);
     __syncthreads();
     // Pieces of prompts beside decodes: the first are bound by the tensor pipe, the others by HBM, which fewer SMs can keep busy.  So
-    // the two-tile kernel leaves some SMs to the decode kernel, which starts there at once: the number that lets both end
-    // soonest, by the time of a stage on an SM (kStageUs) and the rates of HBM and of an SM's decodes (bytes a us).
+    // the two-tile kernel leaves some SMs to the decode kernel, which starts there at once: the number that lets both end soonest,
+    // by the time of a stage on an SM and the rates of HBM and of an SM's decodes (bytes a us).  (Over the 8-bit cache both kernels
+    // are bound by the SMs: 445 us one behind the other, 495 side by side.)
     constexpr float kHbm = 6.9e6f, kSm = 75e3f;
     const float stage_us = p.D == 128 ? 2.3f : 1.5f, bytes = (float)s_sum * p.Hkv * p.dec_stage_bytes;
     if (sums[1] > 0 && tid < p.grid) {
@@ -442,37 +443,77 @@ __device__ __forceinline__ void merge_row(const PackedParams& p, int pieces, F p
   for (int i = 0; i < V; i += 2) *reinterpret_cast<uint32_t*>(dst + lane * V + i) = pack_bf16x2(acc[i] * inv, acc[i + 1] * inv);
 }
 
-constexpr int kMergeSplit = 16;  // CTAs that share the rows of a pair (147 pairs of 256 rows in two: 7 us, with 4 CTAs each 21)
+// The same for `kRows` neighbouring columns in two pieces, the usual case of a pair that was cut: all their loads in flight together.
+// first, second = partial rows of the first column; row(c) = where column c goes, for c < n.
+template <int D, int kRows, typename F>
+__device__ __forceinline__ void merge_pairs(const PackedParams& p, int first, int second, int n, F row) {
+  constexpr int V = D / 32;
+  const int lane = threadIdx.x & 31;
+  float a[kRows], b[kRows], x[kRows][V], y[kRows][V];
+#pragma unroll
+  for (int c = 0; c < kRows; ++c) {
+    a[c] = b[c] = -INFINITY;
+    if (c >= n) continue;
+    a[c] = p.part_lse[first + c];
+    b[c] = p.part_lse[second + c];
+    const float* u = p.part_o + (int64_t)(first + c) * D + lane * V;
+    const float* w = p.part_o + (int64_t)(second + c) * D + lane * V;
+#pragma unroll
+    for (int i = 0; i < V; i += 2) {
+      *reinterpret_cast<float2*>(&x[c][i]) = *reinterpret_cast<const float2*>(u + i);
+      *reinterpret_cast<float2*>(&y[c][i]) = *reinterpret_cast<const float2*>(w + i);
+    }
+  }
+#pragma unroll
+  for (int c = 0; c < kRows; ++c) {
+    if (c >= n) continue;
+    const float M = fmaxf(a[c], b[c]), Ms = M == -INFINITY ? 0.f : M;
+    const float wa = exp2f(a[c] - Ms), wb = exp2f(b[c] - Ms), den = wa + wb, inv = den > 0.f ? 1.f / den : 0.f;
+    __nv_bfloat16* dst = row(c);
+#pragma unroll
+    for (int i = 0; i < V; i += 2)
+      *reinterpret_cast<uint32_t*>(dst + lane * V + i) =
+          pack_bf16x2((wa * x[c][i] + wb * y[c][i]) * inv, (wa * x[c][i + 1] + wb * y[c][i + 1]) * inv);
+  }
+}
 
-// The first CTAs: for each tile list and cut, the pair that it goes through (if it is the pair's first cut), by kMergeSplit CTAs
-// each.  The others: the decode list.
+constexpr int kMergeRows = 4;  // neighbouring columns of a pair that a warp merges at a time
+
+// A warp's units of work: for each tile list that was cut into pieces, each cut and each group of kMergeRows columns (those of the
+// pair that the cut goes through, if it is the pair's first); then the rows of the decode list.
 template <int D>
-__global__ void __launch_bounds__(256) packed_merge_kernel(const PackedParams p, const int lists, const int cut_ctas) {
-  const int warp = threadIdx.x >> 5;
+__global__ void __launch_bounds__(256) packed_merge_kernel(const PackedParams p) {
   grid_dep_launch();
   grid_dep_wait();
-  if ((int)blockIdx.x < cut_ctas) {
-    const int u = blockIdx.x / kMergeSplit, list = lists == 3 ? u & 1 : (lists == 2 ? 1 : 0), k = 1 + (lists == 3 ? u >> 1 : u);
+  const int warps = gridDim.x * 8, me = blockIdx.x * 8 + (threadIdx.x >> 5);
+  for (int list = 0; list < 2; ++list) {
     const int64_t stages = p.hdr->stages[list];
-    const int pieces = p.hdr->pieces[list];
-    if (stages == 0 || p.hdr->pull[list] || k >= pieces) return;
-    const int4 at = p.start[list][k];
-    if (at.z <= kPackedUnitCost) return;  // between two pairs
-    const PackedTile t = p.tiles[at.x];
-    const int h = at.y, cols = packed_cols(p, t, list);
-    const int64_t begin = packed_cut(stages, k, pieces) - at.z + kPackedUnitCost, end = begin + t.stages;
-    if (packed_cut(stages, k - 1, pieces) > begin) return;  // not the pair's first cut
-    int last = k;  // the piece that holds the pair's last stage
-    while (last + 1 < pieces && packed_cut(stages, last + 1, pieces) < end) ++last;
-    for (int col = (blockIdx.x % kMergeSplit) * 8 + warp; col < cols; col += 8 * kMergeSplit) {
-      const int column = t.c0 + col;
-      merge_row<D>(p, last - k + 2, [&](int c) { return packed_part(p, list, k - 1 + c, c == 0) + col; },
-                   p.out + (int64_t)(t.r0 + column / p.G) * p.out_stride + (int64_t)(h * p.G + column % p.G) * D);
+    if (stages == 0 || p.hdr->pull[list]) continue;
+    const int pieces = p.hdr->pieces[list], groups = packed_tile(list) / kMergeRows;
+    for (int u = me; u < (pieces - 1) * groups; u += warps) {
+      const int k = 1 + u / groups, col0 = u % groups * kMergeRows;
+      const int4 at = p.start[list][k];
+      if (at.z <= kPackedUnitCost) continue;  // between two pairs
+      const PackedTile t = p.tiles[at.x];
+      const int h = at.y, cols = packed_cols(p, t, list);
+      const int64_t begin = packed_cut(stages, k, pieces) - at.z + kPackedUnitCost, end = begin + t.stages;
+      if (col0 >= cols || packed_cut(stages, k - 1, pieces) > begin) continue;  // (not the pair's first cut)
+      int last = k;  // the piece that holds the pair's last stage
+      while (last + 1 < pieces && packed_cut(stages, last + 1, pieces) < end) ++last;
+      auto row = [&](int c) {
+        const int column = t.c0 + col0 + c;
+        return p.out + (int64_t)(t.r0 + column / p.G) * p.out_stride + (int64_t)(h * p.G + column % p.G) * D;
+      };
+      const int n = min(kMergeRows, cols - col0);
+      if (last == k)
+        merge_pairs<D, kMergeRows>(p, packed_part(p, list, k - 1, true) + col0, packed_part(p, list, k, false) + col0, n, row);
+      else
+        for (int c = 0; c < n; ++c)
+          merge_row<D>(p, last - k + 2, [&](int i) { return packed_part(p, list, k - 1 + i, i == 0) + col0 + c; }, row(c));
     }
-    return;
   }
   const int rows = p.hdr->merge_rows;
-  for (int r = (blockIdx.x - cut_ctas) * 8 + warp; r < rows; r += (gridDim.x - cut_ctas) * 8) {
+  for (int r = me; r < rows; r += warps) {
     const int4 m = p.merge[r / p.Hq];
     const int hq = r % p.Hq;
     if (!checked(chk_index((long long)m.w + (long long)m.z * p.Hq - 1, p.max_part_rows), &p.hdr->dec.status, kStatusBadIndex)) continue;
