@@ -17,9 +17,9 @@ template <int D, bool KV8>
 __global__ void __launch_bounds__(kRopeThreads, 4) norm_rope_append_kernel(const RopeParams p, const HeadNormParams hn,
                                                                         const int interleaved) {
   constexpr int UPH = D / 16;  // units (lanes) per head
-  __shared__ float4 s_w4[2][D / 4];  // weights with their offset, of q and of k
-  float(*s_w)[D] = reinterpret_cast<float(*)[D]>(s_w4);
-  __shared__ float2 s_cs[kRopeMaxTile][D / 2];
+  // By the place in the head, so that neighbouring lanes read neighbouring vectors (no bank conflicts): the 16 weights with their
+  // offset, of q and of k; the cosines and sines of 8 pairs, of each token of the tile.
+  __shared__ float4 s_w[2][4][UPH], s_cs[kRopeMaxTile][4][UPH];
   __shared__ int s_pos[kRopeMaxTile], s_slot[kRopeMaxTile];
   grid_dep_wait();
   grid_dep_launch();
@@ -29,9 +29,12 @@ __global__ void __launch_bounds__(kRopeThreads, 4) norm_rope_append_kernel(const
   const bool turned = c < rot_units, turned_halves = !interleaved && turned;
   const int d_lo = turned_halves ? 8 * c : 16 * c, d_hi = turned_halves ? p.half + 8 * c : 16 * c + 8;
   const uint4 none = make_uint4(0u, 0u, 0u, 0u);
-  for (int i = threadIdx.x; i < 2 * D; i += kRopeThreads) {
-    const uint16_t* w = i < D ? hn.q_weight : hn.k_weight;
-    s_w[i / D][i % D] = w ? __uint_as_float((uint32_t)w[i % D] << 16) + hn.offset : 1.f;
+  if (threadIdx.x < 2 * D) {
+    const int kind = threadIdx.x / D, place = threadIdx.x % D / 16, e = threadIdx.x % 16;  // element e of a thread's 16
+    const bool halves = !interleaved && place < rot_units;
+    const int dim = halves ? (e < 8 ? 8 * place + e : p.half + 8 * place + e - 8) : 16 * place + e;
+    const uint16_t* w = kind ? hn.k_weight : hn.q_weight;
+    reinterpret_cast<float*>(&s_w[kind][e / 4][place])[e % 4] = w ? __uint_as_float((uint32_t)w[dim] << 16) + hn.offset : 1.f;
   }
   for (int t0 = blockIdx.x * p.tile; t0 < p.T; t0 += gridDim.x * p.tile) {
     const int nt = min(p.tile, p.T - t0);
@@ -41,7 +44,7 @@ __global__ void __launch_bounds__(kRopeThreads, 4) norm_rope_append_kernel(const
       const double turns = (double)p.positions[t0 + tk] * (double)p.inv_freq[j] * 0.15915494309189533577;
       float s, co;
       sincospif((float)(2.0 * (turns - rint(turns))), &s, &co);
-      s_cs[tk][j] = make_float2(co * p.magnitude, s * p.magnitude);
+      reinterpret_cast<float2*>(&s_cs[tk][j % 8 / 2][j / 8])[j % 2] = make_float2(co * p.magnitude, s * p.magnitude);
     }
     if ((int)threadIdx.x < nt) {
       s_pos[threadIdx.x] = p.positions[t0 + threadIdx.x];
@@ -87,32 +90,29 @@ __global__ void __launch_bounds__(kRopeThreads, 4) norm_rope_append_kernel(const
         if (tk[i] < 0) continue;
         if (!is_v) {
           const float r = __frsqrt_rn(ss * (1.f / D) + hn.eps);
-          const float4* w = reinterpret_cast<const float4*>(s_w[is_q ? 0 : 1]);
+          const float4(*w)[UPH] = s_w[is_q ? 0 : 1];
 #pragma unroll
           for (int m = 0; m < 2; ++m) {
-            const float4 u = w[d_lo / 4 + m], z = w[d_hi / 4 + m];
+            const float4 u = w[m][c], z = w[2 + m][c];
             x[4 * m] *= r * u.x, x[4 * m + 1] *= r * u.y, x[4 * m + 2] *= r * u.z, x[4 * m + 3] *= r * u.w;
             y[4 * m] *= r * z.x, y[4 * m + 1] *= r * z.y, y[4 * m + 2] *= r * z.z, y[4 * m + 3] *= r * z.w;
           }
           if (turned) {
-            const float2* cs = &s_cs[tk[i]][8 * c];
-            if (interleaved) {
+            auto turn = [](float& a0, float& b0, float co, float si) {
+              const float a1 = a0;
+              a0 = a0 * co - b0 * si;
+              b0 = b0 * co + a1 * si;
+            };
 #pragma unroll
-              for (int m = 0; m < 4; ++m) {
-                const float2 w0 = cs[m], w1 = cs[4 + m];
-                const float x0 = x[2 * m], y0 = y[2 * m];
-                x[2 * m] = x0 * w0.x - x[2 * m + 1] * w0.y;
-                x[2 * m + 1] = x[2 * m + 1] * w0.x + x0 * w0.y;
-                y[2 * m] = y0 * w1.x - y[2 * m + 1] * w1.y;
-                y[2 * m + 1] = y[2 * m + 1] * w1.x + y0 * w1.y;
-              }
-            } else {
-#pragma unroll
-              for (int m = 0; m < 8; ++m) {
-                const float2 w = cs[m];
-                const float x0 = x[m];
-                x[m] = x0 * w.x - y[m] * w.y;
-                y[m] = y[m] * w.x + x0 * w.y;
+            for (int m = 0; m < 4; ++m) {  // pairs 8 c + 2 m, + 1
+              const float4 cs = s_cs[tk[i]][m][c];
+              if (interleaved) {
+                float* v = m < 2 ? x + 4 * m : y + 4 * (m - 2);
+                turn(v[0], v[1], cs.x, cs.y);
+                turn(v[2], v[3], cs.z, cs.w);
+              } else {
+                turn(x[2 * m], y[2 * m], cs.x, cs.y);
+                turn(x[2 * m + 1], y[2 * m + 1], cs.z, cs.w);
               }
             }
           }
