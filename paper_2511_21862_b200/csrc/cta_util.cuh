@@ -80,8 +80,10 @@ __device__ __forceinline__ uint4 pack8_bf16(const float (&x)[8]) {
 __device__ __forceinline__ uint2 pack8_e4m3(const float (&x)[8], float scale) {
   uint32_t w[2] = {0u, 0u};
 #pragma unroll
-  for (int i = 0; i < 8; ++i)
-    w[i >> 2] |= (uint32_t)__nv_cvt_float_to_fp8(__fdiv_rn(x[i], scale), __NV_SATFINITE, __NV_E4M3) << (8 * (i & 3));
+  for (int i = 0; i < 8; i += 2) {
+    const float2 v = make_float2(__fdiv_rn(x[i], scale), __fdiv_rn(x[i + 1], scale));
+    w[i >> 2] |= (uint32_t)__nv_cvt_float2_to_fp8x2(v, __NV_SATFINITE, __NV_E4M3) << (8 * (i & 3));
+  }
   return make_uint2(w[0], w[1]);
 }
 __device__ __forceinline__ void unpack8(const uint4 w, float (&x)[8]) {

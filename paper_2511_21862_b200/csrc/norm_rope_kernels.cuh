@@ -44,7 +44,9 @@ __global__ void __launch_bounds__(kRopeThreads, 4) norm_rope_append_kernel(const
       const double turns = (double)p.positions[t0 + tk] * (double)p.inv_freq[j] * 0.15915494309189533577;
       float s, co;
       sincospif((float)(2.0 * (turns - rint(turns))), &s, &co);
-      reinterpret_cast<float2*>(&s_cs[tk][j % 8 / 2][j / 8])[j % 2] = make_float2(co * p.magnitude, s * p.magnitude);
+      float* cs = reinterpret_cast<float*>(&s_cs[tk][j % 8 / 2][j / 8]);  // cosines of two pairs, sines of both
+      cs[j % 2] = co * p.magnitude;
+      cs[2 + j % 2] = s * p.magnitude;
     }
     if ((int)threadIdx.x < nt) {
       s_pos[threadIdx.x] = p.positions[t0 + threadIdx.x];
@@ -82,40 +84,46 @@ __global__ void __launch_bounds__(kRopeThreads, 4) norm_rope_append_kernel(const
         float x[8], y[8];
         unpack8(a[i], x);
         unpack8(b[i], y);
-        float ss = 0.f;
+        // (two values an instruction where the pairs are neighbours)
+        float2 xx[4], yy[4], sq = make_float2(0.f, 0.f);
 #pragma unroll
-        for (int m = 0; m < 8; ++m) ss = fmaf(x[m], x[m], fmaf(y[m], y[m], ss));
+        for (int m = 0; m < 4; ++m) {
+          xx[m] = make_float2(x[2 * m], x[2 * m + 1]);
+          yy[m] = make_float2(y[2 * m], y[2 * m + 1]);
+          sq = ffma2(xx[m], xx[m], ffma2(yy[m], yy[m], sq));
+        }
+        float ss = sq.x + sq.y;
 #pragma unroll
         for (int o = 1; o < UPH; o <<= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);  // (all lanes of a head take part alike)
         if (tk[i] < 0) continue;
         if (!is_v) {
           const float r = __frsqrt_rn(ss * (1.f / D) + hn.eps);
           const float4(*w)[UPH] = s_w[is_q ? 0 : 1];
+          const float2 rr = make_float2(r, r);
 #pragma unroll
-          for (int m = 0; m < 2; ++m) {
-            const float4 u = w[m][c], z = w[2 + m][c];
-            x[4 * m] *= r * u.x, x[4 * m + 1] *= r * u.y, x[4 * m + 2] *= r * u.z, x[4 * m + 3] *= r * u.w;
-            y[4 * m] *= r * z.x, y[4 * m + 1] *= r * z.y, y[4 * m + 2] *= r * z.z, y[4 * m + 3] *= r * z.w;
+          for (int m = 0; m < 4; ++m) {
+            const float4 u = w[m][c];
+            float2* v = m < 2 ? xx + 2 * m : yy + 2 * (m - 2);
+            v[0] = fmul2(fmul2(v[0], rr), make_float2(u.x, u.y));
+            v[1] = fmul2(fmul2(v[1], rr), make_float2(u.z, u.w));
           }
           if (turned) {
-            auto turn = [](float& a0, float& b0, float co, float si) {
-              const float a1 = a0;
-              a0 = a0 * co - b0 * si;
-              b0 = b0 * co + a1 * si;
-            };
 #pragma unroll
             for (int m = 0; m < 4; ++m) {  // pairs 8 c + 2 m, + 1
               const float4 cs = s_cs[tk[i]][m][c];
               if (interleaved) {
-                float* v = m < 2 ? x + 4 * m : y + 4 * (m - 2);
-                turn(v[0], v[1], cs.x, cs.y);
-                turn(v[2], v[3], cs.z, cs.w);
+                float2* v = m < 2 ? xx + 2 * m : yy + 2 * (m - 2);
+                v[0] = make_float2(v[0].x * cs.x - v[0].y * cs.z, v[0].y * cs.x + v[0].x * cs.z);
+                v[1] = make_float2(v[1].x * cs.y - v[1].y * cs.w, v[1].y * cs.y + v[1].x * cs.w);
               } else {
-                turn(x[2 * m], y[2 * m], cs.x, cs.y);
-                turn(x[2 * m + 1], y[2 * m + 1], cs.z, cs.w);
+                const float2 x0 = xx[m];
+                xx[m] = make_float2(x0.x * cs.x - yy[m].x * cs.z, x0.y * cs.y - yy[m].y * cs.w);
+                yy[m] = ffma2(x0, make_float2(cs.z, cs.w), fmul2(yy[m], make_float2(cs.x, cs.y)));
               }
             }
           }
+#pragma unroll
+          for (int m = 0; m < 4; ++m) x[2 * m] = xx[m].x, x[2 * m + 1] = xx[m].y, y[2 * m] = yy[m].x, y[2 * m + 1] = yy[m].y;
         }
         if (is_q) {
           uint16_t* dst = p.q_out + (size_t)(t0 + tk[i]) * p.q_out_stride + (size_t)head[i] * D;

@@ -97,6 +97,8 @@ int rope_append(const ooco_shape_t* s, const ooco_rope_t* r, const ooco_head_nor
   const bool pdl = pdl_enabled();
   cudaError_t e;
   if (norm) {
+    const int resident = 4 * sms;  // CTAs that fit at a time: the tiles in whole waves
+    const dim3 grid(tiles < resident ? tiles : resident);
     const HeadNormParams hn = {(const uint16_t*)norm->q_weight, (const uint16_t*)norm->k_weight, norm->eps, norm->weight_offset};
     e = kv8 ? launch_ex(norm_rope_append_kernel<128, true>, grid, block, 0, st, pdl, p, hn, (int)r->interleaved)
         : s->head_dim == 128
