@@ -68,6 +68,8 @@ extern "C" {
  * becomes the smaller of itself and keep_lens, blocks_held the blocks kept; table entries stay.  A row outside
  * [0, batch) or named twice is refused; a row's blocks_held is clamped to [0, max_blocks_per_seq].
  *   free_ids is written in [new free_head, free_head); the rest as above.  One launch, or five for many table entries.
+ * The last block that a cut row keeps may have other holders: new tokens must not be written into it.  Such a row goes on
+ * as a fork of itself into an empty row (whose partly filled block is a copy).
  */
 #define OOCO_MAX_PAGE_ROWS (1 << 18)
 size_t ooco_pages_workspace_bytes(const ooco_shape_t* shape, int32_t num_rows);
@@ -164,7 +166,7 @@ int ooco_shape_logits(const ooco_logits_t* shape, const void* logits, const floa
  *   n_b            first_row[b + 1] - first_row[b], or the smaller of that and chunk_lens[b]; negative counts as 0,
  *                  rows at or beyond num_rows do not exist
  *   num_rows       rows of q and out; rows that belong to no query token are left as they were
- *   max_chunk      the caller's bound of n_b, at most num_rows (which always is one): it decides which kernels are
+ *   max_chunk      the caller's bound of n_b, 1 .. num_rows (which always is one): it decides which kernels are
  *                  launched and how large the workspace is.  A sequence that brings more is passed over, its rows left
  *                  as they were, and sets OOCO_STATUS_REFUSED in the workspace's status word
  *   q, out         device, bf16 [num_rows, Hq, head_dim], rows q_stride (out_stride) elements apart: multiples of 8, at
@@ -174,7 +176,9 @@ int ooco_shape_logits(const ooco_logits_t* shape, const void* logits, const floa
  *   workspace      >= ooco_chunk_workspace_bytes(shape, num_rows, max_chunk), 256-byte aligned, read by
  *                  ooco_workspace_status
  * num_rows = 0 launches nothing.  Slots at or beyond T_b, table entries behind the last block used, and entries outside
- * the pool are treated as in ooco_decode_attention.  The 8-bit variant as ooco_decode_step_mq_fp8.
+ * the pool are treated as in ooco_decode_attention.  The K / V of a sequence's context must be finite, those of its later
+ * new tokens among them: the products that the causal mask gives weight 0 are still formed inside a sequence.  The 8-bit
+ * variant as ooco_decode_step_mq_fp8.  Up to five launches (plan, the kernels that max_chunk asks for, merge).
  */
 size_t ooco_chunk_workspace_bytes(const ooco_shape_t* shape, int32_t num_rows, int32_t max_chunk);
 int ooco_chunk_attention(const ooco_shape_t* shape, int32_t num_rows, int32_t max_chunk, const void* q, int64_t q_stride,

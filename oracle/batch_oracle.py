@@ -5,6 +5,7 @@ Written from the definitions, one fork, one row, one head at a time; nothing is 
 from __future__ import annotations
 
 import math
+from collections import Counter
 
 import numpy as np
 
@@ -15,12 +16,13 @@ def fork_pages(parents, children, lens, ctx, table, held, free_ids, head, shares
     B, MB = table.shape
     table, ctx_out, held_out, shares = table.copy(), ctx.copy(), held.copy(), shares.copy()
     F = len(parents)
+    named, kin = Counter(int(x) for x in children), {int(x) for x in parents}
     src, dst, granted = np.full(F, -1), np.full(F, -1), np.zeros(F, np.int64)
     head0, promised, status = max(0, int(head)), 0, 0
     head = head0
     for c in range(F):
         p, k = int(parents[c]), int(children[c])
-        ok = 0 <= p < B and 0 <= k < B and list(children).count(k) == 1 and k not in list(parents) and held[k] <= 0
+        ok = 0 <= p < B and 0 <= k < B and named[k] == 1 and k not in kin and held[k] <= 0
         L = need = full = 0
         if ok:
             L = max(0, int(ctx[p]))
@@ -58,10 +60,10 @@ def fork_pages(parents, children, lens, ctx, table, held, free_ids, head, shares
 def release_pages(rows, keep, ctx, table, held, free_ids, head, shares, *, block_size, num_blocks):
     B, MB = table.shape
     ctx_out, held_out, shares, free_ids = ctx.copy(), held.copy(), shares.copy(), free_ids.copy()
-    status, given = 0, []
+    status, given, named = 0, [], Counter(int(x) for x in rows)
     for c, r in enumerate(rows):
         r = int(r)
-        if not 0 <= r < B or list(rows).count(r) != 1:
+        if not 0 <= r < B or named[r] != 1:
             status |= REFUSED
             continue
         k = 0 if keep is None else max(0, int(keep[c]))
@@ -73,9 +75,9 @@ def release_pages(rows, keep, ctx, table, held, free_ids, head, shares, *, block
             else:
                 status |= BAD
         ctx_out[r], held_out[r] = min(max(0, int(ctx[r])), k), stay
-    freed = []
+    freed, times = [], Counter(given)
     for b in dict.fromkeys(given):           # in the order of their first places
-        left = int(shares[b]) - given.count(b)
+        left = int(shares[b]) - times[b]
         if left < 0:
             freed.append(b)
         shares[b] = max(0, left)

@@ -56,6 +56,7 @@ static PagesParams page_params(const ooco_shape_t* s, int32_t n, int32_t num_fre
   p.ws_off = (int32_t*)workspace;
   p.ws_from = (int32_t*)((uint8_t*)workspace + up256(((size_t)n + 1) * 4));
   p.ws_total = (int32_t*)((uint8_t*)workspace + 2 * up256(((size_t)n + 1) * 4));
+  p.ws_head = p.ws_total + kPagesThreads;
   p.n = n;
   p.B = s->batch;
   p.NB = s->num_blocks;
@@ -98,7 +99,7 @@ extern "C" {
 
 size_t ooco_pages_workspace_bytes(const ooco_shape_t* s, int32_t num_rows) {
   if (validate_shape(s) || num_rows < 0) return 0;
-  return 2 * up256(((size_t)num_rows + 1) * 4) + kPagesThreads * 4;
+  return 2 * up256(((size_t)num_rows + 1) * 4) + up256((kPagesThreads + 1) * 4);
 }
 
 int ooco_fork_pages(const ooco_shape_t* s, int32_t n, const int32_t* parents, const int32_t* children,

@@ -35,7 +35,7 @@ static PackedLayout packed_layout(const ooco_shape_t* s, int64_t num_rows, int64
   const int64_t decodes = s->batch < num_rows ? s->batch : num_rows;
   int64_t chunks = decodes + 4ll * kPackedGridCap * kPackedDecodeItems / s->num_kv_heads + 1;
   if (chunks > decodes * (longest + 1)) chunks = decodes * (longest + 1);
-  w.max_tiles = (int)(tiles > INT32_MAX / 4 ? INT32_MAX / 4 : tiles);
+  w.max_tiles = (int)tiles;
   w.max_merge = (int)decodes;
   w.max_dec_chunks = (int)chunks;
   w.part_rows[0] = (int)(chunks * s->num_q_heads);
@@ -106,8 +106,11 @@ static int launch_decodes(const CUtensorMap& tk, const CUtensorMap& tv, DecodePa
   return e == cudaSuccess ? OOCO_OK : fail_cuda("launch of the decode attention kernel", (long)e);
 }
 
-static int check_rows(int64_t num_rows, int64_t max_chunk) {
-  if (num_rows < 0 || max_chunk < 0 || max_chunk > num_rows) return OOCO_E_SHAPE;
+static int check_rows(const ooco_shape_t* s, int64_t num_rows, int64_t max_chunk) {
+  if (num_rows < 0 || max_chunk < 0 || max_chunk > num_rows || (num_rows > 0 && max_chunk == 0)) return OOCO_E_SHAPE;
+  // partial rows, tiles and columns are counted in 32 bits
+  if (num_rows * (s->num_q_heads / s->num_kv_heads) > INT32_MAX / 4 || (int64_t)s->batch * s->num_q_heads > INT32_MAX / 4)
+    return OOCO_E_UNSUPPORTED;
   return OOCO_OK;
 }
 
@@ -117,14 +120,13 @@ static int chunk_core(const ooco_shape_t* s, int32_t num_rows, int32_t max_chunk
                       void* out, int64_t out_stride, void* workspace, size_t workspace_bytes, void* cuda_stream) {
   int rc = validate_shape(s);
   if (rc) return rc;
-  if ((rc = check_rows(num_rows, max_chunk))) return rc;
+  if ((rc = check_rows(s, num_rows, max_chunk))) return rc;
   if (!(scale > 0.f) || !(scale <= 3.0e38f)) return OOCO_E_SHAPE;
   if (kv8) {
     if (!(k_scale > 0.f) || !(v_scale > 0.f) || !(k_scale <= 3.0e38f) || !(v_scale <= 3.0e38f)) return OOCO_E_SHAPE;
     if (s->head_dim != 128 || ((s->kv_block_stride | s->kv_head_stride | s->kv_token_stride) & 15)) return OOCO_E_UNSUPPORTED;
   }
   const int64_t row = (int64_t)s->num_q_heads * s->head_dim, G = s->num_q_heads / s->num_kv_heads;
-  if (G * num_rows > INT32_MAX / 2) return OOCO_E_UNSUPPORTED;
   if (!k_cache || !v_cache || !block_table || !context_lens || !first_row || !workspace) return OOCO_E_NULLPTR;
   if (num_rows > 0 && (!q || !out)) return OOCO_E_NULLPTR;
   if (q_stride < row || out_stride < row) return OOCO_E_SHAPE;
@@ -134,7 +136,7 @@ static int chunk_core(const ooco_shape_t* s, int32_t num_rows, int32_t max_chunk
   const bool two = !kv8;
   const PackedLayout w = packed_layout(s, num_rows, max_chunk);
   if (workspace_bytes < w.total || ((uintptr_t)workspace & 255)) return OOCO_E_WORKSPACE;
-  if (num_rows == 0 || max_chunk == 0) return OOCO_OK;
+  if (num_rows == 0) return OOCO_OK;
   int dev = 0;
   if ((rc = current_device(&dev))) return rc;
   const DeviceInfo di = device_info(dev);
@@ -281,9 +283,7 @@ using namespace ooco;
 extern "C" {
 
 size_t ooco_chunk_workspace_bytes(const ooco_shape_t* s, int32_t num_rows, int32_t max_chunk) {
-  if (validate_shape(s) || check_rows(num_rows, max_chunk) ||
-      (int64_t)(s->num_q_heads / s->num_kv_heads) * num_rows > INT32_MAX / 2)
-    return 0;
+  if (validate_shape(s) || check_rows(s, num_rows, max_chunk)) return 0;
   return packed_layout(s, num_rows, max_chunk).total;
 }
 

@@ -28,6 +28,7 @@ struct PagesParams {
   int32_t *copy_src, *copy_dst, *granted, *status;
   int32_t *ws_from, *ws_off;       // [n] first table entry concerned; [n + 1] entries concerned before each
   int32_t *ws_total;               // [CTAs] blocks freed by each
+  int32_t *ws_head;                // [1] free_head as it was (it may be updated in place while late CTAs still need it)
   int32_t n, B, NB, MB, bs_log2, num_free;
   int32_t phase;                   // -1: all phases in this launch, by a cluster of CTAs; else this one, by a grid
 };
@@ -260,7 +261,6 @@ __global__ void __launch_bounds__(kPagesThreads, 1) release_pages_kernel(const P
   grid_dep_wait();
   grid_dep_launch();
   if (t.all || p.phase == 1) pages_copy_shares(p, t.rank * kPagesThreads + tid, t.count * kPagesThreads);
-  const int head0 = min(max(0, *p.free_head), p.num_free);
   if (t.rank == 0 && (t.all || p.phase == 1)) {
     pages_copy_lens(p);
     const RowMaps m = row_maps(s_pages, p.B, false);
@@ -290,7 +290,10 @@ __global__ void __launch_bounds__(kPagesThreads, 1) release_pages_kernel(const P
         p.ws_off[c] = (int)before;
       }
     }
-    if (tid == 0) p.ws_off[p.n] = (int)entries;
+    if (tid == 0) {
+      p.ws_off[p.n] = (int)entries;
+      *p.ws_head = min(max(0, *p.free_head), p.num_free);
+    }
   }
   if (p.phase == 1) return;
   pages_sync(t);
@@ -385,6 +388,7 @@ __global__ void __launch_bounds__(kPagesThreads, 1) release_pages_kernel(const P
     block_scan(tid < t.rank ? v : 0, s_warp, &total);
     before = (int)total;
   }
+  const int head0 = *p.ws_head;
   const int put = min(all, head0), head1 = head0 - put;  // (ids for which the list has no room are dropped)
   int at = before + s_count[wid];
   rounds(false, [&](int g0) {
