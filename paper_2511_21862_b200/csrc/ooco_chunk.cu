@@ -14,6 +14,13 @@ namespace ooco {
 
 static_assert(kPackedStatusRefused == OOCO_STATUS_REFUSED, "status bit");
 
+// Up to this many tokens by the table's width, and pairs per SM by max_chunk, a call is the one-tile kernel alone, whose CTAs then
+// find their pairs by themselves: no plan, decode list or merge, but no cutting of long contexts either.  Measured, without and with
+// a plan (1 to 8 new tokens): 4 sequences of 2 kv heads, up to 1024 or 2048 tokens 20 and 37, 28 and 41 us; 37 of 8 heads 37 and 65,
+// 60 and 90 us; one new token: 28 and 30, 58 and 71 us.  Beyond: 4 sequences of up to 4096 tokens, one new 43 and 32 us; 74 of 8
+// heads, 2048 tokens of an 8-bit cache 101 and 83 us.
+constexpr int64_t kDirectTokens = 2048, kDirectPairsPerSm = 2;
+
 struct PackedLayout {
   size_t off_first, off_tiles, off_before[2], off_start[2], off_order[2], off_dec_first, off_dec_items, off_merge, off_lse, off_o, total;
   int max_tiles, max_merge, max_dec_chunks, max_part_rows, part_rows[2];
@@ -190,6 +197,10 @@ static int chunk_core(const ooco_shape_t* s, int32_t num_rows, int32_t max_chunk
   p.tile_rows = s->block_size < kTc2StageTok ? s->block_size : kTc2StageTok;
   p.scale_log2e = scale * 1.4426950408889634f * (kv8 ? k_scale * kE4m3WidenFactor : 1.f);
   p.v_scale = kv8 ? v_scale * kE4m3WidenFactor : 1.f;
+  // (The checked build has a plan always: its kernels may report before a kernel without one has cleared the status word.)
+  const int64_t direct_tiles = (G * max_chunk + kTcRows - 1) / kTcRows;
+  if (!kChecked && (int64_t)p.MB * p.bs <= kDirectTokens && direct_tiles * p.B * p.Hkv <= kDirectPairsPerSm * di.sm_count)
+    p.direct_tiles = (int)direct_tiles;
   CUtensorMap tk, tv;
   if (kv8) {
     if ((rc = encode_kv8_map(&tk, s, k_cache, p.tile_rows)) || (rc = encode_kv8_map(&tv, s, v_cache, p.tile_rows))) return rc;
@@ -243,6 +254,14 @@ static int chunk_core(const ooco_shape_t* s, int32_t num_rows, int32_t max_chunk
   }
   const int cps = decode_ctas_per_sm(s->head_dim, kv8, G);
   cudaStream_t st = (cudaStream_t)cuda_stream;
+  if (p.direct_tiles) {
+    const int64_t pairs = direct_tiles * p.B * p.Hkv;
+    p.early = 0;
+    if (pairs < p.grid) p.grid = (int)pairs;
+    return kv8 ? launch_packed<128, true, true>(tk, tv, p, di, dev, st, false)
+               : (s->head_dim == 128 ? launch_packed<128, false, true>(tk, tv, p, di, dev, st, false)
+                                     : launch_packed<64, false, true>(tk, tv, p, di, dev, st, false));
+  }
   auto decodes = [&](bool dry) -> int {
     if (kv8) return wide ? launch_decodes<128, 8, 2, 2>(dk, dv, d, di, cps, st, dev, dry) : launch_decodes<128, 8, 1, 2>(dk, dv, d, di, cps, st, dev, dry);
     return s->head_dim == 128 ? launch_decodes<128, 4, 1, 0>(dk, dv, d, di, cps, st, dev, dry)

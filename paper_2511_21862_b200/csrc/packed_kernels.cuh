@@ -13,6 +13,7 @@
 // which is cut into as many pieces of equal length as there are CTAs; a pair that a cut goes through becomes two or more units,
 // whose rows are merged, at most two of them per CTA.  Measured, pulled and cut: 16 or 4 pieces of 480 tokens of prompts beside 48
 // or 60 decodes 432 and 481, 240 and 260 us; one piece of 1024 or 128 tokens of a prompt of 8192, 64 q heads 293 and 284, 164 and 86.
+// Few pairs with short contexts (both known to the host) need none of this: the one-tile kernel alone finds its pairs by itself.
 // The CTA is that of chunk_tc2_kernel (chunk_tc2_kernels.cuh), which has one number of query tokens for all sequences; there
 // also stands why its MMAs, slots and warps are as they are.  What differs: a stage's meta words say all about its unit (rows,
 // columns, partial rows), so that sequences of any lengths share a launch; head_dim 64 has half the slot, twice the slots and half
@@ -83,6 +84,7 @@ struct PackedParams {
   int32_t B, Hq, Hkv, G, D, bs, MB, NB, num_rows, max_chunk;
   int32_t two_tiles;     // 1: more than 128 columns go to the two-tile list
   int32_t decode;        // 1: sequences with one query token go to the decode list
+  int32_t direct_tiles;  // > 0: no plan, no merge: the one-tile kernel alone, this many tiles for every sequence (some may be empty)
   int32_t early;         // one-tile kernel: it may start before the kernel in front of it has ended (see packed_plan_kernel)
   int32_t grid, dec_grid, max_tiles, max_merge, max_part_rows, max_dec_chunks, tile_rows;
   int32_t part_rows[2];  // first partial row of each tile list
@@ -612,6 +614,14 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
   constexpr int kList = kOne ? 0 : 1;
   const long long cap_tokens = (long long)p.MB * p.bs;
 
+  if (kOne && p.direct_tiles > 0 && blockIdx.x == 0 && warp == kWarpM + 1) {
+    // the status word, which no plan has written (any other bit of it comes from a wait of seconds, long after this)
+    bool refused = false;
+    for (int b = lane; b < p.B; b += 32) packed_seq(p, b, &refused);
+    refused = __any_sync(0xffffffffu, refused);
+    if (lane == 0) p.hdr->dec.status = refused ? kPackedStatusRefused : 0;
+    __syncwarp();
+  }
   if (warp == kWarpK) {
     // ================================================================= K producer (and the walk over the units)
     if (lane == 0) prefetch_tmap(&tm_k);
@@ -619,8 +629,9 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
     const uint32_t box_rows_bytes = (uint32_t)p.tile_rows * 128;
     int it = 0;
     bool ok = true, violated = false;
-    const int64_t stages_all = p.hdr->stages[kList];
-    const bool pull = p.hdr->pull[kList];
+    const bool direct = kOne && p.direct_tiles > 0;
+    const int64_t stages_all = direct ? 0 : p.hdr->stages[kList];
+    const bool pull = direct || p.hdr->pull[kList];
     const int pieces = pull || stages_all == 0 ? 0 : p.hdr->pieces[kList];
     int unit = blockIdx.x;  // where pairs are pulled: the next one
     int64_t left = 0;       // else: what is left of the CTA's piece,
@@ -629,7 +640,7 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
       left = packed_cut(stages_all, blockIdx.x + 1, pieces) - packed_cut(stages_all, blockIdx.x, pieces);
       at = p.start[kList][blockIdx.x];
     }
-    const int n_pairs = pull ? p.hdr->pairs[kList] : 0;
+    const int n_pairs = direct ? p.B * p.direct_tiles * p.Hkv : (pull ? p.hdr->pairs[kList] : 0);
     auto table_entry = [&](const int32_t* e) {
       const int v = *e;
       return checked(chk_table_entry(v, p.NB), &p.hdr->dec.status, kStatusBadTableEntry) ? v : p.NB;
@@ -642,14 +653,32 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
     };
     while ((pull ? unit < n_pairs : left > 0) && ok) {
       int nxt = 0;
-      if (pull) {
-        if (lane == 0) nxt = atomicAdd(&p.hdr->next[kList], 1);
-        nxt = __shfl_sync(0xffffffffu, nxt, 0);
-        at = make_int4(p.order[kList][unit / p.Hkv], unit % p.Hkv, 0, 0);
+      PackedTile tile;
+      if (direct) {
+        nxt = unit + gridDim.x;
+        at = make_int4(unit / p.Hkv, unit % p.Hkv, 0, 0);
+        const PackedSeq q = packed_seq(p, at.x / p.direct_tiles);
+        tile.b = at.x / p.direct_tiles;
+        tile.c0 = at.x % p.direct_tiles * kTcRows;
+        tile.first = tile.end = at.x;
+        tile.r0 = q.r0;
+        tile.n = q.n;
+        tile.T = q.T;
+        if (tile.c0 >= p.G * q.n) {
+          unit = nxt;
+          continue;
+        }
+        tile.stages = max(1, (packed_seen(p, tile, kList) + kTc2StageTok - 1) / kTc2StageTok);
+      } else {
+        if (pull) {
+          if (lane == 0) nxt = atomicAdd(&p.hdr->next[kList], 1);
+          nxt = __shfl_sync(0xffffffffu, nxt, 0);
+          at = make_int4(p.order[kList][unit / p.Hkv], unit % p.Hkv, 0, 0);
+        }
+        tile = p.tiles[at.x];
       }
-      const PackedTile tile = p.tiles[at.x];
       if (!checked(chk_item(tile.b, 0, 0, tile.T, p.B, 1, cap_tokens) && chk_span(tile.r0, tile.n, 0, p.num_rows) && tile.stages > 0 &&
-                       chk_index(at.x, p.max_tiles), &p.hdr->dec.status, kStatusBadItem)) {
+                       (direct || chk_index(at.x, p.max_tiles)), &p.hdr->dec.status, kStatusBadItem)) {
         *s_abort = 1;
         violated = true;
         ok = false;

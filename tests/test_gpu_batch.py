@@ -299,13 +299,14 @@ def tolerance(q, k, v, mag, spread, scale, fp8):
 
 
 def run_chunk(new, ctx, *, hq=8, hkv=2, D=128, bs=16, fp8=False, layout="head_major", seed=0, scale=None, pad=3, max_chunk=None,
-              chunk_lens=None, strided=False, spread=1.0, check=True, holes=7):
-    """Runs the call on random data (slots behind a context hold NaN, table padding is out of range) and checks every row."""
+              chunk_lens=None, strided=False, spread=1.0, check=True, holes=7, room=0):
+    """Runs the call on random data (slots behind a context hold NaN, table padding is out of range) and checks every row.
+    room: tokens that the table has room for, if more than the longest context."""
     rng = np.random.default_rng(seed)
     B = len(new)
     scale = scale or 1 / math.sqrt(D)
     held = [-(-max(0, t) // bs) for t in ctx]
-    MB, NB = max(1, max(held)), sum(held) + holes
+    MB, NB = max(1, max(held), room // bs), sum(held) + holes
     perm = rng.permutation(NB)
     table, at = np.full((B, MB), 2 ** 31 - 1), 0
     for b in range(B):
@@ -369,7 +370,8 @@ def run_chunk(new, ctx, *, hq=8, hkv=2, D=128, bs=16, fp8=False, layout="head_ma
     ([1], [1]), ([1], [300]), ([3], [3]), ([1, 1, 1, 1], [17, 64, 130, 256]), ([0, 1, 0, 2], [50, 1, 0, 700]),
     ([5, 1, 40, 0, 33, 1], [5, 900, 41, 77, 1000, 128]), ([70, 1, 130], [70, 2000, 400]), ([7, 2], [3, 0]), ([65], [600])])
 def test_chunk(new, ctx, D, fp8):
-    run_chunk(new, ctx, D=D, fp8=fp8, seed=len(new) + D)
+    for room in (0, 8192):   # narrow tables of few pairs are one launch
+        run_chunk(new, ctx, D=D, fp8=fp8, seed=len(new) + D, room=room)
 
 
 @pytest.mark.parametrize("hq,hkv,D,bs,fp8,layout", [(8, 8, 128, 32, False, "token_major"), (5, 1, 64, 16, False, "head_major"),
@@ -377,13 +379,18 @@ def test_chunk(new, ctx, D, fp8):
                                                     (16, 1, 128, 256, True, "head_major"), (9, 1, 128, 16, False, "head_major"),
                                                     (6, 2, 64, 256, False, "token_major"), (7, 1, 128, 16, True, "head_major")])
 def test_chunk_heads_blocks_layouts(hq, hkv, D, bs, fp8, layout):
-    run_chunk([1, 9, 0, 30, 2], [400, 30, 9, 333, 1], hq=hq, hkv=hkv, D=D, bs=bs, fp8=fp8, layout=layout, seed=hq, strided=True)
+    for room in (0, 8192):
+        run_chunk([1, 9, 0, 30, 2], [400, 30, 9, 333, 1], hq=hq, hkv=hkv, D=D, bs=bs, fp8=fp8, layout=layout, seed=hq, strided=True, room=room)
 
 
 def test_chunk_lens_and_bounds():
-    run_chunk([5, 4, 3, 6], [50, 40, 30, 60], chunk_lens=[2, 9, 0, -1], seed=1)
-    _, _, ws, _ = run_chunk([2, 9, 1, 4], [50, 40, 30, 60], max_chunk=4, seed=2)       # the second brings too many
-    assert binding.workspace_status(ws) == 128
+    for room in (0, 8192):
+        run_chunk([5, 4, 3, 6], [50, 40, 30, 60], chunk_lens=[2, 9, 0, -1], seed=1, room=room)
+        _, call, ws, _ = run_chunk([2, 9, 1, 4], [50, 40, 30, 60], max_chunk=4, seed=2, room=room)   # the second brings too many
+        assert binding.workspace_status(ws) == 128
+        ws.fill_(255)
+        call()
+        assert binding.workspace_status(ws) == 128
 
 
 def test_chunk_splits_long_contexts():
