@@ -83,6 +83,8 @@ struct Counter {
 // biases on the tokens concerned; the largest; weights and their sum; one exchange in the cluster; probabilities.  So logits are
 // read once and probabilities written once, which is what bounds the kernel for many rows, beside the instructions (about 15 a
 // token); few rows are bound by the chain of loads, reductions and the exchange.
+// The largest value is found on the way: over the masked logits as they come and over the values that penalties change.  Only where
+// the second cannot stand for the true one (biases, a largest logit that fell far, a greedy row) are the values gone through again.
 // Sums are fp32: 2^-24 relative a step, over the 20 to 64 values of a thread, a tree of 8 levels, and a tree over the CTAs.
 // kWide: rows of logits and outputs begin on boundaries of four values, so a thread has groups of four neighbours, which every
 // access to shared and global memory moves without conflicts or partial sectors; else single tokens, side by side across the lanes.
@@ -91,13 +93,15 @@ __global__ void __launch_bounds__(kLogitsThreads, 3) shape_logits_kernel(const L
   using C = Counter<kHalf>;
   constexpr int W = kWide ? 4 : 1;
   using G = Group<W>;
-  extern __shared__ uint4 s_dyn[];  // values [share]; with penalties: counters [share], ancestors of the nodes
+  extern __shared__ uint4 s_dyn[];  // values [share]; biases: tokens, places; with penalties: counters [share], ancestors of the nodes
   float* s_val = reinterpret_cast<float*>(s_dyn);
-  uint32_t* s_count = reinterpret_cast<uint32_t*>(s_val + p.share);
+  int* s_bias_token = reinterpret_cast<int*>(s_val + p.share);
+  int* s_bias_at = s_bias_token + ((p.M + 3) & ~3);
+  uint32_t* s_count = reinterpret_cast<uint32_t*>(s_bias_at + ((p.M + 3) & ~3));
   uint32_t* s_above = s_count + (kHalf ? p.share / 2 : p.share);  // [N][words]
-  __shared__ float s_warp[2][kLogitsWarps], s_factor;
+  __shared__ float s_warp[4][kLogitsWarps], s_factor;
   __shared__ Softmax s_rank[2][kLogitsMaxCluster];
-  __shared__ int s_token[kTreeMaxNodes], s_parent[kTreeMaxNodes], s_bias_at[kLogitsMaxBias], s_bias_token[kLogitsMaxBias], s_listed;
+  __shared__ int s_token[kTreeMaxNodes], s_parent[kTreeMaxNodes], s_listed;
   __shared__ uint16_t s_list[kLogitsList];
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
   const int cluster = 1 << p.cluster_log2, runs = (p.N + p.run - 1) / p.run;
@@ -244,16 +248,24 @@ __global__ void __launch_bounds__(kLogitsThreads, 3) shape_logits_kernel(const L
     else
       s_val[i] = x[0];
   };
-  auto reduce = [&](float v, float* s, auto op) {
+  // reductions over the CTA, by a barrier between the two halves
+  auto post = [&](float v, float* s, auto op) {
 #pragma unroll
     for (int o = 16; o; o >>= 1) v = op(v, __shfl_xor_sync(0xffffffffu, v, o));
     if (lane == 0) s[wid] = v;
-    __syncthreads();
-    v = s[lane & (kLogitsWarps - 1)];
+  };
+  auto fetch = [&](const float* s, auto op) {
+    float v = s[lane & (kLogitsWarps - 1)];
 #pragma unroll
     for (int o = kLogitsWarps / 2; o; o >>= 1) v = op(v, __shfl_xor_sync(0xffffffffu, v, o));
     return v;
   };
+  auto reduce = [&](float v, float* s, auto op) {
+    post(v, s, op);
+    __syncthreads();
+    return fetch(s, op);
+  };
+  auto larger = [](float a, float c) { return fmaxf(a, c); };
   // the weight of a logit beside a reference; equal infinite logits have a weight of 1 each, whatever the temperature
   auto weight = [&](float v, float ref) { return v == ref ? 1.f : (v == -INFINITY ? 0.f : ex2((v - ref) * factor)); };
 
@@ -286,9 +298,13 @@ __global__ void __launch_bounds__(kLogitsThreads, 3) shape_logits_kernel(const L
 
   for (int node = node0; node < node1; ++node) {
     // ---- masked logits to shared memory
+    float top = -INFINITY;
     auto finish = [&](int i, G& x, uint32_t allowed) {
 #pragma unroll
-      for (int j = 0; j < W; ++j) x[j] = (allowed >> j) & 1u ? fmaxf(x[j], -INFINITY) : -INFINITY;
+      for (int j = 0; j < W; ++j) {
+        x[j] = (allowed >> j) & 1u ? fmaxf(x[j], -INFINITY) : -INFINITY;
+        top = fmaxf(top, x[j]);
+      }
       put(i, x);
     };
 #pragma unroll
@@ -322,8 +338,13 @@ __global__ void __launch_bounds__(kLogitsThreads, 3) shape_logits_kernel(const L
       const int at = place(s_token[tid]);
       if (at >= 0 && !C::add(s_count, at, 1u)) list(at);
     }
-    if (p.penalties || p.M > 0) __syncthreads();
-    if (p.penalties) {
+    post(top, s_warp[0], larger);
+    __syncthreads();
+    bool exact = p.M == 0;  // top does for a reference
+    if (!p.penalties) {
+      top = fetch(s_warp[0], larger);
+    } else {
+      float changed = -INFINITY;
       const int listed = s_listed;
       const bool all = listed > kLogitsList;  // a share with more tokens than the list holds is walked through
       for (int i = tid; i < (all ? p.share : listed); i += kLogitsThreads) {
@@ -331,9 +352,19 @@ __global__ void __launch_bounds__(kLogitsThreads, 3) shape_logits_kernel(const L
         const uint32_t word = C::read(s_count, at);
         if (!word || (all && token(at) >= p.V)) continue;
         const float x = s_val[at];
-        if (x != -INFINITY) s_val[at] = fmaxf(penalised(x, word & (C::kPrompt - 1), w), -INFINITY);
+        if (x == -INFINITY) continue;
+        const float y = fmaxf(penalised(x, word & (C::kPrompt - 1), w), -INFINITY);
+        s_val[at] = y;
+        changed = fmaxf(changed, y);
       }
-      __syncthreads();
+      changed = reduce(changed, s_warp[1], larger);
+      top = fmaxf(fetch(s_warp[0], larger), changed);
+      // What was the largest may have fallen.  The largest now is then at least the largest of the values changed; if that is near
+      // what was, it does for a reference: no weight is above 2^16, and those that fall below the smallest numbers do not matter.
+      if (listed > 0) {
+        exact = exact && soft && (top - changed) * factor < 16.f;
+        if (exact) top = changed;
+      }
       if (tid == 0) s_listed = listed0;
       if (drafts && tid > 0 && tid <= node && ((s_above[node * words + (tid >> 5)] >> (tid & 31)) & 1u)) {
         const int at = place(s_token[tid]);
@@ -361,15 +392,17 @@ __global__ void __launch_bounds__(kLogitsThreads, 3) shape_logits_kernel(const L
       __syncthreads();
       continue;
     }
-    // ---- softmax: the CTA's own largest logit is its reference, so one exchange between the CTAs does
-    float top = -INFINITY;
-    groups([&](int i, int, auto) {
-      G x;
-      get(i, x);
+    // ---- softmax: a CTA has a reference of its own, at most its largest logit, so one exchange between the CTAs does
+    if (!exact) {  // its largest logit
+      top = -INFINITY;
+      groups([&](int i, int, auto) {
+        G x;
+        get(i, x);
 #pragma unroll
-      for (int j = 0; j < W; ++j) top = fmaxf(top, x[j]);
-    });
-    top = reduce(top, s_warp[0], [](float a, float c) { return fmaxf(a, c); });
+        for (int j = 0; j < W; ++j) top = fmaxf(top, x[j]);
+      });
+      top = reduce(top, s_warp[3], larger);
+    }
     float sum;
     if (soft) {
       sum = 0.f;
@@ -403,7 +436,7 @@ __global__ void __launch_bounds__(kLogitsThreads, 3) shape_logits_kernel(const L
           put(i, x);
         });
       }
-      sum = reduce(sum, s_warp[1], [](float a, float c) { return a + c; });
+      sum = reduce(sum, s_warp[2], [](float a, float c) { return a + c; });
     } else {
       sum = INFINITY;  // the lowest index (below 2^24: exact) of the CTA's largest logit
       groups([&](int i, int v, auto end) {
@@ -414,7 +447,7 @@ __global__ void __launch_bounds__(kLogitsThreads, 3) shape_logits_kernel(const L
         for (int j = 0; j < W; ++j)
           if (x[j] == top && v + j < p.V) sum = fminf(sum, (float)(v + j));
       });
-      sum = reduce(sum, s_warp[1], [](float a, float c) { return fminf(a, c); });
+      sum = reduce(sum, s_warp[2], [](float a, float c) { return fminf(a, c); });
     }
     Softmax all = {top, sum};
     if (exchange) {

@@ -286,10 +286,10 @@ int ooco_shape_logits(const ooco_logits_t* s, const void* logits, const float* t
   p.L = s->history_width;
   p.M = s->max_bias;
   p.penalties = penalties;
-  // CTAs per row: shares of at most 10240 tokens, so that three CTAs fit an SM (256 rows of 152064 tokens in trees of 16: 150 us;
+  // CTAs per row: shares of at most 10240 tokens, so that three CTAs fit an SM (256 rows of 152064 tokens in trees of 16: 143 us;
   // with shares of 20480: 350), and more while the rows alone do not fill the SMs twice and shares of more than 4096 tokens can
   // be halved.  Nodes per cluster: up to 8 share the counting of their text (the same rows: 220 us with 1, 160 with 4, 155 with
-  // 16), as long as there are enough clusters for three CTAs an SM.
+  // 16, each measured beside 150 with 8), as long as there are enough clusters for three CTAs an SM.
   const int64_t blocks = (V + kLogitsBlock - 1) / kLogitsBlock;
   int cluster = 1;
   while (cluster < kLogitsMaxCluster && (V > cluster * 10240ll || (B * N * cluster < 2ll * sms && V > cluster * 4096ll))) {
@@ -300,7 +300,7 @@ int ooco_shape_logits(const ooco_logits_t* s, const void* logits, const float* t
   p.run = 1;
   while (p.run < 8 && p.run < N && B * ((N + 2 * p.run - 1) / (2 * p.run)) * cluster >= 3ll * sms) p.run *= 2;
   const bool half = s->history_width + N < 32768;
-  const size_t smem = (size_t)p.share * 4 + (penalties ? (size_t)p.share * (half ? 2 : 4) + N * ((N + 31) / 32) * 4 : 0);
+  const size_t smem = (size_t)p.share * 4 + (size_t)((p.M + 3) & ~3) * 8 + (penalties ? (size_t)p.share * (half ? 2 : 4) + N * ((N + 31) / 32) * 4 : 0);
   auto aligned = [&](const void* ptr, int64_t seq, int64_t node, int64_t bytes) {
     const int64_t rest = 4 * bytes - 1;
     return !ptr || (!((uintptr_t)ptr & rest) && (B == 1 || !(seq & 3)) && (N == 1 || !(node & 3)));
@@ -315,8 +315,8 @@ int ooco_shape_logits(const ooco_logits_t* s, const void* logits, const float* t
                                shape_logits_kernel<__nv_bfloat16, true, false>, shape_logits_kernel<__nv_bfloat16, true, true>,
                                shape_logits_kernel<float, false, false>, shape_logits_kernel<float, false, true>,
                                shape_logits_kernel<float, true, false>, shape_logits_kernel<float, true, true>};
-  // the most that any call takes: a share's values and whole-word counters, the ancestors of a full tree
-  if ((rc = configure((const void*)kernels[which], done[which], OOCO_MAX_SHAPED_VOCAB / kLogitsMaxCluster * 8 + 8192))) return rc;
+  // the most that any call takes: a share's values and whole-word counters, the biases, the ancestors of a full tree
+  if ((rc = configure((const void*)kernels[which], done[which], OOCO_MAX_SHAPED_VOCAB / kLogitsMaxCluster * 8 + kLogitsMaxBias * 8 + 8192))) return rc;
   const int64_t runs = (N + p.run - 1) / p.run;
   return finish(launch_clustered(kernels[which], dim3((unsigned)(B * runs * cluster)), dim3(kLogitsThreads), smem,
                                  (cudaStream_t)cuda_stream, pdl_enabled(), (unsigned)cluster, p),

@@ -197,9 +197,8 @@ static int chunk_core(const ooco_shape_t* s, int32_t num_rows, int32_t max_chunk
   p.tile_rows = s->block_size < kTc2StageTok ? s->block_size : kTc2StageTok;
   p.scale_log2e = scale * 1.4426950408889634f * (kv8 ? k_scale * kE4m3WidenFactor : 1.f);
   p.v_scale = kv8 ? v_scale * kE4m3WidenFactor : 1.f;
-  // (The checked build has a plan always: its kernels may report before a kernel without one has cleared the status word.)
   const int64_t direct_tiles = (G * max_chunk + kTcRows - 1) / kTcRows;
-  if (!kChecked && (int64_t)p.MB * p.bs <= kDirectTokens && direct_tiles * p.B * p.Hkv <= kDirectPairsPerSm * di.sm_count)
+  if ((int64_t)p.MB * p.bs <= kDirectTokens && direct_tiles * p.B * p.Hkv <= kDirectPairsPerSm * di.sm_count)
     p.direct_tiles = (int)direct_tiles;
   CUtensorMap tk, tv;
   if (kv8) {
@@ -258,6 +257,10 @@ static int chunk_core(const ooco_shape_t* s, int32_t num_rows, int32_t max_chunk
     const int64_t pairs = direct_tiles * p.B * p.Hkv;
     p.early = 0;
     if (pairs < p.grid) p.grid = (int)pairs;
+    if (kChecked) {  // any CTA may report before the first has written the status word
+      const cudaError_t e = cudaMemsetAsync(&p.hdr->dec.status, 0, sizeof(p.hdr->dec.status), st);
+      if (e != cudaSuccess) return fail_cuda("clearing the status word", (long)e);
+    }
     return kv8 ? launch_packed<128, true, true>(tk, tv, p, di, dev, st, false)
                : (s->head_dim == 128 ? launch_packed<128, false, true>(tk, tv, p, di, dev, st, false)
                                      : launch_packed<64, false, true>(tk, tv, p, di, dev, st, false));

@@ -619,7 +619,8 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
     bool refused = false;
     for (int b = lane; b < p.B; b += 32) packed_seq(p, b, &refused);
     refused = __any_sync(0xffffffffu, refused);
-    if (lane == 0) p.hdr->dec.status = refused ? kPackedStatusRefused : 0;
+    const int word = refused ? kPackedStatusRefused : 0;
+    if (lane == 0) kChecked ? (void)atomicOr(&p.hdr->dec.status, word) : (void)(p.hdr->dec.status = word);  // (checked: cleared by the host)
     __syncwarp();
   }
   if (warp == kWarpK) {

@@ -531,9 +531,10 @@ def run_logits(B, N, V, *, dtype=torch.bfloat16, pen=True, bias=0, mask=True, tr
                 got = host(p[b, i])
                 assert not np.isnan(got).any()
                 if T > 0:
-                    # the exponent: off by 2 err / T and by three roundings of (l - top) / T; exp, sum and quotient: 2^-19
+                    # the exponent: off by 2 err / T and by three roundings of (l - r) / T, where r may lie 16 binary orders (11.1
+                    # in units of T) beside the largest; exp, sum and quotient: 2^-19
                     d = np.where(prob > 0, -np.log(np.maximum(prob, 1e-300) / max(prob.max(), 1e-300)), 0)
-                    rel = np.expm1(2 * err / T + 3 * 2.0 ** -24 * d) + 2.0 ** -19
+                    rel = np.expm1(2 * err / T + 3 * 2.0 ** -24 * (d + 11.1)) + 2.0 ** -19
                     assert (np.abs(got - prob) <= rel * prob + 1e-37).all(), (b, i)
                 else:
                     assert np.array_equal(got, prob)
@@ -549,6 +550,39 @@ def run_logits(B, N, V, *, dtype=torch.bfloat16, pen=True, bias=0, mask=True, tr
     (2, 4, 777, dict(dtype=torch.float32, in_place="out", probs=True)), (2, 4, 1024, dict(dtype=torch.float32, in_place="probs"))])
 def test_logits(B, N, V, kw):
     run_logits(B, N, V, seed=B + V, **kw)
+
+
+@pytest.mark.parametrize("V", [700, 40000])
+def test_logits_whose_largest_falls(V):
+    """The largest logit is named by the text and falls a little, far, to just above the rest, or behind everything; or it rises."""
+    falls = [0.0, 1.0, 9.0, 20.0, 26.0, 27.5, 60.0, 300.0, -5.0, float("inf")]
+    B = len(falls)
+    g = torch.Generator().manual_seed(V)
+    x = torch.randn((B, V), generator=g)
+    x[:, 5] = 30.0
+    x[1, 17] = 29.5
+    text = torch.tensor([5, 40, 77, 5, 300])
+    pres = torch.tensor(falls)
+    out, probs = torch.empty((B, V), device=DEV), torch.empty((B, V), device=DEV)
+    for temp in (0.25, 1.0, 0.0):
+        t = torch.full((B,), temp)
+        batch.shape_logits(x.to(DEV), temperature=t.to(DEV), presence=pres.to(DEV), history=gpu(text.repeat(B, 1)),
+                           history_lens=gpu([5] * B), out=out, probs=probs)
+        want = x.double().clone()
+        want[:, text.unique()] -= pres.double()[:, None]
+        want[torch.isnan(want)] = -math.inf
+        got, p = host(out), host(probs)
+        fin = np.isfinite(want.numpy())
+        assert np.array_equal(np.isfinite(got), fin)
+        assert (np.abs(got[fin] - want.numpy()[fin]) <= 2.0 ** -24 * 330).all()           # one rounding of at most 330
+        if temp == 0.0:
+            assert np.array_equal(p.argmax(-1), got.argmax(-1)) and (p.sum(-1) == 1).all()
+            continue
+        z = torch.from_numpy(got).double() / temp                                       # of the logits as they were rounded
+        prob = torch.softmax(z, -1).numpy()
+        d = np.where(prob > 0, (z.max(-1, keepdim=True).values - z).numpy(), 0)
+        rel = np.expm1(3 * 2.0 ** -24 * (d + 11.1)) + 2.0 ** -19                     # as in run_logits
+        assert (np.abs(p - prob) <= rel * prob + 1e-37).all()
 
 
 def test_logits_equal_runs_and_shared_masks():

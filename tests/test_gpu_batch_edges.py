@@ -180,18 +180,21 @@ def test_two_chunk_calls_at_once_with_workspaces_of_their_own():
 
 def test_checked_build_agrees():
     build.build(checked=True)
-    plain = t.run_chunk([1, 40, 0, 200, 3], [900, 300, 7, 200, 64], seed=8)[0]
+    rooms = (0, 8192)   # one launch, and with a plan
+    plain = [t.run_chunk([1, 40, 0, 200, 3], [900, 300, 7, 200, 64], seed=8, room=room)[0] for room in rooms]
     old = binding.use_library(build.LIB_CHECKED)
     try:
-        assert torch.equal(plain, t.run_chunk([1, 40, 0, 200, 3], [900, 300, 7, 200, 64], seed=8)[0])
+        for want, room in zip(plain, rooms):
+            assert torch.equal(want, t.run_chunk([1, 40, 0, 200, 3], [900, 300, 7, 200, 64], seed=8, room=room)[0])
         t.run_chunk([1, 9, 1], [700, 80, 3000], fp8=True, seed=9)
         # a table entry outside the pool reads as zeros and is reported
-        sh = pool_shape(1, 4, 4, 128, 16, 5, 2)
         kc, vc = (torch.ones((5, 4, 16, 128), dtype=torch.bfloat16, device=DEV) for _ in range(2))
         q, out = torch.ones((20, 4, 128), dtype=torch.bfloat16, device=DEV), torch.empty((20, 4, 128), dtype=torch.bfloat16, device=DEV)
-        ws = torch.empty(batch.chunk_workspace_bytes(sh, 20, 20), dtype=torch.uint8, device=DEV)
-        batch.chunk_attention(sh, q, kc, vc, gpu([[99, 1]]), gpu([20]), gpu([0, 20]), 20, 0.1, out, ws)
-        assert binding.workspace_status(ws) & 8 and not out[:16].any()
+        for width in (2, 512):
+            sh = pool_shape(1, 4, 4, 128, 16, 5, width)
+            ws = torch.empty(batch.chunk_workspace_bytes(sh, 20, 20), dtype=torch.uint8, device=DEV)
+            batch.chunk_attention(sh, q, kc, vc, gpu([[99, 1] + [0] * (width - 2)]), gpu([20]), gpu([0, 20]), 20, 0.1, out, ws)
+            assert binding.workspace_status(ws) & 8 and not out[:16].any()
     finally:
         binding.use_library(old if old != build.LIB_CHECKED else None)
 
@@ -200,10 +203,10 @@ def test_first_rows_that_overlap_or_run_over_are_harmless():
     """Rows outside the tensor do not exist, counts below zero are zero, and rows that several sequences claim stay inside it."""
     hq, hkv, D, bs = 4, 2, 128, 16
     kc, vc = (torch.randn((8, hkv, bs, D), device=DEV).to(torch.bfloat16) for _ in range(2))
-    sh = pool_shape(4, hq, hkv, D, bs, 8, 2)
-    table = gpu(np.arange(8).reshape(4, 2))
     q = torch.randn((12, hq, D), device=DEV).to(torch.bfloat16)
-    for first in ([-5, 3, 1, 9, 12], [0, 100, 2, 2 ** 31 - 1, 5], [0, 12, 0, 12, 0], [11, 12, 13, 14, 15], [5, 4, 3, 2, 1]):
+    firsts = [-5, 3, 1, 9, 12], [0, 100, 2, 2 ** 31 - 1, 5], [0, 12, 0, 12, 0], [11, 12, 13, 14, 15], [5, 4, 3, 2, 1]
+    for first, width in [(f, w) for f in firsts for w in (2, 512)]:
+        sh, table = pool_shape(4, hq, hkv, D, bs, 8, width), gpu(np.pad(np.arange(8).reshape(4, 2), ((0, 0), (0, width - 2))))
         wide = torch.full((14, hq, D), 7.0, dtype=torch.bfloat16, device=DEV)
         ws = torch.empty(batch.chunk_workspace_bytes(sh, 12, 12), dtype=torch.uint8, device=DEV)
         batch.chunk_attention(sh, q, kc, vc, table, gpu([20, 32, 9, 1]), gpu(first), 12, 0.1, wide[1:13], ws)
