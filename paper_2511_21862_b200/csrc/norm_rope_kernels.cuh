@@ -12,7 +12,10 @@ struct HeadNormParams {
 // The work is cut as in rope_append_kernel: a unit is 16 dims of one head of one token, two 16-byte pieces (with the halves
 // layout the two members of eight pairs).  Consecutive lanes hold the units of a head, so a head's sum of squares is the sum
 // over 16 values of a thread and a butterfly over its D / 16 lanes, in 32 bits; and since a thread keeps its place in the head
-// from unit to unit, it finds the weights of its 16 dims at a place of its own.  Bound by HBM: q, k and v are read and written once.
+// from unit to unit, it finds the weights of its 16 dims at a place of its own.  Bound by HBM and, nearly as much, by issue slots: q, k
+// and v are read and written once, sums and rotations run on pairs of fp32 values.  Tokens of 64 q and 8 kv heads of 128: 16384 over
+// a bf16 cache 122 us, 5.5 TB/s, and over codes 129 us, 5.0 TB/s; 158 when lanes' weights, cosines and sines met in the banks
+// of shared memory, 135 with single operations; 64 tokens 4.6 us, a launch and two trips to memory.
 template <int D, bool KV8>
 __global__ void __launch_bounds__(kRopeThreads, 4) norm_rope_append_kernel(const RopeParams p, const HeadNormParams hn,
                                                                         const int interleaved) {
