@@ -81,9 +81,9 @@ struct Counter {
 // share, which is cheaper than sending counts through the cluster; tokens that it meets are listed, so that the arithmetic of the
 // penalties runs with full warps.  Then, for each node: the masked logits to shared memory, one word a token; penalties and
 // biases on the tokens concerned; the largest; weights and their sum; one exchange in the cluster; probabilities.  So logits are
-// read once and probabilities written once, which is what bounds the kernel for many rows, beside the instructions and,
-// with clusters of 16, the SMs that hold none (256 rows of 152064 in trees of 16: 141 us, 1.7 TB/s); few rows are bound by the chain of loads, reductions and the exchange (4 rows of 128256:
-// 12 us).
+// read once and probabilities written once.  Many rows are bound by instructions, by the chain of a node's steps and, with clusters
+// of 16, by the SMs that hold none (256 rows of 152064 in trees of 16: 141 us, 1.7 TB/s), few rows by the chain of loads, reductions
+// and the exchange (4 rows of 128256: 12 us).
 // The largest value is found on the way: over the masked logits as they come and over the values that penalties change.  Only where
 // the second cannot stand for the true one (biases, a largest logit that fell far, a greedy row) are the values gone through again.
 // Sums are fp32: 2^-24 relative a step, over the up to 100 values of a thread, a tree of 8 levels, and a tree over the CTAs.

@@ -299,7 +299,7 @@ __global__ void __launch_bounds__(kPagesThreads, 1) release_pages_kernel(const P
   pages_sync(t);
   const Entries e = load_entries(p, reinterpret_cast<int32_t*>(s_pages), t);
   const bool once = e.last - e.first <= 32 * kPagesRound;  // (of the warp's first lane, which has the most: else ids are loaded anew)
-  const bool one_round = __shfl_sync(0xffffffffu, once ? 1 : 0, 0) && t.all;
+  const bool one_round = __shfl_sync(0xffffffffu, once ? 1 : 0, 0);
   int id[kPagesRound];  // blocks of a round's entries; -1: none, or outside the pool
   bool bad = false;
   int owner = 0;
@@ -338,7 +338,7 @@ __global__ void __launch_bounds__(kPagesThreads, 1) release_pages_kernel(const P
   }
   pages_sync(t);
   if (t.all || p.phase == 3) {
-    rounds(false, [&](int g0) {
+    rounds(!t.all, [&](int g0) {
       look();
 #pragma unroll
       for (int k = 0; k < kPagesRound; ++k)
@@ -348,7 +348,7 @@ __global__ void __launch_bounds__(kPagesThreads, 1) release_pages_kernel(const P
   if (p.phase == 2 || p.phase == 3) return;
   pages_sync(t);
   int mine = 0;  // of the warp
-  rounds(false, [&](int g0) {
+  rounds(!t.all, [&](int g0) {
     look();
 #pragma unroll
     for (int k = 0; k < kPagesRound; ++k) mine += __popc(__ballot_sync(0xffffffffu, left[k] == g0 + 32 * k + INT32_MIN));
