@@ -28,6 +28,34 @@ static int configure(const void* kern, std::atomic<int>* done, int smem) {
   return OOCO_OK;
 }
 
+// Clusters of the logits kernel that run at a time on the current device.  The last answer is kept (device, size, memory and answer in
+// one word): the question takes the host longer than a launch.
+static int64_t resident_clusters(const void* kern, std::atomic<uint64_t>& kept, int cluster_log2, size_t smem, int sms) {
+  int dev = 0;
+  cudaGetDevice(&dev);
+  const uint64_t key = ((uint64_t)dev << 40 | (uint64_t)cluster_log2 << 32 | (uint64_t)smem) << 16;
+  const uint64_t had = kept.load();
+  if ((had & ~0xffffull) == key && (had & 0xffff)) return (int64_t)(had & 0xffff);
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = 1u << cluster_log2;
+  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(1u << cluster_log2);
+  cfg.blockDim = dim3(kLogitsThreads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  int n = 0;
+  if (cudaOccupancyMaxActiveClusters(&n, kern, &cfg) != cudaSuccess || n < 1) {
+    cudaGetLastError();
+    return sms >> cluster_log2 > 0 ? sms >> cluster_log2 : 1;  // (a share of the work for every CTA is all that hangs on it)
+  }
+  if (n > 0xffff) n = 0xffff;
+  kept.store(key | (uint64_t)n);
+  return n;
+}
+
 static int check_pages(const ooco_shape_t* s, int32_t n, int32_t num_free, const void* workspace, size_t workspace_bytes) {
   int rc = validate_shape(s);
   if (rc) return rc;
@@ -286,10 +314,10 @@ int ooco_shape_logits(const ooco_logits_t* s, const void* logits, const float* t
   p.L = s->history_width;
   p.M = s->max_bias;
   p.penalties = penalties;
-  // CTAs per row: shares of at most 10240 tokens, so that three CTAs fit an SM (256 rows of 152064 tokens in trees of 16: 143 us;
-  // with shares of 20480: 350), and more while the rows alone do not fill the SMs twice and shares of more than 4096 tokens can
-  // be halved.  Nodes per cluster: up to 8 share the counting of their text (the same rows: 220 us with 1, 160 with 4, 155 with
-  // 16, each measured beside 150 with 8), as long as there are enough clusters for three CTAs an SM.
+  // CTAs per row: shares of at most 10240 tokens, so that three CTAs fit an SM (256 rows of 152064 tokens in trees of 16: 116 us; an
+  // earlier form took 150, and 350 with shares of 20480), and more while the rows alone do not fill the SMs twice and shares of
+  // more than 4096 tokens can be halved.  As many clusters as run at a time have equal parts of the rows: the text of a sequence is
+  // counted once per part, and no cluster is left for a second wave (the same rows, a launch of 8 nodes per cluster: 133 us).
   const int64_t blocks = (V + kLogitsBlock - 1) / kLogitsBlock;
   int cluster = 1;
   while (cluster < kLogitsMaxCluster && (V > cluster * 10240ll || (B * N * cluster < 2ll * sms && V > cluster * 4096ll))) {
@@ -297,8 +325,6 @@ int ooco_shape_logits(const ooco_logits_t* s, const void* logits, const float* t
     ++p.cluster_log2;
   }
   p.share = (int)((blocks + cluster - 1) / cluster * kLogitsBlock);
-  p.run = 1;
-  while (p.run < 8 && p.run < N && B * ((N + 2 * p.run - 1) / (2 * p.run)) * cluster >= 3ll * sms) p.run *= 2;
   const bool half = s->history_width + N < 32768;
   const size_t smem = (size_t)p.share * 4 + (size_t)((p.M + 3) & ~3) * 8 + (penalties ? (size_t)p.share * (half ? 2 : 4) + N * ((N + 31) / 32) * 4 : 0);
   auto aligned = [&](const void* ptr, int64_t seq, int64_t node, int64_t bytes) {
@@ -309,6 +335,7 @@ int ooco_shape_logits(const ooco_logits_t* s, const void* logits, const float* t
                     aligned(out_logits, s->out_seq_stride, s->out_node_stride, 4) &&
                     aligned(out_probs, s->probs_seq_stride, s->probs_node_stride, 4);
   static std::atomic<int> done[8][64];
+  static std::atomic<uint64_t> resident_at[8];
   const int which = (s->logits_fp32 ? 4 : 0) + (wide ? 2 : 0) + (half ? 1 : 0);
   using K = void (*)(LogitsParams);
   static const K kernels[8] = {shape_logits_kernel<__nv_bfloat16, false, false>, shape_logits_kernel<__nv_bfloat16, false, true>,
@@ -317,8 +344,9 @@ int ooco_shape_logits(const ooco_logits_t* s, const void* logits, const float* t
                                shape_logits_kernel<float, true, false>, shape_logits_kernel<float, true, true>};
   // the most that any call takes: a share's values and whole-word counters, the biases, the ancestors of a full tree
   if ((rc = configure((const void*)kernels[which], done[which], OOCO_MAX_SHAPED_VOCAB / kLogitsMaxCluster * 8 + kLogitsMaxBias * 8 + 8192))) return rc;
-  const int64_t runs = (N + p.run - 1) / p.run;
-  return finish(launch_clustered(kernels[which], dim3((unsigned)(B * runs * cluster)), dim3(kLogitsThreads), smem,
+  const int64_t resident = resident_clusters((const void*)kernels[which], resident_at[which], p.cluster_log2, smem, sms);
+  const int64_t clusters = B * N < resident ? B * N : resident;
+  return finish(launch_clustered(kernels[which], dim3((unsigned)(clusters * cluster)), dim3(kLogitsThreads), smem,
                                  (cudaStream_t)cuda_stream, pdl_enabled(), (unsigned)cluster, p),
                 "launch of the logits kernel");
 }

@@ -3,7 +3,7 @@
 // this concerns; then all warps share the entries evenly, 16 of them in the registers of a lane at a time.  Few entries are bound
 // by latency (dependent trips to memory): one launch of one CTA, or of a thread-block cluster whose barriers order the phases.
 // Many are bound by the rate at which an SM sends scattered atomics and loads to L2: a launch per phase, on all SMs (176000 entries
-// of 512 rows given back: 39 us, 62 in a cluster of 16 CTAs; 512 forks of prefixes of 32 rows: 14 and 24; a few forks or rows: 7 to 10).
+// of 512 rows given back: 33 us, 62 in a cluster of 16 CTAs; 512 forks of prefixes of 32 rows: 14 and 24; a few forks or rows: 7 to 10).
 #pragma once
 #include <cuda_runtime.h>
 #include <stdint.h>

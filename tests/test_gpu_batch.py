@@ -547,6 +547,7 @@ def run_logits(B, N, V, *, dtype=torch.bfloat16, pen=True, bias=0, mask=True, tr
     (3, 2, 50257, dict(special=True)), (2, 3, 1000, dict(pen=False)), (2, 3, 1000, dict(pen=False, mask=False, temperature=False)),
     (2, 3, 4099, dict(out=False)), (2, 3, 4099, dict(probs=False)), (3, 1, 4096, dict(pad=5)), (3, 1, 4096, dict(pad=8, L=1)),
     (1, 2, 300000, dict(L=100)), (1, 1, 409600, dict(mask=False, bias=3, L=40000)), (320, 1, 200, dict(bias=1, dtype=torch.float32)),
+    (330, 3, 300, dict(bias=2, sizes=[i % 4 for i in range(330)])), (90, 7, 4097, dict(L=30, out=False)),   # more rows than fit the GPU at a time
     (2, 4, 777, dict(dtype=torch.float32, in_place="out", probs=True)), (2, 4, 1024, dict(dtype=torch.float32, in_place="probs"))])
 def test_logits(B, N, V, kw):
     run_logits(B, N, V, seed=B + V, **kw)
@@ -607,6 +608,28 @@ def test_logits_greedy_ties_and_odd_temperatures():
         assert p[r, 300] == 1 and p[r].sum() == 1
     assert torch.allclose(p[3], torch.full((1000,), 1e-3, device=DEV), rtol=1e-5)
     assert p[4, 300] == 0.5 and p[4, 700] == 0.5 and p[4].sum() == 1
+
+
+def test_logits_huge_values_and_temperatures():
+    """Products of logit and factor that overflow, infinite logits at an infinite temperature; in one CTA and across a cluster."""
+    inf = float("inf")
+    for V in (8, 30000):
+        x = torch.full((6, V), -3e38, device=DEV)
+        x[:, 1], x[:, V - 2], x[:, 3] = 3e38, 3e38, 1.0
+        x[2, 5] = inf
+        x[3, 5], x[4, 5] = inf, 2.9e38
+        t = torch.tensor([0.25, 1.0, inf, 0.25, 1e37, inf], device=DEV)
+        p = torch.empty_like(x)
+        batch.shape_logits(x, probs=p, temperature=t)
+        assert not torch.isnan(p).any()
+        for row in (0, 1):
+            assert p[row, 1] == 0.5 and p[row, V - 2] == 0.5 and p[row].sum() == 1
+        for row in (2, 3):
+            assert p[row, 5] == 1 and p[row].sum() == 1
+        want = torch.softmax(x[4].double() / t[4].double(), 0)
+        # differences of exponents of up to 87 binary orders: factor and difference rounded, 2 * 2^-24 * 87 * ln 2 = 7.2e-6; exp, sum, quotient 2^-19
+        assert torch.allclose(p[4].double(), want, rtol=1e-5, atol=1e-37)
+        assert torch.allclose(p[5], torch.full_like(p[5], 1.0 / V), rtol=1e-5)
 
 
 # ------------------------------------------------------------------------------------------------ together
