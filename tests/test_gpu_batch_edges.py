@@ -212,3 +212,22 @@ def test_first_rows_that_overlap_or_run_over_are_harmless():
         batch.chunk_attention(sh, q, kc, vc, table, gpu([20, 32, 9, 1]), gpu(first), 12, 0.1, wide[1:13], ws)
         torch.cuda.synchronize()
         assert (wide[0] == 7).all() and (wide[13] == 7).all()
+
+
+def test_logits_of_a_new_size_are_captured():
+    """The first call of a size is the captured one; its replays read new logits."""
+    x = torch.randn((50, 6, 70001), device=DEV)
+    p = torch.empty_like(x)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=s):
+        batch.shape_logits(x, probs=p, presence=torch.ones(50, device=DEV), history=torch.zeros((50, 4), dtype=torch.int32, device=DEV),
+                           history_lens=torch.full((50,), 4, dtype=torch.int32, device=DEV))
+    for _ in range(2):
+        x.normal_()
+        g.replay()
+        want = x.double()
+        want[..., 0] -= 1
+        # exponents of up to 12 nats, two roundings of 2^-24 * 12 and the penalised logit's; exp, sum, quotient 2^-19
+        assert torch.allclose(p.double(), torch.softmax(want, -1), rtol=1e-5, atol=0)
