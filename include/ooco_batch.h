@@ -172,7 +172,9 @@ int ooco_shape_logits(const ooco_logits_t* shape, const void* logits, const floa
  *   q, out         device, bf16 [num_rows, Hq, head_dim], rows q_stride (out_stride) elements apart: multiples of 8, at
  *                  least the row's length; they share no memory (OOCO_E_SHAPE)
  *   first_row      device, int32 [B + 1]; chunk_lens: device, int32 [B] or NULL.  (ooco_plan_slots writes first_token,
- *                  granted_lens, and total_lens for context_lens.)  Rows of different sequences are distinct
+ *                  granted_lens, and total_lens for context_lens.)  Rows of different sequences are distinct: where claims
+ *                  of the same rows need more room than the workspace has for num_rows, all sequences, or all with one
+ *                  new token, are passed over, and the status word is 1 (work list overflow)
  *   workspace      >= ooco_chunk_workspace_bytes(shape, num_rows, max_chunk), 256-byte aligned, read by
  *                  ooco_workspace_status
  * num_rows = 0 launches nothing.  Slots at or beyond T_b, table entries behind the last block used, and entries outside

@@ -337,7 +337,8 @@ __global__ void __launch_bounds__(1024) packed_plan_kernel(const PackedParams p,
     }
   }
   // ---- decode list
-  int n_merge = 0, merge_rows = 0, n_items = 0;
+  int merge_rows = 0, n_items = 0;
+  bool dec_overflow = false;
   if (decodes) {
     const long long ctas = (long long)p.dec_grid * kPackedDecodeItems;
     const int longest = max(kPackedMinStages, (int)((s_sum * p.Hkv + ctas - 1) / ctas));
@@ -373,14 +374,19 @@ __global__ void __launch_bounds__(1024) packed_plan_kernel(const PackedParams p,
       atomicAdd(&s_hist[bucket(t.stages - (nch - 1) * len)], 1);
       if (nch > 1 && m < p.max_merge) p.merge[m] = make_int4(t.r0, 0, nch, chunk * p.Hq);
     });
-    n_items = (int)(run >> 32);
-    n_merge = min((int)(run & 0xffffffff), p.max_merge);
-    merge_rows = n_merge * p.Hq;
-    places();
-    visit(true, [&](const PackedTile& t, int nch, int len, int chunk, int) {
+    // Rows that several sequences claim: more chunks, or more sequences in several, than the workspace was sized for by the rows.
+    // Partial rows would lie behind its end, so the list is dropped as a whole, as too many tiles are.
+    const int cut_sequences = (int)(run & 0xffffffff);
+    dec_overflow = run >> 32 > p.max_dec_chunks || cut_sequences > p.max_merge;
+    if (!dec_overflow) {
+      n_items = (int)(run >> 32);
+      merge_rows = cut_sequences * p.Hq;
+      places();
+    }
+    if (!dec_overflow) visit(true, [&](const PackedTile& t, int nch, int len, int chunk, int) {
       for (int c = 0; c < nch; ++c) {
         const int at = atomicAdd(&s_hist[bucket(min(len, t.stages - c * len))], 1);
-        if (!checked(chk_index(at, p.max_dec_chunks), &p.hdr->dec.status, kStatusBadIndex) || at >= p.max_dec_chunks) continue;
+        if (!checked(chk_index(at, p.max_dec_chunks), &p.hdr->dec.status, kStatusBadIndex)) continue;
         const int t0 = c * len * kTc2StageTok;
         for (int h = 0; h < p.Hkv; ++h)
           p.dec_items[(size_t)at * p.Hkv + h] = make_int4(t.b, (chunk + c) * p.Hkv + h, t0, min(t.T, t0 + len * kTc2StageTok));
@@ -388,8 +394,8 @@ __global__ void __launch_bounds__(1024) packed_plan_kernel(const PackedParams p,
     });
   }
   if (tid == 0) {
-    p.hdr->dec.status = (overflow ? kStatusPlanOverflow : 0) | (refused ? kPackedStatusRefused : 0);
-    p.hdr->dec.n_items = min(n_items, p.max_dec_chunks) * p.Hkv;
+    p.hdr->dec.status = (overflow || dec_overflow ? kStatusPlanOverflow : 0) | (refused ? kPackedStatusRefused : 0);
+    p.hdr->dec.n_items = n_items * p.Hkv;
     p.hdr->dec.next_item = p.dec_grid;
     p.hdr->merge_rows = merge_rows;
   }
