@@ -1091,23 +1091,49 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
     float m_ref[2] = {-INFINITY, -INFINITY};  // reference maximum per row (scaled, log2 domain)
     float l_part[2] = {0.f, 0.f};             // this thread's share of the row's sum of weights
     int lim_row[2] = {0, 0};
-    uint32_t n_unit = 0;  // units in which this tile had rows
+    // Units in which this tile had rows, times kUnit; below that, 127 + the binary orders that the warp's rows of Q were lowered by
+    // (load_q).  One register for both, and one number for all rows of the warp: kept apart, or by rows, the loop over the stages
+    // took 11 and 16 % longer over the 8-bit cache.
+    constexpr uint32_t kUnit = 512;
+    uint32_t n_unit = 127;
     bool ok = true;
     bool q_ahead = false;  // the Q rows of the unit that starts with the next stage are in shared memory already
     // Q of the tile's columns from c0_ on, of a sequence whose rows of q begin at row0_, into the swizzled K-major tile
-    // ([half][row][64 dims], 16-byte chunk ^= row & 7): thread i of the tile writes half of row i >> 1; then the q-ready
-    // arrival
+    // ([half][row][64 dims], 16-byte chunk ^= row & 7): a warp writes its own 16 rows, two lanes a row; then the q-ready
+    // arrival.  KV8: f16 ends at 65504 and has 11 bits down to 2^-14, bf16 goes far beyond, so a warp's rows are moved by the power of
+    // two that brings the largest of their values to 2^15, which the scale of their scores takes back.  A value x is off by at most
+    // 2^-11 |x|, or half a step of the smallest f16 numbers: 2^-40 of that largest one, 2^-125 where that is below 2^-85.
     auto load_q = [&](int row0_, int h_, int c0_, int columns_) {
-      const int r_ = tid_t >> 1, part_ = tid_t & 1;
+      const int r_ = 32 * q4 + 16 * hf + (lane >> 1), part_ = lane & 1;
       const int col_ = c0_ + t * kTcRows + tile_col(r_);
       const int qi_ = col_ / p.G, head_ = col_ - qi_ * p.G;
       const bool real_ = col_ < columns_;
       const uint4* src = reinterpret_cast<const uint4*>(p.q + (int64_t)(row0_ + (real_ ? qi_ : 0)) * p.q_stride +
                                                         (int64_t)(h_ * p.G + (real_ ? head_ : 0)) * D + part_ * (D / 2));
+      uint4 w_[D / 16];
+#pragma unroll
+      for (int c = 0; c < D / 16; ++c) w_[c] = real_ ? src[c] : make_uint4(0u, 0u, 0u, 0u);
+      float factor = 1.f;
+      if (KV8) {
+        uint32_t top = 0u;  // the largest magnitude, as bits: of the even and of the odd dims, then of the warp's rows
+#pragma unroll
+        for (int c = 0; c < D / 16; ++c)
+          top = __vmaxu2(top, __vmaxu2(__vmaxu2(w_[c].x & 0x7fff7fffu, w_[c].y & 0x7fff7fffu),
+                                       __vmaxu2(w_[c].z & 0x7fff7fffu, w_[c].w & 0x7fff7fffu)));
+        top = max(top & 0xffffu, top >> 16);
+        top = __reduce_max_sync(0xffffffffu, top);
+        const int e = (int)(top >> 7) - 127;  // 2^e <= the largest value < 2^(e + 1)
+        const int shift = top ? max(e - 15, -100) : 0;  // (-100: the scores and their scale stay far from the ends of fp32)
+        factor = __uint_as_float((uint32_t)(127 - shift) << 23);
+        n_unit = (n_unit & ~(kUnit - 1)) | (uint32_t)(127 + shift);
+      }
 #pragma unroll
       for (int c = 0; c < D / 16; ++c) {
-        uint4 v = real_ ? src[c] : make_uint4(0u, 0u, 0u, 0u);
-        if (KV8) v = make_uint4(bf16x2_to_f16x2(v.x), bf16x2_to_f16x2(v.y), bf16x2_to_f16x2(v.z), bf16x2_to_f16x2(v.w));
+        uint4 v = w_[c];
+        if (KV8) {
+          auto narrow = [&](uint32_t x) { return pack_f16x2(bf16_lo(x) * factor, bf16_hi(x) * factor); };
+          v = make_uint4(narrow(v.x), narrow(v.y), narrow(v.z), narrow(v.w));
+        }
         const int cc = part_ * (D / 16) + c;
         *reinterpret_cast<uint4*>(q_gen + (size_t)(cc >> 3) * kTc2HalfBytes + (size_t)r_ * 128 + (((cc & 7) ^ (r_ & 7)) << 4)) = v;
       }
@@ -1191,7 +1217,7 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
         }
         if (ntok > 0 && !q_ahead) load_q(meta.y, h, c0, columns);
         q_ahead = false;
-        ++n_unit;
+        n_unit += kUnit;
       }
       if (!warp_wait(s_sready + 8 * (2 * t + (n & 1)), (n >> 1) & 1u, s_abort)) {
         ok = false;
@@ -1237,6 +1263,7 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
             mxr[rr] = fmaxf(ma, mb);
           }
         }
+        const float scale = KV8 ? p.scale_log2e * __uint_as_float(n_unit << 23) : p.scale_log2e;
         float alpha[2] = {1.f, 1.f}, neg_mu[2];
         bool raise_any = false;
 #pragma unroll
@@ -1244,7 +1271,7 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
           float mx = mxr[rr];
           mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
           mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-          mx *= p.scale_log2e;  // the scale is positive
+          mx *= scale;  // positive
           // reference maximum: raised only when the row maximum is more than kTcRescaleStep above it
           const bool raise = m_ref[rr] != -INFINITY && mx > m_ref[rr] + kTcRescaleStep;
           if (m_ref[rr] == -INFINITY) {
@@ -1277,7 +1304,7 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
           l_part[0] *= alpha[0];
           l_part[1] *= alpha[1];
         }
-        const float2 scale2 = make_float2(p.scale_log2e, p.scale_log2e);
+        const float2 scale2 = make_float2(scale, scale);
         const float2 nm0 = make_float2(neg_mu[0], neg_mu[0]), nm1 = make_float2(neg_mu[1], neg_mu[1]);
         float2 add0 = {0.f, 0.f}, add1 = {0.f, 0.f};
 #pragma unroll
@@ -1344,8 +1371,8 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
         }
         // ---- the unit is complete: normalise the rows of O and write them
         const int part = meta.x;  // first partial row of the unit, or -1: the rows are complete
-        // use number n_unit - 1 of the tile's pv-done barrier
-        if (!warp_wait(s_pvdone + 8 * t, (n_unit - 1) & 1u, s_abort)) {
+        // the use of the tile's pv-done barrier that is the unit's
+        if (!warp_wait(s_pvdone + 8 * t, (n_unit / kUnit - 1) & 1u, s_abort)) {
           ok = false;
           break;
         }
