@@ -149,8 +149,9 @@ typedef struct {
  *                  passed over, as in the history and the drafts
  *   mask           device, int32 words, bit v % 32 of word v / 32 set = v allowed; NULL: everything is
  *   out_logits, out_probs   device, fp32; one of them may be NULL.  Rows i >= tree_sizes[b] are left as they were
- * fp32 logits may be one of the outputs (same address and strides); memory is not shared otherwise
- * (OOCO_E_SHAPE).  One launch.
+ * fp32 logits may be one of the outputs (same address and strides); otherwise the spans from the first to the last
+ * element of an output, of another output and of an input do not meet, and an output's rows are distinct, with either of
+ * its two strides the larger one (OOCO_E_SHAPE).  One launch.
  */
 int ooco_shape_logits(const ooco_logits_t* shape, const void* logits, const float* temperature, const float* repetition,
                       const float* frequency, const float* presence, const int32_t* history, const int32_t* history_lens,

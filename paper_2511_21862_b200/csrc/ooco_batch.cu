@@ -249,9 +249,12 @@ int ooco_shape_logits(const ooco_logits_t* s, const void* logits, const float* t
   if (penalties && (!history_lens || (s->history_width > 0 && !history))) return OOCO_E_NULLPTR;
   if (!bias_tokens != !bias_values || (s->max_bias > 0 && !bias_tokens)) return OOCO_E_NULLPTR;
   const int64_t B = s->batch, N = s->max_nodes, V = s->vocab, cell = s->logits_fp32 ? 4 : 2;
-  // rows of an output must not meet one another; masks may be shared
+  // rows of an output must not meet one another, whichever of the two dimensions is the outer one; masks may be shared
+  auto nested = [&](int64_t outer, int64_t n_outer, int64_t inner, int64_t n_inner) {
+    return (n_inner == 1 || inner >= V) && (n_outer == 1 || (n_inner == 1 ? outer >= V : (outer - V) / inner >= n_inner - 1));
+  };
   auto rows_ok = [&](int64_t seq, int64_t node) {
-    return seq >= 0 && node >= 0 && (N == 1 || node >= V) && (B == 1 || seq >= (N - 1) * node + V);
+    return seq >= 0 && node >= 0 && (nested(seq, B, node, N) || nested(node, N, seq, B));
   };
   if (s->logits_seq_stride < 0 || s->logits_node_stride < 0 || (mask && (s->mask_seq_stride < 0 || s->mask_node_stride < 0)) ||
       (out_logits && !rows_ok(s->out_seq_stride, s->out_node_stride)) ||
