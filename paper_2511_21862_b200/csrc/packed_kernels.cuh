@@ -1092,8 +1092,8 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
     float l_part[2] = {0.f, 0.f};             // this thread's share of the row's sum of weights
     int lim_row[2] = {0, 0};
     // Units in which this tile had rows, times kUnit; below that, 127 + the binary orders that the warp's rows of Q were lowered by
-    // (load_q).  One register for both, and one number for all rows of the warp: kept apart, or by rows, the loop over the stages
-    // took 11 and 16 % longer over the 8-bit cache.
+    // (load_q).  One register for both, and one number for all rows of the warp: kept apart, or by rows, prompts over the 8-bit cache
+    // took 11 and 16 % longer than without (this form: 3 %).
     constexpr uint32_t kUnit = 512;
     uint32_t n_unit = 127;
     bool ok = true;
@@ -1123,7 +1123,8 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
         top = max(top & 0xffffu, top >> 16);
         top = __reduce_max_sync(0xffffffffu, top);
         const int e = (int)(top >> 7) - 127;  // 2^e <= the largest value < 2^(e + 1)
-        const int shift = top ? max(e - 15, -100) : 0;  // (-100: the scores and their scale stay far from the ends of fp32)
+        // (not below -100, so that the scores and their scale stay far from the ends of fp32)
+        const int shift = e > 15 ? e - 15 : (e < 15 && top ? max(e - 15, -100) : 0);
         factor = __uint_as_float((uint32_t)(127 - shift) << 23);
         n_unit = (n_unit & ~(kUnit - 1)) | (uint32_t)(127 + shift);
       }
@@ -1247,6 +1248,7 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
               }
           }
         };
+        const float scale = KV8 ? p.scale_log2e * __uint_as_float(n_unit << 23) : p.scale_log2e;
         float mxr[2] = {-INFINITY, -INFINITY};
 #pragma unroll
         for (int h2 = 0; h2 < 2; ++h2) {
@@ -1263,7 +1265,6 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
             mxr[rr] = fmaxf(ma, mb);
           }
         }
-        const float scale = KV8 ? p.scale_log2e * __uint_as_float(n_unit << 23) : p.scale_log2e;
         float alpha[2] = {1.f, 1.f}, neg_mu[2];
         bool raise_any = false;
 #pragma unroll
