@@ -67,9 +67,11 @@ extern "C" {
  * ending at free_head; ids for which the list has no room are dropped with OOCO_STATUS_REFUSED.  context_lens
  * becomes the smaller of itself and keep_lens, blocks_held the blocks kept; table entries stay.  A row outside
  * [0, batch) or named twice is refused; a row's blocks_held is clamped to [0, max_blocks_per_seq].
- *   free_ids is written in [new free_head, free_head); the rest as above.  One launch, or five for many table entries.
- * The last block that a cut row keeps may have other holders: new tokens must not be written into it.  Such a row goes on
- * as a fork of itself into an empty row (whose partly filled block is a copy).
+ *   free_ids is written in [new free_head, free_head); the rest as above.  One launch, or five for many table entries
+ *   (num_rows * max_blocks_per_seq: the width of the table counts, as for the forks).
+ * The last block that a cut row keeps may have other holders (shares of block_table[row, (keep - 1) / block_size] above 0, where
+ * keep is no multiple of block_size): new tokens must not be written into it, though ooco_plan_slots would hand out its slots.
+ * Such a row goes on as a fork of itself into an empty row (whose partly filled block is a copy).
  */
 #define OOCO_MAX_PAGE_ROWS (1 << 18)
 size_t ooco_pages_workspace_bytes(const ooco_shape_t* shape, int32_t num_rows);
@@ -165,7 +167,7 @@ int ooco_shape_logits(const ooco_logits_t* shape, const void* logits, const floa
  * context (their K / V are in the cache, context_lens[b] counts them); query i attends to tokens
  * [0, T_b - n_b + i + 1), with the formula of ooco_decode_attention.  A query that sees no token gives a zero row.
  *   n_b            first_row[b + 1] - first_row[b], or the smaller of that and chunk_lens[b]; negative counts as 0,
- *                  rows at or beyond num_rows do not exist
+ *                  rows at or beyond num_rows do not exist and are not counted
  *   num_rows       rows of q and out; rows that belong to no query token are left as they were
  *   max_chunk      the caller's bound of n_b, 1 .. num_rows (which always is one): it decides which kernels are
  *                  launched and how large the workspace is.  A sequence that brings more is passed over, its rows left
@@ -183,7 +185,8 @@ int ooco_shape_logits(const ooco_logits_t* shape, const void* logits, const floa
  * new tokens among them: the products that the causal mask gives weight 0 are still formed inside a sequence.  The 8-bit
  * variant as ooco_decode_step_mq_fp8, but that a value x of q is rounded to f16 relative to the largest magnitude M of the
  * rows of its sequence and kv head: it is off by at most 2^-11 |x|, 2^-40 M or 2^-125.  One launch for few
- * sequences over a narrow table, else up to five (plan, the kernels that max_chunk asks for, merge).
+ * sequences over a narrow table (of at most 2048 tokens, whatever the contexts), else up to five (plan, the kernels that
+ * max_chunk asks for, merge).
  */
 size_t ooco_chunk_workspace_bytes(const ooco_shape_t* shape, int32_t num_rows, int32_t max_chunk);
 int ooco_chunk_attention(const ooco_shape_t* shape, int32_t num_rows, int32_t max_chunk, const void* q, int64_t q_stride,

@@ -97,13 +97,16 @@ struct Counter {
 // penalties runs with full warps.  Then, for each node: the masked logits to shared memory, one word a token; penalties and
 // biases on the tokens concerned; the largest; weights and their sum; one exchange in the cluster; probabilities.  So logits are
 // read once and probabilities written once.  Many rows are bound by instructions, by the chain of a node's steps and, with clusters
-// of 16, by the SMs that hold none (256 rows of 152064 in trees of 16: 116 us, 2.0 TB/s), few rows by the chain of loads, reductions
-// and the exchange (4 rows of 128256: 12 us).
+// of 16, by the SMs that hold none (256 rows of 152064 in trees of 16: 116 us, 2.0 TB/s; fp32 logits 149, shaped logits out as well
+// 141), few rows by the chain of loads, reductions and the exchange (4 rows of 128256: 12 us).
 // The largest value is found on the way: over the masked logits as they come and over the values that penalties change.  Only where
 // the second cannot stand for the true one (biases, a largest logit that fell far, a greedy row) are the values gone through again.
 // Sums are fp32: 2^-24 relative a step, over the up to 100 values of a thread, a tree of 8 levels, and a tree over the CTAs.
 // kWide: rows of logits and outputs begin on boundaries of four values, so a thread has groups of four neighbours, which every
-// access to shared and global memory moves without conflicts or partial sectors; else single tokens, side by side across the lanes.
+// access to shared and global memory moves without conflicts or partial sectors; else single tokens, side by side across the lanes
+// (256 rows of 152064 and 152065: 116 and 305 us; of 50256 and 50257: 59 and 106).
+// Biases: a token's first entry looks for its others, for every row again: 16 entries cost nothing, 256 16 us and 1024 155 us a row
+// of a cluster.
 template <typename T, bool kWide, bool kHalf>
 __global__ void __launch_bounds__(kLogitsThreads, 3) shape_logits_kernel(const LogitsParams p) {
   using C = Counter<kHalf>;

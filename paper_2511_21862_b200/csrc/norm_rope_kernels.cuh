@@ -14,8 +14,9 @@ struct HeadNormParams {
 // over 16 values of a thread and a butterfly over its D / 16 lanes, in 32 bits; and since a thread keeps its place in the head
 // from unit to unit, it finds the weights of its 16 dims at a place of its own.  Bound by HBM and, nearly as much, by issue slots: q, k
 // and v are read and written once, sums and rotations run on pairs of fp32 values.  Tokens of 64 q and 8 kv heads of 128: 16384 over
-// a bf16 cache 122 us, 5.5 TB/s, and over codes 129 us, 5.0 TB/s; 158 when lanes' weights, cosines and sines met in the banks
-// of shared memory, 135 with single operations; 64 tokens 4.6 us, a launch and two trips to memory.
+// a bf16 cache 121 us, 5.5 TB/s, and over codes 126 to 135 us, 4.7 to 5.0 TB/s (66 % of the issue slots, ALU pipe 46 %, special
+// functions 17 %, fp64, which forms the angles, 0.2 %); over bf16 158 when lanes' weights, cosines and sines met in the banks
+// of shared memory, 135 with single operations; 64 tokens 4.3 to 4.6 us, a launch and two trips to memory.
 template <int D, bool KV8>
 __global__ void __launch_bounds__(kRopeThreads, 4) norm_rope_append_kernel(const RopeParams p, const HeadNormParams hn,
                                                                         const int interleaved) {

@@ -18,7 +18,8 @@ static_assert(kPackedStatusRefused == OOCO_STATUS_REFUSED, "status bit");
 // find their pairs by themselves: no plan, decode list or merge, but no cutting of long contexts either.  Measured, without and with
 // a plan (1 to 8 new tokens): 4 sequences of 2 kv heads, up to 1024 or 2048 tokens 20 and 37, 28 and 41 us; 37 of 8 heads 37 and 65,
 // 60 and 90 us; one new token: 28 and 30, 58 and 71 us.  Beyond: 4 sequences of up to 4096 tokens, one new 43 and 32 us; 74 of 8
-// heads, 2048 tokens of an 8-bit cache 101 and 83 us.
+// heads, 2048 tokens of an 8-bit cache 101 and 83 us.  The table's width decides, since the host does not know the contexts: 4 sequences
+// of at most 256 tokens take 10 to 12 us in a table of 256 tokens, in one of 32768 29 (1 to 8 new tokens) and 20 us (one).
 constexpr int64_t kDirectTokens = 2048, kDirectPairsPerSm = 2;
 
 struct PackedLayout {
