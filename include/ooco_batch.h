@@ -183,7 +183,7 @@ int ooco_shape_logits(const ooco_logits_t* shape, const void* logits, const floa
  * num_rows = 0 launches nothing.  Slots at or beyond T_b, table entries behind the last block used, and entries outside
  * the pool are treated as in ooco_decode_attention.  The K / V of a sequence's context must be finite, those of its later
  * new tokens among them: the products that the causal mask gives weight 0 are still formed inside a sequence.  The 8-bit
- * variant as ooco_decode_step_mq_fp8, but that a value x of q is rounded to f16 relative to the largest magnitude M of the
+ * variant as ooco_decode_step_mq_fp8, but that a value x of q is rounded to f16 relative to the largest finite magnitude M of the
  * rows of its sequence and kv head: it is off by at most 2^-11 |x|, 2^-40 M or 2^-125.  One launch for few
  * sequences over a narrow table (of at most 2048 tokens, whatever the contexts), else up to five (plan, the kernels that
  * max_chunk asks for, merge).

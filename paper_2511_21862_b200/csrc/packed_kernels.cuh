@@ -1096,7 +1096,7 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
     int lim_row[2] = {0, 0};
     // Units in which this tile had rows, times kUnit; below that, 127 + the binary orders that the warp's rows of Q were lowered by
     // (load_q).  One register for both, and one number for all rows of the warp: kept apart, or by rows, prompts over the 8-bit cache
-    // took 11 and 16 % longer than without (this form: 3 %).
+    // took 11 and 16 % longer than without (this form: 3 to 4 %).
     constexpr uint32_t kUnit = 512;
     uint32_t n_unit = 127;
     bool ok = true;
@@ -1104,7 +1104,7 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
     // Q of the tile's columns from c0_ on, of a sequence whose rows of q begin at row0_, into the swizzled K-major tile
     // ([half][row][64 dims], 16-byte chunk ^= row & 7): a warp writes its own 16 rows, two lanes a row; then the q-ready
     // arrival.  KV8: f16 ends at 65504 and has 11 bits down to 2^-14, bf16 goes far beyond, so a warp's rows are moved by the power of
-    // two that brings the largest of their values to 2^15, which the scale of their scores takes back.  A value x is off by at most
+    // two that brings the largest finite one of their values to 2^15, which the scale of their scores takes back.  A value x is off by at most
     // 2^-11 |x|, or half a step of the smallest f16 numbers: 2^-40 of that largest one, 2^-125 where that is below 2^-85.
     auto load_q = [&](int row0_, int h_, int c0_, int columns_) {
       const int r_ = 32 * q4 + 16 * hf + (lane >> 1), part_ = lane & 1;
@@ -1124,6 +1124,7 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
           top = __vmaxu2(top, __vmaxu2(__vmaxu2(w_[c].x & 0x7fff7fffu, w_[c].y & 0x7fff7fffu),
                                        __vmaxu2(w_[c].z & 0x7fff7fffu, w_[c].w & 0x7fff7fffu)));
         top = max(top & 0xffffu, top >> 16);
+        if (top >= 0x7f80u) top = 0u;  // (what is not finite stays so, and must not move its neighbours)
         top = __reduce_max_sync(0xffffffffu, top);
         const int e = (int)(top >> 7) - 127;  // 2^e <= the largest value < 2^(e + 1)
         // (not below -100, so that the scores and their scale stay far from the ends of fp32)

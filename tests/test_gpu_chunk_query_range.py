@@ -83,3 +83,33 @@ def test_rows_of_very_different_size(base, odd):
     """Small rows beside large ones keep their scores."""
     for room in (0, 8192):
         run([5, 1, 20, 2], [60, 200, 20, 333], base, hq=8, hkv=2, room=room, seed=6, odd=odd)
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
+@pytest.mark.parametrize("fp8", [True, False])
+def test_a_query_that_is_not_finite_stays_alone(bad, fp8):
+    """Rows with one value that is not finite give what they give; every other row is as if they were zeros."""
+    D, bs, hq, hkv, n, T = 128, 16, 8, 2, 20, 100
+    g = torch.Generator(device=DEV).manual_seed(3)
+    x = (torch.randn((2 * 7, hkv, bs, D), generator=g, device=DEV) for _ in range(2))
+    kc, vc = ((t_ * 16).to(torch.float8_e4m3fn).view(torch.uint8) if fp8 else t_.to(torch.bfloat16) for t_ in x)
+    q = torch.randn((2 * n, hq, D), generator=g, device=DEV).to(torch.bfloat16)
+    hit = torch.zeros((2 * n, hq), dtype=torch.bool, device=DEV)
+    hit[3, 1] = hit[9, 6] = hit[n + 1, 0] = True
+    q[hit] = 0
+    for room in (112, 8192):
+        sh = t.pool_shape(2, hq, hkv, D, bs, 14, room // bs)
+        table = torch.zeros((2, room // bs), dtype=torch.int32, device=DEV)
+        table[:, :7] = torch.arange(14, dtype=torch.int32, device=DEV).view(2, 7)
+        ws = torch.empty(batch.chunk_workspace_bytes(sh, 2 * n, n), dtype=torch.uint8, device=DEV)
+        outs = []
+        for value in (0.0, bad):
+            q[hit, 70] = value
+            out = torch.full_like(q, 5.0)
+            args = (sh, q, kc, vc, table, t.gpu([T, T - 7]), t.gpu([0, n, 2 * n]), n, 0.05)
+            if fp8:
+                batch.chunk_attention_fp8(*args, 0.07, 0.11, out, ws)
+            else:
+                batch.chunk_attention(*args, out, ws)
+            outs.append(out)
+        assert torch.equal(outs[0][~hit], outs[1][~hit])
